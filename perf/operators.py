@@ -50,30 +50,30 @@ def _linear_grad(name, rows, c_in, c_out, act):
 def listed():
     return [
         # the class token of one image before the classifier: latency alone
-        _norm("norm, one token", 1, 768, "bf16", stats=False),
+        _norm("norm one token", 1, 768, "bf16", stats=False),
         # a ViT-B block's norm at the benchmark's batch (64 images of 197 tokens), statistics kept for the backward pass
-        _norm("norm, vit", 12608, 768, "bf16"),
+        _norm("norm vit", 12608, 768, "bf16"),
         # fp32 features of an odd width (rows start at no 16-byte boundary)
-        _norm("norm, odd and wide", 1009, 5003, "fp32"),
+        _norm("norm odd and wide", 1009, 5003, "fp32"),
         # the backward pass of the ViT-B norm: bf16 activations, fp32 gradients as the weight gradients take them,
         # the gradient of the skip connection added on the way
-        _norm_grad("norm grad, vit", 12608, 768, "bf16", "fp32"),
+        _norm_grad("norm grad vit", 12608, 768, "bf16", "fp32"),
         # Segformer-B5's first stage on one 1024x1024 image: many short rows, gradients in bf16
-        _norm_grad("norm grad, segformer stage 1", 65536, 64, "bf16", "bf16"),
+        _norm_grad("norm grad segformer stage 1", 65536, 64, "bf16", "bf16"),
         # the norm layers' parameters alone, adapted as in "SURGEON (BN)": ResNet-50's 106 short tensors
-        _clip("clip, norm layers", "resnet50_bn", "fp32", 0.5, 128),
+        _clip("clip norm layers", "resnet50_bn", "fp32", 0.5, 128),
         # every weight and bias of ViT-B: 86 million fp32 gradients
-        _clip("clip, vit", "vit", "fp32", 0.3, 128),
+        _clip("clip vit", "vit", "fp32", 0.3, 128),
         # the classifier on one image: a single row, fp32 logits
-        _linear("linear, classifier of one image", 1, 2048, 1000, "none", out="fp32"),
+        _linear("linear classifier of one image", 1, 2048, 1000, "none", out="fp32"),
         # Segformer's MLP in its second stage, the pre-activation kept for the backward pass
-        _linear("linear, segformer stage 2 mlp", 16384, 128, 512, "gelu", keep=True),
+        _linear("linear segformer stage 2 mlp", 16384, 128, 512, "gelu", keep=True),
         # a wide layer with its skip connection: the matrix product is the whole of it
-        _linear("linear, wide with residual", 16384, 2048, 2048, "none", residual=True),
+        _linear("linear wide with residual", 16384, 2048, 2048, "none", residual=True),
         # the input gradient of ViT-B's qkv layer
-        _linear_grad("linear grad, vit qkv", 12608, 768, 2304, "none"),
+        _linear_grad("linear grad vit qkv", 12608, 768, 2304, "none"),
         # Segformer's third-stage MLP on an image that fills no whole tile
-        _linear_grad("linear grad, segformer stage 3 mlp", 4037, 320, 1280, "gelu"),
+        _linear_grad("linear grad segformer stage 3 mlp", 4037, 320, 1280, "gelu"),
     ]
 
 
