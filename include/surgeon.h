@@ -280,6 +280,88 @@ surgeon_status surgeon_weight_grad_flags(const surgeon_compressed* act, const su
  * ---------------------------------------------------------------------------------------- */
 surgeon_status surgeon_decompress(const surgeon_compressed* act, void* x_out, void* cuda_stream);
 
+/* ==========================================================================================
+ * The layers around the store.  An adaptation step over a network with layer norms and linear
+ * layers (ViT, Segformer) also runs what produces the activations that are pruned (Eq. 1) and
+ * what carries the gradient to the layer before (Eq. 2, first line).  Channels are the last,
+ * contiguous dimension; parameters are fp32, sums are fp32 or wider and taken in a fixed order,
+ * so results are bitwise reproducible from call to call.
+ * ======================================================================================== */
+
+/* ------------------------------------------------------------------------------------------
+ * Layer norm over the channels of x [rows, channels]:
+ *   mean_t = sum_c x_tc / C;  r_t = 1 / sqrt(sum_c (x_tc - mean_t)^2 / C + eps);
+ *   y_tc = (x_tc - mean_t) r_t gamma_c + beta_c
+ * y is the input activation of the layer behind it, the tensor surgeon_prune_compact takes.
+ * x, y: device, dt; y may be x.  gamma, beta: device, fp32, `channels` each; NULL: 1 and 0.
+ * stats: device, fp32, 2 * rows (the means, then the r) for surgeon_layer_norm_grad, or NULL.
+ * A NaN or an infinity stays in its row.  rows = 0 is legal.  Asynchronous on cuda_stream.
+ * Errors: INVALID_ARG (null or misaligned pointer, rows < 0, channels <= 0, bad dt, eps not a
+ * positive fp32 number), UNSUPPORTED (more than SURGEON_MAX_N elements), CUDA.
+ * ---------------------------------------------------------------------------------------- */
+surgeon_status surgeon_layer_norm(const void* x, int64_t rows, int32_t channels, surgeon_dtype dt,
+                                  const float* gamma, const float* beta, double eps, void* y,
+                                  float* stats, void* cuda_stream);
+
+/* Device scratch (bytes) surgeon_layer_norm_grad needs for dgamma or dbeta; 0 on bad arguments. */
+size_t surgeon_layer_norm_grad_workspace(int64_t rows, int32_t channels);
+
+/* ------------------------------------------------------------------------------------------
+ * Backward pass of surgeon_layer_norm, with xh = (x - mean) r and g = dy gamma:
+ *   dx = r (g - sum_c g / C - xh sum_c (g xh) / C) + residual_grad
+ *   dgamma = sum_t dy xh;  dbeta = sum_t dy
+ * x: dt; stats: as the forward call wrote them for this x.  dy, residual_grad (NULL: zero; the gradient that
+ * passes the norm by, through the skip connection) and dx: grad_dt.  dx may be dy or residual_grad.
+ * dx, dgamma, dbeta: any may be NULL (not wanted).  accumulate = 0 overwrites dgamma and dbeta,
+ * 1 adds to them (dx is always overwritten).  workspace: scratch of the size that the query
+ * gives (it may be NULL where neither dgamma nor dbeta is wanted), not shared with a call in flight.
+ * Element types (dt, grad_dt): (F32, F32), (BF16, F32), (BF16, BF16).  Asynchronous.
+ * Errors: INVALID_ARG, BUFFER_TOO_SMALL, UNSUPPORTED ((F32, BF16); size), CUDA.
+ * ---------------------------------------------------------------------------------------- */
+surgeon_status surgeon_layer_norm_grad(const void* x, const void* dy, int64_t rows, int32_t channels,
+                                       surgeon_dtype dt, surgeon_dtype grad_dt, const float* gamma,
+                                       const float* stats, const void* residual_grad, void* dx,
+                                       float* dgamma, float* dbeta, int32_t accumulate,
+                                       void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * A list of gradients: the norm over all of them, Eq. 4 for each, and clipping by the norm.
+ *   S_i = sum_j g_ij^2;  gi_out[i] = sqrt(S_i / n_i) (0 for n_i = 0);  norm = sqrt(sum_i S_i)
+ *   clip: out_ij = g_ij * c with c = max_norm / (norm + 1e-6) where that is below 1 (rounded to
+ *   fp32, the product rounded once more to dt); else, and where the norm is infinite or NaN (some
+ *   gradient is), out_ij = g_ij: the caller reads the norm and decides.
+ * ---------------------------------------------------------------------------------------- */
+typedef struct surgeon_gradient {
+  const void* grad;  /* device, n elements of dt, aligned to one element (NULL if n = 0)          */
+  void* out;         /* device, n elements of dt, the clipped gradient; may be grad (in place);
+                        not read by surgeon_gradient_norm                                         */
+  int64_t n;         /* at most SURGEON_MAX_N                                                     */
+  int32_t dt;        /* surgeon_dtype                                                             */
+  int32_t reserved;
+} surgeon_gradient;
+#define SURGEON_MAX_GRADIENTS 65536
+
+/* Device scratch (bytes) for a list of `count` gradients; 0 on a bad count. */
+size_t surgeon_gradient_norm_workspace(int32_t count);
+
+/* list: HOST pointer to `count` entries (not kept).  norm_out: DEVICE pointer to one double, or
+ * NULL.  gi_out: DEVICE pointer to `count` doubles, or NULL.  workspace: device scratch, not shared
+ * with a call in flight.  Squares and sums in double, in a fixed order.  Asynchronous; a captured call
+ * keeps the list as it was.  count = 0 gives the norm 0.
+ * Errors: INVALID_ARG (null or misaligned pointer, count or n negative, bad dt, both outputs
+ * NULL), BUFFER_TOO_SMALL, UNSUPPORTED (count or n too large), CUDA. */
+surgeon_status surgeon_gradient_norm(const surgeon_gradient* list, int32_t count, double* norm_out,
+                                     double* gi_out, void* workspace, size_t workspace_bytes,
+                                     void* cuda_stream);
+
+/* The same, and the clipped gradients to `out` of each entry.  Either of norm_out and gi_out may
+ * be NULL, or both.  Also INVALID_ARG: max_norm negative or NaN (infinity: nothing is clipped), an
+ * output that overlaps another output or a gradient other than its own (the same tensor
+ * twice), or its own in part. */
+surgeon_status surgeon_clip_gradients(const surgeon_gradient* list, int32_t count, double max_norm,
+                                      double* norm_out, double* gi_out, void* workspace,
+                                      size_t workspace_bytes, void* cuda_stream);
+
 /* Static text for a status code. */
 const char* surgeon_status_string(surgeon_status s);
 

@@ -49,6 +49,10 @@ class Compressed(C.Structure):
                 ("header", C.c_void_p)]
 
 
+class Gradient(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dt", C.c_int32), ("reserved", C.c_int32)]
+
+
 class LayerDesc(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("kind", "batch", "c_in", "h", "w", "c_out", "kh", "kw",
                                          "stride", "pad", "path", "groups")]
@@ -94,6 +98,19 @@ def lib():
         l.surgeon_weight_grad_flags.restype = C.c_int
         l.surgeon_weight_grad_flags.argtypes = [C.POINTER(Compressed), C.POINTER(LayerDesc), C.c_void_p, C.c_void_p,
                                                 C.c_int32, C.c_uint32, C.c_void_p, C.c_size_t, C.c_void_p]
+        P, I64, I32, F64 = C.c_void_p, C.c_int64, C.c_int32, C.c_double
+        l.surgeon_layer_norm.restype = C.c_int
+        l.surgeon_layer_norm.argtypes = [P, I64, I32, C.c_int, P, P, F64, P, P, P]
+        l.surgeon_layer_norm_grad_workspace.restype = C.c_size_t
+        l.surgeon_layer_norm_grad_workspace.argtypes = [I64, I32]
+        l.surgeon_layer_norm_grad.restype = C.c_int
+        l.surgeon_layer_norm_grad.argtypes = [P, P, I64, I32, C.c_int, C.c_int, P, P, P, P, P, P, I32, P, C.c_size_t, P]
+        l.surgeon_gradient_norm_workspace.restype = C.c_size_t
+        l.surgeon_gradient_norm_workspace.argtypes = [I32]
+        l.surgeon_gradient_norm.restype = C.c_int
+        l.surgeon_gradient_norm.argtypes = [P, I32, P, P, P, C.c_size_t, P]
+        l.surgeon_clip_gradients.restype = C.c_int
+        l.surgeon_clip_gradients.argtypes = [P, I32, F64, P, P, P, C.c_size_t, P]
         l.surgeon_decompress.restype = C.c_int
         l.surgeon_decompress.argtypes = [C.POINTER(Compressed), C.c_void_p, C.c_void_p]
         l.surgeon_launch_count.restype = C.c_uint64
@@ -401,3 +418,169 @@ def surgeon_weight_grad(act: CompressedActivation, desc: LayerDesc, grad_out: to
                                          workspace.numel() * workspace.element_size(), _stream_ptr(stream))
     _check(st, "surgeon_weight_grad")
     return dw
+
+
+# ---------------------------------------------------------------------------------------------
+# The layers around the store: what produces the activations (Eq. 1) and carries the gradient back
+# (Eq. 2, first line), and the list of gradients that a step ends with
+# ---------------------------------------------------------------------------------------------
+
+def _operand(t: Optional[torch.Tensor], name: str, shape=None, dtype=None):
+    """Checks one tensor of a call (None: left out) and returns its address."""
+    if t is None:
+        return None
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous CUDA tensor" % name)
+    if t.device.index != torch._C._cuda_getDevice():
+        raise ValueError("%s is on %s, which is not the current device" % (name, t.device))
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError("%s must have the shape %s, got %s" % (name, shape, tuple(t.shape)))
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    return t.data_ptr()
+
+
+def _new(shape, dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """A tensor made here for kernels on ``stream``, from that stream's part of the allocator's memory:
+    a block of the current stream's may still be in use there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _work(workspace: Optional[torch.Tensor], nbytes: int, device, stream: Optional[torch.cuda.Stream]):
+    """Address and size of a call's scratch, which is made here where the caller passed none."""
+    if workspace is None:
+        workspace = _new(max(int(nbytes), 16), torch.uint8, device, stream)
+    return _operand(workspace, "workspace"), workspace.numel() * workspace.element_size()
+
+
+def _rows(t: torch.Tensor, name: str):
+    if t.dim() < 1 or t.shape[-1] == 0:
+        raise ValueError("%s must have channels in its last dimension" % name)
+    return t.numel() // t.shape[-1], t.shape[-1]
+
+
+def surgeon_layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
+                       eps: float = 1e-5, out: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Layer norm over the last dimension of ``x`` (fp32 or bf16); returns ``out``, which may be ``x``.
+    ``gamma``, ``beta``: fp32.  ``stats``: an fp32 tensor [2, rows] that receives the means and the reciprocal
+    standard deviations for ``surgeon_layer_norm_grad``."""
+    rows, channels = _rows(x, "x")
+    dt = dtype_code(x.dtype)
+    xp = _operand(x, "x")
+    if out is None:
+        out = _new(x.shape, x.dtype, x.device, stream)
+    st = lib().surgeon_layer_norm(xp, rows, channels, dt, _operand(gamma, "gamma", (channels,), torch.float32),
+                                  _operand(beta, "beta", (channels,), torch.float32), float(eps),
+                                  _operand(out, "out", tuple(x.shape), x.dtype),
+                                  _operand(stats, "stats", (2, rows), torch.float32), _stream_ptr(stream))
+    if st != SURGEON_OK:
+        _check(st, "surgeon_layer_norm")
+    return out
+
+
+def surgeon_layer_norm_grad_workspace(rows: int, channels: int) -> int:
+    return int(lib().surgeon_layer_norm_grad_workspace(int(rows), int(channels)))
+
+
+def surgeon_layer_norm_grad(x: torch.Tensor, dy: torch.Tensor, gamma: Optional[torch.Tensor], stats: torch.Tensor,
+                            residual_grad: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                            dgamma: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None,
+                            accumulate: bool = False, workspace: Optional[torch.Tensor] = None,
+                            stream: Optional[torch.cuda.Stream] = None, want_dx: bool = True) -> Optional[torch.Tensor]:
+    """Backward pass of ``surgeon_layer_norm``; returns ``dx`` (of dy's type, made here if None; None with
+    ``want_dx=False``).  ``residual_grad`` (dy's shape and type) is added to it; ``dx`` may be ``dy`` or
+    ``residual_grad``.  ``dgamma``, ``dbeta``: fp32, written (``accumulate=True``: added to) where given."""
+    rows, channels = _rows(x, "x")
+    shape = tuple(x.shape)
+    xp, dyp = _operand(x, "x"), _operand(dy, "dy", shape)
+    if not want_dx:
+        if dx is not None:
+            raise ValueError("dx given, but not wanted")
+    elif dx is None:
+        dx = _new(shape, dy.dtype, dy.device, stream)
+    ws = None, 0
+    if dgamma is not None or dbeta is not None:
+        ws = _work(workspace, surgeon_layer_norm_grad_workspace(rows, channels) if workspace is None else 0, x.device, stream)
+    f32 = torch.float32
+    st = lib().surgeon_layer_norm_grad(xp, dyp, rows, channels, dtype_code(x.dtype), dtype_code(dy.dtype),
+                                       _operand(gamma, "gamma", (channels,), f32), _operand(stats, "stats", (2, rows), f32),
+                                       _operand(residual_grad, "residual_grad", shape, dy.dtype),
+                                       _operand(dx, "dx", shape, dy.dtype), _operand(dgamma, "dgamma", (channels,), f32),
+                                       _operand(dbeta, "dbeta", (channels,), f32), 1 if accumulate else 0, *ws,
+                                       _stream_ptr(stream))
+    if st != SURGEON_OK:
+        _check(st, "surgeon_layer_norm_grad")
+    return dx
+
+
+class GradientList:
+    """A list of gradients (fp32 or bf16, contiguous) and where their clipped values go (``outs``; None: in place),
+    as the C array that the two calls below take.  The tensors are kept alive, and must not be reallocated."""
+
+    def __init__(self, grads, outs=None):
+        self.grads = list(grads)
+        self.outs = self.grads if outs is None else list(outs)
+        if len(self.outs) != len(self.grads):
+            raise ValueError("%d outputs for %d gradients" % (len(self.outs), len(self.grads)))
+        self.device = self.grads[0].device if self.grads else None
+        entries = []
+        for i, (g, o) in enumerate(zip(self.grads, self.outs)):
+            for t, what in ((g, "gradient"), (o, "output")):
+                if not t.is_cuda or not t.is_contiguous() or t.device != self.device:
+                    raise ValueError("%s %d must be a contiguous CUDA tensor on the device of the first" % (what, i))
+            if o.dtype != g.dtype or o.shape != g.shape:
+                raise ValueError("output %d must have its gradient's shape and type" % i)
+            entries.append((g.data_ptr() or None, o.data_ptr() or None, g.numel(), dtype_code(g.dtype), 0))
+        self.c = (Gradient * max(len(entries), 1))(*entries)
+        self.address = C.addressof(self.c)
+
+    def __len__(self):
+        return len(self.grads)
+
+
+def surgeon_gradient_norm_workspace(grads) -> int:
+    """Scratch bytes for a ``GradientList`` (or any sequence as long)."""
+    return int(lib().surgeon_gradient_norm_workspace(len(grads)))
+
+
+def _list_call(grads, norm, gi, workspace, stream, new_gi):
+    lst = grads if isinstance(grads, GradientList) else GradientList(grads)
+    device = lst.device
+    if device is None:
+        device = norm.device if norm is not None else torch.device("cuda", torch._C._cuda_getDevice())
+    if device.index != torch._C._cuda_getDevice():
+        raise ValueError("the gradients are on %s, which is not the current device" % device)
+    if norm is None:
+        norm = _new(1, torch.float64, device, stream)
+    if gi is None and new_gi:
+        gi = _new(len(lst), torch.float64, device, stream)
+    ws = _work(workspace, surgeon_gradient_norm_workspace(lst) if workspace is None else 0, device, stream)
+    return (lst, norm, gi, (_operand(norm, "norm", (1,), torch.float64),
+                            _operand(gi, "gi", (len(lst),), torch.float64), *ws, _stream_ptr(stream)))
+
+
+def surgeon_gradient_norm(grads, norm: Optional[torch.Tensor] = None, gi: Optional[torch.Tensor] = None,
+                          workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """``(norm, gi)`` of a ``GradientList`` or a sequence of gradients: the global norm (one float64 on the device)
+    and every tensor's Gradient Importance (Eq. 4, float64), as the ratio rule takes them."""
+    lst, norm, gi, args = _list_call(grads, norm, gi, workspace, stream, True)
+    st = lib().surgeon_gradient_norm(lst.address, len(lst), *args)
+    if st != SURGEON_OK:
+        _check(st, "surgeon_gradient_norm")
+    return norm, gi
+
+
+def surgeon_clip_gradients(grads, max_norm: float, norm: Optional[torch.Tensor] = None, gi: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None,
+                           stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Scales the gradients by min(1, max_norm / (norm + 1e-6)) into their outputs (a sequence: in place) and returns the
+    norm before.  An infinite or NaN norm leaves them as they are.  ``gi``: receives Eq. 4 of each, if given."""
+    lst, norm, gi, args = _list_call(grads, norm, gi, workspace, stream, False)
+    st = lib().surgeon_clip_gradients(lst.address, len(lst), float(max_norm), *args)
+    if st != SURGEON_OK:
+        _check(st, "surgeon_clip_gradients")
+    return norm

@@ -104,6 +104,34 @@ bool desc_ok(const surgeon_layer_desc* d, surgeon_status* why) {
   return true;
 }
 
+inline bool known_dtype(int dt) { return dt == SURGEON_F32 || dt == SURGEON_BF16; }
+
+surgeon_status rows_ok(int64_t rows, int32_t channels) {
+  if (rows < 0 || channels <= 0) return SURGEON_ERR_INVALID_ARG;
+  if (rows > SURGEON_MAX_N / channels) return SURGEON_ERR_UNSUPPORTED;
+  return SURGEON_OK;
+}
+
+surgeon_status gradients_ok(const surgeon_gradient* list, int32_t count, bool outputs, const double* norm_out,
+                            const double* gi_out, const void* workspace, size_t workspace_bytes) {
+  if (count < 0 || (count > 0 && (!list || !workspace))) return SURGEON_ERR_INVALID_ARG;
+  if (count > SURGEON_MAX_GRADIENTS) return SURGEON_ERR_UNSUPPORTED;
+  if ((reinterpret_cast<uintptr_t>(norm_out) | reinterpret_cast<uintptr_t>(gi_out) |
+       reinterpret_cast<uintptr_t>(workspace)) & 7u)
+    return SURGEON_ERR_INVALID_ARG;
+  for (int i = 0; i < count; ++i) {
+    const surgeon_gradient& g = list[i];
+    if (g.n < 0 || !known_dtype(g.dt)) return SURGEON_ERR_INVALID_ARG;
+    if (g.n > 0 && (!g.grad || (outputs && !g.out))) return SURGEON_ERR_INVALID_ARG;
+    const uintptr_t mask = g.dt == SURGEON_F32 ? 3u : 1u;
+    if ((reinterpret_cast<uintptr_t>(g.grad) & mask) || (outputs && (reinterpret_cast<uintptr_t>(g.out) & mask)))
+      return SURGEON_ERR_INVALID_ARG;
+    if (g.n > SURGEON_MAX_N) return SURGEON_ERR_UNSUPPORTED;
+  }
+  if (count > 0 && workspace_bytes < gradient_list_workspace(count)) return SURGEON_ERR_BUFFER_TOO_SMALL;
+  return SURGEON_OK;
+}
+
 }  // namespace
 }  // namespace surgeon
 
@@ -300,6 +328,71 @@ surgeon_status surgeon_gradient_importance(const float* dw, int64_t n_weights, d
   const cudaError_t e = launch_gradient_importance(dw, n_weights, gi_out, workspace,
                                                    static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? SURGEON_OK : SURGEON_ERR_CUDA;
+}
+
+surgeon_status surgeon_layer_norm(const void* x, int64_t rows, int32_t channels, surgeon_dtype dt,
+                                  const float* gamma, const float* beta, double eps, void* y,
+                                  float* stats, void* cuda_stream) {
+  const surgeon_status st = rows_ok(rows, channels);
+  if (st != SURGEON_OK) return st;
+  const float e = static_cast<float>(eps);
+  if (!known_dtype(dt) || !(e > 0.0f) || !isfinite(e)) return SURGEON_ERR_INVALID_ARG;
+  if (rows > 0 && (!x || !y)) return SURGEON_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(y) || !aligned16(gamma) || !aligned16(beta) || !aligned16(stats))
+    return SURGEON_ERR_INVALID_ARG;
+  return launch_layer_norm(x, rows, channels, static_cast<int>(dt), gamma, beta, e, y, stats,
+                           static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? SURGEON_OK : SURGEON_ERR_CUDA;
+}
+
+size_t surgeon_layer_norm_grad_workspace(int64_t rows, int32_t channels) {
+  return rows_ok(rows, channels) == SURGEON_OK ? layer_norm_grad_workspace(rows, channels) : 0;
+}
+
+surgeon_status surgeon_layer_norm_grad(const void* x, const void* dy, int64_t rows, int32_t channels,
+                                       surgeon_dtype dt, surgeon_dtype grad_dt, const float* gamma,
+                                       const float* stats, const void* residual_grad, void* dx,
+                                       float* dgamma, float* dbeta, int32_t accumulate,
+                                       void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  const surgeon_status st = rows_ok(rows, channels);
+  if (st != SURGEON_OK) return st;
+  if (!known_dtype(dt) || !known_dtype(grad_dt)) return SURGEON_ERR_INVALID_ARG;
+  if (rows > 0 && (!x || !dy || !stats)) return SURGEON_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(dy) || !aligned16(gamma) || !aligned16(stats) || !aligned16(residual_grad) ||
+      !aligned16(dx) || !aligned16(dgamma) || !aligned16(dbeta) || !aligned16(workspace))
+    return SURGEON_ERR_INVALID_ARG;
+  if (dt == SURGEON_F32 && grad_dt == SURGEON_BF16) return SURGEON_ERR_UNSUPPORTED;
+  if ((dgamma || dbeta) && rows > 0) {
+    if (!workspace) return SURGEON_ERR_INVALID_ARG;
+    if (workspace_bytes < layer_norm_grad_workspace(rows, channels)) return SURGEON_ERR_BUFFER_TOO_SMALL;
+  }
+  return launch_layer_norm_grad(x, dy, rows, channels, static_cast<int>(dt), static_cast<int>(grad_dt), gamma, stats,
+                                residual_grad, dx, dgamma, dbeta, accumulate ? 1 : 0, workspace,
+                                static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? SURGEON_OK : SURGEON_ERR_CUDA;
+}
+
+size_t surgeon_gradient_norm_workspace(int32_t count) {
+  return count < 0 || count > SURGEON_MAX_GRADIENTS ? 0 : gradient_list_workspace(count);
+}
+
+surgeon_status surgeon_gradient_norm(const surgeon_gradient* list, int32_t count, double* norm_out,
+                                     double* gi_out, void* workspace, size_t workspace_bytes,
+                                     void* cuda_stream) {
+  if (!norm_out && !gi_out) return SURGEON_ERR_INVALID_ARG;
+  const surgeon_status st = gradients_ok(list, count, false, norm_out, gi_out, workspace, workspace_bytes);
+  if (st != SURGEON_OK) return st;
+  return launch_gradient_list(list, count, 0, 0.0, norm_out, gi_out, workspace,
+                              static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? SURGEON_OK : SURGEON_ERR_CUDA;
+}
+
+surgeon_status surgeon_clip_gradients(const surgeon_gradient* list, int32_t count, double max_norm,
+                                      double* norm_out, double* gi_out, void* workspace,
+                                      size_t workspace_bytes, void* cuda_stream) {
+  if (!(max_norm >= 0.0)) return SURGEON_ERR_INVALID_ARG;
+  const surgeon_status st = gradients_ok(list, count, true, norm_out, gi_out, workspace, workspace_bytes);
+  if (st != SURGEON_OK) return st;
+  if (gradient_list_overlaps(list, count)) return SURGEON_ERR_INVALID_ARG;
+  return launch_gradient_list(list, count, 1, max_norm, norm_out, gi_out, workspace,
+                              static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? SURGEON_OK : SURGEON_ERR_CUDA;
 }
 
 uint64_t surgeon_launch_count(void) { return launches_so_far(); }

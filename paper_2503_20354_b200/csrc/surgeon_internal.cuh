@@ -103,6 +103,18 @@ cudaError_t launch_weight_grad_tc(const surgeon_compressed& act, const surgeon_l
                                   const float* grad_out, float* dw, int accumulate, int share,
                                   void* workspace, cudaStream_t stream);
 
+cudaError_t launch_layer_norm(const void* x, long long rows, int channels, int dt, const float* gamma, const float* beta,
+                              float eps, void* y, float* stats, cudaStream_t stream);
+size_t layer_norm_grad_workspace(long long rows, int channels);
+cudaError_t launch_layer_norm_grad(const void* x, const void* dy, long long rows, int channels, int dt, int grad_dt,
+                                   const float* gamma, const float* stats, const void* residual, void* dx, float* dgamma,
+                                   float* dbeta, int accumulate, void* workspace, cudaStream_t stream);
+
+size_t gradient_list_workspace(int count);
+int gradient_list_overlaps(const surgeon_gradient* list, int count);
+cudaError_t launch_gradient_list(const surgeon_gradient* list, int count, int clip, double max_norm, double* norm_out,
+                                 double* gi_out, void* workspace, cudaStream_t stream);
+
 // The driver's cuTensorMapEncodeTiled, looked up through the runtime (the library carries no
 // link-time dependency on the driver library); nullptr if unavailable.
 void* tensor_map_encode_fn();
