@@ -325,6 +325,45 @@ surgeon_status surgeon_layer_norm_grad(const void* x, const void* dy, int64_t ro
                                        void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Linear layer (Eq. 1) with bias, activation and residual:
+ *   z = x W^T + bias;  y = act(z) + residual
+ * d: kind 0 (batch = rows, c_in, c_out), path 0.  x [rows, c_in] and weight [c_out, c_in]: device,
+ * bf16 (products and sums in fp32 on the tensor cores).  bias: device, fp32 [c_out], or NULL.
+ * residual [rows, c_out] (NULL: none; the skip connection) and y: out_dt; y may be residual, not
+ * x.  pre: bf16 [rows, c_out], receives z rounded, for surgeon_linear_grad; or NULL.
+ * act: GELU is z Phi(z) with the error function (Phi to 8e-8), and 0 at -infinity.
+ * workspace: scratch of the size that the query gives, not shared with a call in flight.  Its first
+ * word holds a surgeon_status afterwards: SURGEON_ERR_TIMEOUT if a bounded wait ran out, which no
+ * valid call does (calls of a few rows do not write it).  Asynchronous on cuda_stream.
+ * Errors: INVALID_ARG, BUFFER_TOO_SMALL, UNSUPPORTED (path 1; sizes beyond 2^31-1), CUDA.
+ * ---------------------------------------------------------------------------------------- */
+typedef enum { SURGEON_ACT_NONE = 0, SURGEON_ACT_RELU = 1, SURGEON_ACT_GELU = 2 } surgeon_activation;
+size_t surgeon_linear_workspace(const surgeon_layer_desc* d);      /* 0 on a bad desc */
+surgeon_status surgeon_linear(const surgeon_layer_desc* d, const void* x, const void* weight,
+                              const float* bias, surgeon_activation act, const void* residual,
+                              surgeon_dtype out_dt, void* y, void* pre, void* workspace,
+                              size_t workspace_bytes, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Backward pass of surgeon_linear but for the weights' gradient, which is surgeon_weight_grad's
+ * from the stored activation and dz:
+ *   dz = dy act'(z);  dbias = sum_t dz;  dx = dz W  (Eq. 2, first line)
+ * d, weight, workspace: as above.  dy [rows, c_out]: grad_dt.  pre: z as the forward call stored it
+ * (not read for SURGEON_ACT_NONE).  dz: fp32 [rows, c_out], the grad_out of surgeon_weight_grad.
+ * dx [rows, c_in]: dx_dt, from dz rounded to bf16 (dy itself, without a rounding, where it is
+ * bf16 and there is no activation; not rounded for up to 4 rows).  dbias: fp32 [c_out]; accumulate = 1 adds to it.
+ * dx, dz, dbias: any may be NULL (not wanted), none may be dy.  The residual's gradient is dy.
+ * ReLU's derivative at 0 is 0.  Asynchronous on cuda_stream.
+ * Errors: as above.
+ * ---------------------------------------------------------------------------------------- */
+size_t surgeon_linear_grad_workspace(const surgeon_layer_desc* d); /* 0 on a bad desc */
+surgeon_status surgeon_linear_grad(const surgeon_layer_desc* d, const void* dy, surgeon_dtype grad_dt,
+                                   const void* weight, const void* pre, surgeon_activation act,
+                                   surgeon_dtype dx_dt, void* dx, float* dz, float* dbias,
+                                   int32_t accumulate, void* workspace, size_t workspace_bytes,
+                                   void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
  * A list of gradients: the norm over all of them, Eq. 4 for each, and clipping by the norm.
  *   S_i = sum_j g_ij^2;  gi_out[i] = sqrt(S_i / n_i) (0 for n_i = 0);  norm = sqrt(sum_i S_i)
  *   clip: out_ij = g_ij * c with c = max_norm / (norm + 1e-6) where that is below 1 (rounded to

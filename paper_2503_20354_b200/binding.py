@@ -105,6 +105,15 @@ def lib():
         l.surgeon_layer_norm_grad_workspace.argtypes = [I64, I32]
         l.surgeon_layer_norm_grad.restype = C.c_int
         l.surgeon_layer_norm_grad.argtypes = [P, P, I64, I32, C.c_int, C.c_int, P, P, P, P, P, P, I32, P, C.c_size_t, P]
+        D = C.POINTER(LayerDesc)
+        l.surgeon_linear_workspace.restype = C.c_size_t
+        l.surgeon_linear_workspace.argtypes = [D]
+        l.surgeon_linear.restype = C.c_int
+        l.surgeon_linear.argtypes = [D, P, P, P, C.c_int, P, C.c_int, P, P, P, C.c_size_t, P]
+        l.surgeon_linear_grad_workspace.restype = C.c_size_t
+        l.surgeon_linear_grad_workspace.argtypes = [D]
+        l.surgeon_linear_grad.restype = C.c_int
+        l.surgeon_linear_grad.argtypes = [D, P, C.c_int, P, P, C.c_int, C.c_int, P, P, P, I32, P, C.c_size_t, P]
         l.surgeon_gradient_norm_workspace.restype = C.c_size_t
         l.surgeon_gradient_norm_workspace.argtypes = [I32]
         l.surgeon_gradient_norm.restype = C.c_int
@@ -514,6 +523,72 @@ def surgeon_layer_norm_grad(x: torch.Tensor, dy: torch.Tensor, gamma: Optional[t
                                        _stream_ptr(stream))
     if st != SURGEON_OK:
         _check(st, "surgeon_layer_norm_grad")
+    return dx
+
+
+SURGEON_ACT_NONE, SURGEON_ACT_RELU, SURGEON_ACT_GELU = 0, 1, 2
+
+
+def linear_desc(rows: int, c_in: int, c_out: int) -> LayerDesc:
+    """The descriptor of a linear layer on ``rows`` rows, tensor-core path (as ``layer_desc`` makes it of a layer)."""
+    return LayerDesc(0, int(rows), int(c_in), 1, 1, int(c_out), 1, 1, 1, 0, PATH_TENSOR_CORE, 1)
+
+
+def surgeon_linear_workspace(desc: LayerDesc) -> int:
+    return int(lib().surgeon_linear_workspace(C.byref(desc)))
+
+
+def surgeon_linear(desc: LayerDesc, x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                   act: int = SURGEON_ACT_NONE, residual: Optional[torch.Tensor] = None,
+                   out: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None,
+                   out_dtype: torch.dtype = torch.bfloat16, workspace: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """act(x W^T + bias) + residual; returns ``out`` (made here as ``out_dtype`` if None; it may be ``residual``).
+    ``x`` [rows, c_in], ``weight`` [c_out, c_in]: bf16; ``bias``: fp32; ``residual``: of the output's type.
+    ``pre``: a bf16 tensor [rows, c_out] that receives x W^T + bias for ``surgeon_linear_grad``."""
+    rows, ci, co = desc.batch, desc.c_in, desc.c_out
+    b16 = torch.bfloat16
+    xp, wp = _operand(x, "x", (rows, ci), b16), _operand(weight, "weight", (co, ci), b16)
+    if out is None:
+        out = _new((rows, co), out_dtype, x.device, stream)
+    ws = _work(workspace, surgeon_linear_workspace(desc) if workspace is None else 0, x.device, stream)
+    st = lib().surgeon_linear(desc, xp, wp, _operand(bias, "bias", (co,), torch.float32), int(act),
+                              _operand(residual, "residual", (rows, co), out.dtype), dtype_code(out.dtype),
+                              _operand(out, "out", (rows, co)), _operand(pre, "pre", (rows, co), b16), *ws,
+                              _stream_ptr(stream))
+    if st != SURGEON_OK:
+        _check(st, "surgeon_linear")
+    return out
+
+
+def surgeon_linear_grad_workspace(desc: LayerDesc) -> int:
+    return int(lib().surgeon_linear_grad_workspace(C.byref(desc)))
+
+
+def surgeon_linear_grad(desc: LayerDesc, dy: torch.Tensor, weight: Optional[torch.Tensor], pre: Optional[torch.Tensor] = None,
+                        act: int = SURGEON_ACT_NONE, dx: Optional[torch.Tensor] = None, dz: Optional[torch.Tensor] = None,
+                        dbias: Optional[torch.Tensor] = None, accumulate: bool = False,
+                        workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None,
+                        want_dx: bool = True) -> Optional[torch.Tensor]:
+    """Backward pass of ``surgeon_linear`` but for the weights' gradient; returns ``dx`` (bf16 if made here; bf16 or
+    fp32 if given; None with ``want_dx=False``).  ``dy`` [rows, c_out]: fp32 or bf16.  ``dz``: fp32 [rows, c_out], receives
+    dy act'(pre), the ``grad_out`` of ``surgeon_weight_grad``.  ``dbias``: fp32, written (``accumulate=True``: added to)."""
+    rows, ci, co = desc.batch, desc.c_in, desc.c_out
+    dyp = _operand(dy, "dy", (rows, co))
+    if not want_dx:
+        if dx is not None:
+            raise ValueError("dx given, but not wanted")
+    elif dx is None:
+        dx = _new((rows, ci), torch.bfloat16, dy.device, stream)
+    ws = _work(workspace, surgeon_linear_grad_workspace(desc) if workspace is None else 0, dy.device, stream)
+    st = lib().surgeon_linear_grad(desc, dyp, dtype_code(dy.dtype), _operand(weight, "weight", (co, ci), torch.bfloat16),
+                                   _operand(pre, "pre", (rows, co), torch.bfloat16), int(act),
+                                   SURGEON_BF16 if dx is None else dtype_code(dx.dtype), _operand(dx, "dx", (rows, ci)),
+                                   _operand(dz, "dz", (rows, co), torch.float32),
+                                   _operand(dbias, "dbias", (co,), torch.float32), 1 if accumulate else 0, *ws,
+                                   _stream_ptr(stream))
+    if st != SURGEON_OK:
+        _check(st, "surgeon_linear_grad")
     return dx
 
 

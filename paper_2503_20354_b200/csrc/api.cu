@@ -112,6 +112,14 @@ surgeon_status rows_ok(int64_t rows, int32_t channels) {
   return SURGEON_OK;
 }
 
+surgeon_status linear_ok(const surgeon_layer_desc* d) {
+  surgeon_status why;
+  if (!desc_ok(d, &why)) return why;
+  if (d->kind != 0) return SURGEON_ERR_INVALID_ARG;
+  return d->path == 0 ? SURGEON_OK : SURGEON_ERR_UNSUPPORTED;
+}
+inline bool known_activation(int act) { return act == SURGEON_ACT_NONE || act == SURGEON_ACT_RELU || act == SURGEON_ACT_GELU; }
+
 surgeon_status gradients_ok(const surgeon_gradient* list, int32_t count, bool outputs, const double* norm_out,
                             const double* gi_out, const void* workspace, size_t workspace_bytes) {
   if (count < 0 || (count > 0 && (!list || !workspace))) return SURGEON_ERR_INVALID_ARG;
@@ -368,6 +376,49 @@ surgeon_status surgeon_layer_norm_grad(const void* x, const void* dy, int64_t ro
   return launch_layer_norm_grad(x, dy, rows, channels, static_cast<int>(dt), static_cast<int>(grad_dt), gamma, stats,
                                 residual_grad, dx, dgamma, dbeta, accumulate ? 1 : 0, workspace,
                                 static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? SURGEON_OK : SURGEON_ERR_CUDA;
+}
+
+size_t surgeon_linear_workspace(const surgeon_layer_desc* d) {
+  return linear_ok(d) == SURGEON_OK ? linear_workspace(*d) : 0;
+}
+
+surgeon_status surgeon_linear(const surgeon_layer_desc* d, const void* x, const void* weight,
+                              const float* bias, surgeon_activation act, const void* residual,
+                              surgeon_dtype out_dt, void* y, void* pre, void* workspace,
+                              size_t workspace_bytes, void* cuda_stream) {
+  const surgeon_status st = linear_ok(d);
+  if (st != SURGEON_OK) return st;
+  if (!x || !weight || !y || !workspace || !known_activation(act) || !known_dtype(out_dt)) return SURGEON_ERR_INVALID_ARG;
+  if (y == x || y == weight || pre == x || pre == weight || pre == y) return SURGEON_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(weight) || !aligned16(bias) || !aligned16(residual) || !aligned16(y) || !aligned16(pre) ||
+      !aligned16(workspace))
+    return SURGEON_ERR_INVALID_ARG;
+  if (workspace_bytes < linear_workspace(*d)) return SURGEON_ERR_BUFFER_TOO_SMALL;
+  return launch_linear(*d, x, weight, bias, residual, static_cast<int>(act), static_cast<int>(out_dt), y, pre, workspace,
+                       static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? SURGEON_OK : SURGEON_ERR_CUDA;
+}
+
+size_t surgeon_linear_grad_workspace(const surgeon_layer_desc* d) {
+  return linear_ok(d) == SURGEON_OK ? linear_grad_workspace(*d) : 0;
+}
+
+surgeon_status surgeon_linear_grad(const surgeon_layer_desc* d, const void* dy, surgeon_dtype grad_dt,
+                                   const void* weight, const void* pre, surgeon_activation act,
+                                   surgeon_dtype dx_dt, void* dx, float* dz, float* dbias,
+                                   int32_t accumulate, void* workspace, size_t workspace_bytes,
+                                   void* cuda_stream) {
+  const surgeon_status st = linear_ok(d);
+  if (st != SURGEON_OK) return st;
+  if (!dy || !workspace || !known_activation(act) || !known_dtype(grad_dt) || !known_dtype(dx_dt)) return SURGEON_ERR_INVALID_ARG;
+  if ((dx && !weight) || (act != SURGEON_ACT_NONE && !pre)) return SURGEON_ERR_INVALID_ARG;
+  if (dx == dy || static_cast<const void*>(dz) == dy) return SURGEON_ERR_INVALID_ARG;
+  if (!aligned16(dy) || !aligned16(weight) || !aligned16(pre) || !aligned16(dx) || !aligned16(dz) || !aligned16(dbias) ||
+      !aligned16(workspace))
+    return SURGEON_ERR_INVALID_ARG;
+  if (workspace_bytes < linear_grad_workspace(*d)) return SURGEON_ERR_BUFFER_TOO_SMALL;
+  return launch_linear_grad(*d, dy, static_cast<int>(grad_dt), weight, pre, static_cast<int>(act), static_cast<int>(dx_dt), dx, dz,
+                            dbias, accumulate ? 1 : 0, workspace, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
+             ? SURGEON_OK : SURGEON_ERR_CUDA;
 }
 
 size_t surgeon_gradient_norm_workspace(int32_t count) {

@@ -1,0 +1,516 @@
+// Matrix product of a linear layer on the tensor cores, bias, activation and residual in its epilogue.
+//
+//   z[m, n] = sum_k a[m, k] b[n, k] + bias[n];  y = act(z) + residual;  z itself, rounded to bf16, where it is kept
+//
+// Persistent CTAs (or CTA pairs, cta_group::2: 256 rows, each CTA its 128 and half of the columns' operand) walk the output
+// tiles, columns fastest.  Warp 0 fetches operands by TMA into a ring, warp 1 issues the MMAs into one of two accumulators
+// in tensor memory, eight warps take the other one: lane = row, 32 or 64 columns at a time.  A piece of 32 rows of 128 bytes
+// goes through 4 KB of shared memory, where the residual has been fetched by TMA before, and leaves by TMA.
+// b is K-major (weights [n, k], forward) or N-major (weights [k, n], the input's gradient): both are read as they lie.
+#include <cuda.h>
+#include <string.h>
+
+#include "linear.cuh"
+#include "tc_common.cuh"
+
+namespace surgeon {
+
+namespace {
+
+using namespace tc;
+
+constexpr int kTileK = 64;                       // 128 bytes of bf16
+constexpr int kTileM = 128;                      // rows of a CTA
+constexpr int kABytes = kTileM * 128;
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = (2 + kEpiWarps) * 32;
+constexpr int kMaxStages = 8;
+constexpr int kPiece = 4096;                     // 32 rows of 128 bytes
+
+struct TileArgs {
+  int m, n, k;
+  int tile_n;                                    // columns of a tile
+  int tiles_n, tiles;
+  int stages, stage_bytes, ktiles;
+  int tmem_cols;
+  int vec_y, vec_pre;                            // rows of y (and the residual), of pre, start at 16-byte boundaries: TMA
+  int act;
+  const float* bias;
+  const void* residual;
+  void* y;
+  unsigned short* pre;
+  uint32_t* status;
+};
+
+__device__ __forceinline__ void tma_store_2d(const void* tmap, uint32_t smem_src, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(tmap), "r"(x), "r"(y),
+               "r"(smem_src)
+               : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void bulk_wait_read() {
+  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+        "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// Descriptor of an N-major operand: rows of 64 elements per k, slabs of 64 k-rows (8 KB) along n.
+__device__ __forceinline__ uint64_t make_desc_rows(uint32_t saddr) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>((kTileK * 128) >> 4) << 16;
+  d |= static_cast<uint64_t>(1024 >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(2) << 61;
+  return d;
+}
+
+// Byte offset of 16-byte chunk `j` of row `r` in a piece of rows of 128 (64) bytes, as TMA lays it out.
+template <int ROW>
+__device__ __forceinline__ uint32_t piece_at(int r, int j) {
+  return ROW == 128 ? static_cast<uint32_t>(r * 128 + ((j ^ (r & 7)) << 4)) : static_cast<uint32_t>(r * 64 + ((j ^ ((r >> 1) & 3)) << 4));
+}
+
+// DT: type of y and of the residual.  A piece of y has 64 (bf16) or 32 (fp32) columns, one of pre as many.
+template <int PAIR, int B_MN, int DT>
+__global__ void __launch_bounds__(kThreads, 1)
+linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
+              const __grid_constant__ CUtensorMap y_map, const __grid_constant__ CUtensorMap r_map,
+              const __grid_constant__ CUtensorMap p_map, const __grid_constant__ TileArgs p) {
+  constexpr int kCols = DT ? 64 : 32;            // columns of a piece
+  constexpr int kPreRow = kCols * 2;             // bytes of a row of pre's piece
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 4 + 2 * kEpiWarps];
+  __shared__ __align__(16) float s_bias[kEpiWarps][kCols];
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile uint32_t fail;
+
+  const int tid = threadIdx.x, warp = tid >> 5;
+  const uint32_t lane = lane_id();
+  const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
+  const uint32_t full = smem_u32(bars), empty = full + 8 * kMaxStages, acc_full = full + 16 * kMaxStages, acc_empty = acc_full + 16;
+  const uint32_t res_bar = acc_empty + 16;       // two per epilogue warp
+  const int b_rows = PAIR ? p.tile_n / 2 : p.tile_n;            // columns' operand: rows that this CTA fetches
+  const int tile_step = PAIR ? static_cast<int>(gridDim.x >> 1) : static_cast<int>(gridDim.x);
+  const int tile_first = PAIR ? static_cast<int>(blockIdx.x >> 1) : static_cast<int>(blockIdx.x);
+
+  if (tid == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(full + 8 * s, 1);
+      mbar_init(empty + 8 * s, 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(acc_full + 8 * a, 1);
+      mbar_init(acc_empty + 8 * a, (PAIR ? 2 : 1) * kEpiWarps);
+    }
+    for (int w = 0; w < 2 * kEpiWarps; ++w) mbar_init(res_bar + 8 * w, 1);
+    fail = 0;
+    fence_barrier_init();
+  }
+  if (warp == 1) {
+    if (PAIR) tmem_alloc_pair(smem_u32(&tmem_slot), p.tmem_cols);
+    else tmem_alloc(smem_u32(&tmem_slot), p.tmem_cols);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (PAIR) cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_slot;
+  pdl_wait();
+  pdl_trigger();
+  if (blockIdx.x == 0 && tid == 0) *p.status = 0u;              // (a wait gives up after seconds, long behind this)
+
+  const auto give_up = [&]() {
+    fail = 1;
+    atomicMax(p.status, static_cast<uint32_t>(SURGEON_ERR_TIMEOUT));
+  };
+
+  if (warp == 0) {
+    // ---- operands ----
+    if (lane == 0) {
+      tma_prefetch_desc(&a_map);
+      tma_prefetch_desc(&b_map);
+      int s = 0;
+      uint32_t phase = 1;                        // (a fresh barrier counts as passed in its phase before)
+      bool ok = true;
+      for (int t = tile_first; t < p.tiles && ok; t += tile_step) {
+        const int m0 = (t / p.tiles_n) * (PAIR ? 2 * kTileM : kTileM) + static_cast<int>(rank) * kTileM;
+        const int n0 = (t % p.tiles_n) * p.tile_n + static_cast<int>(rank) * b_rows;
+        for (int kt = 0; kt < p.ktiles; ++kt) {
+          if (fail || !mbar_wait_suspend(empty + 8 * s, phase)) { give_up(); ok = false; break; }
+          const uint32_t a_at = smem_u32(smem) + s * p.stage_bytes, b_at = a_at + kABytes, bar = full + 8 * s;
+          if (rank == 0) mbar_arrive_expect_tx(bar, (PAIR ? 2u : 1u) * static_cast<uint32_t>(p.stage_bytes));
+          if (PAIR) tma_load_2d_pair(a_at, &a_map, kt * kTileK, m0, bar);
+          else tma_load_2d(a_at, &a_map, kt * kTileK, m0, bar);
+          if (B_MN) {
+            for (int g = 0; g < b_rows / 64; ++g) {
+              if (PAIR) tma_load_2d_pair(b_at + g * (kTileK * 128), &b_map, n0 + g * 64, kt * kTileK, bar);
+              else tma_load_2d(b_at + g * (kTileK * 128), &b_map, n0 + g * 64, kt * kTileK, bar);
+            }
+          } else if (PAIR) {
+            tma_load_2d_pair(b_at, &b_map, kt * kTileK, n0, bar);
+          } else {
+            tma_load_2d(b_at, &b_map, kt * kTileK, n0, bar);
+          }
+          if (++s == p.stages) { s = 0; phase ^= 1; }
+        }
+      }
+      if (!ok)
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);       // copies in flight land
+    }
+  } else if (warp == 1) {
+    // ---- MMAs ----
+    if (lane == 0 && rank == 0) {
+      const uint32_t idesc = make_idesc(PAIR ? 2 * kTileM : kTileM, p.tile_n) | (B_MN ? 1u << 16 : 0u);
+      const uint64_t a_base = make_desc(smem_u32(smem));
+      const uint64_t b_base = B_MN ? make_desc_rows(smem_u32(smem) + kABytes) : make_desc(smem_u32(smem) + kABytes);
+      constexpr int kStepB = B_MN ? 128 : 2;
+      int s = 0, it = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int t = tile_first; t < p.tiles && ok; t += tile_step, ++it) {
+        const int acc = it & 1;
+        if (fail || !(PAIR ? mbar_wait_suspend_cluster(acc_empty + 8 * acc, ((it >> 1) & 1) ^ 1)
+                           : mbar_wait_suspend(acc_empty + 8 * acc, ((it >> 1) & 1) ^ 1))) { give_up(); break; }
+        tc_fence_after();
+        const uint32_t d = tmem_base + acc * (p.tmem_cols >> 1);
+        for (int kt = 0; kt < p.ktiles; ++kt) {
+          if (fail || !mbar_wait_suspend(full + 8 * s, phase)) { give_up(); ok = false; break; }
+          tc_fence_after();
+          const uint64_t off = static_cast<uint64_t>((s * p.stage_bytes) >> 4);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            const uint64_t da = a_base + off + 2 * kk, db = b_base + off + kStepB * kk;
+            if (PAIR) umma_bf16_pair(d, da, db, idesc, kt > 0 || kk > 0 ? 1u : 0u);
+            else umma_bf16(d, da, db, idesc, kt > 0 || kk > 0 ? 1u : 0u);
+          }
+          if (PAIR) umma_commit_pair(empty + 8 * s);
+          else umma_commit(empty + 8 * s);
+          if (++s == p.stages) { s = 0; phase ^= 1; }
+        }
+        if (PAIR) umma_commit_pair(acc_full + 8 * acc);
+        else umma_commit(acc_full + 8 * acc);
+      }
+    }
+  } else {
+    // ---- epilogue: rows of tensor memory's quarter `warp % 4`, every other piece of columns (the rest: another warp's) ----
+    const int w = warp - 2, quarter = warp & 3, half = w >> 2;
+    unsigned char* stage = smem + p.stages * p.stage_bytes + w * (p.pre ? 3 : 2) * kPiece;
+    const uint32_t stage_at = smem_u32(stage);
+    const bool has_res = p.residual != nullptr, tma_res = has_res && p.vec_y;
+    const uint32_t my_res = res_bar + 16 * w;
+    const int pieces = p.tile_n / kCols;
+    const int r = static_cast<int>(lane);        // this lane's row of a piece
+    const auto row_of = [&](int t) {
+      return (t / p.tiles_n) * (PAIR ? 2 * kTileM : kTileM) + static_cast<int>(rank) * kTileM + quarter * 32;
+    };
+    const auto exists = [&](int t, int c) {
+      return c < pieces && (t % p.tiles_n) * p.tile_n + c * kCols < p.n && row_of(t) < p.m;
+    };
+    // the warp's next piece whose residual is to be fetched
+    int ft = tile_first, fc = half;
+    uint32_t fetched = 0;
+    const auto fetch_next = [&]() {              // (lane 0)
+      while (ft < p.tiles && !exists(ft, fc)) { ft += tile_step; fc = half; }
+      if (ft >= p.tiles) return;
+      const uint32_t buf = fetched & 1;
+      mbar_arrive_expect_tx(my_res + 8 * buf, kPiece);
+      tma_load_2d(stage_at + buf * kPiece, &r_map, (ft % p.tiles_n) * p.tile_n + fc * kCols, row_of(ft), my_res + 8 * buf);
+      ++fetched;
+      fc += 2;
+    };
+    if (tma_res && lane == 0) fetch_next();
+    int it = 0;
+    uint32_t piece = 0;
+    bool ok = true;
+    for (int t = tile_first; t < p.tiles && ok; t += tile_step, ++it) {
+      const int n0 = (t % p.tiles_n) * p.tile_n, m0 = row_of(t);
+      const int acc = it & 1;
+      bool waited = false;
+      for (int c = half; exists(t, c); c += 2) {
+        const uint32_t buf = piece & 1;
+        unsigned char* mine = stage + buf * kPiece;
+        const int x = n0 + c * kCols;
+        if (lane == 0) {
+          if (has_res || p.pre) bulk_wait_read<0>();            // what left the other places has been read
+          else bulk_wait_read<1>();
+          if (tma_res) fetch_next();
+        }
+        if (p.bias) {                            // the piece's bias, where every lane can read all of it
+#pragma unroll
+          for (int i = 0; i < kCols; i += 32) {
+            const int n = x + i + r;
+            s_bias[w][i + r] = n < p.n ? __ldg(p.bias + n) : 0.0f;
+          }
+        }
+        __syncwarp();
+        if (has_res && !tma_res) {
+          for (int q = 0; q < 32 && m0 + q < p.m; ++q) {
+            const long long at = static_cast<long long>(m0 + q) * p.n + x;
+            for (int c1 = r; c1 < kCols && x + c1 < p.n; c1 += 32) {
+              if (DT) *reinterpret_cast<unsigned short*>(mine + piece_at<128>(q, c1 >> 3) + (c1 & 7) * 2) =
+                  static_cast<const unsigned short*>(p.residual)[at + c1];
+              else *reinterpret_cast<float*>(mine + piece_at<128>(q, c1 >> 2) + (c1 & 3) * 4) =
+                  static_cast<const float*>(p.residual)[at + c1];
+            }
+          }
+          __syncwarp();
+        }
+        if (!waited) {
+          // (all lanes go the same way: behind are instructions of the whole warp)
+          if (!__all_sync(0xFFFFFFFFu, !fail && mbar_wait_suspend(acc_full + 8 * acc, (it >> 1) & 1))) { give_up(); ok = false; break; }
+          tc_fence_after();
+          waited = true;
+        }
+        uint32_t v[kCols];
+        {
+          const uint32_t at = tmem_base + acc * (p.tmem_cols >> 1) + (static_cast<uint32_t>(quarter) << 21) + c * kCols;
+          tmem_ld32(at, *reinterpret_cast<uint32_t (*)[32]>(v));
+          if constexpr (DT == 1) tmem_ld32(at + 32, *reinterpret_cast<uint32_t (*)[32]>(v + 32));
+          tmem_ld_wait();
+        }
+        if (!exists(t, c + 2)) {                 // the accumulator has been read: it may be written again
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if (PAIR) mbar_arrive_rank0(acc_empty + 8 * acc);
+            else mbar_arrive(acc_empty + 8 * acc);
+          }
+        }
+        if (p.bias) {
+#pragma unroll
+          for (int j = 0; j < kCols / 4; ++j) {
+            const float4 b = *reinterpret_cast<const float4*>(&s_bias[w][4 * j]);
+            v[4 * j] = __float_as_uint(__uint_as_float(v[4 * j]) + b.x);
+            v[4 * j + 1] = __float_as_uint(__uint_as_float(v[4 * j + 1]) + b.y);
+            v[4 * j + 2] = __float_as_uint(__uint_as_float(v[4 * j + 2]) + b.z);
+            v[4 * j + 3] = __float_as_uint(__uint_as_float(v[4 * j + 3]) + b.w);
+          }
+        }
+        if (p.pre) {
+#pragma unroll
+          for (int j = 0; j < kCols / 8; ++j) {
+            uint32_t o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              o[i] = to_bf16x2(__uint_as_float(v[8 * j + 2 * i]), __uint_as_float(v[8 * j + 2 * i + 1]));
+            *reinterpret_cast<uint4*>(stage + 2 * kPiece + piece_at<kPreRow>(r, j)) = make_uint4(o[0], o[1], o[2], o[3]);
+          }
+        }
+        if (p.act == kActGelu) {
+#pragma unroll
+          for (int i = 0; i < kCols; ++i) v[i] = __float_as_uint(activate<kActGelu>(__uint_as_float(v[i])));
+        } else if (p.act == kActRelu) {
+#pragma unroll
+          for (int i = 0; i < kCols; ++i) v[i] = __float_as_uint(activate<kActRelu>(__uint_as_float(v[i])));
+        }
+        if (tma_res && !__all_sync(0xFFFFFFFFu, !fail && mbar_wait_suspend(my_res + 8 * buf, (piece >> 1) & 1))) {
+          give_up();
+          ok = false;
+          break;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          uint4* at = reinterpret_cast<uint4*>(mine + piece_at<128>(r, j));
+          if constexpr (DT == 1) {
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[8 * j + i]);
+            if (has_res) {
+              const uint4 q = *at;
+              f[0] += bf16_lo(q.x); f[1] += bf16_hi(q.x); f[2] += bf16_lo(q.y); f[3] += bf16_hi(q.y);
+              f[4] += bf16_lo(q.z); f[5] += bf16_hi(q.z); f[6] += bf16_lo(q.w); f[7] += bf16_hi(q.w);
+            }
+            *at = make_uint4(to_bf16x2(f[0], f[1]), to_bf16x2(f[2], f[3]), to_bf16x2(f[4], f[5]), to_bf16x2(f[6], f[7]));
+          } else {
+            float4 f = make_float4(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1]), __uint_as_float(v[4 * j + 2]),
+                                   __uint_as_float(v[4 * j + 3]));
+            if (has_res) {
+              const float4 q = *reinterpret_cast<const float4*>(at);
+              f.x += q.x; f.y += q.y; f.z += q.z; f.w += q.w;
+            }
+            *reinterpret_cast<float4*>(at) = f;
+          }
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+          if (p.vec_y) tma_store_2d(&y_map, stage_at + buf * kPiece, x, m0);
+          if (p.pre && p.vec_pre) tma_store_2d(&p_map, stage_at + 2 * kPiece, x, m0);
+          bulk_commit();
+        }
+        if (!p.vec_y || (p.pre && !p.vec_pre)) {
+          for (int q = 0; q < 32 && m0 + q < p.m; ++q) {
+            const long long at = static_cast<long long>(m0 + q) * p.n + x;
+            for (int c1 = r; c1 < kCols && x + c1 < p.n; c1 += 32) {
+              if (!p.vec_y) {
+                if (DT) static_cast<unsigned short*>(p.y)[at + c1] =
+                    *reinterpret_cast<const unsigned short*>(mine + piece_at<128>(q, c1 >> 3) + (c1 & 7) * 2);
+                else static_cast<float*>(p.y)[at + c1] =
+                    *reinterpret_cast<const float*>(mine + piece_at<128>(q, c1 >> 2) + (c1 & 3) * 4);
+              }
+              if (p.pre && !p.vec_pre)
+                p.pre[at + c1] = *reinterpret_cast<const unsigned short*>(stage + 2 * kPiece + piece_at<kPreRow>(q, c1 >> 3) + (c1 & 7) * 2);
+            }
+          }
+          __syncwarp();                          // before the next piece takes the place
+        }
+        ++piece;
+      }
+      if (ok && !waited) {                       // no piece of this tile: pass the accumulator on
+        if (!__all_sync(0xFFFFFFFFu, !fail && mbar_wait_suspend(acc_full + 8 * acc, (it >> 1) & 1))) { give_up(); break; }
+        if (lane == 0) {
+          if (PAIR) mbar_arrive_rank0(acc_empty + 8 * acc);
+          else mbar_arrive(acc_empty + 8 * acc);
+        }
+      }
+    }
+    if (lane == 0) {
+      if (!ok)
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);       // copies in flight land
+      bulk_wait_read<0>();                       // the pieces have left shared memory
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (PAIR) cluster_sync_all();
+  if (warp == 1) {
+    tc_fence_after();
+    if (PAIR) tmem_dealloc_pair(tmem_base, p.tmem_cols);
+    else tmem_dealloc(tmem_base, p.tmem_cols);
+  }
+}
+
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// A row-major matrix [rows][cols], rows `pitch` elements apart, in boxes of box_cols x box_rows.
+bool encode(CUtensorMap* map, const void* base, int dt, long long rows, long long cols, long long pitch, int box_rows, int box_cols) {
+  const EncodeFn fn = reinterpret_cast<EncodeFn>(tensor_map_encode_fn());
+  if (!fn) return false;
+  const int size = dt == 0 ? 4 : 2;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(pitch) * size};
+  const cuuint32_t box[2] = {static_cast<cuuint32_t>(box_cols), static_cast<cuuint32_t>(box_rows)};
+  const cuuint32_t step[2] = {1, 1};
+  return fn(map, dt == 0 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims,
+            strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            box_cols * size == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Shape {
+  int pair, tile_n;
+};
+
+// The tile with the shortest estimate: waves of tiles times a tile's clocks (tile_n per 64 of k while the tensor cores are the
+// bound, the operands' bytes otherwise, and its epilogue where that is longer).
+Shape choose_tile(const Product& p) {
+  static const Shape all[] = {{1, 256}, {1, 128}, {0, 256}, {0, 128}, {0, 64}};
+  const int sms = sm_count();
+  const long long ktiles = (p.k + kTileK - 1) / kTileK;
+  Shape best = all[0];
+  double least = 0.0;
+  for (const Shape& s : all) {
+    const long long rows = s.pair ? 2 * kTileM : kTileM;
+    const long long tiles = ((p.m + rows - 1) / rows) * ((p.n + s.tile_n - 1) / s.tile_n);
+    const long long at_once = s.pair ? sms / 2 : sms;
+    const double waves = static_cast<double>((tiles + at_once - 1) / at_once);
+    const double bytes = kABytes + (s.pair ? s.tile_n / 2 : s.tile_n) * 128.0;
+    const double loop = ktiles * (s.tile_n > bytes / 90.0 ? s.tile_n : bytes / 90.0);
+    const double epilogue = s.tile_n * 8.0;
+    const double cost = waves * (loop > epilogue ? loop : epilogue) + (loop > epilogue ? epilogue : loop);
+    if (least == 0.0 || cost < least) {
+      least = cost;
+      best = s;
+    }
+  }
+  return best;
+}
+
+template <int PAIR, int B_MN, int DT>
+cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream_t stream) {
+  constexpr int kCols = DT ? 64 : 32;
+  TileArgs t = {};
+  t.m = p.m; t.n = p.n; t.k = p.k;
+  t.tile_n = tile_n;
+  const int rows = PAIR ? 2 * kTileM : kTileM;
+  t.tiles_n = (p.n + tile_n - 1) / tile_n;
+  t.tiles = (p.m + rows - 1) / rows * t.tiles_n;
+  t.ktiles = (p.k + kTileK - 1) / kTileK;
+  const int b_rows = PAIR ? tile_n / 2 : tile_n;
+  t.stage_bytes = kABytes + b_rows * 128;
+  const int staging = kEpiWarps * (p.pre ? 3 : 2) * kPiece;
+  t.stages = (227 * 1024 - 4096 - staging) / t.stage_bytes;
+  if (t.stages > kMaxStages) t.stages = kMaxStages;
+  if (t.stages > t.ktiles + 2) t.stages = t.ktiles + 2;
+  t.tmem_cols = 2 * tile_n;
+  const int size = DT ? 2 : 4;
+  t.vec_y = (static_cast<long long>(p.n) * size) % 16 == 0;
+  t.vec_pre = p.n % 8 == 0;
+  t.act = p.act;
+  t.bias = p.bias;
+  t.residual = p.residual;
+  t.y = p.y;
+  t.pre = static_cast<unsigned short*>(p.pre);
+  t.status = status;
+  CUtensorMap maps[5];
+  memset(maps, 0, sizeof(maps));
+  bool ok = encode(&maps[0], p.a, 1, p.m, p.k, p.lda, kTileM, kTileK);
+  ok = ok && (B_MN ? encode(&maps[1], p.b, 1, p.k, p.n, p.ldb, kTileK, 64) : encode(&maps[1], p.b, 1, p.n, p.k, p.ldb, b_rows, kTileK));
+  if (t.vec_y) {
+    ok = ok && encode(&maps[2], p.y, DT, p.m, p.n, p.n, 32, kCols);
+    if (p.residual) ok = ok && encode(&maps[3], p.residual, DT, p.m, p.n, p.n, 32, kCols);
+  }
+  if (p.pre && t.vec_pre) ok = ok && encode(&maps[4], p.pre, 1, p.m, p.n, p.n, 32, kCols);
+  if (!ok) return cudaErrorInvalidValue;
+  const int smem = 1024 + t.stages * t.stage_bytes + staging;
+  const auto kernel = linear_kernel<PAIR, B_MN, DT>;
+  cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
+  if (e != cudaSuccess) return e;
+  const int at_once = PAIR ? sm_count() / 2 : sm_count();
+  const int groups = t.tiles < at_once ? t.tiles : at_once;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(PAIR ? 2 * groups : groups);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = static_cast<size_t>(smem);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = PAIR ? 2 : 1;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  e = cudaLaunchKernelEx(&cfg, kernel, maps[0], maps[1], maps[2], maps[3], maps[4], t);
+  note_launches(1);
+  return e;
+}
+
+}  // namespace
+
+cudaError_t launch_product(const Product& p, uint32_t* status, cudaStream_t stream) {
+  const Shape s = choose_tile(p);
+#define SURGEON_PRODUCT(PAIR)                                                                              \
+  (p.b_mn ? (p.dt ? launch_as<PAIR, 1, 1>(p, s.tile_n, status, stream) : launch_as<PAIR, 1, 0>(p, s.tile_n, status, stream)) \
+          : (p.dt ? launch_as<PAIR, 0, 1>(p, s.tile_n, status, stream) : launch_as<PAIR, 0, 0>(p, s.tile_n, status, stream)))
+  return s.pair ? SURGEON_PRODUCT(1) : SURGEON_PRODUCT(0);
+#undef SURGEON_PRODUCT
+}
+
+}  // namespace surgeon

@@ -110,6 +110,13 @@ cudaError_t launch_layer_norm_grad(const void* x, const void* dy, long long rows
                                    const float* gamma, const float* stats, const void* residual, void* dx, float* dgamma,
                                    float* dbeta, int accumulate, void* workspace, cudaStream_t stream);
 
+size_t linear_workspace(const surgeon_layer_desc& d);
+cudaError_t launch_linear(const surgeon_layer_desc& d, const void* x, const void* weight, const float* bias, const void* residual,
+                          int act, int dt, void* y, void* pre, void* workspace, cudaStream_t stream);
+size_t linear_grad_workspace(const surgeon_layer_desc& d);
+cudaError_t launch_linear_grad(const surgeon_layer_desc& d, const void* dy, int grad_dt, const void* weight, const void* pre, int act,
+                               int dx_dt, void* dx, float* dz, float* dbias, int accumulate, void* workspace, cudaStream_t stream);
+
 size_t gradient_list_workspace(int count);
 int gradient_list_overlaps(const surgeon_gradient* list, int count);
 cudaError_t launch_gradient_list(const surgeon_gradient* list, int count, int clip, double max_norm, double* norm_out,
