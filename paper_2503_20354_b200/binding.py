@@ -434,16 +434,16 @@ def surgeon_weight_grad(act: CompressedActivation, desc: LayerDesc, grad_out: to
 # (Eq. 2, first line), and the list of gradients that a step ends with
 # ---------------------------------------------------------------------------------------------
 
-def _operand(t: Optional[torch.Tensor], name: str, shape=None, dtype=None):
-    """Checks one tensor of a call (None: left out) and returns its address."""
+def _operand(t: Optional[torch.Tensor], name: str, device: int, shape=None, dtype=None):
+    """Checks one tensor of a call (None: left out) and returns its address.  ``device``: the current one."""
     if t is None:
         return None
-    if not t.is_cuda or not t.is_contiguous():
+    if t.get_device() != device or not t.is_contiguous():
+        if t.is_cuda and t.is_contiguous():
+            raise ValueError("%s is on %s, which is not the current device" % (name, t.device))
         raise ValueError("%s must be a contiguous CUDA tensor" % name)
-    if t.device.index != torch._C._cuda_getDevice():
-        raise ValueError("%s is on %s, which is not the current device" % (name, t.device))
-    if shape is not None and tuple(t.shape) != shape:
-        raise ValueError("%s must have the shape %s, got %s" % (name, shape, tuple(t.shape)))
+    if shape is not None and t.shape != shape:
+        raise ValueError("%s must have the shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
     if dtype is not None and t.dtype != dtype:
         raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
     return t.data_ptr()
@@ -462,13 +462,14 @@ def _work(workspace: Optional[torch.Tensor], nbytes: int, device, stream: Option
     """Address and size of a call's scratch, which is made here where the caller passed none."""
     if workspace is None:
         workspace = _new(max(int(nbytes), 16), torch.uint8, device, stream)
-    return _operand(workspace, "workspace"), workspace.numel() * workspace.element_size()
+    return _operand(workspace, "workspace", torch._C._cuda_getDevice()), workspace.numel() * workspace.element_size()
 
 
 def _rows(t: torch.Tensor, name: str):
     if t.dim() < 1 or t.shape[-1] == 0:
         raise ValueError("%s must have channels in its last dimension" % name)
-    return t.numel() // t.shape[-1], t.shape[-1]
+    channels = t.shape[-1]
+    return t.numel() // channels, channels
 
 
 def surgeon_layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
@@ -478,14 +479,15 @@ def surgeon_layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, be
     ``gamma``, ``beta``: fp32.  ``stats``: an fp32 tensor [2, rows] that receives the means and the reciprocal
     standard deviations for ``surgeon_layer_norm_grad``."""
     rows, channels = _rows(x, "x")
+    dev, f32 = torch._C._cuda_getDevice(), torch.float32
+    xp = _operand(x, "x", dev)
     dt = dtype_code(x.dtype)
-    xp = _operand(x, "x")
     if out is None:
         out = _new(x.shape, x.dtype, x.device, stream)
-    st = lib().surgeon_layer_norm(xp, rows, channels, dt, _operand(gamma, "gamma", (channels,), torch.float32),
-                                  _operand(beta, "beta", (channels,), torch.float32), float(eps),
-                                  _operand(out, "out", tuple(x.shape), x.dtype),
-                                  _operand(stats, "stats", (2, rows), torch.float32), _stream_ptr(stream))
+    st = lib().surgeon_layer_norm(xp, rows, channels, dt, _operand(gamma, "gamma", dev, (channels,), f32),
+                                  _operand(beta, "beta", dev, (channels,), f32), eps,
+                                  _operand(out, "out", dev, x.shape, x.dtype),
+                                  _operand(stats, "stats", dev, (2, rows), f32), _stream_ptr(stream))
     if st != SURGEON_OK:
         _check(st, "surgeon_layer_norm")
     return out
@@ -504,22 +506,22 @@ def surgeon_layer_norm_grad(x: torch.Tensor, dy: torch.Tensor, gamma: Optional[t
     ``want_dx=False``).  ``residual_grad`` (dy's shape and type) is added to it; ``dx`` may be ``dy`` or
     ``residual_grad``.  ``dgamma``, ``dbeta``: fp32, written (``accumulate=True``: added to) where given."""
     rows, channels = _rows(x, "x")
-    shape = tuple(x.shape)
-    xp, dyp = _operand(x, "x"), _operand(dy, "dy", shape)
+    dev, f32, shape, gt = torch._C._cuda_getDevice(), torch.float32, x.shape, dy.dtype
+    xp, dyp = _operand(x, "x", dev), _operand(dy, "dy", dev, shape)
     if not want_dx:
         if dx is not None:
             raise ValueError("dx given, but not wanted")
     elif dx is None:
-        dx = _new(shape, dy.dtype, dy.device, stream)
+        dx = _new(shape, gt, dy.device, stream)
     ws = None, 0
     if dgamma is not None or dbeta is not None:
         ws = _work(workspace, surgeon_layer_norm_grad_workspace(rows, channels) if workspace is None else 0, x.device, stream)
-    f32 = torch.float32
-    st = lib().surgeon_layer_norm_grad(xp, dyp, rows, channels, dtype_code(x.dtype), dtype_code(dy.dtype),
-                                       _operand(gamma, "gamma", (channels,), f32), _operand(stats, "stats", (2, rows), f32),
-                                       _operand(residual_grad, "residual_grad", shape, dy.dtype),
-                                       _operand(dx, "dx", shape, dy.dtype), _operand(dgamma, "dgamma", (channels,), f32),
-                                       _operand(dbeta, "dbeta", (channels,), f32), 1 if accumulate else 0, *ws,
+    st = lib().surgeon_layer_norm_grad(xp, dyp, rows, channels, dtype_code(x.dtype), dtype_code(gt),
+                                       _operand(gamma, "gamma", dev, (channels,), f32),
+                                       _operand(stats, "stats", dev, (2, rows), f32),
+                                       _operand(residual_grad, "residual_grad", dev, shape, gt),
+                                       _operand(dx, "dx", dev, shape, gt), _operand(dgamma, "dgamma", dev, (channels,), f32),
+                                       _operand(dbeta, "dbeta", dev, (channels,), f32), 1 if accumulate else 0, *ws,
                                        _stream_ptr(stream))
     if st != SURGEON_OK:
         _check(st, "surgeon_layer_norm_grad")
@@ -547,14 +549,14 @@ def surgeon_linear(desc: LayerDesc, x: torch.Tensor, weight: torch.Tensor, bias:
     ``x`` [rows, c_in], ``weight`` [c_out, c_in]: bf16; ``bias``: fp32; ``residual``: of the output's type.
     ``pre``: a bf16 tensor [rows, c_out] that receives x W^T + bias for ``surgeon_linear_grad``."""
     rows, ci, co = desc.batch, desc.c_in, desc.c_out
-    b16 = torch.bfloat16
-    xp, wp = _operand(x, "x", (rows, ci), b16), _operand(weight, "weight", (co, ci), b16)
+    dev, b16 = torch._C._cuda_getDevice(), torch.bfloat16
+    xp, wp = _operand(x, "x", dev, (rows, ci), b16), _operand(weight, "weight", dev, (co, ci), b16)
     if out is None:
         out = _new((rows, co), out_dtype, x.device, stream)
     ws = _work(workspace, surgeon_linear_workspace(desc) if workspace is None else 0, x.device, stream)
-    st = lib().surgeon_linear(desc, xp, wp, _operand(bias, "bias", (co,), torch.float32), int(act),
-                              _operand(residual, "residual", (rows, co), out.dtype), dtype_code(out.dtype),
-                              _operand(out, "out", (rows, co)), _operand(pre, "pre", (rows, co), b16), *ws,
+    st = lib().surgeon_linear(desc, xp, wp, _operand(bias, "bias", dev, (co,), torch.float32), int(act),
+                              _operand(residual, "residual", dev, (rows, co), out.dtype), dtype_code(out.dtype),
+                              _operand(out, "out", dev, (rows, co)), _operand(pre, "pre", dev, (rows, co), b16), *ws,
                               _stream_ptr(stream))
     if st != SURGEON_OK:
         _check(st, "surgeon_linear")
@@ -574,18 +576,19 @@ def surgeon_linear_grad(desc: LayerDesc, dy: torch.Tensor, weight: Optional[torc
     fp32 if given; None with ``want_dx=False``).  ``dy`` [rows, c_out]: fp32 or bf16.  ``dz``: fp32 [rows, c_out], receives
     dy act'(pre), the ``grad_out`` of ``surgeon_weight_grad``.  ``dbias``: fp32, written (``accumulate=True``: added to)."""
     rows, ci, co = desc.batch, desc.c_in, desc.c_out
-    dyp = _operand(dy, "dy", (rows, co))
+    dev = torch._C._cuda_getDevice()
+    dyp = _operand(dy, "dy", dev, (rows, co))
     if not want_dx:
         if dx is not None:
             raise ValueError("dx given, but not wanted")
     elif dx is None:
         dx = _new((rows, ci), torch.bfloat16, dy.device, stream)
     ws = _work(workspace, surgeon_linear_grad_workspace(desc) if workspace is None else 0, dy.device, stream)
-    st = lib().surgeon_linear_grad(desc, dyp, dtype_code(dy.dtype), _operand(weight, "weight", (co, ci), torch.bfloat16),
-                                   _operand(pre, "pre", (rows, co), torch.bfloat16), int(act),
-                                   SURGEON_BF16 if dx is None else dtype_code(dx.dtype), _operand(dx, "dx", (rows, ci)),
-                                   _operand(dz, "dz", (rows, co), torch.float32),
-                                   _operand(dbias, "dbias", (co,), torch.float32), 1 if accumulate else 0, *ws,
+    st = lib().surgeon_linear_grad(desc, dyp, dtype_code(dy.dtype), _operand(weight, "weight", dev, (co, ci), torch.bfloat16),
+                                   _operand(pre, "pre", dev, (rows, co), torch.bfloat16), int(act),
+                                   SURGEON_BF16 if dx is None else dtype_code(dx.dtype), _operand(dx, "dx", dev, (rows, ci)),
+                                   _operand(dz, "dz", dev, (rows, co), torch.float32),
+                                   _operand(dbias, "dbias", dev, (co,), torch.float32), 1 if accumulate else 0, *ws,
                                    _stream_ptr(stream))
     if st != SURGEON_OK:
         _check(st, "surgeon_linear_grad")
@@ -624,18 +627,18 @@ def surgeon_gradient_norm_workspace(grads) -> int:
 
 def _list_call(grads, norm, gi, workspace, stream, new_gi):
     lst = grads if isinstance(grads, GradientList) else GradientList(grads)
-    device = lst.device
+    dev, device = torch._C._cuda_getDevice(), lst.device
     if device is None:
-        device = norm.device if norm is not None else torch.device("cuda", torch._C._cuda_getDevice())
-    if device.index != torch._C._cuda_getDevice():
+        device = norm.device if norm is not None else torch.device("cuda", dev)
+    if device.index != dev:
         raise ValueError("the gradients are on %s, which is not the current device" % device)
     if norm is None:
         norm = _new(1, torch.float64, device, stream)
     if gi is None and new_gi:
         gi = _new(len(lst), torch.float64, device, stream)
     ws = _work(workspace, surgeon_gradient_norm_workspace(lst) if workspace is None else 0, device, stream)
-    return (lst, norm, gi, (_operand(norm, "norm", (1,), torch.float64),
-                            _operand(gi, "gi", (len(lst),), torch.float64), *ws, _stream_ptr(stream)))
+    return (lst, norm, gi, (_operand(norm, "norm", dev, (1,), torch.float64),
+                            _operand(gi, "gi", dev, (len(lst),), torch.float64), *ws, _stream_ptr(stream)))
 
 
 def surgeon_gradient_norm(grads, norm: Optional[torch.Tensor] = None, gi: Optional[torch.Tensor] = None,

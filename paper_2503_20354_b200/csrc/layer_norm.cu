@@ -8,6 +8,7 @@
 // centred squares (of E[x^2] - mean^2 nothing is left where the mean is large).  All sums are fp32, in a fixed order.
 // Forward and backward are bound by HBM: 2 and 3 (4 with the residual's gradient) passes over the row.
 #include "row_vectors.cuh"
+#include "tc_common.cuh"
 
 namespace surgeon {
 
@@ -131,114 +132,6 @@ ln_forward_long_kernel(const void* __restrict__ x, long long rows, int channels,
   }
 }
 
-// A CTA takes every gridDim.x-th group of rows and keeps its columns' sums in registers; at the end it leaves one row
-// of partial sums per array, partial[cta][0: dgamma, 1: dbeta][channels].
-template <int XDT, int GDT, int E, int V, int TPR>
-__global__ void __launch_bounds__(TPR > 32 ? TPR : kLnThreads)
-ln_backward_kernel(const void* __restrict__ x, const void* __restrict__ dy, long long rows, int channels,
-                   const float* __restrict__ gamma, const float* __restrict__ stats,
-                   const void* __restrict__ residual, void* __restrict__ dx, float* __restrict__ partial) {
-  constexpr int kThreads = TPR > 32 ? TPR : kLnThreads;
-  constexpr int kRows = kThreads / TPR;
-  __shared__ float buf[4][TPR > 32 ? TPR / 32 : 1];
-  __shared__ float sums[kRows > 1 ? kThreads * V * E : 1];
-  pdl_wait();
-  pdl_trigger();
-  const int l = static_cast<int>(threadIdx.x) % TPR, group = static_cast<int>(threadIdx.x) / TPR;
-  const float inv_c = 1.0f / static_cast<float>(channels);
-  float dg[V][E], db[V][E];
-#pragma unroll
-  for (int v = 0; v < V; ++v)
-#pragma unroll
-    for (int e = 0; e < E; ++e) dg[v][e] = db[v][e] = 0.0f;
-  int turn = 0;
-  for (long long first = static_cast<long long>(blockIdx.x) * kRows; first < rows;
-       first += static_cast<long long>(gridDim.x) * kRows) {
-    const long long row = first + group;
-    const bool on = row < rows;
-    const float mean = on ? stats[row] : 0.0f, r = on ? stats[rows + row] : 0.0f;
-    float xh[V][E], g[V][E];
-    float c1 = 0.0f, c2 = 0.0f;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int c = (v * TPR + l) * E;
-      if (on && c < channels) {
-        load_elems<XDT, E>(x, row * channels + c, xh[v]);
-        load_elems<GDT, E>(dy, row * channels + c, g[v]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) xh[v][e] = mean, g[v][e] = 0.0f;
-      }
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int c = (v * TPR + l) * E;
-      float w[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) w[e] = 1.0f;
-      if (gamma && c < channels) load_elems<0, E>(gamma, c, w);
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        xh[v][e] = (xh[v][e] - mean) * r;
-        dg[v][e] += g[v][e] * xh[v][e];
-        db[v][e] += g[v][e];
-        g[v][e] *= w[e];
-        c1 += g[v][e];
-        c2 += g[v][e] * xh[v][e];
-      }
-    }
-    c1 = row_sum<TPR>(c1, buf[turn]) * inv_c;
-    c2 = row_sum<TPR>(c2, buf[turn + 1]) * inv_c;
-    turn ^= 2;
-    if (on && dx) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int c = (v * TPR + l) * E;
-        if (c < channels) {
-          float o[E];
-#pragma unroll
-          for (int e = 0; e < E; ++e) o[e] = r * (g[v][e] - c1 - xh[v][e] * c2);
-          if (residual) {
-            float k[E];
-            load_elems<GDT, E>(residual, row * channels + c, k);
-#pragma unroll
-            for (int e = 0; e < E; ++e) o[e] += k[e];
-          }
-          store_elems<GDT, E>(dx, row * channels + c, o);
-        }
-      }
-    }
-  }
-  if (!partial) return;
-  float* out = partial + static_cast<long long>(blockIdx.x) * 2 * channels;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    if constexpr (kRows == 1) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int c = (v * TPR + l) * E;
-        if (c < channels) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) out[k * channels + c + e] = k ? db[v][e] : dg[v][e];
-        }
-      }
-    } else {
-      __syncthreads();
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int e = 0; e < E; ++e) sums[group * (V * TPR * E) + (v * TPR + l) * E + e] = k ? db[v][e] : dg[v][e];
-      __syncthreads();
-      for (int c = threadIdx.x; c < channels; c += kThreads) {
-        float t = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) t += sums[i * (V * TPR * E) + c];
-        out[k * channels + c] = t;
-      }
-    }
-  }
-}
-
 // Rows too long for registers: the row's two sums, then dx; the columns' sums are another kernel's.
 template <int XDT, int GDT>
 __global__ void __launch_bounds__(1024)
@@ -323,6 +216,336 @@ ln_final_kernel(const float* __restrict__ partial, int n_partials, int channels,
   }
 }
 
+// ---- a ring of chunks in shared memory ----
+//
+// A chunk is some consecutive rows, one contiguous piece of memory.  A producer warp fetches chunks of x (and dy,
+// residual_grad) with bulk copies, rounded to 16-byte boundaries on either side, so that rows of any width arrive with wide
+// asynchronous loads and some 150 KB per SM are in flight.  Two groups of eight warps take the chunks in turn.  One CTA per SM.
+
+constexpr int kRingGroups = 2, kGroupThreads = 256;
+constexpr int kRingThreads = kRingGroups * kGroupThreads + 32;
+constexpr int kSmemBytes = 224 * 1024;           // ring and parameters
+constexpr int kMaxRing = 8;
+
+struct RingArgs {
+  const void* src[3];
+  int elem[3];                                   // bytes of an element
+  int at[3];                                     // where the array's rows lie in a stage
+  int n_src;
+  long long rows;
+  int channels;
+  int chunk_rows, stages, stage_bytes;
+  int params;                                    // parameters' place in shared memory
+  long long chunks;
+};
+
+// Where row `row` of array i starts behind the 16-byte boundary that its copy begins at.
+__device__ __forceinline__ uint32_t ring_shift(const RingArgs& a, int i, long long row) {
+  return static_cast<uint32_t>(row * a.channels * a.elem[i]) & 15u;
+}
+
+// The producer warp: every gridDim.x-th chunk into the ring.
+__device__ __forceinline__ void ring_produce(const RingArgs& a, unsigned char* ring, uint32_t full, uint32_t empty) {
+  const bool leader = tc::elected();
+  int s = 0;
+  uint32_t phase = 1;
+  for (long long chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
+    if (!__all_sync(0xFFFFFFFFu, tc::mbar_wait_suspend(empty + 8 * s, phase))) return;
+    const long long row = chunk * a.chunk_rows;
+    const long long here = a.rows - row < a.chunk_rows ? a.rows - row : a.chunk_rows;
+    if (leader) {
+      uint32_t bytes[3], total = 0;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        if (i >= a.n_src) break;
+        const long long pitch = static_cast<long long>(a.channels) * a.elem[i];
+        const long long begin = row * pitch, end = begin + here * pitch, lo = begin & ~15LL, last = (a.rows * pitch) & ~15LL;
+        long long hi = (end + 15) & ~15LL;
+        if (hi > last) hi = last > lo ? last : lo;              // the tensor's last bytes, below 16, one by one
+        for (long long b = hi > begin ? hi : begin; b < end; b += 2)
+          *reinterpret_cast<unsigned short*>(ring + s * a.stage_bytes + a.at[i] + (b - lo)) =
+              *reinterpret_cast<const unsigned short*>(static_cast<const unsigned char*>(a.src[i]) + b);
+        bytes[i] = static_cast<uint32_t>(hi - lo);
+        total += bytes[i];
+      }
+      tc::mbar_arrive_expect_tx(full + 8 * s, total);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        if (i >= a.n_src) break;
+        if (bytes[i])
+          tc::bulk_load(tc::smem_u32(ring + s * a.stage_bytes + a.at[i]),
+                        static_cast<const unsigned char*>(a.src[i]) + ((row * a.channels * a.elem[i]) & ~15LL), bytes[i], full + 8 * s);
+      }
+    }
+    __syncwarp();
+    if (++s == a.stages) { s = 0; phase ^= 1; }
+  }
+}
+
+// Sum over the TPR threads of a row inside a group of 256; `buf` [2][8], `turn` flips with every call.
+template <int TPR>
+__device__ __forceinline__ float ring_sum(float v, float* buf, int& turn, int group) {
+  v = lanes_sum<(TPR < 32 ? TPR : 32)>(v);
+  if constexpr (TPR > 32) {
+    float* b = buf + (group * 2 + turn) * 8;
+    if ((threadIdx.x & 31) == 0) b[(threadIdx.x >> 5) & 7] = v;
+    asm volatile("bar.sync %0, 256;" ::"r"(group + 1) : "memory");
+    v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) v += b[w];
+    turn ^= 1;
+  }
+  return v;
+}
+
+__device__ __forceinline__ void ring_begin(const RingArgs& a, uint32_t full, uint32_t empty) {
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < a.stages; ++s) {
+      tc::mbar_init(full + 8 * s, 1);
+      tc::mbar_init(empty + 8 * s, kGroupThreads / 32);
+    }
+    tc::fence_barrier_init();
+  }
+  __syncthreads();
+  pdl_wait();
+  pdl_trigger();
+}
+
+// Parameters in shared memory, in the order in which the lanes read them: four at a time, without bank conflicts.
+template <int E, int V, int TPR>
+__device__ __forceinline__ void fill_params(float* to, const float* __restrict__ from, float none, int channels) {
+  if constexpr (E == 1) {
+#pragma unroll 8
+    for (int c = threadIdx.x; c < channels; c += kRingGroups * kGroupThreads) to[c] = from ? __ldg(from + c) : none;
+  } else {
+#pragma unroll 4
+    for (int q = threadIdx.x; q < channels / 4; q += kRingGroups * kGroupThreads) {
+      const int vec = q / (E / 4), h = q % (E / 4), v = vec / TPR, l = vec % TPR;
+      reinterpret_cast<float4*>(to)[(v * (E / 4) + h) * TPR + l] =
+          from ? __ldg(reinterpret_cast<const float4*>(from) + q) : make_float4(none, none, none, none);
+    }
+  }
+}
+template <int E, int TPR>
+__device__ __forceinline__ void load_params(const float* from, int v, int l, float (&w)[E]) {
+  if constexpr (E == 1) {
+    w[0] = from[v * TPR + l];
+  } else {
+#pragma unroll
+    for (int h = 0; h < E / 4; ++h) {
+      const float4 q = *reinterpret_cast<const float4*>(from + ((v * (E / 4) + h) * TPR + l) * 4);
+      w[4 * h] = q.x; w[4 * h + 1] = q.y; w[4 * h + 2] = q.z; w[4 * h + 3] = q.w;
+    }
+  }
+}
+__device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 3, 512;" ::: "memory"); }
+
+template <int DT, int E, int V, int TPR>
+__global__ void __launch_bounds__(kRingThreads, 1)
+ln_forward_ring_kernel(const __grid_constant__ RingArgs a, const float* __restrict__ gamma, const float* __restrict__ beta, float eps,
+                       void* __restrict__ y, float* __restrict__ stats) {
+  extern __shared__ __align__(128) unsigned char ring[];
+  __shared__ __align__(8) unsigned long long bars[2 * kMaxRing];
+  __shared__ float buf[kRingGroups * 2 * 8];
+  constexpr int kRows = kGroupThreads / TPR;     // rows of a group at a time
+  const uint32_t full = tc::smem_u32(bars), empty = full + 8 * kMaxRing;
+  ring_begin(a, full, empty);
+  if (threadIdx.x >= kRingGroups * kGroupThreads) {
+    ring_produce(a, ring, full, empty);
+    return;
+  }
+  float* s_gamma = reinterpret_cast<float*>(ring + a.params);
+  float* s_beta = s_gamma + V * TPR * E;
+  fill_params<E, V, TPR>(s_gamma, gamma, 1.0f, a.channels);
+  fill_params<E, V, TPR>(s_beta, beta, 0.0f, a.channels);
+  consumers_sync();
+  const int group = threadIdx.x / kGroupThreads;
+  const int l = static_cast<int>(threadIdx.x) % TPR, sub = static_cast<int>(threadIdx.x) % kGroupThreads / TPR;
+  const float inv_c = 1.0f / static_cast<float>(a.channels);
+  int turn = 0, i = 0;
+  for (long long chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x, ++i) {
+    if (i % kRingGroups != group) continue;
+    const int s = i % a.stages;
+    const long long row0 = chunk * a.chunk_rows;
+    const bool there = tc::mbar_wait_suspend(full + 8 * s, (i / a.stages) & 1);
+    const unsigned char* x = ring + s * a.stage_bytes + (E == 1 ? ring_shift(a, 0, row0) : 0);
+    const int here = static_cast<int>(a.rows - row0 < a.chunk_rows ? a.rows - row0 : a.chunk_rows);
+    for (int first = 0; first < here; first += kRows) {
+      const int k = first + sub;
+      const bool on = k < here;
+      float f[V][E], sum = 0.0f, q = 0.0f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int c = (v * TPR + l) * E;
+        if (on && c < a.channels) load_elems<DT, E>(x, k * a.channels + c, f[v]);
+        else {
+#pragma unroll
+          for (int e = 0; e < E; ++e) f[v][e] = 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum += f[v][e];
+      }
+      const float mean = ring_sum<TPR>(sum, buf, turn, group) * inv_c;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        if ((v * TPR + l) * E < a.channels) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            f[v][e] -= mean;
+            q += f[v][e] * f[v][e];
+          }
+        }
+      }
+      q = ring_sum<TPR>(q, buf, turn, group);
+      const float r = there ? rsqrtf(q * inv_c + eps) : __int_as_float(0x7FC00000);   // a copy that never came shows as NaN
+      if (on) {
+        const long long row = row0 + k;
+        if (stats && l == 0) {
+          stats[row] = mean;
+          stats[a.rows + row] = r;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const int c = (v * TPR + l) * E;
+          if (c < a.channels) {
+            float w[E], b[E];
+            load_params<E, TPR>(s_gamma, v, l, w);
+            load_params<E, TPR>(s_beta, v, l, b);
+#pragma unroll
+            for (int e = 0; e < E; ++e) f[v][e] = fmaf(f[v][e] * r, w[e], b[e]);
+            store_elems<DT, E>(y, row * a.channels + c, f[v]);
+          }
+        }
+      }
+    }
+    __syncwarp();
+    if (lane_id() == 0) tc::mbar_arrive(empty + 8 * s);
+  }
+}
+
+// The columns' sums stay in registers over all chunks of the CTA; x and dy are read twice from shared memory.  At the end a CTA
+// leaves one row of partial sums per array, partial[cta][0: dgamma, 1: dbeta][channels].
+template <int XDT, int GDT, int E, int V, int TPR>
+__global__ void __launch_bounds__(kRingThreads, 1)
+ln_backward_ring_kernel(const __grid_constant__ RingArgs a, const float* __restrict__ gamma, const float* __restrict__ stats,
+                        void* __restrict__ dx, float* __restrict__ partial) {
+  extern __shared__ __align__(128) unsigned char ring[];
+  __shared__ __align__(8) unsigned long long bars[2 * kMaxRing];
+  __shared__ float buf[2][kRingGroups * 2 * 8];
+  constexpr int kRows = kGroupThreads / TPR, kWidth = V * TPR * E;
+  const uint32_t full = tc::smem_u32(bars), empty = full + 8 * kMaxRing;
+  ring_begin(a, full, empty);
+  const bool producer = threadIdx.x >= kRingGroups * kGroupThreads;
+  float dg[V][E], db[V][E];
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int e = 0; e < E; ++e) dg[v][e] = db[v][e] = 0.0f;
+  const int group = threadIdx.x / kGroupThreads;
+  const int l = static_cast<int>(threadIdx.x) % TPR, sub = static_cast<int>(threadIdx.x) % kGroupThreads / TPR;
+  if (producer) {
+    ring_produce(a, ring, full, empty);
+  } else {
+    float* s_gamma = reinterpret_cast<float*>(ring + a.params);
+    fill_params<E, V, TPR>(s_gamma, gamma, 1.0f, a.channels);
+    consumers_sync();
+    const float inv_c = 1.0f / static_cast<float>(a.channels);
+    int turn1 = 0, turn2 = 0, i = 0;
+    for (long long chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x, ++i) {
+      if (i % kRingGroups != group) continue;
+      const int s = i % a.stages;
+      const long long row0 = chunk * a.chunk_rows;
+      const int here = static_cast<int>(a.rows - row0 < a.chunk_rows ? a.rows - row0 : a.chunk_rows);
+      // a row's statistics are asked for one turn ahead (the first: while the chunk is on its way)
+      float next_mean = sub < here ? __ldg(stats + row0 + sub) : 0.0f, next_r = sub < here ? __ldg(stats + a.rows + row0 + sub) : 0.0f;
+      const bool there = tc::mbar_wait_suspend(full + 8 * s, (i / a.stages) & 1);
+      const unsigned char* stage = ring + s * a.stage_bytes;
+      const unsigned char* x = stage + (E == 1 ? ring_shift(a, 0, row0) : 0);
+      const unsigned char* dy = stage + a.at[1] + (E == 1 ? ring_shift(a, 1, row0) : 0);
+      const unsigned char* res = stage + a.at[2] + (E == 1 ? ring_shift(a, 2, row0) : 0);
+      for (int first = 0; first < here; first += kRows) {
+        const int k = first + sub;
+        const bool on = k < here;
+        const float mean = next_mean, r = there ? next_r : __int_as_float(0x7FC00000);   // (a copy that never came shows as NaN)
+        if (k + kRows < here) {
+          next_mean = __ldg(stats + row0 + k + kRows);
+          next_r = __ldg(stats + a.rows + row0 + k + kRows);
+        }
+        float c1 = 0.0f, c2 = 0.0f;
+        if (on) {
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            const int c = (v * TPR + l) * E;
+            if (c < a.channels) {
+              float xh[E], g[E], w[E];
+              load_elems<XDT, E>(x, k * a.channels + c, xh);
+              load_elems<GDT, E>(dy, k * a.channels + c, g);
+              load_params<E, TPR>(s_gamma, v, l, w);
+#pragma unroll
+              for (int e = 0; e < E; ++e) {
+                xh[e] = (xh[e] - mean) * r;
+                dg[v][e] += g[e] * xh[e];
+                db[v][e] += g[e];
+                g[e] *= w[e];
+                c1 += g[e];
+                c2 += g[e] * xh[e];
+              }
+            }
+          }
+        }
+        c1 = ring_sum<TPR>(c1, buf[0], turn1, group) * inv_c;
+        c2 = ring_sum<TPR>(c2, buf[1], turn2, group) * inv_c;
+        if (on && dx) {
+          const long long row = row0 + k;
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            const int c = (v * TPR + l) * E;
+            if (c < a.channels) {
+              float xh[E], g[E], w[E];
+              load_elems<XDT, E>(x, k * a.channels + c, xh);
+              load_elems<GDT, E>(dy, k * a.channels + c, g);
+              load_params<E, TPR>(s_gamma, v, l, w);
+#pragma unroll
+              for (int e = 0; e < E; ++e) g[e] = r * (g[e] * w[e] - c1 - (xh[e] - mean) * r * c2);
+              if (a.n_src > 2) {
+                float q[E];
+                load_elems<GDT, E>(res, k * a.channels + c, q);
+#pragma unroll
+                for (int e = 0; e < E; ++e) g[e] += q[e];
+              }
+              store_elems<GDT, E>(dx, row * a.channels + c, g);
+            }
+          }
+        }
+      }
+      __syncwarp();
+      if (lane_id() == 0) tc::mbar_arrive(empty + 8 * s);
+    }
+  }
+  if (!partial) return;
+  // the rows' shares of each column, added in order in the place of the ring
+  float* sums = reinterpret_cast<float*>(ring);
+  float* out = partial + static_cast<long long>(blockIdx.x) * 2 * a.channels;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    __syncthreads();
+    if (!producer) {
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          sums[(group * kRows + sub) * kWidth + (v * TPR + l) * E + e] = k ? db[v][e] : dg[v][e];
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.channels; c += kRingThreads) {
+      float t = 0.0f;
+#pragma unroll 8
+      for (int j = 0; j < kRingGroups * kRows; ++j) t += sums[j * kWidth + c];
+      out[k * a.channels + c] = t;
+    }
+  }
+}
+
 bool whole_vectors(int channels, int elems) { return channels % elems == 0; }
 
 template <int DT, int E, int V, int TPR>
@@ -333,53 +556,10 @@ void forward_as(const void* x, long long rows, int channels, const float* gamma,
                 dim3(TPR > 32 ? TPR : kLnThreads), 0, stream, true, x, rows, channels, gamma, beta, eps, y, stats);
 }
 
-// E: elements of a vector; N = V * E elements per thread.
-template <int DT, int E>
-void forward_of(const void* x, long long rows, int channels, const float* gamma, const float* beta, float eps, void* y,
-                float* stats, cudaStream_t stream) {
-#define SURGEON_LN(TPR, N)                                                                                \
-  if (channels <= TPR * N) return forward_as<DT, E, N / E, TPR>(x, rows, channels, gamma, beta, eps, y, stats, stream)
-  SURGEON_LN(8, 8);
-  SURGEON_LN(32, 8);
-  SURGEON_LN(32, 16);
-  SURGEON_LN(32, 24);
-  SURGEON_LN(32, 32);
-  SURGEON_LN(128, 16);
-  SURGEON_LN(256, 16);
-  SURGEON_LN(512, 16);
-#undef SURGEON_LN
-  launch_kernel(ln_forward_long_kernel<DT>, dim3(static_cast<unsigned>(rows)), dim3(1024), 0, stream, true, x, rows, channels,
-                gamma, beta, eps, y, stats);
-}
-
-template <int XDT, int GDT, int E, int V, int TPR>
-int backward_as(const void* x, const void* dy, long long rows, int channels, const float* gamma, const float* stats,
-                const void* residual, void* dx, float* partial, cudaStream_t stream) {
-  constexpr int kRows = TPR > 32 ? 1 : kLnThreads / TPR;
-  const long long groups = (rows + kRows - 1) / kRows;
-  const int ctas = static_cast<int>(groups < kLnPartials ? groups : kLnPartials);
-  launch_kernel(ln_backward_kernel<XDT, GDT, E, V, TPR>, dim3(ctas), dim3(TPR > 32 ? TPR : kLnThreads), 0, stream, true, x, dy,
-                rows, channels, gamma, stats, residual, dx, partial);
-  note_launches(1);
-  return ctas;
-}
-
-// Returns how many rows of partial sums there are.
-template <int XDT, int GDT, int E>
-int backward_of(const void* x, const void* dy, long long rows, int channels, const float* gamma, const float* stats,
-                const void* residual, void* dx, float* partial, cudaStream_t stream) {
-#define SURGEON_LN(TPR, N)                                                                                         \
-  if (channels <= TPR * N)                                                                                         \
-    return backward_as<XDT, GDT, E, N / E, TPR>(x, dy, rows, channels, gamma, stats, residual, dx, partial, stream)
-  SURGEON_LN(8, 8);
-  SURGEON_LN(32, 8);
-  SURGEON_LN(32, 16);
-  SURGEON_LN(32, 24);
-  SURGEON_LN(64, 16);
-  SURGEON_LN(128, 16);
-  SURGEON_LN(256, 16);
-  SURGEON_LN(512, 16);
-#undef SURGEON_LN
+// Rows that no ring holds.  Returns how many rows of partial sums there are.
+template <int XDT, int GDT>
+int backward_long(const void* x, const void* dy, long long rows, int channels, const float* gamma, const float* stats,
+                  const void* residual, void* dx, float* partial, cudaStream_t stream) {
   int slabs = 0;
   if (partial) {                                 // (before dx, which may take the place of dy)
     const long long per = (rows + kLnPartials - 1) / kLnPartials;
@@ -394,6 +574,126 @@ int backward_of(const void* x, const void* dy, long long rows, int channels, con
     note_launches(1);
   }
   return slabs;
+}
+
+// The ring of a call, or false where not even two chunks of one row fit.  `parallel`: rows that a group takes at a time;
+// `arrays`: what the call may read at most, by which the chunks go (so that the columns' sums are the same whether dx and the
+// residual's gradient are wanted or not); `param_bytes`: of the parameters behind the ring.
+bool plan_ring(RingArgs* a, int parallel, int arrays, int param_bytes) {
+  long long bytes = 0;
+  for (int i = 0; i < arrays; ++i) bytes += static_cast<long long>(a->channels) * a->elem[i];
+  const long long room = kSmemBytes - param_bytes;
+  // whole turns of the group while three stages of them fit; more rows where rows are short and every CTA still has work
+  long long rows = parallel;
+  if (rows * bytes > room / 3 - 512) rows = (room / 3 - 512) / bytes > 1 ? (room / 3 - 512) / bytes : 1;
+  while (2 * rows * bytes <= 24 * 1024 && 4 * rows * sm_count() <= a->rows) rows *= 2;
+  long long stage = 0, most = 0;
+  for (int i = 0; i < arrays; ++i) {
+    a->at[i] = static_cast<int>(most);
+    most += (rows * a->channels * a->elem[i] + 16 + 127) & ~127LL;
+    if (most > room / 2) return false;
+    if (i < a->n_src) stage = most;
+  }
+  a->chunk_rows = static_cast<int>(rows);
+  a->stage_bytes = static_cast<int>(stage);
+  a->stages = static_cast<int>(room / stage);
+  if (a->stages > kMaxRing) a->stages = kMaxRing;
+  a->params = a->stages * a->stage_bytes;
+  a->chunks = (a->rows + rows - 1) / rows;
+  return true;
+}
+
+template <int DT, int E, int V, int TPR>
+bool forward_ring_as(const void* x, long long rows, int channels, const float* gamma, const float* beta, float eps, void* y,
+                     float* stats, cudaStream_t stream) {
+  RingArgs a = {};
+  a.src[0] = x; a.elem[0] = DT ? 2 : 4; a.n_src = 1;
+  a.rows = rows; a.channels = channels;
+  constexpr int kParams = 2 * V * TPR * E * 4;
+  if (!plan_ring(&a, kGroupThreads / TPR, 1, kParams)) return false;
+  const auto kernel = ln_forward_ring_kernel<DT, E, V, TPR>;
+  const int smem = a.params + kParams;
+  if (allow_dynamic_smem(reinterpret_cast<const void*>(kernel), smem) != cudaSuccess) return false;
+  const int ctas = static_cast<int>(a.chunks < sm_count() ? a.chunks : sm_count());
+  launch_kernel(kernel, dim3(ctas), dim3(kRingThreads), smem, stream, true, a, gamma, beta, eps, y, stats);
+  return true;
+}
+
+template <int XDT, int GDT, int E, int V, int TPR>
+int backward_ring_as(const void* x, const void* dy, long long rows, int channels, const float* gamma, const float* stats,
+                     const void* residual, void* dx, float* partial, cudaStream_t stream) {
+  RingArgs a = {};
+  a.src[0] = x; a.src[1] = dy; a.src[2] = residual;
+  a.elem[0] = XDT ? 2 : 4; a.elem[1] = a.elem[2] = GDT ? 2 : 4;
+  a.n_src = residual && dx ? 3 : 2;
+  a.rows = rows; a.channels = channels;
+  constexpr int kParams = V * TPR * E * 4;
+  if (!plan_ring(&a, kGroupThreads / TPR, 3, kParams)) return 0;
+  const auto kernel = ln_backward_ring_kernel<XDT, GDT, E, V, TPR>;
+  int smem = a.params + kParams;
+  const int sums = kRingGroups * (kGroupThreads / TPR) * V * TPR * E * 4;
+  if (smem < sums) smem = sums;
+  if (allow_dynamic_smem(reinterpret_cast<const void*>(kernel), smem) != cudaSuccess) return 0;
+  const int ctas = static_cast<int>(a.chunks < sm_count() ? a.chunks : sm_count());
+  launch_kernel(kernel, dim3(ctas), dim3(kRingThreads), smem, stream, true, a, gamma, stats, dx, partial);
+  note_launches(1);
+  return ctas;
+}
+
+// E: elements of a vector, 1 where rows start at no 16-byte boundary; N elements per thread.  Whole vectors go to the kernel
+// without a ring, whose many short CTAs hide each other's latencies (12608 x 768 bf16 11.8 us against 13.0, 4096 x 1024 6.1
+// against 7.5); other widths to the ring, which still reads them in wide pieces (3000 x 2047 bf16 16.7 us against 32.4).
+template <int DT, int E>
+void forward_of(const void* x, long long rows, int channels, const float* gamma, const float* beta, float eps, void* y,
+                float* stats, cudaStream_t stream) {
+  if constexpr (E > 1) {
+#define SURGEON_LN(TPR, N)                                                                                \
+  if (channels <= TPR * N) return forward_as<DT, E, N / E, TPR>(x, rows, channels, gamma, beta, eps, y, stats, stream)
+    SURGEON_LN(8, 8);
+    SURGEON_LN(32, 8);
+    SURGEON_LN(32, 16);
+    SURGEON_LN(32, 24);
+    SURGEON_LN(32, 32);
+    SURGEON_LN(128, 16);
+    SURGEON_LN(256, 16);
+    SURGEON_LN(512, 16);
+#undef SURGEON_LN
+  } else {
+#define SURGEON_LN(TPR, N)                                                                                            \
+  if (channels <= TPR * N && forward_ring_as<DT, 1, N, TPR>(x, rows, channels, gamma, beta, eps, y, stats, stream)) return
+    SURGEON_LN(8, 8);
+    SURGEON_LN(16, 8);
+    SURGEON_LN(32, 8);
+    SURGEON_LN(32, 16);
+    SURGEON_LN(32, 32);
+    SURGEON_LN(256, 8);
+    SURGEON_LN(256, 16);
+    SURGEON_LN(256, 32);
+#undef SURGEON_LN
+  }
+  launch_kernel(ln_forward_long_kernel<DT>, dim3(static_cast<unsigned>(rows)), dim3(1024), 0, stream, true, x, rows, channels,
+                gamma, beta, eps, y, stats);
+}
+
+// Returns how many rows of partial sums there are.
+template <int XDT, int GDT, int E>
+int backward_of(const void* x, const void* dy, long long rows, int channels, const float* gamma, const float* stats,
+                const void* residual, void* dx, float* partial, cudaStream_t stream) {
+  int n = 0;
+#define SURGEON_LN(TPR, N)                                                                                                         \
+  if (n == 0 && channels <= TPR * N)                                                                                               \
+    n = backward_ring_as<XDT, GDT, E, N / E, TPR>(x, dy, rows, channels, gamma, stats, residual, dx, partial, stream)
+  SURGEON_LN(8, 8);
+  SURGEON_LN(16, 8);
+  SURGEON_LN(32, 8);
+  SURGEON_LN(32, 16);
+  SURGEON_LN(32, 24);
+  SURGEON_LN(32, 32);
+  SURGEON_LN(256, 8);
+  SURGEON_LN(256, 16);
+  SURGEON_LN(256, 32);
+#undef SURGEON_LN
+  return n ? n : backward_long<XDT, GDT>(x, dy, rows, channels, gamma, stats, residual, dx, partial, stream);
 }
 
 }  // namespace
@@ -428,7 +728,7 @@ cudaError_t launch_layer_norm_grad(const void* x, const void* dy, long long rows
       if (whole_vectors(channels, 4)) SURGEON_LN(0, 0, 4);
       else SURGEON_LN(0, 0, 1);
     } else if (grad_dt == 0) {
-      if (whole_vectors(channels, 8)) SURGEON_LN(1, 0, 8);
+      if (whole_vectors(channels, 8)) SURGEON_LN(1, 0, 4);
       else SURGEON_LN(1, 0, 1);
     } else {
       if (whole_vectors(channels, 8)) SURGEON_LN(1, 1, 8);

@@ -45,7 +45,7 @@ act_grad_kernel(const void* __restrict__ dy, const unsigned short* __restrict__ 
         float z[E];
         load_elems<1, E>(pre, t * cols + c, z);
 #pragma unroll
-        for (int e = 0; e < E; ++e) g[e] *= slope(z[e], act);
+        for (int e = 0; e < E; ++e) g[e] *= act == kActGelu ? slope<kActGelu>(z[e]) : slope<kActRelu>(z[e]);
       }
 #pragma unroll
       for (int e = 0; e < E; ++e) acc[e] += g[e];
@@ -200,7 +200,7 @@ void pad_rows(const void* src, long long rows, int cols, void* dst, cudaStream_t
 // Rows of a slab in the pass over dy: enough CTAs for the SMs, at least 8 rows each.
 long long slab_rows(long long rows, int cols) {
   const long long across = (cols + 255) / 256;
-  long long slabs = (kMaxSlabs * 2 + across - 1) / across;
+  long long slabs = kMaxSlabs * 2 / across > 0 ? kMaxSlabs * 2 / across : 1;
   if (slabs > kMaxSlabs) slabs = kMaxSlabs;
   const long long per = (rows + slabs - 1) / slabs;
   return (per + 7) / 8 * 8;

@@ -7,42 +7,53 @@ namespace surgeon {
 
 constexpr int kActNone = 0, kActRelu = 1, kActGelu = 2;
 
-// Phi(z) = erfc(-z / sqrt 2) / 2 and e^(-z^2/2), the two parts of GELU(z) = z Phi(z) and of its derivative
-// Phi(z) + z e^(-z^2/2) / sqrt(2 pi).  erfc by Abramowitz and Stegun, "Handbook of Mathematical Functions", 7.1.26
-// (error below 1.5e-7 of erf): t = 1 / (1 + 0.3275911 |x|), erfc(|x|) = (a1 t + ... + a5 t^5) e^(-x^2).  Some 14 instructions,
-// two of them approximate ones of the special function unit, and no branch.
-__device__ __forceinline__ void normal_parts(float z, float& phi, float& e) {
-  const float t = __fdividef(1.0f, fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.0f));
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(-0.72134752f * z * z));      // e^(-z^2/2)
-  float p = fmaf(1.061405429f, t, -1.453152027f);
-  p = fmaf(p, t, 1.421413741f);
-  p = fmaf(p, t, -0.284496736f);
-  p = fmaf(p, t, 0.254829592f);
-  const float tail = 0.5f * (p * t) * e;              // Phi(-|z|)
-  phi = z < 0.0f ? tail : 1.0f - tail;
+// Phi(-a) and e^(-a^2/2) for a >= 0, the parts of GELU and of its derivative.  Phi(-a) = erfc(a / sqrt 2) / 2; erfc by Abramowitz
+// and Stegun, "Handbook of Mathematical Functions", 7.1.26 (error below 1.5e-7 of erf): t = 1 / (1 + 0.3275911 x),
+// erfc(x) = (a1 t + ... + a5 t^5) e^(-x^2); the coefficients below are halved.  Ten instructions of the FMA pipe and two
+// approximate ones of the special function unit, no branch.
+__device__ __forceinline__ void normal_tail(float a, float& tail, float& e) {
+  float t;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(fmaf(0.3275911f * 0.70710678f, a, 1.0f)));
+  const float u = 0.84932180f * a;                    // sqrt(log2(e) / 2) a
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(-u * u));
+  float p = fmaf(0.5307027145f, t, -0.7265760135f);
+  p = fmaf(p, t, 0.7107068705f);
+  p = fmaf(p, t, -0.142248368f);
+  p = fmaf(p, t, 0.127414796f);
+  tail = p * t * e;
+}
+// max(z, 0), NaN for NaN; min(|z|, 16), where Phi(-16) is 0 in fp32
+__device__ __forceinline__ float positive(float z) {
+  float m;
+  asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(m) : "f"(z));
+  return m;
 }
 
-// ReLU and GELU let a NaN through.  GELU(-inf): -inf * 0 would be NaN, and is 0.
+// GELU(z) = z Phi(z) = max(z, 0) - |z| Phi(-|z|).  ReLU and GELU let a NaN through; GELU(-inf) is 0 (not -inf * 0).
 template <int ACT>
 __device__ __forceinline__ float activate(float z) {
-  if (ACT == kActRelu) return z < 0.0f ? 0.0f : z;
+  if (ACT == kActRelu) return positive(z);
   if (ACT == kActGelu) {
-    float phi, e;
-    normal_parts(z, phi, e);
-    return z < -14.0f ? 0.0f : z * phi;
+    const float a = fminf(fabsf(z), 16.0f);
+    float tail, e;
+    normal_tail(a, tail, e);
+    return fmaf(-a, tail, positive(z));
   }
   return z;
 }
 __device__ __forceinline__ float activate(float z, int act) {
   return act == kActRelu ? activate<kActRelu>(z) : act == kActGelu ? activate<kActGelu>(z) : z;
 }
-// The derivative; 0 at 0 for ReLU.  NaN for a NaN.
-__device__ __forceinline__ float slope(float z, int act) {
-  if (act == kActRelu) return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
-  if (act == kActGelu) {
-    float phi, e;
-    normal_parts(z, phi, e);
-    return fabsf(z) > 14.0f ? (z > 0.0f ? 1.0f : 0.0f) : fmaf(z * 0.39894228f, e, phi);
+// The derivative: ReLU 1 above 0, else 0; GELU Phi(z) + z e^(-z^2/2) / sqrt(2 pi).  NaN for a NaN.
+template <int ACT>
+__device__ __forceinline__ float slope(float z) {
+  if (ACT == kActRelu) return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
+  if (ACT == kActGelu) {
+    const float a = fminf(fabsf(z), 16.0f);
+    float tail, e;
+    normal_tail(a, tail, e);
+    const float half = fmaf(-0.39894228f * a, e, tail);         // the derivative at -|z|
+    return z > 0.0f ? 1.0f - half : (z <= 0.0f ? half : z);
   }
   return 1.0f;
 }

@@ -4,8 +4,8 @@
 //
 // Persistent CTAs (or CTA pairs, cta_group::2: 256 rows, each CTA its 128 and half of the columns' operand) walk the output
 // tiles, columns fastest.  Warp 0 fetches operands by TMA into a ring, warp 1 issues the MMAs into one of two accumulators
-// in tensor memory, eight warps take the other one: lane = row, 32 or 64 columns at a time.  A piece of 32 rows of 128 bytes
-// goes through 4 KB of shared memory, where the residual has been fetched by TMA before, and leaves by TMA.
+// in tensor memory, sixteen warps (eight for fp32 outputs) take the other one: lane = row, 32 columns at a time.  A piece of
+// 32 x 32 goes through shared memory, where the residual has been fetched by TMA before, and leaves by TMA.
 // b is K-major (weights [n, k], forward) or N-major (weights [k, n], the input's gradient): both are read as they lie.
 #include <cuda.h>
 #include <string.h>
@@ -22,15 +22,18 @@ using namespace tc;
 constexpr int kTileK = 64;                       // 128 bytes of bf16
 constexpr int kTileM = 128;                      // rows of a CTA
 constexpr int kABytes = kTileM * 128;
-constexpr int kEpiWarps = 8;
-constexpr int kThreads = (2 + kEpiWarps) * 32;
 constexpr int kMaxStages = 8;
-constexpr int kPiece = 4096;                     // 32 rows of 128 bytes
+constexpr int kCols = 32;                        // columns (and rows) of a piece
+constexpr int kPrePiece = 32 * kCols * 2;
+template <int DT> constexpr int kEpiWarps = DT ? 16 : 8;
+template <int DT> constexpr int kThreads = (2 + kEpiWarps<DT>) * 32;
+template <int DT> constexpr int kPiece = 32 * kCols * (DT ? 2 : 4);
 
 struct TileArgs {
   int m, n, k;
   int tile_n;                                    // columns of a tile
   int tiles_n, tiles;
+  int step_m, step_n;                            // from a CTA's tile to its next: rows and columns of tiles
   int stages, stage_bytes, ktiles;
   int tmem_cols;
   int vec_y, vec_pre;                            // rows of y (and the residual), of pre, start at 16-byte boundaries: TMA
@@ -82,40 +85,50 @@ __device__ __forceinline__ uint32_t piece_at(int r, int j) {
   return ROW == 128 ? static_cast<uint32_t>(r * 128 + ((j ^ (r & 7)) << 4)) : static_cast<uint32_t>(r * 64 + ((j ^ ((r >> 1) & 3)) << 4));
 }
 
-// DT: type of y and of the residual.  A piece of y has 64 (bf16) or 32 (fp32) columns, one of pre as many.
+// DT: type of y and of the residual.
 template <int PAIR, int B_MN, int DT>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads<DT>, 1)
 linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
               const __grid_constant__ CUtensorMap y_map, const __grid_constant__ CUtensorMap r_map,
               const __grid_constant__ CUtensorMap p_map, const __grid_constant__ TileArgs p) {
-  constexpr int kCols = DT ? 64 : 32;            // columns of a piece
-  constexpr int kPreRow = kCols * 2;             // bytes of a row of pre's piece
+  constexpr int kWarps = kEpiWarps<DT>, kSlots = kWarps / 4, kRow = kCols * (DT ? 2 : 4), kPreRow = kCols * 2;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 4 + 2 * kEpiWarps];
-  __shared__ __align__(16) float s_bias[kEpiWarps][kCols];
+  __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 4 + 2 * kWarps];
+  __shared__ __align__(16) float s_bias[kWarps][kCols];
   __shared__ uint32_t tmem_slot;
   __shared__ volatile uint32_t fail;
 
-  const int tid = threadIdx.x, warp = tid >> 5;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);      // (uniform for the compiler too)
   const uint32_t lane = lane_id();
+  const bool leader = elected();
   const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
   const uint32_t full = smem_u32(bars), empty = full + 8 * kMaxStages, acc_full = full + 16 * kMaxStages, acc_empty = acc_full + 16;
   const uint32_t res_bar = acc_empty + 16;       // two per epilogue warp
   const int b_rows = PAIR ? p.tile_n / 2 : p.tile_n;            // columns' operand: rows that this CTA fetches
   const int tile_step = PAIR ? static_cast<int>(gridDim.x >> 1) : static_cast<int>(gridDim.x);
   const int tile_first = PAIR ? static_cast<int>(blockIdx.x >> 1) : static_cast<int>(blockIdx.x);
+  const int first_m = tile_first / p.tiles_n, first_n = tile_first - first_m * p.tiles_n;
+  constexpr int kTileRows = PAIR ? 2 * kTileM : kTileM;
+  // the tile behind (tm, tn)
+  const auto advance = [&](int& tm, int& tn) {
+    tm += p.step_m;
+    tn += p.step_n;
+    if (tn >= p.tiles_n) { tn -= p.tiles_n; ++tm; }
+  };
 
   if (tid == 0) {
+    tma_prefetch_desc(&a_map);
+    tma_prefetch_desc(&b_map);
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(full + 8 * s, 1);
       mbar_init(empty + 8 * s, 1);
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(acc_full + 8 * a, 1);
-      mbar_init(acc_empty + 8 * a, (PAIR ? 2 : 1) * kEpiWarps);
+      mbar_init(acc_empty + 8 * a, (PAIR ? 2 : 1) * kWarps);
     }
-    for (int w = 0; w < 2 * kEpiWarps; ++w) mbar_init(res_bar + 8 * w, 1);
+    for (int w = 0; w < 2 * kWarps; ++w) mbar_init(res_bar + 8 * w, 1);
     fail = 0;
     fence_barrier_init();
   }
@@ -139,18 +152,16 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
 
   if (warp == 0) {
     // ---- operands ----
-    if (lane == 0) {
-      tma_prefetch_desc(&a_map);
-      tma_prefetch_desc(&b_map);
-      int s = 0;
-      uint32_t phase = 1;                        // (a fresh barrier counts as passed in its phase before)
-      bool ok = true;
-      for (int t = tile_first; t < p.tiles && ok; t += tile_step) {
-        const int m0 = (t / p.tiles_n) * (PAIR ? 2 * kTileM : kTileM) + static_cast<int>(rank) * kTileM;
-        const int n0 = (t % p.tiles_n) * p.tile_n + static_cast<int>(rank) * b_rows;
-        for (int kt = 0; kt < p.ktiles; ++kt) {
-          if (fail || !mbar_wait_suspend(empty + 8 * s, phase)) { give_up(); ok = false; break; }
-          const uint32_t a_at = smem_u32(smem) + s * p.stage_bytes, b_at = a_at + kABytes, bar = full + 8 * s;
+    int s = 0, tm = first_m, tn = first_n;
+    uint32_t phase = 1;                          // (a fresh barrier counts as passed in its phase before)
+    bool ok = true;
+    for (int t = tile_first; t < p.tiles && ok; t += tile_step, advance(tm, tn)) {
+      const int m0 = tm * kTileRows + static_cast<int>(rank) * kTileM;
+      const int n0 = tn * p.tile_n + static_cast<int>(rank) * b_rows;
+      for (int kt = 0; kt < p.ktiles; ++kt) {
+        if (!__all_sync(0xFFFFFFFFu, !fail && mbar_wait_suspend(empty + 8 * s, phase))) { give_up(); ok = false; break; }
+        const uint32_t a_at = smem_u32(smem) + s * p.stage_bytes, b_at = a_at + kABytes, bar = full + 8 * s;
+        if (leader) {
           if (rank == 0) mbar_arrive_expect_tx(bar, (PAIR ? 2u : 1u) * static_cast<uint32_t>(p.stage_bytes));
           if (PAIR) tma_load_2d_pair(a_at, &a_map, kt * kTileK, m0, bar);
           else tma_load_2d(a_at, &a_map, kt * kTileK, m0, bar);
@@ -164,16 +175,17 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
           } else {
             tma_load_2d(b_at, &b_map, kt * kTileK, n0, bar);
           }
-          if (++s == p.stages) { s = 0; phase ^= 1; }
         }
+        __syncwarp();
+        if (++s == p.stages) { s = 0; phase ^= 1; }
       }
-      if (!ok)
-        for (int i = 0; i < 1000; ++i) __nanosleep(1000);       // copies in flight land
     }
+    if (!ok)
+      for (int i = 0; i < 1000; ++i) __nanosleep(1000);         // copies in flight land
   } else if (warp == 1) {
     // ---- MMAs ----
-    if (lane == 0 && rank == 0) {
-      const uint32_t idesc = make_idesc(PAIR ? 2 * kTileM : kTileM, p.tile_n) | (B_MN ? 1u << 16 : 0u);
+    if (rank == 0) {
+      const uint32_t idesc = make_idesc(kTileRows, p.tile_n) | (B_MN ? 1u << 16 : 0u);
       const uint64_t a_base = make_desc(smem_u32(smem));
       const uint64_t b_base = B_MN ? make_desc_rows(smem_u32(smem) + kABytes) : make_desc(smem_u32(smem) + kABytes);
       constexpr int kStepB = B_MN ? 128 : 2;
@@ -182,90 +194,89 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
       bool ok = true;
       for (int t = tile_first; t < p.tiles && ok; t += tile_step, ++it) {
         const int acc = it & 1;
-        if (fail || !(PAIR ? mbar_wait_suspend_cluster(acc_empty + 8 * acc, ((it >> 1) & 1) ^ 1)
-                           : mbar_wait_suspend(acc_empty + 8 * acc, ((it >> 1) & 1) ^ 1))) { give_up(); break; }
+        if (!__all_sync(0xFFFFFFFFu, !fail && (PAIR ? mbar_wait_suspend_cluster(acc_empty + 8 * acc, ((it >> 1) & 1) ^ 1)
+                                                    : mbar_wait_suspend(acc_empty + 8 * acc, ((it >> 1) & 1) ^ 1)))) { give_up(); break; }
         tc_fence_after();
         const uint32_t d = tmem_base + acc * (p.tmem_cols >> 1);
         for (int kt = 0; kt < p.ktiles; ++kt) {
-          if (fail || !mbar_wait_suspend(full + 8 * s, phase)) { give_up(); ok = false; break; }
+          if (!__all_sync(0xFFFFFFFFu, !fail && mbar_wait_suspend(full + 8 * s, phase))) { give_up(); ok = false; break; }
           tc_fence_after();
           const uint64_t off = static_cast<uint64_t>((s * p.stage_bytes) >> 4);
+          if (leader) {
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) {
-            const uint64_t da = a_base + off + 2 * kk, db = b_base + off + kStepB * kk;
-            if (PAIR) umma_bf16_pair(d, da, db, idesc, kt > 0 || kk > 0 ? 1u : 0u);
-            else umma_bf16(d, da, db, idesc, kt > 0 || kk > 0 ? 1u : 0u);
+            for (int kk = 0; kk < 4; ++kk) {
+              const uint64_t da = a_base + off + 2 * kk, db = b_base + off + kStepB * kk;
+              if (PAIR) umma_bf16_pair(d, da, db, idesc, kt > 0 || kk > 0 ? 1u : 0u);
+              else umma_bf16(d, da, db, idesc, kt > 0 || kk > 0 ? 1u : 0u);
+            }
+            if (PAIR) umma_commit_pair(empty + 8 * s);
+            else umma_commit(empty + 8 * s);
+            if (kt + 1 == p.ktiles) {
+              if (PAIR) umma_commit_pair(acc_full + 8 * acc);
+              else umma_commit(acc_full + 8 * acc);
+            }
           }
-          if (PAIR) umma_commit_pair(empty + 8 * s);
-          else umma_commit(empty + 8 * s);
+          __syncwarp();
           if (++s == p.stages) { s = 0; phase ^= 1; }
         }
-        if (PAIR) umma_commit_pair(acc_full + 8 * acc);
-        else umma_commit(acc_full + 8 * acc);
       }
     }
   } else {
-    // ---- epilogue: rows of tensor memory's quarter `warp % 4`, every other piece of columns (the rest: another warp's) ----
-    const int w = warp - 2, quarter = warp & 3, half = w >> 2;
-    unsigned char* stage = smem + p.stages * p.stage_bytes + w * (p.pre ? 3 : 2) * kPiece;
-    const uint32_t stage_at = smem_u32(stage);
-    const bool has_res = p.residual != nullptr, tma_res = has_res && p.vec_y;
-    const uint32_t my_res = res_bar + 16 * w;
-    const int pieces = p.tile_n / kCols;
+    // ---- epilogue: rows of tensor memory's quarter `warp % 4`, every kSlots-th piece of columns ----
+    const int w = warp - 2, quarter = warp & 3, slot = w >> 2;
+    const bool has_res = p.residual != nullptr, tma_res = has_res && p.vec_y, keep = p.pre != nullptr;
+    // y's places, two of them where a residual comes early, then pre's
+    const int y_places = has_res ? 2 : 1;
+    unsigned char* stage = smem + p.stages * p.stage_bytes + w * (y_places * kPiece<DT> + (keep ? kPrePiece : 0));
+    unsigned char* pre_stage = stage + y_places * kPiece<DT>;
+    const uint32_t stage_at = smem_u32(stage), my_res = res_bar + 16 * w;
     const int r = static_cast<int>(lane);        // this lane's row of a piece
-    const auto row_of = [&](int t) {
-      return (t / p.tiles_n) * (PAIR ? 2 * kTileM : kTileM) + static_cast<int>(rank) * kTileM + quarter * 32;
-    };
-    const auto exists = [&](int t, int c) {
-      return c < pieces && (t % p.tiles_n) * p.tile_n + c * kCols < p.n && row_of(t) < p.m;
+    const int row_in_tile = static_cast<int>(rank) * kTileM + quarter * 32;
+    // pieces of columns of tile (tm, tn), none where its rows lie behind the last
+    const auto pieces_of = [&](int tm, int tn) {
+      if (tm * kTileRows + row_in_tile >= p.m) return 0;
+      const int left = p.n - tn * p.tile_n;
+      return ((left < p.tile_n ? left : p.tile_n) + kCols - 1) / kCols;
     };
     // the warp's next piece whose residual is to be fetched
-    int ft = tile_first, fc = half;
+    int ft = tile_first, fm = first_m, fn = first_n, fc = slot;
     uint32_t fetched = 0;
-    const auto fetch_next = [&]() {              // (lane 0)
-      while (ft < p.tiles && !exists(ft, fc)) { ft += tile_step; fc = half; }
+    const auto fetch_next = [&]() {              // (the leader)
+      while (ft < p.tiles && fc >= pieces_of(fm, fn)) { ft += tile_step; advance(fm, fn); fc = slot; }
       if (ft >= p.tiles) return;
       const uint32_t buf = fetched & 1;
-      mbar_arrive_expect_tx(my_res + 8 * buf, kPiece);
-      tma_load_2d(stage_at + buf * kPiece, &r_map, (ft % p.tiles_n) * p.tile_n + fc * kCols, row_of(ft), my_res + 8 * buf);
+      mbar_arrive_expect_tx(my_res + 8 * buf, kPiece<DT>);
+      tma_load_2d(stage_at + buf * kPiece<DT>, &r_map, fn * p.tile_n + fc * kCols, fm * kTileRows + row_in_tile, my_res + 8 * buf);
       ++fetched;
-      fc += 2;
+      fc += kSlots;
     };
-    if (tma_res && lane == 0) fetch_next();
-    int it = 0;
+    if (tma_res && leader) fetch_next();
+    int it = 0, tm = first_m, tn = first_n;
     uint32_t piece = 0;
     bool ok = true;
-    for (int t = tile_first; t < p.tiles && ok; t += tile_step, ++it) {
-      const int n0 = (t % p.tiles_n) * p.tile_n, m0 = row_of(t);
+    for (int t = tile_first; t < p.tiles && ok; t += tile_step, ++it, advance(tm, tn)) {
+      const int n0 = tn * p.tile_n, m0 = tm * kTileRows + row_in_tile, pieces = pieces_of(tm, tn);
       const int acc = it & 1;
+      const uint32_t tmem_at = tmem_base + acc * (p.tmem_cols >> 1) + (static_cast<uint32_t>(quarter) << 21);
       bool waited = false;
-      for (int c = half; exists(t, c); c += 2) {
-        const uint32_t buf = piece & 1;
-        unsigned char* mine = stage + buf * kPiece;
+      for (int c = slot; c < pieces; c += kSlots) {
+        const uint32_t buf = y_places == 2 ? piece & 1 : 0;
+        unsigned char* mine = stage + buf * kPiece<DT>;
         const int x = n0 + c * kCols;
-        if (lane == 0) {
-          if (has_res || p.pre) bulk_wait_read<0>();            // what left the other places has been read
-          else bulk_wait_read<1>();
+        if (leader) {
+          bulk_wait_read<0>();                   // what left the places has been read
           if (tma_res) fetch_next();
         }
-        if (p.bias) {                            // the piece's bias, where every lane can read all of it
-#pragma unroll
-          for (int i = 0; i < kCols; i += 32) {
-            const int n = x + i + r;
-            s_bias[w][i + r] = n < p.n ? __ldg(p.bias + n) : 0.0f;
-          }
-        }
+        if (p.bias) s_bias[w][r] = x + r < p.n ? __ldg(p.bias + x + r) : 0.0f;       // the piece's, for every lane to read
         __syncwarp();
         if (has_res && !tma_res) {
-          for (int q = 0; q < 32 && m0 + q < p.m; ++q) {
-            const long long at = static_cast<long long>(m0 + q) * p.n + x;
-            for (int c1 = r; c1 < kCols && x + c1 < p.n; c1 += 32) {
-              if (DT) *reinterpret_cast<unsigned short*>(mine + piece_at<128>(q, c1 >> 3) + (c1 & 7) * 2) =
-                  static_cast<const unsigned short*>(p.residual)[at + c1];
-              else *reinterpret_cast<float*>(mine + piece_at<128>(q, c1 >> 2) + (c1 & 3) * 4) =
-                  static_cast<const float*>(p.residual)[at + c1];
+          if (x + r < p.n)
+            for (int q = 0; q < 32 && m0 + q < p.m; ++q) {
+              const long long at = static_cast<long long>(m0 + q) * p.n + x + r;
+              if (DT) *reinterpret_cast<unsigned short*>(mine + piece_at<kRow>(q, r >> 3) + (r & 7) * 2) =
+                  static_cast<const unsigned short*>(p.residual)[at];
+              else *reinterpret_cast<float*>(mine + piece_at<kRow>(q, r >> 2) + (r & 3) * 4) = static_cast<const float*>(p.residual)[at];
             }
-          }
           __syncwarp();
         }
         if (!waited) {
@@ -275,16 +286,12 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
           waited = true;
         }
         uint32_t v[kCols];
-        {
-          const uint32_t at = tmem_base + acc * (p.tmem_cols >> 1) + (static_cast<uint32_t>(quarter) << 21) + c * kCols;
-          tmem_ld32(at, *reinterpret_cast<uint32_t (*)[32]>(v));
-          if constexpr (DT == 1) tmem_ld32(at + 32, *reinterpret_cast<uint32_t (*)[32]>(v + 32));
-          tmem_ld_wait();
-        }
-        if (!exists(t, c + 2)) {                 // the accumulator has been read: it may be written again
+        tmem_ld32(tmem_at + c * kCols, v);
+        tmem_ld_wait();
+        if (c + kSlots >= pieces) {              // the accumulator has been read: it may be written again
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) {
+          if (leader) {
             if (PAIR) mbar_arrive_rank0(acc_empty + 8 * acc);
             else mbar_arrive(acc_empty + 8 * acc);
           }
@@ -299,14 +306,14 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
             v[4 * j + 3] = __float_as_uint(__uint_as_float(v[4 * j + 3]) + b.w);
           }
         }
-        if (p.pre) {
+        if (keep) {
 #pragma unroll
           for (int j = 0; j < kCols / 8; ++j) {
             uint32_t o[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               o[i] = to_bf16x2(__uint_as_float(v[8 * j + 2 * i]), __uint_as_float(v[8 * j + 2 * i + 1]));
-            *reinterpret_cast<uint4*>(stage + 2 * kPiece + piece_at<kPreRow>(r, j)) = make_uint4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<uint4*>(pre_stage + piece_at<kPreRow>(r, j)) = make_uint4(o[0], o[1], o[2], o[3]);
           }
         }
         if (p.act == kActGelu) {
@@ -322,8 +329,8 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
           break;
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          uint4* at = reinterpret_cast<uint4*>(mine + piece_at<128>(r, j));
+        for (int j = 0; j < kRow / 16; ++j) {
+          uint4* at = reinterpret_cast<uint4*>(mine + piece_at<kRow>(r, j));
           if constexpr (DT == 1) {
             float f[8];
 #pragma unroll
@@ -346,38 +353,36 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
         }
         fence_proxy_async();
         __syncwarp();
-        if (lane == 0) {
-          if (p.vec_y) tma_store_2d(&y_map, stage_at + buf * kPiece, x, m0);
-          if (p.pre && p.vec_pre) tma_store_2d(&p_map, stage_at + 2 * kPiece, x, m0);
+        if (leader) {
+          if (p.vec_y) tma_store_2d(&y_map, stage_at + buf * kPiece<DT>, x, m0);
+          if (keep && p.vec_pre) tma_store_2d(&p_map, smem_u32(pre_stage), x, m0);
           bulk_commit();
         }
-        if (!p.vec_y || (p.pre && !p.vec_pre)) {
-          for (int q = 0; q < 32 && m0 + q < p.m; ++q) {
-            const long long at = static_cast<long long>(m0 + q) * p.n + x;
-            for (int c1 = r; c1 < kCols && x + c1 < p.n; c1 += 32) {
+        if (!p.vec_y || (keep && !p.vec_pre)) {
+          if (x + r < p.n)
+            for (int q = 0; q < 32 && m0 + q < p.m; ++q) {
+              const long long at = static_cast<long long>(m0 + q) * p.n + x + r;
               if (!p.vec_y) {
-                if (DT) static_cast<unsigned short*>(p.y)[at + c1] =
-                    *reinterpret_cast<const unsigned short*>(mine + piece_at<128>(q, c1 >> 3) + (c1 & 7) * 2);
-                else static_cast<float*>(p.y)[at + c1] =
-                    *reinterpret_cast<const float*>(mine + piece_at<128>(q, c1 >> 2) + (c1 & 3) * 4);
+                if (DT) static_cast<unsigned short*>(p.y)[at] =
+                    *reinterpret_cast<const unsigned short*>(mine + piece_at<kRow>(q, r >> 3) + (r & 7) * 2);
+                else static_cast<float*>(p.y)[at] = *reinterpret_cast<const float*>(mine + piece_at<kRow>(q, r >> 2) + (r & 3) * 4);
               }
-              if (p.pre && !p.vec_pre)
-                p.pre[at + c1] = *reinterpret_cast<const unsigned short*>(stage + 2 * kPiece + piece_at<kPreRow>(q, c1 >> 3) + (c1 & 7) * 2);
+              if (keep && !p.vec_pre)
+                p.pre[at] = *reinterpret_cast<const unsigned short*>(pre_stage + piece_at<kPreRow>(q, r >> 3) + (r & 7) * 2);
             }
-          }
           __syncwarp();                          // before the next piece takes the place
         }
         ++piece;
       }
       if (ok && !waited) {                       // no piece of this tile: pass the accumulator on
         if (!__all_sync(0xFFFFFFFFu, !fail && mbar_wait_suspend(acc_full + 8 * acc, (it >> 1) & 1))) { give_up(); break; }
-        if (lane == 0) {
+        if (leader) {
           if (PAIR) mbar_arrive_rank0(acc_empty + 8 * acc);
           else mbar_arrive(acc_empty + 8 * acc);
         }
       }
     }
-    if (lane == 0) {
+    if (leader) {
       if (!ok)
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);       // copies in flight land
       bulk_wait_read<0>();                       // the pieces have left shared memory
@@ -391,6 +396,198 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
     if (PAIR) tmem_dealloc_pair(tmem_base, p.tmem_cols);
     else tmem_dealloc(tmem_base, p.tmem_cols);
   }
+}
+
+// ---- few tiles: the reduction is split over the CTAs of a cluster ----
+//
+// An SM takes in some 85 GB/s of operands, whatever the tile, so a product of few tiles goes by how many SMs fetch them.  Each CTA
+// of a cluster of S sums its share of k for the same tile of 128 x tile_n, puts its sums into its shared memory, and after
+// a cluster barrier finishes 128 / S of the rows: the S sums of an element are added in the order of the CTAs' ranks.
+
+constexpr int kSplitThreads = 256;
+
+struct SplitArgs {
+  int m, n;
+  int tile_n, tiles_n;
+  int splits, stages, stage_bytes, ktiles;
+  int act, dt;
+  const float* bias;
+  const void* residual;
+  void* y;
+  unsigned short* pre;
+  uint32_t* status;
+};
+
+__device__ __forceinline__ float4 load_cluster(uint32_t addr, uint32_t rank) {
+  float4 v;
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+  return v;
+}
+
+template <int B_MN>
+__global__ void __launch_bounds__(kSplitThreads)
+linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
+                    const __grid_constant__ SplitArgs p) {
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 1];
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile uint32_t fail;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
+  const uint32_t lane = lane_id();
+  const bool leader = elected();
+  const uint32_t rank = cluster_ctarank();
+  const int tile = static_cast<int>(blockIdx.x) / p.splits;
+  const int m0 = tile / p.tiles_n * kTileM, n0 = tile % p.tiles_n * p.tile_n;
+  const int kt_begin = static_cast<int>(static_cast<long long>(p.ktiles) * rank / p.splits);
+  const int kt_end = static_cast<int>(static_cast<long long>(p.ktiles) * (rank + 1) / p.splits);
+  const uint32_t full = smem_u32(bars), empty = full + 8 * kMaxStages, acc_full = full + 16 * kMaxStages;
+  if (tid == 0) {
+    tma_prefetch_desc(&a_map);
+    tma_prefetch_desc(&b_map);
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(full + 8 * s, 1);
+      mbar_init(empty + 8 * s, 1);
+    }
+    mbar_init(acc_full, 1);
+    fail = 0;
+    fence_barrier_init();
+  }
+  if (warp == 1) tmem_alloc(smem_u32(&tmem_slot), p.tile_n);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_slot;
+  pdl_wait();
+  pdl_trigger();
+  if (blockIdx.x == 0 && tid == 0) *p.status = 0u;              // (a wait gives up after seconds, long behind this)
+  const auto give_up = [&]() {
+    fail = 1;
+    atomicMax(p.status, static_cast<uint32_t>(SURGEON_ERR_TIMEOUT));
+  };
+  if (warp == 0) {
+    int s = 0;
+    uint32_t phase = 1;
+    bool ok = true;
+    for (int kt = kt_begin; kt < kt_end; ++kt) {
+      if (!__all_sync(0xFFFFFFFFu, !fail && mbar_wait_suspend(empty + 8 * s, phase))) { give_up(); ok = false; break; }
+      const uint32_t a_at = smem_u32(smem) + s * p.stage_bytes, b_at = a_at + kABytes, bar = full + 8 * s;
+      if (leader) {
+        mbar_arrive_expect_tx(bar, static_cast<uint32_t>(p.stage_bytes));
+        tma_load_2d(a_at, &a_map, kt * kTileK, m0, bar);
+        if (B_MN) {
+          for (int g = 0; g < p.tile_n / 64; ++g) tma_load_2d(b_at + g * (kTileK * 128), &b_map, n0 + g * 64, kt * kTileK, bar);
+        } else {
+          tma_load_2d(b_at, &b_map, kt * kTileK, n0, bar);
+        }
+      }
+      __syncwarp();
+      if (++s == p.stages) { s = 0; phase ^= 1; }
+    }
+    if (!ok)
+      for (int i = 0; i < 1000; ++i) __nanosleep(1000);         // copies in flight land
+  } else if (warp == 1) {
+    const uint32_t idesc = make_idesc(kTileM, p.tile_n) | (B_MN ? 1u << 16 : 0u);
+    const uint64_t a_base = make_desc(smem_u32(smem));
+    const uint64_t b_base = B_MN ? make_desc_rows(smem_u32(smem) + kABytes) : make_desc(smem_u32(smem) + kABytes);
+    constexpr int kStepB = B_MN ? 128 : 2;
+    int s = 0;
+    uint32_t phase = 0;
+    for (int kt = kt_begin; kt < kt_end; ++kt) {
+      if (!__all_sync(0xFFFFFFFFu, !fail && mbar_wait_suspend(full + 8 * s, phase))) { give_up(); break; }
+      tc_fence_after();
+      const uint64_t off = static_cast<uint64_t>((s * p.stage_bytes) >> 4);
+      if (leader) {
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+          umma_bf16(tmem_base, a_base + off + 2 * kk, b_base + off + kStepB * kk, idesc, kt > kt_begin || kk > 0 ? 1u : 0u);
+        umma_commit(empty + 8 * s);
+        if (kt + 1 == kt_end) umma_commit(acc_full);
+      }
+      __syncwarp();
+      if (++s == p.stages) { s = 0; phase ^= 1; }
+    }
+  }
+  __syncwarp();
+  // all MMAs of this CTA are done, and with them the ring: the sums take its place, rows of tile_n + 4
+  if (!__all_sync(0xFFFFFFFFu, mbar_wait_suspend(acc_full, 0))) give_up();
+  tc_fence_after();
+  const int pitch = p.tile_n + 4;
+  float* sums = reinterpret_cast<float*>(smem);
+  {
+    const int quarter = warp & 3, row = quarter * 32 + static_cast<int>(lane);
+    for (int c = (warp >> 2) * 32; c < p.tile_n; c += 64) {
+      uint32_t v[32];
+      tmem_ld32(tmem_base + (static_cast<uint32_t>(quarter) << 21) + c, v);
+      tmem_ld_wait();
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        *reinterpret_cast<uint4*>(sums + row * pitch + c + 4 * j) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, p.tile_n);
+  }
+  cluster_sync_all();
+  const int rows = kTileM / p.splits, across = p.tile_n / 4;
+  for (int i = tid; i < rows * across; i += kSplitThreads) {
+    const int row = static_cast<int>(rank) * rows + i / across, c = i % across * 4;
+    const int m = m0 + row, n = n0 + c;
+    if (m >= p.m || n >= p.n) continue;
+    const uint32_t at = smem_u32(sums + row * pitch + c);
+    float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k = 0; k < p.splits; ++k) {
+      const float4 q = load_cluster(at, static_cast<uint32_t>(k));
+      f[0] += q.x; f[1] += q.y; f[2] += q.z; f[3] += q.w;
+    }
+    const long long out = static_cast<long long>(m) * p.n + n;
+    const bool vec = (p.n & 3) == 0;             // four columns are one aligned vector of every array
+    const int left = p.n - n < 4 ? p.n - n : 4;
+    if (p.bias) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (e < left) f[e] += __ldg(p.bias + n + e);
+    }
+    if (p.pre) {
+      if (vec) store_elems<1, 4>(p.pre, out, f);
+      else
+        for (int e = 0; e < left; ++e) { const float g[1] = {f[e]}; store_elems<1, 1>(p.pre, out + e, g); }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = activate(f[e], p.act);
+    if (p.residual) {
+      float q[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (vec) {
+        if (p.dt) load_elems<1, 4>(p.residual, out, q);
+        else load_elems<0, 4>(p.residual, out, q);
+      } else {
+        for (int e = 0; e < left; ++e) {
+          float g[1];
+          if (p.dt) load_elems<1, 1>(p.residual, out + e, g);
+          else load_elems<0, 1>(p.residual, out + e, g);
+          q[e] = g[0];
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[e] += q[e];
+    }
+    if (vec) {
+      if (p.dt) store_elems<1, 4>(p.y, out, f);
+      else store_elems<0, 4>(p.y, out, f);
+    } else {
+      for (int e = 0; e < left; ++e) {
+        const float g[1] = {f[e]};
+        if (p.dt) store_elems<1, 1>(p.y, out + e, g);
+        else store_elems<0, 1>(p.y, out + e, g);
+      }
+    }
+  }
+  cluster_sync_all();                            // the others may still read this CTA's sums
 }
 
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -413,13 +610,13 @@ bool encode(CUtensorMap* map, const void* base, int dt, long long rows, long lon
 }
 
 struct Shape {
-  int pair, tile_n;
+  int pair, tile_n, splits;                      // splits > 0: the kernel for few tiles
 };
 
 // The tile with the shortest estimate: waves of tiles times a tile's clocks (tile_n per 64 of k while the tensor cores are the
 // bound, the operands' bytes otherwise, and its epilogue where that is longer).
 Shape choose_tile(const Product& p) {
-  static const Shape all[] = {{1, 256}, {1, 128}, {0, 256}, {0, 128}, {0, 64}};
+  static const Shape all[] = {{1, 256, 0}, {1, 128, 0}, {0, 256, 0}, {0, 128, 0}, {0, 64, 0}};
   const int sms = sm_count();
   const long long ktiles = (p.k + kTileK - 1) / kTileK;
   Shape best = all[0];
@@ -443,7 +640,6 @@ Shape choose_tile(const Product& p) {
 
 template <int PAIR, int B_MN, int DT>
 cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream_t stream) {
-  constexpr int kCols = DT ? 64 : 32;
   TileArgs t = {};
   t.m = p.m; t.n = p.n; t.k = p.k;
   t.tile_n = tile_n;
@@ -453,11 +649,11 @@ cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream
   t.ktiles = (p.k + kTileK - 1) / kTileK;
   const int b_rows = PAIR ? tile_n / 2 : tile_n;
   t.stage_bytes = kABytes + b_rows * 128;
-  const int staging = kEpiWarps * (p.pre ? 3 : 2) * kPiece;
+  const int staging = kEpiWarps<DT> * ((p.residual ? 2 : 1) * kPiece<DT> + (p.pre ? kPrePiece : 0));
   t.stages = (227 * 1024 - 4096 - staging) / t.stage_bytes;
   if (t.stages > kMaxStages) t.stages = kMaxStages;
-  if (t.stages > t.ktiles + 2) t.stages = t.ktiles + 2;
-  t.tmem_cols = 2 * tile_n;
+  t.tmem_cols = 128;                             // two accumulators; an allocation is a power of two
+  while (t.tmem_cols < 2 * tile_n) t.tmem_cols *= 2;
   const int size = DT ? 2 : 4;
   t.vec_y = (static_cast<long long>(p.n) * size) % 16 == 0;
   t.vec_pre = p.n % 8 == 0;
@@ -483,9 +679,11 @@ cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream
   if (e != cudaSuccess) return e;
   const int at_once = PAIR ? sm_count() / 2 : sm_count();
   const int groups = t.tiles < at_once ? t.tiles : at_once;
+  t.step_m = groups / t.tiles_n;
+  t.step_n = groups % t.tiles_n;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(PAIR ? 2 * groups : groups);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(kThreads<DT>);
   cfg.dynamicSmemBytes = static_cast<size_t>(smem);
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
@@ -502,10 +700,61 @@ cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream
   return e;
 }
 
+template <int B_MN>
+cudaError_t launch_split(const Product& p, int tile_n, int splits, uint32_t* status, cudaStream_t stream) {
+  SplitArgs t = {};
+  t.m = p.m; t.n = p.n;
+  t.tile_n = tile_n;
+  t.tiles_n = (p.n + tile_n - 1) / tile_n;
+  t.splits = splits;
+  t.ktiles = (p.k + kTileK - 1) / kTileK;
+  if (splits > t.ktiles) return cudaErrorInvalidValue;           // (a CTA without a share would never be done)
+  t.stage_bytes = kABytes + tile_n * 128;
+  const int share = (t.ktiles + splits - 1) / splits;
+  t.stages = (200 * 1024) / t.stage_bytes;
+  if (t.stages > kMaxStages) t.stages = kMaxStages;
+  if (t.stages > share) t.stages = share;
+  t.act = p.act; t.dt = p.dt;
+  t.bias = p.bias; t.residual = p.residual; t.y = p.y;
+  t.pre = static_cast<unsigned short*>(p.pre);
+  t.status = status;
+  CUtensorMap maps[2];
+  memset(maps, 0, sizeof(maps));
+  bool ok = encode(&maps[0], p.a, 1, p.m, p.k, p.lda, kTileM, kTileK);
+  ok = ok && (B_MN ? encode(&maps[1], p.b, 1, p.k, p.n, p.ldb, kTileK, 64) : encode(&maps[1], p.b, 1, p.n, p.k, p.ldb, tile_n, kTileK));
+  if (!ok) return cudaErrorInvalidValue;
+  int smem = t.stages * t.stage_bytes;
+  const int sums = kTileM * (tile_n + 4) * 4;
+  smem = 1024 + (smem > sums ? smem : sums);
+  const auto kernel = linear_split_kernel<B_MN>;
+  cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
+  if (e != cudaSuccess) return e;
+  const int tiles = (p.m + kTileM - 1) / kTileM * t.tiles_n;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(tiles * splits);
+  cfg.blockDim = dim3(kSplitThreads);
+  cfg.dynamicSmemBytes = static_cast<size_t>(smem);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = splits;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  e = cudaLaunchKernelEx(&cfg, kernel, maps[0], maps[1], t);
+  note_launches(1);
+  return e;
+}
+
 }  // namespace
 
 cudaError_t launch_product(const Product& p, uint32_t* status, cudaStream_t stream) {
   const Shape s = choose_tile(p);
+  if (s.splits)
+    return p.b_mn ? launch_split<1>(p, s.tile_n, s.splits, status, stream) : launch_split<0>(p, s.tile_n, s.splits, status, stream);
 #define SURGEON_PRODUCT(PAIR)                                                                              \
   (p.b_mn ? (p.dt ? launch_as<PAIR, 1, 1>(p, s.tile_n, status, stream) : launch_as<PAIR, 1, 0>(p, s.tile_n, status, stream)) \
           : (p.dt ? launch_as<PAIR, 0, 1>(p, s.tile_n, status, stream) : launch_as<PAIR, 0, 0>(p, s.tile_n, status, stream)))

@@ -198,6 +198,14 @@ __device__ __forceinline__ unsigned short to_bf16_bits(float v) {
 }
 
 
+// True in one lane of a converged warp, always the same.  Copies and MMAs issued under this predicate cost the issuing warp some 60
+// clocks each, under `lane == 0` 130: two operands per 64 of k were then the bound of every tile below 128 x 256.
+__device__ __forceinline__ bool elected() {
+  uint32_t on;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(on));
+  return on != 0;
+}
+
 // ---- CTA pairs (cta_group::2): two CTAs of a cluster of 2 act as one MMA of M = 256 ---------
 // Each CTA holds 128 rows of A, half of the N rows of B and its own 128 x N accumulator; the
 // CTA of rank 0 issues the MMAs and owns the "full" barriers, commits arrive in both CTAs.
