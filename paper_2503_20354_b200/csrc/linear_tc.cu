@@ -97,7 +97,6 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
   __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 4 + 2 * kWarps];
   __shared__ __align__(16) float s_bias[kWarps][kCols];
   __shared__ uint32_t tmem_slot;
-  __shared__ volatile uint32_t fail;
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);      // (uniform for the compiler too)
   const uint32_t lane = lane_id();
@@ -129,7 +128,6 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
       mbar_init(acc_empty + 8 * a, (PAIR ? 2 : 1) * kWarps);
     }
     for (int w = 0; w < 2 * kWarps; ++w) mbar_init(res_bar + 8 * w, 1);
-    fail = 0;
     fence_barrier_init();
   }
   if (warp == 1) {
@@ -145,23 +143,20 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
   pdl_trigger();
   if (blockIdx.x == 0 && tid == 0) *p.status = 0u;              // (a wait gives up after seconds, long behind this)
 
-  const auto give_up = [&]() {
-    fail = 1;
-    atomicMax(p.status, static_cast<uint32_t>(SURGEON_ERR_TIMEOUT));
-  };
+  const auto give_up = [&]() { atomicMax(p.status, static_cast<uint32_t>(SURGEON_ERR_TIMEOUT)); };
 
   if (warp == 0) {
     // ---- operands ----
-    int s = 0, tm = first_m, tn = first_n;
-    uint32_t phase = 1;                          // (a fresh barrier counts as passed in its phase before)
-    bool ok = true;
-    for (int t = tile_first; t < p.tiles && ok; t += tile_step, advance(tm, tn)) {
-      const int m0 = tm * kTileRows + static_cast<int>(rank) * kTileM;
-      const int n0 = tn * p.tile_n + static_cast<int>(rank) * b_rows;
-      for (int kt = 0; kt < p.ktiles; ++kt) {
-        if (!__all_sync(0xFFFFFFFFu, !fail && mbar_wait_suspend(empty + 8 * s, phase))) { give_up(); ok = false; break; }
-        const uint32_t a_at = smem_u32(smem) + s * p.stage_bytes, b_at = a_at + kABytes, bar = full + 8 * s;
-        if (leader) {
+    if (leader) {
+      int s = 0, tm = first_m, tn = first_n;
+      uint32_t phase = 1;                        // (a fresh barrier counts as passed in its phase before)
+      bool ok = true, free = true;
+      for (int t = tile_first; t < p.tiles && ok; t += tile_step, advance(tm, tn)) {
+        const int m0 = tm * kTileRows + static_cast<int>(rank) * kTileM;
+        const int n0 = tn * p.tile_n + static_cast<int>(rank) * b_rows;
+        for (int kt = 0; kt < p.ktiles; ++kt) {
+          if (!free && !mbar_wait_suspend(empty + 8 * s, phase)) { give_up(); ok = false; break; }
+          const uint32_t a_at = smem_u32(smem) + s * p.stage_bytes, b_at = a_at + kABytes, bar = full + 8 * s;
           if (rank == 0) mbar_arrive_expect_tx(bar, (PAIR ? 2u : 1u) * static_cast<uint32_t>(p.stage_bytes));
           if (PAIR) tma_load_2d_pair(a_at, &a_map, kt * kTileK, m0, bar);
           else tma_load_2d(a_at, &a_map, kt * kTileK, m0, bar);
@@ -175,50 +170,47 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
           } else {
             tma_load_2d(b_at, &b_map, kt * kTileK, n0, bar);
           }
+          if (++s == p.stages) { s = 0; phase ^= 1; }
+          free = mbar_test(empty + 8 * s, phase);
         }
-        __syncwarp();
-        if (++s == p.stages) { s = 0; phase ^= 1; }
       }
+      if (!ok)
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);       // copies in flight land
     }
-    if (!ok)
-      for (int i = 0; i < 1000; ++i) __nanosleep(1000);         // copies in flight land
   } else if (warp == 1) {
     // ---- MMAs ----
-    if (rank == 0) {
+    if (leader && rank == 0) {
       const uint32_t idesc = make_idesc(kTileRows, p.tile_n) | (B_MN ? 1u << 16 : 0u);
       const uint64_t a_base = make_desc(smem_u32(smem));
       const uint64_t b_base = B_MN ? make_desc_rows(smem_u32(smem) + kABytes) : make_desc(smem_u32(smem) + kABytes);
       constexpr int kStepB = B_MN ? 128 : 2;
       int s = 0, it = 0;
       uint32_t phase = 0;
-      bool ok = true;
+      bool ok = true, there = false;
       for (int t = tile_first; t < p.tiles && ok; t += tile_step, ++it) {
         const int acc = it & 1;
-        if (!__all_sync(0xFFFFFFFFu, !fail && (PAIR ? mbar_wait_suspend_cluster(acc_empty + 8 * acc, ((it >> 1) & 1) ^ 1)
-                                                    : mbar_wait_suspend(acc_empty + 8 * acc, ((it >> 1) & 1) ^ 1)))) { give_up(); break; }
+        if (!(PAIR ? mbar_wait_suspend_cluster(acc_empty + 8 * acc, ((it >> 1) & 1) ^ 1)
+                   : mbar_wait_suspend(acc_empty + 8 * acc, ((it >> 1) & 1) ^ 1))) { give_up(); break; }
         tc_fence_after();
         const uint32_t d = tmem_base + acc * (p.tmem_cols >> 1);
         for (int kt = 0; kt < p.ktiles; ++kt) {
-          if (!__all_sync(0xFFFFFFFFu, !fail && mbar_wait_suspend(full + 8 * s, phase))) { give_up(); ok = false; break; }
+          if (!there && !mbar_wait_suspend(full + 8 * s, phase)) { give_up(); ok = false; break; }
           tc_fence_after();
           const uint64_t off = static_cast<uint64_t>((s * p.stage_bytes) >> 4);
-          if (leader) {
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-              const uint64_t da = a_base + off + 2 * kk, db = b_base + off + kStepB * kk;
-              if (PAIR) umma_bf16_pair(d, da, db, idesc, kt > 0 || kk > 0 ? 1u : 0u);
-              else umma_bf16(d, da, db, idesc, kt > 0 || kk > 0 ? 1u : 0u);
-            }
-            if (PAIR) umma_commit_pair(empty + 8 * s);
-            else umma_commit(empty + 8 * s);
-            if (kt + 1 == p.ktiles) {
-              if (PAIR) umma_commit_pair(acc_full + 8 * acc);
-              else umma_commit(acc_full + 8 * acc);
-            }
+          for (int kk = 0; kk < 4; ++kk) {
+            const uint64_t da = a_base + off + 2 * kk, db = b_base + off + kStepB * kk;
+            if (PAIR) umma_bf16_pair(d, da, db, idesc, kt > 0 || kk > 0 ? 1u : 0u);
+            else umma_bf16(d, da, db, idesc, kt > 0 || kk > 0 ? 1u : 0u);
           }
-          __syncwarp();
+          const uint32_t done = empty + 8 * s;
           if (++s == p.stages) { s = 0; phase ^= 1; }
+          there = mbar_test(full + 8 * s, phase);
+          if (PAIR) umma_commit_pair(done);
+          else umma_commit(done);
         }
+        if (PAIR) umma_commit_pair(acc_full + 8 * acc);
+        else umma_commit(acc_full + 8 * acc);
       }
     }
   } else {
@@ -281,7 +273,7 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
         }
         if (!waited) {
           // (all lanes go the same way: behind are instructions of the whole warp)
-          if (!__all_sync(0xFFFFFFFFu, !fail && mbar_wait_suspend(acc_full + 8 * acc, (it >> 1) & 1))) { give_up(); ok = false; break; }
+          if (!__all_sync(0xFFFFFFFFu, mbar_wait_suspend(acc_full + 8 * acc, (it >> 1) & 1))) { give_up(); ok = false; break; }
           tc_fence_after();
           waited = true;
         }
@@ -323,7 +315,7 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
 #pragma unroll
           for (int i = 0; i < kCols; ++i) v[i] = __float_as_uint(activate<kActRelu>(__uint_as_float(v[i])));
         }
-        if (tma_res && !__all_sync(0xFFFFFFFFu, !fail && mbar_wait_suspend(my_res + 8 * buf, (piece >> 1) & 1))) {
+        if (tma_res && !__all_sync(0xFFFFFFFFu, mbar_wait_suspend(my_res + 8 * buf, (piece >> 1) & 1))) {
           give_up();
           ok = false;
           break;
@@ -375,7 +367,7 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
         ++piece;
       }
       if (ok && !waited) {                       // no piece of this tile: pass the accumulator on
-        if (!__all_sync(0xFFFFFFFFu, !fail && mbar_wait_suspend(acc_full + 8 * acc, (it >> 1) & 1))) { give_up(); break; }
+        if (!__all_sync(0xFFFFFFFFu, mbar_wait_suspend(acc_full + 8 * acc, (it >> 1) & 1))) { give_up(); break; }
         if (leader) {
           if (PAIR) mbar_arrive_rank0(acc_empty + 8 * acc);
           else mbar_arrive(acc_empty + 8 * acc);
@@ -434,7 +426,6 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 1];
   __shared__ uint32_t tmem_slot;
-  __shared__ volatile uint32_t fail;
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
   const uint32_t lane = lane_id();
   const bool leader = elected();
@@ -452,7 +443,6 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
       mbar_init(empty + 8 * s, 1);
     }
     mbar_init(acc_full, 1);
-    fail = 0;
     fence_barrier_init();
   }
   if (warp == 1) tmem_alloc(smem_u32(&tmem_slot), p.tile_n);
@@ -463,18 +453,15 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
   pdl_wait();
   pdl_trigger();
   if (blockIdx.x == 0 && tid == 0) *p.status = 0u;              // (a wait gives up after seconds, long behind this)
-  const auto give_up = [&]() {
-    fail = 1;
-    atomicMax(p.status, static_cast<uint32_t>(SURGEON_ERR_TIMEOUT));
-  };
+  const auto give_up = [&]() { atomicMax(p.status, static_cast<uint32_t>(SURGEON_ERR_TIMEOUT)); };
   if (warp == 0) {
-    int s = 0;
-    uint32_t phase = 1;
-    bool ok = true;
-    for (int kt = kt_begin; kt < kt_end; ++kt) {
-      if (!__all_sync(0xFFFFFFFFu, !fail && mbar_wait_suspend(empty + 8 * s, phase))) { give_up(); ok = false; break; }
-      const uint32_t a_at = smem_u32(smem) + s * p.stage_bytes, b_at = a_at + kABytes, bar = full + 8 * s;
-      if (leader) {
+    if (leader) {
+      int s = 0;
+      uint32_t phase = 1;
+      bool ok = true, free = true;
+      for (int kt = kt_begin; kt < kt_end; ++kt) {
+        if (!free && !mbar_wait_suspend(empty + 8 * s, phase)) { give_up(); ok = false; break; }
+        const uint32_t a_at = smem_u32(smem) + s * p.stage_bytes, b_at = a_at + kABytes, bar = full + 8 * s;
         mbar_arrive_expect_tx(bar, static_cast<uint32_t>(p.stage_bytes));
         tma_load_2d(a_at, &a_map, kt * kTileK, m0, bar);
         if (B_MN) {
@@ -482,32 +469,34 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
         } else {
           tma_load_2d(b_at, &b_map, kt * kTileK, n0, bar);
         }
+        if (++s == p.stages) { s = 0; phase ^= 1; }
+        free = mbar_test(empty + 8 * s, phase);
       }
-      __syncwarp();
-      if (++s == p.stages) { s = 0; phase ^= 1; }
+      if (!ok)
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);       // copies in flight land
     }
-    if (!ok)
-      for (int i = 0; i < 1000; ++i) __nanosleep(1000);         // copies in flight land
   } else if (warp == 1) {
-    const uint32_t idesc = make_idesc(kTileM, p.tile_n) | (B_MN ? 1u << 16 : 0u);
-    const uint64_t a_base = make_desc(smem_u32(smem));
-    const uint64_t b_base = B_MN ? make_desc_rows(smem_u32(smem) + kABytes) : make_desc(smem_u32(smem) + kABytes);
-    constexpr int kStepB = B_MN ? 128 : 2;
-    int s = 0;
-    uint32_t phase = 0;
-    for (int kt = kt_begin; kt < kt_end; ++kt) {
-      if (!__all_sync(0xFFFFFFFFu, !fail && mbar_wait_suspend(full + 8 * s, phase))) { give_up(); break; }
-      tc_fence_after();
-      const uint64_t off = static_cast<uint64_t>((s * p.stage_bytes) >> 4);
-      if (leader) {
+    if (leader) {
+      const uint32_t idesc = make_idesc(kTileM, p.tile_n) | (B_MN ? 1u << 16 : 0u);
+      const uint64_t a_base = make_desc(smem_u32(smem));
+      const uint64_t b_base = B_MN ? make_desc_rows(smem_u32(smem) + kABytes) : make_desc(smem_u32(smem) + kABytes);
+      constexpr int kStepB = B_MN ? 128 : 2;
+      int s = 0;
+      uint32_t phase = 0;
+      bool there = false;
+      for (int kt = kt_begin; kt < kt_end; ++kt) {
+        if (!there && !mbar_wait_suspend(full + 8 * s, phase)) { give_up(); break; }
+        tc_fence_after();
+        const uint64_t off = static_cast<uint64_t>((s * p.stage_bytes) >> 4);
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk)
           umma_bf16(tmem_base, a_base + off + 2 * kk, b_base + off + kStepB * kk, idesc, kt > kt_begin || kk > 0 ? 1u : 0u);
-        umma_commit(empty + 8 * s);
-        if (kt + 1 == kt_end) umma_commit(acc_full);
+        const uint32_t done = empty + 8 * s;
+        if (++s == p.stages) { s = 0; phase ^= 1; }
+        there = mbar_test(full + 8 * s, phase);
+        umma_commit(done);
       }
-      __syncwarp();
-      if (++s == p.stages) { s = 0; phase ^= 1; }
+      umma_commit(acc_full);
     }
   }
   __syncwarp();

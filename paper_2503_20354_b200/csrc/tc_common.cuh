@@ -206,6 +206,19 @@ __device__ __forceinline__ bool elected() {
   return on != 0;
 }
 
+// Whether a phase is over, without waiting: asked ahead of its use, the answer's latency is hidden.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
 // ---- CTA pairs (cta_group::2): two CTAs of a cluster of 2 act as one MMA of M = 256 ---------
 // Each CTA holds 128 rows of A, half of the N rows of B and its own 128 x N accumulator; the
 // CTA of rank 0 issues the MMAs and owns the "full" barriers, commits arrive in both CTAs.
