@@ -59,42 +59,61 @@ __device__ __forceinline__ int tensor_of(const T& t, uint32_t unit) {
   return lo;
 }
 
-// Calls f(address, element, vec) for the places of unit `u` of a tensor: whole 16-byte vectors, or (vec false) single elements.
-template <int DT, typename F>
-__device__ __forceinline__ void for_unit(const void* grad, long long n, uint32_t u, F&& f) {
-  constexpr int E = DT == 0 ? 4 : 8, kSize = DT == 0 ? 4 : 2, kUnit = kUnitBytes / kSize;
-  const int shift = static_cast<int>(reinterpret_cast<uintptr_t>(grad) & 15) / kSize;     // elements behind a 16-byte boundary
-  const long long at = static_cast<long long>(u) * kUnit - shift;
-#pragma unroll
-  for (int i = 0; i < kUnit / E / kThreads; ++i) {
-    const long long j = at + (i * kThreads + static_cast<int>(threadIdx.x)) * E;
-    if (j >= 0 && j + E <= n) f(j, true);
-    else
-      for (int e = 0; e < E; ++e)
-        if (j + e >= 0 && j + e < n) f(j + e, false);
+// First element of unit `u` (below 0 in front of a tensor that starts behind a 16-byte boundary) and whether all of the unit's
+// elements are the tensor's.
+template <int DT>
+struct Unit {
+  static constexpr int kSize = DT == 0 ? 4 : 2, kElems = 16 / kSize, kUnit = kUnitBytes / kSize, kVecs = kUnitBytes / 16 / kThreads;
+  long long at;
+  bool whole;
+  __device__ __forceinline__ Unit(const void* grad, long long n, uint32_t u) {
+    at = static_cast<long long>(u) * kUnit - static_cast<int>(reinterpret_cast<uintptr_t>(grad) & 15) / kSize;
+    whole = at >= 0 && at + kUnit <= n;
+  }
+  // this thread's i-th vector
+  __device__ __forceinline__ long long vec(int i) const { return at + (i * kThreads + static_cast<int>(threadIdx.x)) * kElems; }
+};
+
+template <int DT>
+__device__ __forceinline__ void vector_elems(uint4 v, float (&f)[DT == 0 ? 4 : 8]) {
+  if constexpr (DT == 0) {
+    f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+  } else {
+    f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
+    f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z); f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
   }
 }
 
 template <int DT>
 __device__ __forceinline__ double unit_squares(const void* grad, long long n, uint32_t u) {
-  constexpr int E = DT == 0 ? 4 : 8;
+  using T = typename Elem<DT>::type;
+  const Unit<DT> unit(grad, n, u);
+  constexpr int E = Unit<DT>::kElems;
   double acc = 0.0;
-  for_unit<DT>(grad, n, u, [&](long long j, bool vec) {
-    if (vec) {
-      float f[E];
-      load_elems<DT, E>(grad, j, f);
+  if (unit.whole) {                          // (a branch around each load would let one load at a time be on its way)
+    uint4 v[Unit<DT>::kVecs];
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const double d = static_cast<double>(f[e]);
-        acc += d * d;
-      }
-    } else {
-      float f[1];
-      load_elems<DT, 1>(grad, j, f);
-      const double d = static_cast<double>(f[0]);
-      acc += d * d;
+    for (int i = 0; i < Unit<DT>::kVecs; ++i) v[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(grad) + unit.vec(i));
+#pragma unroll
+    for (int i = 0; i < Unit<DT>::kVecs; ++i) {
+      float f[E];
+      vector_elems<DT>(v[i], f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc = fma(static_cast<double>(f[e]), static_cast<double>(f[e]), acc);
     }
-  });
+    return acc;
+  }
+#pragma unroll 1
+  for (int i = 0; i < Unit<DT>::kVecs; ++i) {
+    const long long j = unit.vec(i);
+#pragma unroll 1
+    for (int e = 0; e < E; ++e) {
+      if (j + e < 0 || j + e >= n) continue;
+      float f[1];
+      load_elems<DT, 1>(grad, j + e, f);
+      acc = fma(static_cast<double>(f[0]), static_cast<double>(f[0]), acc);
+    }
+  }
   return acc;
 }
 
@@ -173,24 +192,36 @@ __device__ __forceinline__ void scale_one(const void* grad, void* out, long long
 template <int DT>
 __device__ __forceinline__ void scale_unit(const void* grad, void* out, long long n, uint32_t u, float coef, bool copy) {
   using T = typename Elem<DT>::type;
-  constexpr int E = DT == 0 ? 4 : 8;
-  const bool same = ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
-  for_unit<DT>(grad, n, u, [&](long long j, bool vec) {
-    if (!vec) {
-      scale_one<DT>(grad, out, j, coef, copy);
-    } else if (same && copy) {
-      *reinterpret_cast<uint4*>(static_cast<T*>(out) + j) = *reinterpret_cast<const uint4*>(static_cast<const T*>(grad) + j);
-    } else if (same) {
-      float f[E];
-      load_elems<DT, E>(grad, j, f);
+  const Unit<DT> unit(grad, n, u);
+  constexpr int E = Unit<DT>::kElems;
+  if (unit.whole && ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0) {
+    uint4 v[Unit<DT>::kVecs];
 #pragma unroll
-      for (int e = 0; e < E; ++e) f[e] *= coef;
-      store_elems<DT, E>(out, j, f);
-    } else {
+    for (int i = 0; i < Unit<DT>::kVecs; ++i) v[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(grad) + unit.vec(i));
 #pragma unroll
-      for (int e = 0; e < E; ++e) scale_one<DT>(grad, out, j + e, coef, copy);
+    for (int i = 0; i < Unit<DT>::kVecs; ++i) {
+      if (!copy) {
+        float f[E];
+        vector_elems<DT>(v[i], f);
+#pragma unroll
+        for (int e = 0; e < E; ++e) f[e] *= coef;
+        if constexpr (DT == 0)
+          v[i] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+        else
+          v[i] = make_uint4(to_bf16x2(f[0], f[1]), to_bf16x2(f[2], f[3]), to_bf16x2(f[4], f[5]), to_bf16x2(f[6], f[7]));
+      }
+      // (written through: the gradients that are still to be read keep their place in L2)
+      __stcs(reinterpret_cast<uint4*>(static_cast<T*>(out) + unit.vec(i)), v[i]);
     }
-  });
+    return;
+  }
+#pragma unroll 1
+  for (int i = 0; i < Unit<DT>::kVecs; ++i) {
+    const long long j = unit.vec(i);
+#pragma unroll 1
+    for (int e = 0; e < E; ++e)
+      if (j + e >= 0 && j + e < n) scale_one<DT>(grad, out, j + e, coef, copy);
+  }
 }
 
 template <int N>
@@ -218,8 +249,8 @@ list_scale_kernel(const __grid_constant__ Table<N> t, const double* __restrict__
   }
 }
 
-constexpr int kSmall = 96, kLarge = 1024;                   // tensors per launch: below 4 KB of parameters, and all that fit
-static_assert(sizeof(Table<kSmall>) <= 4000 && sizeof(Table<kLarge>) <= 32000, "a launch's parameters");
+constexpr int kLarge = 1024;                 // tensors per launch: all that fit
+static_assert(sizeof(Table<96>) <= 4000 && sizeof(Table<kLarge>) <= 32000, "a launch's parameters");
 
 inline uint32_t units_of(const surgeon_gradient& g) {
   const int size = g.dt == SURGEON_F32 ? 4 : 2;
@@ -243,22 +274,24 @@ cudaError_t launch_list_as(const surgeon_gradient* list, int count, int clip, do
     long long slot = 0;
     for (int at = 0; at < count; at += N) {
       const int n = std::min(N, count - at);
-      uint32_t units = 0;
-      for (int w = 0; w < N / 32; ++w) t.types[w] = 0;
-      for (int i = 0; i < n; ++i) {
-        const surgeon_gradient& g = list[at + i];
-        t.grad[i] = g.grad;
-        t.out[i] = g.out;
-        t.n[i] = g.n;
-        t.first[i] = units;
-        if (g.dt == SURGEON_BF16) t.types[i >> 5] |= 1u << (i & 31);
-        units += units_of(g);
+      if (pass == 0 || count > N) {                         // (one launch's table serves both passes)
+        uint32_t units = 0;
+        for (int w = 0; w < N / 32; ++w) t.types[w] = 0;
+        for (int i = 0; i < n; ++i) {
+          const surgeon_gradient& g = list[at + i];
+          t.grad[i] = g.grad;
+          t.out[i] = g.out;
+          t.n[i] = g.n;
+          t.first[i] = units;
+          if (g.dt == SURGEON_BF16) t.types[i >> 5] |= 1u << (i & 31);
+          units += units_of(g);
+        }
+        t.first[n] = units;
+        t.count = n;
+        t.ctas = ctas_for(units, &t.per);
+        t.slot = slot;
+        t.index = at;
       }
-      t.first[n] = units;
-      t.count = n;
-      t.ctas = ctas_for(units, &t.per);
-      t.slot = slot;
-      t.index = at;
       slot += t.ctas + n - 1;
       if (pass == 0)
         launch_kernel(list_squares_kernel<N>, dim3(t.ctas), dim3(kThreads), 0, stream, true, t, slots);
@@ -318,8 +351,10 @@ cudaError_t launch_gradient_list(const surgeon_gradient* list, int count, int cl
   if (count == 0) {                                         // the norm of nothing
     return norm_out ? cudaMemsetAsync(norm_out, 0, sizeof(double), stream) : cudaSuccess;
   }
-  return count <= kSmall ? launch_list_as<kSmall>(list, count, clip, max_norm, norm_out, gi_out, slots, stream)
-                         : launch_list_as<kLarge>(list, count, clip, max_norm, norm_out, gi_out, slots, stream);
+  // (a launch copies its parameters: short lists take small tables)
+  if (count <= 96) return launch_list_as<96>(list, count, clip, max_norm, norm_out, gi_out, slots, stream);
+  if (count <= 320) return launch_list_as<320>(list, count, clip, max_norm, norm_out, gi_out, slots, stream);
+  return launch_list_as<kLarge>(list, count, clip, max_norm, norm_out, gi_out, slots, stream);
 }
 
 }  // namespace surgeon

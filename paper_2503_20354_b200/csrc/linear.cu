@@ -37,13 +37,8 @@ act_grad_kernel(const void* __restrict__ dy, const unsigned short* __restrict__ 
 #pragma unroll
   for (int e = 0; e < E; ++e) acc[e] = 0.0f;
   if (c < cols) {
-#pragma unroll 2
-    for (long long t = begin + warp; t < end; t += kThreads / 32) {
-      float g[E];
-      load_elems<GDT, E>(dy, t * cols + c, g);
+    const auto finish = [&](long long t, float (&g)[E], const float (&z)[E]) {
       if (pre) {
-        float z[E];
-        load_elems<1, E>(pre, t * cols + c, z);
 #pragma unroll
         for (int e = 0; e < E; ++e) g[e] *= act == kActGelu ? slope<kActGelu>(z[e]) : slope<kActRelu>(z[e]);
       }
@@ -51,6 +46,25 @@ act_grad_kernel(const void* __restrict__ dy, const unsigned short* __restrict__ 
       for (int e = 0; e < E; ++e) acc[e] += g[e];
       if (dz) store_elems<0, E>(dz, t * cols + c, g);
       if (dz16) store_elems<1, E>(dz16, t * pitch + c, g);
+    };
+    constexpr int kBatch = 4;                    // rows whose loads are on their way together
+    long long t = begin + warp;
+    for (; t + (kBatch - 1) * (kThreads / 32) < end; t += kBatch * (kThreads / 32)) {
+      float g[kBatch][E], z[kBatch][E];
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) load_elems<GDT, E>(dy, (t + b * (kThreads / 32)) * cols + c, g[b]);
+      if (pre) {
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) load_elems<1, E>(pre, (t + b * (kThreads / 32)) * cols + c, z[b]);
+      }
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) finish(t + b * (kThreads / 32), g[b], z[b]);
+    }
+    for (; t < end; t += kThreads / 32) {
+      float g[E], z[E];
+      load_elems<GDT, E>(dy, t * cols + c, g);
+      if (pre) load_elems<1, E>(pre, t * cols + c, z);
+      finish(t, g, z);
     }
   }
   if (!partial) return;

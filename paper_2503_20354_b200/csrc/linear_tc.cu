@@ -37,7 +37,6 @@ struct TileArgs {
   int stages, stage_bytes, ktiles;
   int tmem_cols;
   int vec_y, vec_pre;                            // rows of y (and the residual), of pre, start at 16-byte boundaries: TMA
-  int act;
   const float* bias;
   const void* residual;
   void* y;
@@ -54,6 +53,12 @@ __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.comm
 template <int N>
 __device__ __forceinline__ void bulk_wait_read() {
   asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
   asm volatile(
@@ -85,8 +90,8 @@ __device__ __forceinline__ uint32_t piece_at(int r, int j) {
   return ROW == 128 ? static_cast<uint32_t>(r * 128 + ((j ^ (r & 7)) << 4)) : static_cast<uint32_t>(r * 64 + ((j ^ ((r >> 1) & 3)) << 4));
 }
 
-// DT: type of y and of the residual.
-template <int PAIR, int B_MN, int DT>
+// DT: type of y and of the residual.  An N-major b comes with no bias, activation or residual (the input's gradient).
+template <int PAIR, int B_MN, int DT, int ACT>
 __global__ void __launch_bounds__(kThreads<DT>, 1)
 linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
               const __grid_constant__ CUtensorMap y_map, const __grid_constant__ CUtensorMap r_map,
@@ -216,7 +221,7 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
   } else {
     // ---- epilogue: rows of tensor memory's quarter `warp % 4`, every kSlots-th piece of columns ----
     const int w = warp - 2, quarter = warp & 3, slot = w >> 2;
-    const bool has_res = p.residual != nullptr, tma_res = has_res && p.vec_y, keep = p.pre != nullptr;
+    const bool has_bias = !B_MN && p.bias, has_res = !B_MN && p.residual, tma_res = has_res && p.vec_y, keep = !B_MN && p.pre;
     // y's places, two of them where a residual comes early, then pre's
     const int y_places = has_res ? 2 : 1;
     unsigned char* stage = smem + p.stages * p.stage_bytes + w * (y_places * kPiece<DT> + (keep ? kPrePiece : 0));
@@ -259,7 +264,7 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
           bulk_wait_read<0>();                   // what left the places has been read
           if (tma_res) fetch_next();
         }
-        if (p.bias) s_bias[w][r] = x + r < p.n ? __ldg(p.bias + x + r) : 0.0f;       // the piece's, for every lane to read
+        if (has_bias) s_bias[w][r] = x + r < p.n ? __ldg(p.bias + x + r) : 0.0f;       // the piece's, for every lane to read
         __syncwarp();
         if (has_res && !tma_res) {
           if (x + r < p.n)
@@ -277,6 +282,11 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
           tc_fence_after();
           waited = true;
         }
+        if (tma_res && !__all_sync(0xFFFFFFFFu, mbar_wait_suspend(my_res + 8 * buf, (piece >> 1) & 1))) {
+          give_up();
+          ok = false;
+          break;
+        }
         uint32_t v[kCols];
         tmem_ld32(tmem_at + c * kCols, v);
         tmem_ld_wait();
@@ -288,45 +298,23 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
             else mbar_arrive(acc_empty + 8 * acc);
           }
         }
-        if (p.bias) {
 #pragma unroll
-          for (int j = 0; j < kCols / 4; ++j) {
-            const float4 b = *reinterpret_cast<const float4*>(&s_bias[w][4 * j]);
-            v[4 * j] = __float_as_uint(__uint_as_float(v[4 * j]) + b.x);
-            v[4 * j + 1] = __float_as_uint(__uint_as_float(v[4 * j + 1]) + b.y);
-            v[4 * j + 2] = __float_as_uint(__uint_as_float(v[4 * j + 2]) + b.z);
-            v[4 * j + 3] = __float_as_uint(__uint_as_float(v[4 * j + 3]) + b.w);
+        for (int j = 0; j < kCols / 8; ++j) {
+          float f[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[8 * j + i]);
+          if (has_bias) {
+            const float4 b0 = *reinterpret_cast<const float4*>(&s_bias[w][8 * j]), b1 = *reinterpret_cast<const float4*>(&s_bias[w][8 * j + 4]);
+            f[0] += b0.x; f[1] += b0.y; f[2] += b0.z; f[3] += b0.w;
+            f[4] += b1.x; f[5] += b1.y; f[6] += b1.z; f[7] += b1.w;
           }
-        }
-        if (keep) {
+          if (keep)
+            *reinterpret_cast<uint4*>(pre_stage + piece_at<kPreRow>(r, j)) =
+                make_uint4(to_bf16x2(f[0], f[1]), to_bf16x2(f[2], f[3]), to_bf16x2(f[4], f[5]), to_bf16x2(f[6], f[7]));
 #pragma unroll
-          for (int j = 0; j < kCols / 8; ++j) {
-            uint32_t o[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              o[i] = to_bf16x2(__uint_as_float(v[8 * j + 2 * i]), __uint_as_float(v[8 * j + 2 * i + 1]));
-            *reinterpret_cast<uint4*>(pre_stage + piece_at<kPreRow>(r, j)) = make_uint4(o[0], o[1], o[2], o[3]);
-          }
-        }
-        if (p.act == kActGelu) {
-#pragma unroll
-          for (int i = 0; i < kCols; ++i) v[i] = __float_as_uint(activate<kActGelu>(__uint_as_float(v[i])));
-        } else if (p.act == kActRelu) {
-#pragma unroll
-          for (int i = 0; i < kCols; ++i) v[i] = __float_as_uint(activate<kActRelu>(__uint_as_float(v[i])));
-        }
-        if (tma_res && !__all_sync(0xFFFFFFFFu, mbar_wait_suspend(my_res + 8 * buf, (piece >> 1) & 1))) {
-          give_up();
-          ok = false;
-          break;
-        }
-#pragma unroll
-        for (int j = 0; j < kRow / 16; ++j) {
-          uint4* at = reinterpret_cast<uint4*>(mine + piece_at<kRow>(r, j));
+          for (int i = 0; i < 8; ++i) f[i] = activate<ACT>(f[i]);
           if constexpr (DT == 1) {
-            float f[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[8 * j + i]);
+            uint4* at = reinterpret_cast<uint4*>(mine + piece_at<kRow>(r, j));
             if (has_res) {
               const uint4 q = *at;
               f[0] += bf16_lo(q.x); f[1] += bf16_hi(q.x); f[2] += bf16_lo(q.y); f[3] += bf16_hi(q.y);
@@ -334,13 +322,15 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
             }
             *at = make_uint4(to_bf16x2(f[0], f[1]), to_bf16x2(f[2], f[3]), to_bf16x2(f[4], f[5]), to_bf16x2(f[6], f[7]));
           } else {
-            float4 f = make_float4(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1]), __uint_as_float(v[4 * j + 2]),
-                                   __uint_as_float(v[4 * j + 3]));
-            if (has_res) {
-              const float4 q = *reinterpret_cast<const float4*>(at);
-              f.x += q.x; f.y += q.y; f.z += q.z; f.w += q.w;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float4* at = reinterpret_cast<float4*>(mine + piece_at<kRow>(r, 2 * j + h));
+              if (has_res) {
+                const float4 q = *at;
+                f[4 * h] += q.x; f[4 * h + 1] += q.y; f[4 * h + 2] += q.z; f[4 * h + 3] += q.w;
+              }
+              *at = make_float4(f[4 * h], f[4 * h + 1], f[4 * h + 2], f[4 * h + 3]);
             }
-            *reinterpret_cast<float4*>(at) = f;
           }
         }
         fence_proxy_async();
@@ -507,13 +497,16 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
   float* sums = reinterpret_cast<float*>(smem);
   {
     const int quarter = warp & 3, row = quarter * 32 + static_cast<int>(lane);
-    for (int c = (warp >> 2) * 32; c < p.tile_n; c += 64) {
-      uint32_t v[32];
-      tmem_ld32(tmem_base + (static_cast<uint32_t>(quarter) << 21) + c, v);
+#pragma unroll 1
+    for (int c = (warp >> 2) * 16; c < p.tile_n; c += 32) {
+      uint32_t v[8], u[8];
+      tmem_ld8(tmem_base + (static_cast<uint32_t>(quarter) << 21) + c, v);
+      tmem_ld8(tmem_base + (static_cast<uint32_t>(quarter) << 21) + c + 8, u);
       tmem_ld_wait();
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        *reinterpret_cast<uint4*>(sums + row * pitch + c + 4 * j) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+      *reinterpret_cast<uint4*>(sums + row * pitch + c) = make_uint4(v[0], v[1], v[2], v[3]);
+      *reinterpret_cast<uint4*>(sums + row * pitch + c + 4) = make_uint4(v[4], v[5], v[6], v[7]);
+      *reinterpret_cast<uint4*>(sums + row * pitch + c + 8) = make_uint4(u[0], u[1], u[2], u[3]);
+      *reinterpret_cast<uint4*>(sums + row * pitch + c + 12) = make_uint4(u[4], u[5], u[6], u[7]);
     }
   }
   tc_fence_before();
@@ -524,6 +517,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
   }
   cluster_sync_all();
   const int rows = kTileM / p.splits, across = p.tile_n / 4;
+#pragma unroll 1
   for (int i = tid; i < rows * across; i += kSplitThreads) {
     const int row = static_cast<int>(rank) * rows + i / across, c = i % across * 4;
     const int m = m0 + row, n = n0 + c;
@@ -602,32 +596,52 @@ struct Shape {
   int pair, tile_n, splits;                      // splits > 0: the kernel for few tiles
 };
 
-// The tile with the shortest estimate: waves of tiles times a tile's clocks (tile_n per 64 of k while the tensor cores are the
-// bound, the operands' bytes otherwise, and its epilogue where that is longer).
+// The tile with the shortest estimate, from measured times in us: `step` per 64 of k, while operands arrive from L2 as fast as
+// an SM takes them in (the widest tile: while the tensor cores are the bound); `tile` for a tile's epilogue, which runs beside
+// the next tile's products; `once` for a launch.  Waves of tiles take the longer of the two each, the last one both.
 Shape choose_tile(const Product& p) {
-  static const Shape all[] = {{1, 256, 0}, {1, 128, 0}, {0, 256, 0}, {0, 128, 0}, {0, 64, 0}};
+  struct Cost {
+    Shape shape;
+    double step, tile, once;
+  };
+  static const Cost all[] = {{{1, 256, 0}, 0.42, 3.0, 2.3}, {{1, 128, 0}, 0.26, 2.0, 2.3}, {{0, 256, 0}, 0.50, 2.3, 1.5},
+                             {{0, 192, 0}, 0.37, 2.2, 1.5}, {{0, 128, 0}, 0.28, 1.25, 1.5}, {{0, 64, 0}, 0.19, 1.0, 1.5},
+                             {{1, 192, 0}, 0.36, 3.2, 2.3}};
+  constexpr int kKMajorOnly = 6;                 // half a tile's columns are no whole slabs of 64
   const int sms = sm_count();
-  const long long ktiles = (p.k + kTileK - 1) / kTileK;
-  Shape best = all[0];
-  double least = 0.0;
-  for (const Shape& s : all) {
-    const long long rows = s.pair ? 2 * kTileM : kTileM;
-    const long long tiles = ((p.m + rows - 1) / rows) * ((p.n + s.tile_n - 1) / s.tile_n);
-    const long long at_once = s.pair ? sms / 2 : sms;
-    const double waves = static_cast<double>((tiles + at_once - 1) / at_once);
-    const double bytes = kABytes + (s.pair ? s.tile_n / 2 : s.tile_n) * 128.0;
-    const double loop = ktiles * (s.tile_n > bytes / 90.0 ? s.tile_n : bytes / 90.0);
-    const double epilogue = s.tile_n * 8.0;
-    const double cost = waves * (loop > epilogue ? loop : epilogue) + (loop > epilogue ? epilogue : loop);
-    if (least == 0.0 || cost < least) {
+  const int ktiles = (p.k + kTileK - 1) / kTileK;
+  const double heavy = p.act == kActGelu ? 1.5 : 1.0;            // a GELU's share of the epilogue
+  Shape best = all[0].shape;
+  double least = 1e30;
+  for (int i = 0; i < static_cast<int>(sizeof(all) / sizeof(all[0])); ++i) {
+    const Cost& c = all[i];
+    if (p.b_mn && i >= kKMajorOnly) break;
+    const long long rows = c.shape.pair ? 2 * kTileM : kTileM;
+    const long long tiles = ((p.m + rows - 1) / rows) * ((p.n + c.shape.tile_n - 1) / c.shape.tile_n);
+    const long long at_once = c.shape.pair ? sms / 2 : sms;
+    const double waves = static_cast<double>((tiles + at_once - 1) / at_once), loop = ktiles * c.step, tile = c.tile * heavy;
+    const double cost = c.once + waves * (loop > tile ? loop : tile) + (loop > tile ? tile : loop);
+    if (cost < least) {
       least = cost;
-      best = s;
+      best = c.shape;
+    }
+  }
+  // Few tiles: the reduction over the CTAs of a cluster, where all clusters run at once (some SMs are left over by clusters
+  // of four and eight).  64 x 2048 x 1000: 8.8 us by one CTA per tile, 6.1 by eight.
+  for (int tile_n = 64; tile_n <= 128; tile_n *= 2) {
+    const long long tiles = ((p.m + kTileM - 1) / kTileM) * static_cast<long long>((p.n + tile_n - 1) / tile_n);
+    for (int splits = 2; splits <= 8 && splits <= ktiles && tiles * splits <= sms - 4 * (splits - 2); splits *= 2) {
+      const double cost = (ktiles + splits - 1) / splits * (tile_n == 64 ? 0.19 : 0.28) + (tile_n == 64 ? 4.0 : 6.0) + 0.1 * splits;
+      if (cost < least) {
+        least = cost;
+        best = {0, tile_n, splits};
+      }
     }
   }
   return best;
 }
 
-template <int PAIR, int B_MN, int DT>
+template <int PAIR, int B_MN, int DT, int ACT>
 cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream_t stream) {
   TileArgs t = {};
   t.m = p.m; t.n = p.n; t.k = p.k;
@@ -646,7 +660,6 @@ cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream
   const int size = DT ? 2 : 4;
   t.vec_y = (static_cast<long long>(p.n) * size) % 16 == 0;
   t.vec_pre = p.n % 8 == 0;
-  t.act = p.act;
   t.bias = p.bias;
   t.residual = p.residual;
   t.y = p.y;
@@ -663,7 +676,7 @@ cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream
   if (p.pre && t.vec_pre) ok = ok && encode(&maps[4], p.pre, 1, p.m, p.n, p.n, 32, kCols);
   if (!ok) return cudaErrorInvalidValue;
   const int smem = 1024 + t.stages * t.stage_bytes + staging;
-  const auto kernel = linear_kernel<PAIR, B_MN, DT>;
+  const auto kernel = linear_kernel<PAIR, B_MN, DT, ACT>;
   cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
   if (e != cudaSuccess) return e;
   const int at_once = PAIR ? sm_count() / 2 : sm_count();
@@ -744,10 +757,13 @@ cudaError_t launch_product(const Product& p, uint32_t* status, cudaStream_t stre
   const Shape s = choose_tile(p);
   if (s.splits)
     return p.b_mn ? launch_split<1>(p, s.tile_n, s.splits, status, stream) : launch_split<0>(p, s.tile_n, s.splits, status, stream);
-#define SURGEON_PRODUCT(PAIR)                                                                              \
-  (p.b_mn ? (p.dt ? launch_as<PAIR, 1, 1>(p, s.tile_n, status, stream) : launch_as<PAIR, 1, 0>(p, s.tile_n, status, stream)) \
-          : (p.dt ? launch_as<PAIR, 0, 1>(p, s.tile_n, status, stream) : launch_as<PAIR, 0, 0>(p, s.tile_n, status, stream)))
-  return s.pair ? SURGEON_PRODUCT(1) : SURGEON_PRODUCT(0);
+#define SURGEON_PRODUCT(PAIR, DT)                                                                          \
+  (p.b_mn                  ? launch_as<PAIR, 1, DT, kActNone>(p, s.tile_n, status, stream)                  \
+   : p.act == kActNone     ? launch_as<PAIR, 0, DT, kActNone>(p, s.tile_n, status, stream)                  \
+   : p.act == kActRelu     ? launch_as<PAIR, 0, DT, kActRelu>(p, s.tile_n, status, stream)                  \
+                           : launch_as<PAIR, 0, DT, kActGelu>(p, s.tile_n, status, stream))
+  if (s.pair) return p.dt ? SURGEON_PRODUCT(1, 1) : SURGEON_PRODUCT(1, 0);
+  return p.dt ? SURGEON_PRODUCT(0, 1) : SURGEON_PRODUCT(0, 0);
 #undef SURGEON_PRODUCT
 }
 
