@@ -434,19 +434,23 @@ def surgeon_weight_grad(act: CompressedActivation, desc: LayerDesc, grad_out: to
 # (Eq. 2, first line), and the list of gradients that a step ends with
 # ---------------------------------------------------------------------------------------------
 
-def _operand(t: Optional[torch.Tensor], name: str, device: int, shape=None, dtype=None):
+def _operand(t: Optional[torch.Tensor], name: str, device: int, shape, dtype):
     """Checks one tensor of a call (None: left out) and returns its address.  ``device``: the current one."""
     if t is None:
         return None
-    if t.get_device() != device or not t.is_contiguous():
-        if t.is_cuda and t.is_contiguous():
-            raise ValueError("%s is on %s, which is not the current device" % (name, t.device))
-        raise ValueError("%s must be a contiguous CUDA tensor" % name)
-    if shape is not None and t.shape != shape:
-        raise ValueError("%s must have the shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        _refuse(t, name, device, shape, dtype)
     return t.data_ptr()
+
+
+def _refuse(t: torch.Tensor, name: str, device: int, shape, dtype):
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous CUDA tensor" % name)
+    if t.get_device() != device:
+        raise ValueError("%s is on %s, which is not the current device" % (name, t.device))
+    if t.shape != shape:
+        raise ValueError("%s must have the shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
 
 
 def _new(shape, dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
@@ -458,18 +462,24 @@ def _new(shape, dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.Ten
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _work(workspace: Optional[torch.Tensor], nbytes: int, device, stream: Optional[torch.cuda.Stream]):
-    """Address and size of a call's scratch, which is made here where the caller passed none."""
+def _work(workspace: Optional[torch.Tensor], need, dev: int, stream: Optional[torch.cuda.Stream]):
+    """Address and size of a call's scratch; where the caller passed none it is made here, of ``need()`` bytes."""
     if workspace is None:
-        workspace = _new(max(int(nbytes), 16), torch.uint8, device, stream)
-    return _operand(workspace, "workspace", torch._C._cuda_getDevice()), workspace.numel() * workspace.element_size()
+        workspace = _new(max(int(need()), 16), torch.uint8, torch.device("cuda", dev), stream)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        _refuse(workspace, "workspace", dev, workspace.shape, workspace.dtype)
+    return workspace.data_ptr(), workspace.nbytes
+
+
+_TYPES = {torch.float32: SURGEON_F32, torch.bfloat16: SURGEON_BF16}
 
 
 def _rows(t: torch.Tensor, name: str):
-    if t.dim() < 1 or t.shape[-1] == 0:
+    """Shape, rows and channels of a tensor whose channels are its last dimension."""
+    shape = t.shape
+    if not shape or shape[-1] == 0:
         raise ValueError("%s must have channels in its last dimension" % name)
-    channels = t.shape[-1]
-    return t.numel() // channels, channels
+    return shape, t.numel() // shape[-1], shape[-1]
 
 
 def surgeon_layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
@@ -478,16 +488,17 @@ def surgeon_layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, be
     """Layer norm over the last dimension of ``x`` (fp32 or bf16); returns ``out``, which may be ``x``.
     ``gamma``, ``beta``: fp32.  ``stats``: an fp32 tensor [2, rows] that receives the means and the reciprocal
     standard deviations for ``surgeon_layer_norm_grad``."""
-    rows, channels = _rows(x, "x")
-    dev, f32 = torch._C._cuda_getDevice(), torch.float32
-    xp = _operand(x, "x", dev)
-    dt = dtype_code(x.dtype)
+    shape, rows, channels = _rows(x, "x")
+    dev, dt, f32, vector = torch._C._cuda_getDevice(), x.dtype, torch.float32, (channels,)
+    code = _TYPES.get(dt)
+    if code is None:
+        dtype_code(dt)
     if out is None:
-        out = _new(x.shape, x.dtype, x.device, stream)
-    st = lib().surgeon_layer_norm(xp, rows, channels, dt, _operand(gamma, "gamma", dev, (channels,), f32),
-                                  _operand(beta, "beta", dev, (channels,), f32), eps,
-                                  _operand(out, "out", dev, x.shape, x.dtype),
-                                  _operand(stats, "stats", dev, (2, rows), f32), _stream_ptr(stream))
+        out = _new(shape, dt, x.device, stream)
+    st = lib().surgeon_layer_norm(_operand(x, "x", dev, shape, dt), rows, channels, code,
+                                  _operand(gamma, "gamma", dev, vector, f32), _operand(beta, "beta", dev, vector, f32), eps,
+                                  _operand(out, "out", dev, shape, dt), _operand(stats, "stats", dev, (2, rows), f32),
+                                  _stream_ptr(stream))
     if st != SURGEON_OK:
         _check(st, "surgeon_layer_norm")
     return out
@@ -505,9 +516,8 @@ def surgeon_layer_norm_grad(x: torch.Tensor, dy: torch.Tensor, gamma: Optional[t
     """Backward pass of ``surgeon_layer_norm``; returns ``dx`` (of dy's type, made here if None; None with
     ``want_dx=False``).  ``residual_grad`` (dy's shape and type) is added to it; ``dx`` may be ``dy`` or
     ``residual_grad``.  ``dgamma``, ``dbeta``: fp32, written (``accumulate=True``: added to) where given."""
-    rows, channels = _rows(x, "x")
-    dev, f32, shape, gt = torch._C._cuda_getDevice(), torch.float32, x.shape, dy.dtype
-    xp, dyp = _operand(x, "x", dev), _operand(dy, "dy", dev, shape)
+    shape, rows, channels = _rows(x, "x")
+    dev, f32, vector, gt = torch._C._cuda_getDevice(), torch.float32, (channels,), dy.dtype
     if not want_dx:
         if dx is not None:
             raise ValueError("dx given, but not wanted")
@@ -515,13 +525,13 @@ def surgeon_layer_norm_grad(x: torch.Tensor, dy: torch.Tensor, gamma: Optional[t
         dx = _new(shape, gt, dy.device, stream)
     ws = None, 0
     if dgamma is not None or dbeta is not None:
-        ws = _work(workspace, surgeon_layer_norm_grad_workspace(rows, channels) if workspace is None else 0, x.device, stream)
-    st = lib().surgeon_layer_norm_grad(xp, dyp, rows, channels, dtype_code(x.dtype), dtype_code(gt),
-                                       _operand(gamma, "gamma", dev, (channels,), f32),
+        ws = _work(workspace, lambda: surgeon_layer_norm_grad_workspace(rows, channels), dev, stream)
+    st = lib().surgeon_layer_norm_grad(_operand(x, "x", dev, shape, x.dtype), _operand(dy, "dy", dev, shape, gt), rows, channels,
+                                       dtype_code(x.dtype), dtype_code(gt), _operand(gamma, "gamma", dev, vector, f32),
                                        _operand(stats, "stats", dev, (2, rows), f32),
                                        _operand(residual_grad, "residual_grad", dev, shape, gt),
-                                       _operand(dx, "dx", dev, shape, gt), _operand(dgamma, "dgamma", dev, (channels,), f32),
-                                       _operand(dbeta, "dbeta", dev, (channels,), f32), 1 if accumulate else 0, *ws,
+                                       _operand(dx, "dx", dev, shape, gt), _operand(dgamma, "dgamma", dev, vector, f32),
+                                       _operand(dbeta, "dbeta", dev, vector, f32), 1 if accumulate else 0, *ws,
                                        _stream_ptr(stream))
     if st != SURGEON_OK:
         _check(st, "surgeon_layer_norm_grad")
@@ -549,14 +559,15 @@ def surgeon_linear(desc: LayerDesc, x: torch.Tensor, weight: torch.Tensor, bias:
     ``x`` [rows, c_in], ``weight`` [c_out, c_in]: bf16; ``bias``: fp32; ``residual``: of the output's type.
     ``pre``: a bf16 tensor [rows, c_out] that receives x W^T + bias for ``surgeon_linear_grad``."""
     rows, ci, co = desc.batch, desc.c_in, desc.c_out
-    dev, b16 = torch._C._cuda_getDevice(), torch.bfloat16
-    xp, wp = _operand(x, "x", dev, (rows, ci), b16), _operand(weight, "weight", dev, (co, ci), b16)
+    dev, b16, shape = torch._C._cuda_getDevice(), torch.bfloat16, (rows, co)
     if out is None:
-        out = _new((rows, co), out_dtype, x.device, stream)
-    ws = _work(workspace, surgeon_linear_workspace(desc) if workspace is None else 0, x.device, stream)
-    st = lib().surgeon_linear(desc, xp, wp, _operand(bias, "bias", dev, (co,), torch.float32), int(act),
-                              _operand(residual, "residual", dev, (rows, co), out.dtype), dtype_code(out.dtype),
-                              _operand(out, "out", dev, (rows, co)), _operand(pre, "pre", dev, (rows, co), b16), *ws,
+        out = _new(shape, out_dtype, x.device, stream)
+    dt = out.dtype
+    ws = _work(workspace, lambda: surgeon_linear_workspace(desc), dev, stream)
+    st = lib().surgeon_linear(desc, _operand(x, "x", dev, (rows, ci), b16), _operand(weight, "weight", dev, (co, ci), b16),
+                              _operand(bias, "bias", dev, (co,), torch.float32), act,
+                              _operand(residual, "residual", dev, shape, dt), dtype_code(dt),
+                              _operand(out, "out", dev, shape, dt), _operand(pre, "pre", dev, shape, b16), *ws,
                               _stream_ptr(stream))
     if st != SURGEON_OK:
         _check(st, "surgeon_linear")
@@ -576,20 +587,18 @@ def surgeon_linear_grad(desc: LayerDesc, dy: torch.Tensor, weight: Optional[torc
     fp32 if given; None with ``want_dx=False``).  ``dy`` [rows, c_out]: fp32 or bf16.  ``dz``: fp32 [rows, c_out], receives
     dy act'(pre), the ``grad_out`` of ``surgeon_weight_grad``.  ``dbias``: fp32, written (``accumulate=True``: added to)."""
     rows, ci, co = desc.batch, desc.c_in, desc.c_out
-    dev = torch._C._cuda_getDevice()
-    dyp = _operand(dy, "dy", dev, (rows, co))
+    dev, b16, f32, shape, gt = torch._C._cuda_getDevice(), torch.bfloat16, torch.float32, (rows, co), dy.dtype
     if not want_dx:
         if dx is not None:
             raise ValueError("dx given, but not wanted")
     elif dx is None:
-        dx = _new((rows, ci), torch.bfloat16, dy.device, stream)
-    ws = _work(workspace, surgeon_linear_grad_workspace(desc) if workspace is None else 0, dy.device, stream)
-    st = lib().surgeon_linear_grad(desc, dyp, dtype_code(dy.dtype), _operand(weight, "weight", dev, (co, ci), torch.bfloat16),
-                                   _operand(pre, "pre", dev, (rows, co), torch.bfloat16), int(act),
-                                   SURGEON_BF16 if dx is None else dtype_code(dx.dtype), _operand(dx, "dx", dev, (rows, ci)),
-                                   _operand(dz, "dz", dev, (rows, co), torch.float32),
-                                   _operand(dbias, "dbias", dev, (co,), torch.float32), 1 if accumulate else 0, *ws,
-                                   _stream_ptr(stream))
+        dx = _new((rows, ci), b16, dy.device, stream)
+    xt = b16 if dx is None else dx.dtype
+    ws = _work(workspace, lambda: surgeon_linear_grad_workspace(desc), dev, stream)
+    st = lib().surgeon_linear_grad(desc, _operand(dy, "dy", dev, shape, gt), dtype_code(gt),
+                                   _operand(weight, "weight", dev, (co, ci), b16), _operand(pre, "pre", dev, shape, b16), act,
+                                   dtype_code(xt), _operand(dx, "dx", dev, (rows, ci), xt), _operand(dz, "dz", dev, shape, f32),
+                                   _operand(dbias, "dbias", dev, (co,), f32), 1 if accumulate else 0, *ws, _stream_ptr(stream))
     if st != SURGEON_OK:
         _check(st, "surgeon_linear_grad")
     return dx
@@ -627,18 +636,15 @@ def surgeon_gradient_norm_workspace(grads) -> int:
 
 def _list_call(grads, norm, gi, workspace, stream, new_gi):
     lst = grads if isinstance(grads, GradientList) else GradientList(grads)
-    dev, device = torch._C._cuda_getDevice(), lst.device
-    if device is None:
-        device = norm.device if norm is not None else torch.device("cuda", dev)
-    if device.index != dev:
-        raise ValueError("the gradients are on %s, which is not the current device" % device)
+    dev, f64, n = torch._C._cuda_getDevice(), torch.float64, len(lst.grads)
+    if lst.device is not None and lst.device.index != dev:
+        raise ValueError("the gradients are on %s, which is not the current device" % lst.device)
     if norm is None:
-        norm = _new(1, torch.float64, device, stream)
+        norm = _new(1, f64, torch.device("cuda", dev), stream)
     if gi is None and new_gi:
-        gi = _new(len(lst), torch.float64, device, stream)
-    ws = _work(workspace, surgeon_gradient_norm_workspace(lst) if workspace is None else 0, device, stream)
-    return (lst, norm, gi, (_operand(norm, "norm", dev, (1,), torch.float64),
-                            _operand(gi, "gi", dev, (len(lst),), torch.float64), *ws, _stream_ptr(stream)))
+        gi = _new(n, f64, torch.device("cuda", dev), stream)
+    ws = _work(workspace, lambda: surgeon_gradient_norm_workspace(lst), dev, stream)
+    return (lst, norm, gi, (_operand(norm, "norm", dev, (1,), f64), _operand(gi, "gi", dev, (n,), f64), *ws, _stream_ptr(stream)))
 
 
 def surgeon_gradient_norm(grads, norm: Optional[torch.Tensor] = None, gi: Optional[torch.Tensor] = None,
@@ -646,7 +652,7 @@ def surgeon_gradient_norm(grads, norm: Optional[torch.Tensor] = None, gi: Option
     """``(norm, gi)`` of a ``GradientList`` or a sequence of gradients: the global norm (one float64 on the device)
     and every tensor's Gradient Importance (Eq. 4, float64), as the ratio rule takes them."""
     lst, norm, gi, args = _list_call(grads, norm, gi, workspace, stream, True)
-    st = lib().surgeon_gradient_norm(lst.address, len(lst), *args)
+    st = lib().surgeon_gradient_norm(lst.address, len(lst.grads), *args)
     if st != SURGEON_OK:
         _check(st, "surgeon_gradient_norm")
     return norm, gi
@@ -658,7 +664,7 @@ def surgeon_clip_gradients(grads, max_norm: float, norm: Optional[torch.Tensor] 
     """Scales the gradients by min(1, max_norm / (norm + 1e-6)) into their outputs (a sequence: in place) and returns the
     norm before.  An infinite or NaN norm leaves them as they are.  ``gi``: receives Eq. 4 of each, if given."""
     lst, norm, gi, args = _list_call(grads, norm, gi, workspace, stream, False)
-    st = lib().surgeon_clip_gradients(lst.address, len(lst), float(max_norm), *args)
+    st = lib().surgeon_clip_gradients(lst.address, len(lst.grads), max_norm, *args)
     if st != SURGEON_OK:
         _check(st, "surgeon_clip_gradients")
     return norm

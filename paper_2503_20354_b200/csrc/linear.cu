@@ -9,24 +9,38 @@ constexpr int kThreads = 256;
 constexpr int kFewRows = 4;                      // rows up to which the weights' bytes are all there is: no tensor cores
 constexpr int kMaxSlabs = 296;
 
-// Rows of `cols` bf16 elements copied to rows of `pitch` (a multiple of 8): what TMA can read.
+// Up to two matrices of bf16 with `cols` columns copied to rows of `pitch` (a multiple of 8), zeros behind: what TMA can read.
+struct PadArgs {
+  const unsigned short* src[2];
+  uint4* dst[2];
+  uint32_t vecs[2];                              // 16-byte vectors of each
+  FastDiv per_row;                               // by a row's vectors
+  int cols, row_vecs;
+};
 __global__ void __launch_bounds__(kThreads)
-pad_rows_kernel(const unsigned short* __restrict__ src, long long rows, int cols, int pitch, unsigned short* __restrict__ dst) {
+pad_rows_kernel(const __grid_constant__ PadArgs a) {
   pdl_wait();
   pdl_trigger();
-  const long long n = rows * cols, step = static_cast<long long>(gridDim.x) * kThreads;
-  for (long long j = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x; j < n; j += step) {
-    const long long r = j / cols;
-    dst[r * pitch + (j - r * cols)] = src[j];
+  for (uint32_t i = blockIdx.x * kThreads + threadIdx.x; i < a.vecs[0] + a.vecs[1]; i += gridDim.x * kThreads) {
+    const int which = i >= a.vecs[0];
+    const uint32_t j = which ? i - a.vecs[0] : i, row = divide(j, a.per_row);
+    const int c = static_cast<int>(j - row * a.row_vecs) * 8;
+    const unsigned short* from = a.src[which] + static_cast<long long>(row) * a.cols + c;
+    uint32_t v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c + e < a.cols ? from[e] : 0u;
+    a.dst[which][j] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
   }
 }
 
 // dz = dy act'(pre) for a slab of rows (blockIdx.y) of 32 E columns: to dz in fp32, to dz16 in bf16 (rows `pitch` apart), and the
-// slab's column sums to partial[slab][cols]; each where wanted.  A warp takes every eighth row of the slab.
+// slab's column sums to partial[slab][cols] (added to what is there with `accumulate`); each where wanted.  A warp takes
+// every eighth row of the slab.
 template <int GDT, int E>
 __global__ void __launch_bounds__(kThreads)
 act_grad_kernel(const void* __restrict__ dy, const unsigned short* __restrict__ pre, int act, long long rows, int cols,
-                long long rows_per, float* __restrict__ dz, unsigned short* __restrict__ dz16, int pitch, float* __restrict__ partial) {
+                long long rows_per, float* __restrict__ dz, unsigned short* __restrict__ dz16, int pitch, float* __restrict__ partial,
+                int accumulate) {
   __shared__ float sums[kThreads / 32][32 * E];
   pdl_wait();
   pdl_trigger();
@@ -47,7 +61,7 @@ act_grad_kernel(const void* __restrict__ dy, const unsigned short* __restrict__ 
       if (dz) store_elems<0, E>(dz, t * cols + c, g);
       if (dz16) store_elems<1, E>(dz16, t * pitch + c, g);
     };
-    constexpr int kBatch = 4;                    // rows whose loads are on their way together
+    constexpr int kBatch = E == 1 ? 8 : 4;       // rows whose loads are on their way together
     long long t = begin + warp;
     for (; t + (kBatch - 1) * (kThreads / 32) < end; t += kBatch * (kThreads / 32)) {
       float g[kBatch][E], z[kBatch][E];
@@ -76,30 +90,20 @@ act_grad_kernel(const void* __restrict__ dy, const unsigned short* __restrict__ 
     float s = 0.0f;
 #pragma unroll
     for (int w = 0; w < kThreads / 32; ++w) s += sums[w][i];
-    if (col < cols) partial[blockIdx.y * static_cast<long long>(cols) + col] = s;
+    if (col < cols) {
+      float* to = partial + blockIdx.y * static_cast<long long>(cols) + col;
+      *to = accumulate ? *to + s : s;
+    }
   }
 }
 
-// The slabs' column sums, added in order.
-__global__ void __launch_bounds__(kThreads)
-column_sums_kernel(const float* __restrict__ partial, int slabs, int cols, float* __restrict__ out, int accumulate) {
-  __shared__ float part[kThreads / 32][33];
+// The slabs' column sums where no product follows.
+__global__ void __launch_bounds__(256)
+column_sums_kernel(const __grid_constant__ ColumnSums s) {
+  __shared__ float buf[8][32];
   pdl_wait();
   pdl_trigger();
-  const int c = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5;
-  float t = 0.0f;
-  if (c < cols) {
-#pragma unroll 8
-    for (int i = slice; i < slabs; i += kThreads / 32) t += partial[static_cast<long long>(i) * cols + c];
-  }
-  part[slice][threadIdx.x & 31] = t;
-  __syncthreads();
-  if (slice == 0 && c < cols) {
-    t = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kThreads / 32; ++i) t += part[i][threadIdx.x];
-    out[c] = accumulate ? out[c] + t : t;
-  }
+  add_columns<8>(s, blockIdx.x, gridDim.x, threadIdx.x >> 5, buf);
 }
 
 // Few rows, forward: a warp per output, the weights read once.
@@ -204,16 +208,22 @@ constexpr size_t kHead = 256;                    // the status word
 size_t up(size_t bytes) { return (bytes + 255) & ~static_cast<size_t>(255); }
 int pitch_of(int cols) { return (cols + 7) & ~7; }
 
-void pad_rows(const void* src, long long rows, int cols, void* dst, cudaStream_t stream) {
-  const long long blocks = (rows * cols + kThreads * 8 - 1) / (kThreads * 8);
-  launch_kernel(pad_rows_kernel, dim3(static_cast<unsigned>(blocks < 148 * 8 ? blocks : 148 * 8)), dim3(kThreads), 0, stream, true,
-                static_cast<const unsigned short*>(src), rows, cols, pitch_of(cols), static_cast<unsigned short*>(dst));
+void pad_rows(const void* a, long long a_rows, void* a_to, const void* b, long long b_rows, void* b_to, int cols, cudaStream_t stream) {
+  PadArgs p = {{static_cast<const unsigned short*>(a), static_cast<const unsigned short*>(b)},
+               {static_cast<uint4*>(a_to), static_cast<uint4*>(b_to)}, {0, 0}, make_div(pitch_of(cols) / 8), cols, pitch_of(cols) / 8};
+  p.vecs[0] = static_cast<uint32_t>(a_rows * p.row_vecs);
+  p.vecs[1] = static_cast<uint32_t>(b_rows * p.row_vecs);
+  const long long blocks = (static_cast<long long>(p.vecs[0]) + p.vecs[1] + kThreads - 1) / kThreads;
+  launch_kernel(pad_rows_kernel, dim3(static_cast<unsigned>(blocks < 148 * 8 ? blocks : 148 * 8)), dim3(kThreads), 0, stream, true, p);
   note_launches(1);
 }
 
-// Rows of a slab in the pass over dy: enough CTAs for the SMs, at least 8 rows each.
+// Rows of a slab in the pass over dy: enough CTAs for the SMs, at least 8 rows each.  Up to 64 rows are one slab, whose sums
+// need no second kernel.
 long long slab_rows(long long rows, int cols) {
-  const long long across = (cols + 255) / 256;
+  if (rows <= 64) return 64;
+  const int wide = cols % 8 == 0 ? 256 : 32;     // columns of a CTA
+  const long long across = (cols + wide - 1) / wide;
   long long slabs = kMaxSlabs * 2 / across > 0 ? kMaxSlabs * 2 / across : 1;
   if (slabs > kMaxSlabs) slabs = kMaxSlabs;
   const long long per = (rows + slabs - 1) / slabs;
@@ -277,14 +287,13 @@ cudaError_t launch_linear(const surgeon_layer_desc& d, const void* x, const void
   unsigned char* at = static_cast<unsigned char*>(workspace);
   uint32_t* status = reinterpret_cast<uint32_t*>(at);
   at += kHead;
-  Product p = {x, weight, d.batch, d.c_out, d.c_in, d.c_in, d.c_in, 0, bias, residual, y, pre, act, dt};
+  Product p = {x, weight, d.batch, d.c_out, d.c_in, d.c_in, d.c_in, 0, bias, residual, y, pre, act, dt, {}};
   if (d.c_in % 8 != 0) {
     p.lda = p.ldb = pitch_of(d.c_in);
-    pad_rows(x, d.batch, d.c_in, at, stream);
+    unsigned char* b_at = at + up(static_cast<size_t>(d.batch) * p.lda * 2);
+    pad_rows(x, d.batch, at, weight, d.c_out, b_at, d.c_in, stream);
     p.a = at;
-    at += up(static_cast<size_t>(d.batch) * p.lda * 2);
-    pad_rows(weight, d.c_out, d.c_in, at, stream);
-    p.b = at;
+    p.b = b_at;
   }
   const cudaError_t e = launch_product(p, status, stream);
   return e == cudaSuccess ? cudaGetLastError() : e;
@@ -309,7 +318,8 @@ cudaError_t launch_linear_grad(const surgeon_layer_desc& d, const void* dy, int 
     const auto launch = [&](auto kernel, int elems) {
       launch_kernel(kernel, dim3((d.c_out + 32 * elems - 1) / (32 * elems), s.slabs), dim3(kThreads), 0, stream, true, dy,
                     static_cast<const unsigned short*>(pre), act, static_cast<long long>(d.batch), d.c_out, s.per, dz32,
-                    static_cast<unsigned short*>(dz16), pitch_of(d.c_out), dbias ? partial : nullptr);
+                    static_cast<unsigned short*>(dz16), pitch_of(d.c_out), !dbias ? nullptr : s.slabs == 1 ? dbias : partial,
+                    s.slabs == 1 ? accumulate : 0);
       note_launches(1);
     };
     if (grad_dt == SURGEON_F32) {
@@ -319,11 +329,12 @@ cudaError_t launch_linear_grad(const surgeon_layer_desc& d, const void* dy, int 
       if (d.c_out % 8 == 0) launch(act_grad_kernel<1, 8>, 8);
       else launch(act_grad_kernel<1, 1>, 1);
     }
-    if (dbias) {
-      launch_kernel(column_sums_kernel, dim3((d.c_out + 31) / 32), dim3(kThreads), 0, stream, true, partial, s.slabs, d.c_out, dbias,
-                    accumulate);
-      note_launches(1);
-    }
+  }
+  ColumnSums sums = {};
+  if (dbias && s.slabs > 1) sums = {partial, dbias, s.slabs, d.c_out, accumulate};
+  if (sums.out && !dx) {
+    launch_kernel(column_sums_kernel, dim3((d.c_out + 31) / 32), dim3(256), 0, stream, true, sums);
+    note_launches(1);
   }
   if (!dx) return cudaGetLastError();
   if (few) {
@@ -346,9 +357,9 @@ cudaError_t launch_linear_grad(const surgeon_layer_desc& d, const void* dy, int 
     return cudaGetLastError();
   }
   Product p = {direct ? dy : dz16, weight, d.batch, d.c_in, d.c_out, direct ? d.c_out : pitch_of(d.c_out), d.c_in, 1,
-               nullptr, nullptr, dx, nullptr, kActNone, dx_dt};
+               nullptr, nullptr, dx, nullptr, kActNone, dx_dt, sums};
   if (d.c_in % 8 != 0) {
-    pad_rows(weight, d.c_out, d.c_in, base + s.weight, stream);
+    pad_rows(weight, d.c_out, base + s.weight, nullptr, 0, nullptr, d.c_in, stream);
     p.b = base + s.weight;
     p.ldb = pitch_of(d.c_in);
   }

@@ -60,6 +60,39 @@ __device__ __forceinline__ float slope(float z) {
 
 // y = act(a b^T + bias) + residual, z = a b^T + bias.  a: bf16 [m, k], rows `lda` elements apart.  b: bf16, element (n, k)
 // at n * ldb + k, or (b_mn) at k * ldb + n.  y, residual: [m, n] of type dt; pre (z, bf16): [m, n].
+// Column sums that a kernel before left in `slabs` rows of partial sums, to be added in order into `out` (null: none).
+struct ColumnSums {
+  const float* partial;
+  float* out;
+  int slabs, cols, accumulate;
+};
+// Every ctas-th group of 32 columns, by WARPS warps of CTA `cta` (four or eight): eight slices of the slabs, then the slices, in
+// order.  `buf`: 8 x 32.
+template <int WARPS>
+__device__ __forceinline__ void add_columns(const ColumnSums& s, int cta, int ctas, int warp, float (&buf)[8][32]) {
+  const int lane = static_cast<int>(lane_id());
+  for (int g = cta; g * 32 < s.cols; g += ctas) {
+    const int c = g * 32 + lane;
+#pragma unroll 1
+    for (int slice = warp; slice < 8; slice += WARPS) {
+      float t = 0.0f;
+      if (c < s.cols) {
+#pragma unroll 8
+        for (int i = slice; i < s.slabs; i += 8) t += s.partial[static_cast<long long>(i) * s.cols + c];
+      }
+      buf[slice][lane] = t;
+    }
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory");
+    if (warp == 0 && c < s.cols) {
+      float t = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t += buf[i][lane];
+      s.out[c] = s.accumulate ? s.out[c] + t : t;
+    }
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory");
+  }
+}
+
 struct Product {
   const void* a;
   const void* b;
@@ -69,6 +102,7 @@ struct Product {
   void* y;
   void* pre;
   int act, dt;
+  ColumnSums sums;                               // taken along by the first warps that are free
 };
 
 cudaError_t launch_product(const Product& p, uint32_t* status, cudaStream_t stream);

@@ -42,6 +42,7 @@ struct TileArgs {
   void* y;
   unsigned short* pre;
   uint32_t* status;
+  ColumnSums sums;
 };
 
 __device__ __forceinline__ void tma_store_2d(const void* tmap, uint32_t smem_src, int x, int y) {
@@ -90,6 +91,37 @@ __device__ __forceinline__ uint32_t piece_at(int r, int j) {
   return ROW == 128 ? static_cast<uint32_t>(r * 128 + ((j ^ (r & 7)) << 4)) : static_cast<uint32_t>(r * 64 + ((j ^ ((r >> 1) & 3)) << 4));
 }
 
+// Column `c` of row `r` in a piece of 32 columns of type T.
+template <typename T>
+__device__ __forceinline__ uint32_t piece_elem(int r, int c) {
+  constexpr int kPer = 16 / sizeof(T);
+  return piece_at<32 * static_cast<int>(sizeof(T))>(r, c / kPer) + (c % kPer) * static_cast<uint32_t>(sizeof(T));
+}
+// A lane's column of a piece whose rows TMA cannot reach, from and to global memory: eight rows on their way at a time.
+template <typename T, typename F>
+__device__ __forceinline__ void copy_piece(const T* from, long long pitch, int rows, bool on, F&& place) {
+#pragma unroll 1
+  for (int q = 0; q < 32; q += 8) {
+    T v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = on && q + i < rows ? from[(q + i) * pitch] : T(0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) *place(q + i) = v[i];
+  }
+}
+template <typename T, typename F>
+__device__ __forceinline__ void copy_out(T* to, long long pitch, int rows, bool on, F&& value) {
+#pragma unroll 1
+  for (int q = 0; q < 32; q += 8) {
+    T v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = value(q + i);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (on && q + i < rows) to[(q + i) * pitch] = v[i];
+  }
+}
+
 // DT: type of y and of the residual.  An N-major b comes with no bias, activation or residual (the input's gradient).
 template <int PAIR, int B_MN, int DT, int ACT>
 __global__ void __launch_bounds__(kThreads<DT>, 1)
@@ -100,7 +132,7 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 4 + 2 * kWarps];
-  __shared__ __align__(16) float s_bias[kWarps][kCols];
+  __shared__ __align__(16) float s_bias[kWarps][kCols];         // (and the slices of column sums)
   __shared__ uint32_t tmem_slot;
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);      // (uniform for the compiler too)
@@ -247,6 +279,7 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
       ++fetched;
       fc += kSlots;
     };
+    if (B_MN && p.sums.out && w < 4) add_columns<4>(p.sums, blockIdx.x, gridDim.x, w, reinterpret_cast<float (&)[8][32]>(s_bias));
     if (tma_res && leader) fetch_next();
     int it = 0, tm = first_m, tn = first_n;
     uint32_t piece = 0;
@@ -267,13 +300,9 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
         if (has_bias) s_bias[w][r] = x + r < p.n ? __ldg(p.bias + x + r) : 0.0f;       // the piece's, for every lane to read
         __syncwarp();
         if (has_res && !tma_res) {
-          if (x + r < p.n)
-            for (int q = 0; q < 32 && m0 + q < p.m; ++q) {
-              const long long at = static_cast<long long>(m0 + q) * p.n + x + r;
-              if (DT) *reinterpret_cast<unsigned short*>(mine + piece_at<kRow>(q, r >> 3) + (r & 7) * 2) =
-                  static_cast<const unsigned short*>(p.residual)[at];
-              else *reinterpret_cast<float*>(mine + piece_at<kRow>(q, r >> 2) + (r & 3) * 4) = static_cast<const float*>(p.residual)[at];
-            }
+          using T = typename Elem<DT>::type;
+          copy_piece<T>(static_cast<const T*>(p.residual) + static_cast<long long>(m0) * p.n + x + r, p.n, p.m - m0, x + r < p.n,
+                        [&](int q) { return reinterpret_cast<T*>(mine + piece_elem<T>(q, r)); });
           __syncwarp();
         }
         if (!waited) {
@@ -341,17 +370,15 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
           bulk_commit();
         }
         if (!p.vec_y || (keep && !p.vec_pre)) {
-          if (x + r < p.n)
-            for (int q = 0; q < 32 && m0 + q < p.m; ++q) {
-              const long long at = static_cast<long long>(m0 + q) * p.n + x + r;
-              if (!p.vec_y) {
-                if (DT) static_cast<unsigned short*>(p.y)[at] =
-                    *reinterpret_cast<const unsigned short*>(mine + piece_at<kRow>(q, r >> 3) + (r & 7) * 2);
-                else static_cast<float*>(p.y)[at] = *reinterpret_cast<const float*>(mine + piece_at<kRow>(q, r >> 2) + (r & 3) * 4);
-              }
-              if (keep && !p.vec_pre)
-                p.pre[at] = *reinterpret_cast<const unsigned short*>(pre_stage + piece_at<kPreRow>(q, r >> 3) + (r & 7) * 2);
-            }
+          using T = typename Elem<DT>::type;
+          const long long at = static_cast<long long>(m0) * p.n + x + r;
+          if (!p.vec_y)
+            copy_out<T>(static_cast<T*>(p.y) + at, p.n, p.m - m0, x + r < p.n,
+                        [&](int q) { return *reinterpret_cast<const T*>(mine + piece_elem<T>(q, r)); });
+          if (keep && !p.vec_pre)
+            copy_out<unsigned short>(p.pre + at, p.n, p.m - m0, x + r < p.n, [&](int q) {
+              return *reinterpret_cast<const unsigned short*>(pre_stage + piece_elem<unsigned short>(q, r));
+            });
           __syncwarp();                          // before the next piece takes the place
         }
         ++piece;
@@ -398,6 +425,7 @@ struct SplitArgs {
   void* y;
   unsigned short* pre;
   uint32_t* status;
+  ColumnSums sums;
 };
 
 __device__ __forceinline__ float4 load_cluster(uint32_t addr, uint32_t rank) {
@@ -415,6 +443,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 1];
+  __shared__ float s_slices[8][32];
   __shared__ uint32_t tmem_slot;
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
   const uint32_t lane = lane_id();
@@ -489,6 +518,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
       umma_commit(acc_full);
     }
   }
+  if (B_MN && p.sums.out && warp >= 2 && warp < 6) add_columns<4>(p.sums, blockIdx.x, gridDim.x, warp - 2, s_slices);
   __syncwarp();
   // all MMAs of this CTA are done, and with them the ring: the sums take its place, rows of tile_n + 4
   if (!__all_sync(0xFFFFFFFFu, mbar_wait_suspend(acc_full, 0))) give_up();
@@ -665,6 +695,7 @@ cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream
   t.y = p.y;
   t.pre = static_cast<unsigned short*>(p.pre);
   t.status = status;
+  t.sums = p.sums;
   CUtensorMap maps[5];
   memset(maps, 0, sizeof(maps));
   bool ok = encode(&maps[0], p.a, 1, p.m, p.k, p.lda, kTileM, kTileK);
@@ -720,6 +751,7 @@ cudaError_t launch_split(const Product& p, int tile_n, int splits, uint32_t* sta
   t.bias = p.bias; t.residual = p.residual; t.y = p.y;
   t.pre = static_cast<unsigned short*>(p.pre);
   t.status = status;
+  t.sums = p.sums;
   CUtensorMap maps[2];
   memset(maps, 0, sizeof(maps));
   bool ok = encode(&maps[0], p.a, 1, p.m, p.k, p.lda, kTileM, kTileK);
