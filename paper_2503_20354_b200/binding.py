@@ -59,6 +59,20 @@ class LayerDesc(C.Structure):
 
 
 _lib = None
+# Short calls marshalled in C++ (pyext/calls.cpp): each returns the library's status, or None for a call that is not its
+# ordinary case, which then goes through the checks below.  None if the module has not been built: every call does.
+_calls = None
+
+
+def _bind_calls(l):
+    global _calls
+    try:
+        from . import _calls as module
+    except ImportError:
+        return
+    module.bind(*(C.cast(f, C.c_void_p).value for f in (l.surgeon_layer_norm, l.surgeon_layer_norm_grad, l.surgeon_linear,
+                                                        l.surgeon_linear_grad, l.surgeon_gradient_norm, l.surgeon_clip_gradients)))
+    _calls = module
 
 
 def lib():
@@ -126,6 +140,7 @@ def lib():
         l.surgeon_launch_count.argtypes = []
         l.surgeon_status_string.restype = C.c_char_p
         l.surgeon_status_string.argtypes = [C.c_int]
+        _bind_calls(l)
         _lib = l
     return _lib
 
@@ -488,6 +503,12 @@ def surgeon_layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, be
     """Layer norm over the last dimension of ``x`` (fp32 or bf16); returns ``out``, which may be ``x``.
     ``gamma``, ``beta``: fp32.  ``stats``: an fp32 tensor [2, rows] that receives the means and the reciprocal
     standard deviations for ``surgeon_layer_norm_grad``."""
+    if _calls is not None and stream is None and out is not None:
+        st = _calls.layer_norm(x, gamma, beta, eps, out, stats)
+        if st is not None:
+            if st != SURGEON_OK:
+                _check(st, "surgeon_layer_norm")
+            return out
     shape, rows, channels = _rows(x, "x")
     dev, dt, f32, vector = torch._C._cuda_getDevice(), x.dtype, torch.float32, (channels,)
     code = _TYPES.get(dt)
@@ -516,6 +537,12 @@ def surgeon_layer_norm_grad(x: torch.Tensor, dy: torch.Tensor, gamma: Optional[t
     """Backward pass of ``surgeon_layer_norm``; returns ``dx`` (of dy's type, made here if None; None with
     ``want_dx=False``).  ``residual_grad`` (dy's shape and type) is added to it; ``dx`` may be ``dy`` or
     ``residual_grad``.  ``dgamma``, ``dbeta``: fp32, written (``accumulate=True``: added to) where given."""
+    if _calls is not None and stream is None and dx is not None and workspace is not None and want_dx:
+        st = _calls.layer_norm_grad(x, dy, gamma, stats, residual_grad, dx, dgamma, dbeta, accumulate, workspace)
+        if st is not None:
+            if st != SURGEON_OK:
+                _check(st, "surgeon_layer_norm_grad")
+            return dx
     shape, rows, channels = _rows(x, "x")
     dev, f32, vector, gt = torch._C._cuda_getDevice(), torch.float32, (channels,), dy.dtype
     if not want_dx:
@@ -558,6 +585,12 @@ def surgeon_linear(desc: LayerDesc, x: torch.Tensor, weight: torch.Tensor, bias:
     """act(x W^T + bias) + residual; returns ``out`` (made here as ``out_dtype`` if None; it may be ``residual``).
     ``x`` [rows, c_in], ``weight`` [c_out, c_in]: bf16; ``bias``: fp32; ``residual``: of the output's type.
     ``pre``: a bf16 tensor [rows, c_out] that receives x W^T + bias for ``surgeon_linear_grad``."""
+    if _calls is not None and stream is None and out is not None and workspace is not None:
+        st = _calls.linear(desc, x, weight, bias, act, residual, out, pre, workspace)
+        if st is not None:
+            if st != SURGEON_OK:
+                _check(st, "surgeon_linear")
+            return out
     rows, ci, co = desc.batch, desc.c_in, desc.c_out
     dev, b16, shape = torch._C._cuda_getDevice(), torch.bfloat16, (rows, co)
     if out is None:
@@ -586,6 +619,12 @@ def surgeon_linear_grad(desc: LayerDesc, dy: torch.Tensor, weight: Optional[torc
     """Backward pass of ``surgeon_linear`` but for the weights' gradient; returns ``dx`` (bf16 if made here; bf16 or
     fp32 if given; None with ``want_dx=False``).  ``dy`` [rows, c_out]: fp32 or bf16.  ``dz``: fp32 [rows, c_out], receives
     dy act'(pre), the ``grad_out`` of ``surgeon_weight_grad``.  ``dbias``: fp32, written (``accumulate=True``: added to)."""
+    if _calls is not None and stream is None and dx is not None and workspace is not None and want_dx:
+        st = _calls.linear_grad(desc, dy, weight, pre, act, dx, dz, dbias, accumulate, workspace)
+        if st is not None:
+            if st != SURGEON_OK:
+                _check(st, "surgeon_linear_grad")
+            return dx
     rows, ci, co = desc.batch, desc.c_in, desc.c_out
     dev, b16, f32, shape, gt = torch._C._cuda_getDevice(), torch.bfloat16, torch.float32, (rows, co), dy.dtype
     if not want_dx:
@@ -647,10 +686,22 @@ def _list_call(grads, norm, gi, workspace, stream, new_gi):
     return (lst, norm, gi, (_operand(norm, "norm", dev, (1,), f64), _operand(gi, "gi", dev, (n,), f64), *ws, _stream_ptr(stream)))
 
 
+def _list_fast(grads, max_norm, norm, gi, workspace):
+    if type(grads) is not GradientList or grads.device is None:
+        return None
+    return _calls.gradients(grads.address, len(grads.grads), grads.device.index, max_norm, norm, gi, workspace)
+
+
 def surgeon_gradient_norm(grads, norm: Optional[torch.Tensor] = None, gi: Optional[torch.Tensor] = None,
                           workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """``(norm, gi)`` of a ``GradientList`` or a sequence of gradients: the global norm (one float64 on the device)
     and every tensor's Gradient Importance (Eq. 4, float64), as the ratio rule takes them."""
+    if _calls is not None and stream is None and norm is not None and gi is not None and workspace is not None:
+        st = _list_fast(grads, None, norm, gi, workspace)
+        if st is not None:
+            if st != SURGEON_OK:
+                _check(st, "surgeon_gradient_norm")
+            return norm, gi
     lst, norm, gi, args = _list_call(grads, norm, gi, workspace, stream, True)
     st = lib().surgeon_gradient_norm(lst.address, len(lst.grads), *args)
     if st != SURGEON_OK:
@@ -663,6 +714,12 @@ def surgeon_clip_gradients(grads, max_norm: float, norm: Optional[torch.Tensor] 
                            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Scales the gradients by min(1, max_norm / (norm + 1e-6)) into their outputs (a sequence: in place) and returns the
     norm before.  An infinite or NaN norm leaves them as they are.  ``gi``: receives Eq. 4 of each, if given."""
+    if _calls is not None and stream is None and norm is not None and workspace is not None:
+        st = _list_fast(grads, max_norm, norm, gi, workspace)
+        if st is not None:
+            if st != SURGEON_OK:
+                _check(st, "surgeon_clip_gradients")
+            return norm
     lst, norm, gi, args = _list_call(grads, norm, gi, workspace, stream, False)
     st = lib().surgeon_clip_gradients(lst.address, len(lst.grads), max_norm, *args)
     if st != SURGEON_OK:

@@ -19,6 +19,31 @@ NVCC_FLAGS = [
 ]
 
 
+# the marshalling of short calls (a Python module that only passes arguments on)
+CALLS = os.path.join(HERE, "_calls.so")
+CALLS_SOURCE = os.path.join(HERE, "pyext", "calls.cpp")
+
+
+def build_calls(force: bool = False) -> str:
+    """Builds _calls.so with g++ against the installed PyTorch."""
+    import sysconfig
+
+    import torch
+    deps = [CALLS_SOURCE, os.path.join(ROOT, "include", "surgeon.h")]
+    if not force and os.path.exists(CALLS) and all(os.path.getmtime(p) <= os.path.getmtime(CALLS) for p in deps):
+        return CALLS
+    at = os.path.dirname(torch.__file__)
+    include = [os.path.join(ROOT, "include"), os.path.join(at, "include"), os.path.join(at, "include", "torch", "csrc", "api", "include"),
+               sysconfig.get_paths()["include"], os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")]
+    tmp = CALLS + ".tmp%d" % os.getpid()
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
+                           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch.compiled_with_cxx11_abi())]
+                          + [a for p in include for a in ("-I", p)] + [CALLS_SOURCE, "-o", tmp, "-L", os.path.join(at, "lib")]
+                          + ["-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"])
+    os.replace(tmp, CALLS)
+    return CALLS
+
+
 def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.cu")))
 
@@ -51,4 +76,5 @@ def build(force: bool = False, verbose: bool = False, bounds: bool = False) -> s
 
 
 if __name__ == "__main__":
+    build_calls(force="--force" in sys.argv)
     print(build(force="--force" in sys.argv, verbose="-v" in sys.argv, bounds="--bounds" in sys.argv))
