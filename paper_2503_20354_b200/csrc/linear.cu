@@ -234,7 +234,7 @@ long long slab_rows(long long rows, int cols) {
 struct GradScratch {
   size_t dz, weight, partial, total;
   long long per;                                 // rows of a slab
-  int slabs;
+  int slabs, tiles;                              // slabs of the pass over dy, of 128 rows of the product
 };
 GradScratch grad_scratch(const surgeon_layer_desc& d) {
   GradScratch s{};
@@ -246,7 +246,8 @@ GradScratch grad_scratch(const surgeon_layer_desc& d) {
   s.partial = at;
   s.per = slab_rows(d.batch, d.c_out);
   s.slabs = static_cast<int>((d.batch + s.per - 1) / s.per);
-  at += up(static_cast<size_t>(s.slabs) * d.c_out * 4);
+  s.tiles = (d.batch + 127) / 128;
+  at += up(static_cast<size_t>(s.slabs > s.tiles ? s.slabs : s.tiles) * d.c_out * 4);
   s.total = at;
   return s;
 }
@@ -287,7 +288,7 @@ cudaError_t launch_linear(const surgeon_layer_desc& d, const void* x, const void
   unsigned char* at = static_cast<unsigned char*>(workspace);
   uint32_t* status = reinterpret_cast<uint32_t*>(at);
   at += kHead;
-  Product p = {x, weight, d.batch, d.c_out, d.c_in, d.c_in, d.c_in, 0, bias, residual, y, pre, act, dt, {}};
+  Product p = {x, weight, d.batch, d.c_out, d.c_in, d.c_in, d.c_in, 0, bias, residual, y, pre, act, dt, {}, 0, {}};
   if (d.c_in % 8 != 0) {
     p.lda = p.ldb = pitch_of(d.c_in);
     unsigned char* b_at = at + up(static_cast<size_t>(d.batch) * p.lda * 2);
@@ -311,10 +312,12 @@ cudaError_t launch_linear_grad(const surgeon_layer_desc& d, const void* dy, int 
   const bool few = d.batch <= kFewRows;
   // the product's operand: dy itself where that is dz and lies as TMA reads it
   const bool direct = !few && !pre && grad_dt == SURGEON_BF16 && d.c_out % 8 == 0;
+  // then dz and the column sums come from the product's tiles, without a pass over dy
+  const bool copied = direct && dx && (dz || dbias);
   float* dz32 = dz;
   if (few && dx && !dz) dz32 = reinterpret_cast<float*>(base + s.dz);
   void* dz16 = dx && !few && !direct ? base + s.dz : nullptr;
-  if (dz32 || dz16 || dbias) {
+  if (!copied && (dz32 || dz16 || dbias)) {
     const auto launch = [&](auto kernel, int elems) {
       launch_kernel(kernel, dim3((d.c_out + 32 * elems - 1) / (32 * elems), s.slabs), dim3(kThreads), 0, stream, true, dy,
                     static_cast<const unsigned short*>(pre), act, static_cast<long long>(d.batch), d.c_out, s.per, dz32,
@@ -331,7 +334,7 @@ cudaError_t launch_linear_grad(const surgeon_layer_desc& d, const void* dy, int 
     }
   }
   ColumnSums sums = {};
-  if (dbias && s.slabs > 1) sums = {partial, dbias, s.slabs, d.c_out, accumulate};
+  if (!copied && dbias && s.slabs > 1) sums = {partial, dbias, s.slabs, d.c_out, accumulate};
   if (sums.out && !dx) {
     launch_kernel(column_sums_kernel, dim3((d.c_out + 31) / 32), dim3(256), 0, stream, true, sums);
     note_launches(1);
@@ -357,13 +360,19 @@ cudaError_t launch_linear_grad(const surgeon_layer_desc& d, const void* dy, int 
     return cudaGetLastError();
   }
   Product p = {direct ? dy : dz16, weight, d.batch, d.c_in, d.c_out, direct ? d.c_out : pitch_of(d.c_out), d.c_in, 1,
-               nullptr, nullptr, dx, nullptr, kActNone, dx_dt, sums};
+               nullptr, nullptr, dx, nullptr, kActNone, dx_dt, sums, copied ? 1 : 0,
+               {dz, dbias && s.tiles > 1 ? partial : nullptr, dbias && s.tiles == 1 ? dbias : nullptr, accumulate}};
   if (d.c_in % 8 != 0) {
     pad_rows(weight, d.c_out, base + s.weight, nullptr, 0, nullptr, d.c_in, stream);
     p.b = base + s.weight;
     p.ldb = pitch_of(d.c_in);
   }
   const cudaError_t e = launch_product(p, status, stream);
+  if (e == cudaSuccess && copied && dbias && s.tiles > 1) {
+    sums = {partial, dbias, s.tiles, d.c_out, accumulate};
+    launch_kernel(column_sums_kernel, dim3((d.c_out + 31) / 32), dim3(256), 0, stream, true, sums);
+    note_launches(1);
+  }
   return e == cudaSuccess ? cudaGetLastError() : e;
 }
 

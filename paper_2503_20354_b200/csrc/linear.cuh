@@ -93,6 +93,15 @@ __device__ __forceinline__ void add_columns(const ColumnSums& s, int cta, int ct
   }
 }
 
+// a itself in fp32 to `out` [m, k] (where wanted) and its column sums, 128 rows a slab, to `partial` [slabs][k] (or, one slab, to
+// `sums`, added to what is there with `accumulate`): taken from the tiles that the product has in shared memory anyway.
+struct CopyOut {
+  float* out;
+  float* partial;
+  float* sums;
+  int accumulate;
+};
+
 struct Product {
   const void* a;
   const void* b;
@@ -103,6 +112,8 @@ struct Product {
   void* pre;
   int act, dt;
   ColumnSums sums;                               // taken along by the first warps that are free
+  int copy_a;                                    // (an N-major b)
+  CopyOut copy;
 };
 
 cudaError_t launch_product(const Product& p, uint32_t* status, cudaStream_t stream);

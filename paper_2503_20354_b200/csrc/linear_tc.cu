@@ -26,7 +26,8 @@ constexpr int kMaxStages = 8;
 constexpr int kCols = 32;                        // columns (and rows) of a piece
 constexpr int kPrePiece = 32 * kCols * 2;
 template <int DT> constexpr int kEpiWarps = DT ? 16 : 8;
-template <int DT> constexpr int kThreads = (2 + kEpiWarps<DT>) * 32;
+constexpr int kCopyWarps = 4;
+template <int DT, int COPY> constexpr int kThreads = (2 + kEpiWarps<DT> + (COPY ? kCopyWarps : 0)) * 32;
 template <int DT> constexpr int kPiece = 32 * kCols * (DT ? 2 : 4);
 
 struct TileArgs {
@@ -43,6 +44,7 @@ struct TileArgs {
   unsigned short* pre;
   uint32_t* status;
   ColumnSums sums;
+  CopyOut copy;
 };
 
 __device__ __forceinline__ void tma_store_2d(const void* tmap, uint32_t smem_src, int x, int y) {
@@ -122,17 +124,66 @@ __device__ __forceinline__ void copy_out(T* to, long long pitch, int rows, bool 
   }
 }
 
-// DT: type of y and of the residual.  An N-major b comes with no bias, activation or residual (the input's gradient).
-template <int PAIR, int B_MN, int DT, int ACT>
-__global__ void __launch_bounds__(kThreads<DT>, 1)
+__device__ __forceinline__ void mbar_arrive_many(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+
+// One of four warps' 32 rows of an operand tile (128 x 64 bf16 at `tile`, as TMA laid it out; rows m0 ..., columns k0 ... of [m, k],
+// whose tile row is `slab`): to fp32 in c.out, and the columns' sums of all 128 rows.  The rows are taken into registers and the
+// ring's stage given back at `bar` first: held until the copy was written, it kept the MMAs waiting (12608 x 768 x 2304 with both 77 us, now 67; a pass of its own over dy before the product 80).
+// `buf`: [4][64], another one than the call before had.
+__device__ __forceinline__ void copy_tile(const CopyOut& c, const unsigned char* tile, uint32_t bar, bool leader, int warp, int m0, int m,
+                                          int k0, int k, int slab, float (&buf)[4][64]) {
+  const int lane = static_cast<int>(lane_id()), col = k0 + 2 * lane;
+  uint32_t v[32];
+#pragma unroll
+  for (int i = 0; i < 32; ++i)                   // (row & 7 = i & 7)
+    v[i] = *reinterpret_cast<const uint32_t*>(tile + (warp * 32 + i) * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4);
+  __syncwarp();
+  if (leader) mbar_arrive(bar);
+  if (c.out && col < k) {
+    float* to = c.out + static_cast<long long>(m0 + warp * 32) * k + col;
+    const int rows = m - m0 - warp * 32;
+    if (rows >= 32) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) *reinterpret_cast<float2*>(to + static_cast<long long>(i) * k) = make_float2(bf16_lo(v[i]), bf16_hi(v[i]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i < rows) *reinterpret_cast<float2*>(to + static_cast<long long>(i) * k) = make_float2(bf16_lo(v[i]), bf16_hi(v[i]));
+    }
+  }
+  if (!c.partial && !c.sums) return;
+  float2 sum = make_float2(0.0f, 0.0f);          // (rows and columns behind the last are zeros)
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    sum.x += bf16_lo(v[i]);
+    sum.y += bf16_hi(v[i]);
+  }
+  *reinterpret_cast<float2*>(&buf[warp][2 * lane]) = sum;
+  asm volatile("bar.sync 2, 128;" ::: "memory");
+  const int at = warp * 32 + lane;               // two warps finish the 64 columns
+  if (at < 64 && k0 + at < k) {
+    const float t = buf[0][at] + buf[1][at] + buf[2][at] + buf[3][at];
+    if (c.sums) c.sums[k0 + at] = c.accumulate ? c.sums[k0 + at] + t : t;
+    else c.partial[static_cast<long long>(slab) * k + k0 + at] = t;
+  }
+}
+
+// DT: type of y and of the residual.  An N-major b comes with no bias, activation or residual (the input's gradient); COPY (single
+// CTAs only: a pair's second CTA has no barrier that tells it of its tiles) passes a on as CopyOut says, each of its tiles
+// by one of the CTAs that read it.
+template <int PAIR, int B_MN, int DT, int ACT, int COPY>
+__global__ void __launch_bounds__(kThreads<DT, COPY>, 1)
 linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
               const __grid_constant__ CUtensorMap y_map, const __grid_constant__ CUtensorMap r_map,
               const __grid_constant__ CUtensorMap p_map, const __grid_constant__ TileArgs p) {
   constexpr int kWarps = kEpiWarps<DT>, kSlots = kWarps / 4, kRow = kCols * (DT ? 2 : 4), kPreRow = kCols * 2;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 4 + 2 * kWarps];
+  __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 4 + 2 * kWarps + (COPY ? kMaxStages : 0)];
   __shared__ __align__(16) float s_bias[kWarps][kCols];         // (and the slices of column sums)
+  __shared__ __align__(16) float s_copy[COPY ? 2 : 1][4][COPY ? 64 : 1];
   __shared__ uint32_t tmem_slot;
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);      // (uniform for the compiler too)
@@ -141,6 +192,7 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
   const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
   const uint32_t full = smem_u32(bars), empty = full + 8 * kMaxStages, acc_full = full + 16 * kMaxStages, acc_empty = acc_full + 16;
   const uint32_t res_bar = acc_empty + 16;       // two per epilogue warp
+  const uint32_t copy_bar = res_bar + 16 * kWarps;              // a stage's tile is there, and to be copied
   const int b_rows = PAIR ? p.tile_n / 2 : p.tile_n;            // columns' operand: rows that this CTA fetches
   const int tile_step = PAIR ? static_cast<int>(gridDim.x >> 1) : static_cast<int>(gridDim.x);
   const int tile_first = PAIR ? static_cast<int>(blockIdx.x >> 1) : static_cast<int>(blockIdx.x);
@@ -158,13 +210,15 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
     tma_prefetch_desc(&b_map);
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(full + 8 * s, 1);
-      mbar_init(empty + 8 * s, 1);
+      mbar_init(empty + 8 * s, COPY ? 1 + kCopyWarps : 1);
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(acc_full + 8 * a, 1);
       mbar_init(acc_empty + 8 * a, (PAIR ? 2 : 1) * kWarps);
     }
     for (int w = 0; w < 2 * kWarps; ++w) mbar_init(res_bar + 8 * w, 1);
+    if (COPY)
+      for (int s = 0; s < p.stages; ++s) mbar_init(copy_bar + 8 * s, 1);
     fence_barrier_init();
   }
   if (warp == 1) {
@@ -221,10 +275,11 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
       const uint64_t a_base = make_desc(smem_u32(smem));
       const uint64_t b_base = B_MN ? make_desc_rows(smem_u32(smem) + kABytes) : make_desc(smem_u32(smem) + kABytes);
       constexpr int kStepB = B_MN ? 128 : 2;
-      int s = 0, it = 0;
+      int s = 0, it = 0, tm = first_m, tn = first_n;
       uint32_t phase = 0;
       bool ok = true, there = false;
-      for (int t = tile_first; t < p.tiles && ok; t += tile_step, ++it) {
+      for (int t = tile_first; t < p.tiles && ok; t += tile_step, ++it, advance(tm, tn)) {
+        int copied = tn;                         // the next of this tile's steps whose operand tile the copying warps take
         const int acc = it & 1;
         if (!(PAIR ? mbar_wait_suspend_cluster(acc_empty + 8 * acc, ((it >> 1) & 1) ^ 1)
                    : mbar_wait_suspend(acc_empty + 8 * acc, ((it >> 1) & 1) ^ 1))) { give_up(); break; }
@@ -233,6 +288,14 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
         for (int kt = 0; kt < p.ktiles; ++kt) {
           if (!there && !mbar_wait_suspend(full + 8 * s, phase)) { give_up(); ok = false; break; }
           tc_fence_after();
+          if (COPY) {                            // tell them, or give the stage back for them
+            if (kt == copied) {
+              mbar_arrive(copy_bar + 8 * s);
+              copied += p.tiles_n;
+            } else {
+              mbar_arrive_many(empty + 8 * s, kCopyWarps);
+            }
+          }
           const uint64_t off = static_cast<uint64_t>((s * p.stage_bytes) >> 4);
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk) {
@@ -248,6 +311,25 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
         }
         if (PAIR) umma_commit_pair(acc_full + 8 * acc);
         else umma_commit(acc_full + 8 * acc);
+      }
+    }
+  } else if (COPY && warp >= 2 + kWarps) {
+    // ---- operand tiles on to global memory: every tiles_n-th of the row of tiles, from the one that is the tile's column ----
+    if constexpr (COPY) {
+      int at = 0, tm = first_m, tn = first_n, turn = 0;         // at: the stage of the tile's first step
+      uint32_t phases = 0;                       // of each stage's copy_bar
+      bool ok = true;
+      for (int t = tile_first; t < p.tiles && ok; t += tile_step, advance(tm, tn)) {
+        int s = (at + tn) % p.stages;
+        for (int kt = tn; kt < p.ktiles; kt += p.tiles_n) {
+          if (!__all_sync(0xFFFFFFFFu, mbar_wait_suspend(copy_bar + 8 * s, (phases >> s) & 1))) { give_up(); ok = false; break; }
+          phases ^= 1u << s;
+          copy_tile(p.copy, smem + s * p.stage_bytes, empty + 8 * s, leader, warp - 2 - kWarps, tm * kTileRows, p.m, kt * kTileK, p.k, tm,
+                    s_copy[turn]);
+          turn ^= 1;
+          s = (s + p.tiles_n) % p.stages;
+        }
+        at = (at + p.ktiles) % p.stages;
       }
     }
   } else {
@@ -416,7 +498,7 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
 constexpr int kSplitThreads = 256;
 
 struct SplitArgs {
-  int m, n;
+  int m, n, k;
   int tile_n, tiles_n;
   int splits, stages, stage_bytes, ktiles;
   int act, dt;
@@ -426,6 +508,7 @@ struct SplitArgs {
   unsigned short* pre;
   uint32_t* status;
   ColumnSums sums;
+  CopyOut copy;
 };
 
 __device__ __forceinline__ float4 load_cluster(uint32_t addr, uint32_t rank) {
@@ -436,14 +519,15 @@ __device__ __forceinline__ float4 load_cluster(uint32_t addr, uint32_t rank) {
   return v;
 }
 
-template <int B_MN>
+template <int B_MN, int COPY>
 __global__ void __launch_bounds__(kSplitThreads)
 linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
                     const __grid_constant__ SplitArgs p) {
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 1];
-  __shared__ float s_slices[8][32];
+  __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 1 + (COPY ? kMaxStages : 0)];
+  __shared__ __align__(16) float s_slices[8][32];
+  __shared__ __align__(16) float s_copy[COPY ? 2 : 1][4][COPY ? 64 : 1];
   __shared__ uint32_t tmem_slot;
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
   const uint32_t lane = lane_id();
@@ -453,15 +537,18 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
   const int m0 = tile / p.tiles_n * kTileM, n0 = tile % p.tiles_n * p.tile_n;
   const int kt_begin = static_cast<int>(static_cast<long long>(p.ktiles) * rank / p.splits);
   const int kt_end = static_cast<int>(static_cast<long long>(p.ktiles) * (rank + 1) / p.splits);
-  const uint32_t full = smem_u32(bars), empty = full + 8 * kMaxStages, acc_full = full + 16 * kMaxStages;
+  const uint32_t full = smem_u32(bars), empty = full + 8 * kMaxStages, acc_full = full + 16 * kMaxStages, copy_bar = acc_full + 8;
+  const int tn = tile % p.tiles_n;               // COPY: the steps kt with kt % tiles_n = tn are copied by this tile's CTAs
   if (tid == 0) {
     tma_prefetch_desc(&a_map);
     tma_prefetch_desc(&b_map);
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(full + 8 * s, 1);
-      mbar_init(empty + 8 * s, 1);
+      mbar_init(empty + 8 * s, COPY ? 1 + kCopyWarps : 1);
     }
     mbar_init(acc_full, 1);
+    if (COPY)
+      for (int s = 0; s < p.stages; ++s) mbar_init(copy_bar + 8 * s, 1);
     fence_barrier_init();
   }
   if (warp == 1) tmem_alloc(smem_u32(&tmem_slot), p.tile_n);
@@ -506,6 +593,10 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
       for (int kt = kt_begin; kt < kt_end; ++kt) {
         if (!there && !mbar_wait_suspend(full + 8 * s, phase)) { give_up(); break; }
         tc_fence_after();
+        if (COPY) {
+          if (kt % p.tiles_n == tn) mbar_arrive(copy_bar + 8 * s);
+          else mbar_arrive_many(empty + 8 * s, kCopyWarps);
+        }
         const uint64_t off = static_cast<uint64_t>((s * p.stage_bytes) >> 4);
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk)
@@ -517,6 +608,22 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
       }
       umma_commit(acc_full);
     }
+  }
+  if constexpr (COPY) {
+    if (warp >= 2 && warp < 2 + kCopyWarps) {
+      int turn = 0;
+      uint32_t phases = 0;
+      for (int kt = kt_begin; kt < kt_end; ++kt) {
+        if (kt % p.tiles_n != tn) continue;
+        const int s = (kt - kt_begin) % p.stages;
+        if (!__all_sync(0xFFFFFFFFu, mbar_wait_suspend(copy_bar + 8 * s, (phases >> s) & 1))) { give_up(); break; }
+        phases ^= 1u << s;
+        copy_tile(p.copy, smem + s * p.stage_bytes, empty + 8 * s, leader, warp - 2, m0, p.m, kt * kTileK, p.k, tile / p.tiles_n, s_copy[turn]);
+        turn ^= 1;
+      }
+    }
+    // (the sums below take the place of the ring, which the copies have read)
+    asm volatile("bar.sync 3, 256;" ::: "memory");
   }
   if (B_MN && p.sums.out && warp >= 2 && warp < 6) add_columns<4>(p.sums, blockIdx.x, gridDim.x, warp - 2, s_slices);
   __syncwarp();
@@ -641,11 +748,12 @@ Shape choose_tile(const Product& p) {
   const int sms = sm_count();
   const int ktiles = (p.k + kTileK - 1) / kTileK;
   const double heavy = p.act == kActGelu ? 1.5 : 1.0;            // a GELU's share of the epilogue
-  Shape best = all[0].shape;
+  Shape best = all[2].shape;
   double least = 1e30;
   for (int i = 0; i < static_cast<int>(sizeof(all) / sizeof(all[0])); ++i) {
     const Cost& c = all[i];
     if (p.b_mn && i >= kKMajorOnly) break;
+    if (p.copy_a && c.shape.pair) continue;
     const long long rows = c.shape.pair ? 2 * kTileM : kTileM;
     const long long tiles = ((p.m + rows - 1) / rows) * ((p.n + c.shape.tile_n - 1) / c.shape.tile_n);
     const long long at_once = c.shape.pair ? sms / 2 : sms;
@@ -671,7 +779,7 @@ Shape choose_tile(const Product& p) {
   return best;
 }
 
-template <int PAIR, int B_MN, int DT, int ACT>
+template <int PAIR, int B_MN, int DT, int ACT, int COPY>
 cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream_t stream) {
   TileArgs t = {};
   t.m = p.m; t.n = p.n; t.k = p.k;
@@ -683,7 +791,7 @@ cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream
   const int b_rows = PAIR ? tile_n / 2 : tile_n;
   t.stage_bytes = kABytes + b_rows * 128;
   const int staging = kEpiWarps<DT> * ((p.residual ? 2 : 1) * kPiece<DT> + (p.pre ? kPrePiece : 0));
-  t.stages = (227 * 1024 - 4096 - staging) / t.stage_bytes;
+  t.stages = (227 * 1024 - 8192 - staging) / t.stage_bytes;       // (8 KB: alignment, and what is not dynamic)
   if (t.stages > kMaxStages) t.stages = kMaxStages;
   t.tmem_cols = 128;                             // two accumulators; an allocation is a power of two
   while (t.tmem_cols < 2 * tile_n) t.tmem_cols *= 2;
@@ -696,6 +804,7 @@ cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream
   t.pre = static_cast<unsigned short*>(p.pre);
   t.status = status;
   t.sums = p.sums;
+  t.copy = p.copy;
   CUtensorMap maps[5];
   memset(maps, 0, sizeof(maps));
   bool ok = encode(&maps[0], p.a, 1, p.m, p.k, p.lda, kTileM, kTileK);
@@ -707,7 +816,7 @@ cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream
   if (p.pre && t.vec_pre) ok = ok && encode(&maps[4], p.pre, 1, p.m, p.n, p.n, 32, kCols);
   if (!ok) return cudaErrorInvalidValue;
   const int smem = 1024 + t.stages * t.stage_bytes + staging;
-  const auto kernel = linear_kernel<PAIR, B_MN, DT, ACT>;
+  const auto kernel = linear_kernel<PAIR, B_MN, DT, ACT, COPY>;
   cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
   if (e != cudaSuccess) return e;
   const int at_once = PAIR ? sm_count() / 2 : sm_count();
@@ -716,7 +825,7 @@ cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream
   t.step_n = groups % t.tiles_n;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(PAIR ? 2 * groups : groups);
-  cfg.blockDim = dim3(kThreads<DT>);
+  cfg.blockDim = dim3(kThreads<DT, COPY>);
   cfg.dynamicSmemBytes = static_cast<size_t>(smem);
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
@@ -733,10 +842,10 @@ cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream
   return e;
 }
 
-template <int B_MN>
+template <int B_MN, int COPY>
 cudaError_t launch_split(const Product& p, int tile_n, int splits, uint32_t* status, cudaStream_t stream) {
   SplitArgs t = {};
-  t.m = p.m; t.n = p.n;
+  t.m = p.m; t.n = p.n; t.k = p.k;
   t.tile_n = tile_n;
   t.tiles_n = (p.n + tile_n - 1) / tile_n;
   t.splits = splits;
@@ -752,6 +861,7 @@ cudaError_t launch_split(const Product& p, int tile_n, int splits, uint32_t* sta
   t.pre = static_cast<unsigned short*>(p.pre);
   t.status = status;
   t.sums = p.sums;
+  t.copy = p.copy;
   CUtensorMap maps[2];
   memset(maps, 0, sizeof(maps));
   bool ok = encode(&maps[0], p.a, 1, p.m, p.k, p.lda, kTileM, kTileK);
@@ -760,7 +870,7 @@ cudaError_t launch_split(const Product& p, int tile_n, int splits, uint32_t* sta
   int smem = t.stages * t.stage_bytes;
   const int sums = kTileM * (tile_n + 4) * 4;
   smem = 1024 + (smem > sums ? smem : sums);
-  const auto kernel = linear_split_kernel<B_MN>;
+  const auto kernel = linear_split_kernel<B_MN, COPY>;
   cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
   if (e != cudaSuccess) return e;
   const int tiles = (p.m + kTileM - 1) / kTileM * t.tiles_n;
@@ -788,12 +898,16 @@ cudaError_t launch_split(const Product& p, int tile_n, int splits, uint32_t* sta
 cudaError_t launch_product(const Product& p, uint32_t* status, cudaStream_t stream) {
   const Shape s = choose_tile(p);
   if (s.splits)
-    return p.b_mn ? launch_split<1>(p, s.tile_n, s.splits, status, stream) : launch_split<0>(p, s.tile_n, s.splits, status, stream);
+    return p.copy_a ? launch_split<1, 1>(p, s.tile_n, s.splits, status, stream)
+           : p.b_mn ? launch_split<1, 0>(p, s.tile_n, s.splits, status, stream)
+                    : launch_split<0, 0>(p, s.tile_n, s.splits, status, stream);
+  if (p.copy_a)
+    return p.dt ? launch_as<0, 1, 1, kActNone, 1>(p, s.tile_n, status, stream) : launch_as<0, 1, 0, kActNone, 1>(p, s.tile_n, status, stream);
 #define SURGEON_PRODUCT(PAIR, DT)                                                                          \
-  (p.b_mn                  ? launch_as<PAIR, 1, DT, kActNone>(p, s.tile_n, status, stream)                  \
-   : p.act == kActNone     ? launch_as<PAIR, 0, DT, kActNone>(p, s.tile_n, status, stream)                  \
-   : p.act == kActRelu     ? launch_as<PAIR, 0, DT, kActRelu>(p, s.tile_n, status, stream)                  \
-                           : launch_as<PAIR, 0, DT, kActGelu>(p, s.tile_n, status, stream))
+  (p.b_mn                  ? launch_as<PAIR, 1, DT, kActNone, 0>(p, s.tile_n, status, stream)               \
+   : p.act == kActNone     ? launch_as<PAIR, 0, DT, kActNone, 0>(p, s.tile_n, status, stream)               \
+   : p.act == kActRelu     ? launch_as<PAIR, 0, DT, kActRelu, 0>(p, s.tile_n, status, stream)               \
+                           : launch_as<PAIR, 0, DT, kActGelu, 0>(p, s.tile_n, status, stream))
   if (s.pair) return p.dt ? SURGEON_PRODUCT(1, 1) : SURGEON_PRODUCT(1, 0);
   return p.dt ? SURGEON_PRODUCT(0, 1) : SURGEON_PRODUCT(0, 0);
 #undef SURGEON_PRODUCT
