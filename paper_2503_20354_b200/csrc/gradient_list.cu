@@ -75,16 +75,6 @@ struct Unit {
 };
 
 template <int DT>
-__device__ __forceinline__ void vector_elems(uint4 v, float (&f)[DT == 0 ? 4 : 8]) {
-  if constexpr (DT == 0) {
-    f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
-  } else {
-    f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
-    f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z); f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
-  }
-}
-
-template <int DT>
 __device__ __forceinline__ double unit_squares(const void* grad, long long n, uint32_t u) {
   using T = typename Elem<DT>::type;
   const Unit<DT> unit(grad, n, u);

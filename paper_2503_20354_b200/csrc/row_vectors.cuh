@@ -71,6 +71,17 @@ __device__ __forceinline__ void store_elems(void* __restrict__ base, long long a
   }
 }
 
+// A 16-byte vector as numbers.
+template <int DT>
+__device__ __forceinline__ void vector_elems(uint4 v, float (&f)[DT == 0 ? 4 : 8]) {
+  if constexpr (DT == 0) {
+    f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+  } else {
+    f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
+    f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z); f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
+  }
+}
+
 // Sum over groups of W lanes (W a power of two up to 32), the same bits in every lane of the group.
 template <int W, typename T>
 __device__ __forceinline__ T lanes_sum(T v) {
