@@ -291,11 +291,13 @@ ln_columns_kernel(const void* __restrict__ x, const void* __restrict__ dy, long 
   partial[(static_cast<long long>(blockIdx.y) * 2 + 1) * channels + c] = db;
 }
 
-// The partial sums' rows, added in order: 32 columns per CTA, eight slices of the rows.
-__global__ void __launch_bounds__(kLnThreads)
+// The partial sums' rows, added in order: 32 columns per CTA, 32 slices of the rows (each a few loads that are on their way
+// together).
+constexpr int kFinalThreads = 1024;
+__global__ void __launch_bounds__(kFinalThreads)
 ln_final_kernel(const float* __restrict__ partial, int n_partials, int channels, float* __restrict__ dgamma,
                 float* __restrict__ dbeta, int accumulate) {
-  __shared__ float part[kLnThreads / 32][33];
+  __shared__ float part[kFinalThreads / 32][33];
   pdl_wait();
   pdl_trigger();
   const int k = blockIdx.y;
@@ -304,15 +306,15 @@ ln_final_kernel(const float* __restrict__ partial, int n_partials, int channels,
   const int c = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5;
   float t = 0.0f;
   if (c < channels) {
-#pragma unroll 8
-    for (int i = slice; i < n_partials; i += kLnThreads / 32) t += partial[(static_cast<long long>(i) * 2 + k) * channels + c];
+#pragma unroll 5
+    for (int i = slice; i < n_partials; i += kFinalThreads / 32) t += partial[(static_cast<long long>(i) * 2 + k) * channels + c];
   }
   part[slice][threadIdx.x & 31] = t;
   __syncthreads();
   if (slice == 0 && c < channels) {
     t = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kLnThreads / 32; ++i) t += part[i][threadIdx.x];
+    for (int i = 0; i < kFinalThreads / 32; ++i) t += part[i][threadIdx.x];
     out[c] = accumulate ? out[c] + t : t;
   }
 }
@@ -857,7 +859,7 @@ cudaError_t launch_layer_norm_grad(const void* x, const void* dy, long long rows
 #undef SURGEON_LN
   }
   if (partial) {
-    launch_kernel(ln_final_kernel, dim3((channels + 31) / 32, 2), dim3(kLnThreads), 0, stream, true, partial, n, channels, dgamma,
+    launch_kernel(ln_final_kernel, dim3((channels + 31) / 32, 2), dim3(kFinalThreads), 0, stream, true, partial, n, channels, dgamma,
                   dbeta, accumulate);
     note_launches(1);
   }

@@ -98,12 +98,12 @@ act_grad_kernel(const void* __restrict__ dy, const unsigned short* __restrict__ 
 }
 
 // The slabs' column sums where no product follows.
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
 column_sums_kernel(const __grid_constant__ ColumnSums s) {
-  __shared__ float buf[8][32];
+  __shared__ float buf[kSumSlices][32];
   pdl_wait();
   pdl_trigger();
-  add_columns<8>(s, blockIdx.x, gridDim.x, threadIdx.x >> 5, buf);
+  add_columns<32>(s, blockIdx.x, gridDim.x, threadIdx.x >> 5, buf);
 }
 
 // Few rows, forward: a warp per output, the weights read once.
@@ -336,7 +336,7 @@ cudaError_t launch_linear_grad(const surgeon_layer_desc& d, const void* dy, int 
   ColumnSums sums = {};
   if (!copied && dbias && s.slabs > 1) sums = {partial, dbias, s.slabs, d.c_out, accumulate};
   if (sums.out && !dx) {
-    launch_kernel(column_sums_kernel, dim3((d.c_out + 31) / 32), dim3(256), 0, stream, true, sums);
+    launch_kernel(column_sums_kernel, dim3((d.c_out + 31) / 32), dim3(1024), 0, stream, true, sums);
     note_launches(1);
   }
   if (!dx) return cudaGetLastError();
@@ -370,7 +370,7 @@ cudaError_t launch_linear_grad(const surgeon_layer_desc& d, const void* dy, int 
   const cudaError_t e = launch_product(p, status, stream);
   if (e == cudaSuccess && copied && dbias && s.tiles > 1) {
     sums = {partial, dbias, s.tiles, d.c_out, accumulate};
-    launch_kernel(column_sums_kernel, dim3((d.c_out + 31) / 32), dim3(256), 0, stream, true, sums);
+    launch_kernel(column_sums_kernel, dim3((d.c_out + 31) / 32), dim3(1024), 0, stream, true, sums);
     note_launches(1);
   }
   return e == cudaSuccess ? cudaGetLastError() : e;

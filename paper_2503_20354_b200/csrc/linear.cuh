@@ -66,19 +66,19 @@ struct ColumnSums {
   float* out;
   int slabs, cols, accumulate;
 };
-// Every ctas-th group of 32 columns, by WARPS warps of CTA `cta` (four or eight): eight slices of the slabs, then the slices, in
-// order.  `buf`: 8 x 32.
+constexpr int kSumSlices = 32;
+// Every ctas-th group of 32 columns, by WARPS warps of CTA `cta`: 32 slices of the slabs, then the slices, in order.
 template <int WARPS>
-__device__ __forceinline__ void add_columns(const ColumnSums& s, int cta, int ctas, int warp, float (&buf)[8][32]) {
+__device__ __forceinline__ void add_columns(const ColumnSums& s, int cta, int ctas, int warp, float (&buf)[kSumSlices][32]) {
   const int lane = static_cast<int>(lane_id());
   for (int g = cta; g * 32 < s.cols; g += ctas) {
     const int c = g * 32 + lane;
-#pragma unroll 1
-    for (int slice = warp; slice < 8; slice += WARPS) {
+#pragma unroll 4
+    for (int slice = warp; slice < kSumSlices; slice += WARPS) {
       float t = 0.0f;
       if (c < s.cols) {
-#pragma unroll 8
-        for (int i = slice; i < s.slabs; i += 8) t += s.partial[static_cast<long long>(i) * s.cols + c];
+#pragma unroll 4
+        for (int i = slice; i < s.slabs; i += kSumSlices) t += s.partial[static_cast<long long>(i) * s.cols + c];
       }
       buf[slice][lane] = t;
     }
@@ -86,7 +86,7 @@ __device__ __forceinline__ void add_columns(const ColumnSums& s, int cta, int ct
     if (warp == 0 && c < s.cols) {
       float t = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) t += buf[i][lane];
+      for (int i = 0; i < kSumSlices; ++i) t += buf[i][lane];
       s.out[c] = s.accumulate ? s.out[c] + t : t;
     }
     asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory");

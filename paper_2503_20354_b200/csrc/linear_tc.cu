@@ -182,7 +182,8 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 4 + 2 * kWarps + (COPY ? kMaxStages : 0)];
-  __shared__ __align__(16) float s_bias[kWarps][kCols];         // (and the slices of column sums)
+  __shared__ __align__(16) float s_bias[B_MN ? 1 : kWarps][kCols];
+  __shared__ float s_slices[B_MN && !COPY ? kSumSlices : 1][32];
   __shared__ __align__(16) float s_copy[COPY ? 2 : 1][4][COPY ? 64 : 1];
   __shared__ uint32_t tmem_slot;
 
@@ -361,7 +362,9 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
       ++fetched;
       fc += kSlots;
     };
-    if (B_MN && p.sums.out && w < 4) add_columns<4>(p.sums, blockIdx.x, gridDim.x, w, reinterpret_cast<float (&)[8][32]>(s_bias));
+    if constexpr (B_MN && !COPY) {
+      if (p.sums.out && w < 4) add_columns<4>(p.sums, blockIdx.x, gridDim.x, w, s_slices);
+    }
     if (tma_res && leader) fetch_next();
     int it = 0, tm = first_m, tn = first_n;
     uint32_t piece = 0;
@@ -379,7 +382,7 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
           bulk_wait_read<0>();                   // what left the places has been read
           if (tma_res) fetch_next();
         }
-        if (has_bias) s_bias[w][r] = x + r < p.n ? __ldg(p.bias + x + r) : 0.0f;       // the piece's, for every lane to read
+        if (has_bias) s_bias[B_MN ? 0 : w][r] = x + r < p.n ? __ldg(p.bias + x + r) : 0.0f;       // the piece's, for every lane to read
         __syncwarp();
         if (has_res && !tma_res) {
           using T = typename Elem<DT>::type;
@@ -415,7 +418,7 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
 #pragma unroll
           for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[8 * j + i]);
           if (has_bias) {
-            const float4 b0 = *reinterpret_cast<const float4*>(&s_bias[w][8 * j]), b1 = *reinterpret_cast<const float4*>(&s_bias[w][8 * j + 4]);
+            const float4 b0 = *reinterpret_cast<const float4*>(&s_bias[B_MN ? 0 : w][8 * j]), b1 = *reinterpret_cast<const float4*>(&s_bias[B_MN ? 0 : w][8 * j + 4]);
             f[0] += b0.x; f[1] += b0.y; f[2] += b0.z; f[3] += b0.w;
             f[4] += b1.x; f[5] += b1.y; f[6] += b1.z; f[7] += b1.w;
           }
@@ -526,7 +529,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 1 + (COPY ? kMaxStages : 0)];
-  __shared__ __align__(16) float s_slices[8][32];
+  __shared__ float s_slices[B_MN && !COPY ? kSumSlices : 1][32];
   __shared__ __align__(16) float s_copy[COPY ? 2 : 1][4][COPY ? 64 : 1];
   __shared__ uint32_t tmem_slot;
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
@@ -625,7 +628,9 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
     // (the sums below take the place of the ring, which the copies have read)
     asm volatile("bar.sync 3, 256;" ::: "memory");
   }
-  if (B_MN && p.sums.out && warp >= 2 && warp < 6) add_columns<4>(p.sums, blockIdx.x, gridDim.x, warp - 2, s_slices);
+  if constexpr (B_MN && !COPY) {
+    if (p.sums.out && warp >= 2 && warp < 6) add_columns<4>(p.sums, blockIdx.x, gridDim.x, warp - 2, s_slices);
+  }
   __syncwarp();
   // all MMAs of this CTA are done, and with them the ring: the sums take its place, rows of tile_n + 4
   if (!__all_sync(0xFFFFFFFFu, mbar_wait_suspend(acc_full, 0))) give_up();
