@@ -36,9 +36,9 @@ pad_rows_kernel(const __grid_constant__ PadArgs a) {
 // dz = dy act'(pre) for a slab of rows (blockIdx.y) of 32 E columns: to dz in fp32, to dz16 in bf16 (rows `pitch` apart), and the
 // slab's column sums to partial[slab][cols] (added to what is there with `accumulate`); each where wanted.  A warp takes
 // every eighth row of the slab.
-template <int GDT, int E>
-__global__ void __launch_bounds__(kThreads)
-act_grad_kernel(const void* __restrict__ dy, const unsigned short* __restrict__ pre, int act, long long rows, int cols,
+template <int GDT, int E, int ACT>
+__global__ void __launch_bounds__(kThreads, ACT == kActGelu ? 4 : 1)
+act_grad_kernel(const void* __restrict__ dy, const unsigned short* __restrict__ pre, long long rows, int cols,
                 long long rows_per, float* __restrict__ dz, unsigned short* __restrict__ dz16, int pitch, float* __restrict__ partial,
                 int accumulate) {
   __shared__ float sums[kThreads / 32][32 * E];
@@ -52,22 +52,25 @@ act_grad_kernel(const void* __restrict__ dy, const unsigned short* __restrict__ 
   for (int e = 0; e < E; ++e) acc[e] = 0.0f;
   if (c < cols) {
     const auto finish = [&](long long t, float (&g)[E], const float (&z)[E]) {
-      if (pre) {
+      if constexpr (ACT != kActNone) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) g[e] *= act == kActGelu ? slope<kActGelu>(z[e]) : slope<kActRelu>(z[e]);
-      }
+        for (int e = 0; e < E; ++e) g[e] = __fmul_rn(g[e], slope<ACT>(z[e]));      // (rounded also where only the sum takes it:
+      }                                                                            // the same bits whichever outputs are wanted)
 #pragma unroll
       for (int e = 0; e < E; ++e) acc[e] += g[e];
       if (dz) store_elems<0, E>(dz, t * cols + c, g);
       if (dz16) store_elems<1, E>(dz16, t * pitch + c, g);
     };
-    constexpr int kBatch = E == 1 ? 8 : 4;       // rows whose loads are on their way together
+    // Rows whose loads are on their way together. GELU's slope is long enough that two rows and four CTAs per SM
+    // pass four rows and the two CTAs that their registers leave (12608 x 2304, dz and its sums: 42 us, else 52);
+    // without it four rows are the faster (ReLU: 41 us, 50 with two).
+    constexpr int kBatch = E == 1 ? 8 : ACT == kActGelu ? 2 : 4;
     long long t = begin + warp;
     for (; t + (kBatch - 1) * (kThreads / 32) < end; t += kBatch * (kThreads / 32)) {
       float g[kBatch][E], z[kBatch][E];
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) load_elems<GDT, E>(dy, (t + b * (kThreads / 32)) * cols + c, g[b]);
-      if (pre) {
+      if constexpr (ACT != kActNone) {
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) load_elems<1, E>(pre, (t + b * (kThreads / 32)) * cols + c, z[b]);
       }
@@ -77,7 +80,7 @@ act_grad_kernel(const void* __restrict__ dy, const unsigned short* __restrict__ 
     for (; t < end; t += kThreads / 32) {
       float g[E], z[E];
       load_elems<GDT, E>(dy, t * cols + c, g);
-      if (pre) load_elems<1, E>(pre, t * cols + c, z);
+      if constexpr (ACT != kActNone) load_elems<1, E>(pre, t * cols + c, z);
       finish(t, g, z);
     }
   }
@@ -312,26 +315,33 @@ cudaError_t launch_linear_grad(const surgeon_layer_desc& d, const void* dy, int 
   const bool few = d.batch <= kFewRows;
   // the product's operand: dy itself where that is dz and lies as TMA reads it
   const bool direct = !few && !pre && grad_dt == SURGEON_BF16 && d.c_out % 8 == 0;
-  // then dz and the column sums come from the product's tiles, without a pass over dy
-  const bool copied = direct && dx && (dz || dbias);
+  // Then dz and the column sums come from the product's tiles, without a pass over dy: 12608 x 768 x 2304 65 us against 80,
+  // 300 x 256 x 512 7.1 against 8.9.  Not for wide inputs, whose product is better off in pairs of CTAs: 16384 x 2048 x 2048 138
+  // us against 133.
+  const bool copied = direct && dx && (dz || dbias) && d.c_in <= 1536;
   float* dz32 = dz;
   if (few && dx && !dz) dz32 = reinterpret_cast<float*>(base + s.dz);
   void* dz16 = dx && !few && !direct ? base + s.dz : nullptr;
   if (!copied && (dz32 || dz16 || dbias)) {
     const auto launch = [&](auto kernel, int elems) {
       launch_kernel(kernel, dim3((d.c_out + 32 * elems - 1) / (32 * elems), s.slabs), dim3(kThreads), 0, stream, true, dy,
-                    static_cast<const unsigned short*>(pre), act, static_cast<long long>(d.batch), d.c_out, s.per, dz32,
+                    static_cast<const unsigned short*>(pre), static_cast<long long>(d.batch), d.c_out, s.per, dz32,
                     static_cast<unsigned short*>(dz16), pitch_of(d.c_out), !dbias ? nullptr : s.slabs == 1 ? dbias : partial,
                     s.slabs == 1 ? accumulate : 0);
       note_launches(1);
     };
+#define SURGEON_ACT_GRAD(GDT, E)                                                \
+  (act == kActNone ? launch(act_grad_kernel<GDT, E, kActNone>, E)               \
+   : act == kActRelu ? launch(act_grad_kernel<GDT, E, kActRelu>, E)             \
+                     : launch(act_grad_kernel<GDT, E, kActGelu>, E))
     if (grad_dt == SURGEON_F32) {
-      if (d.c_out % 8 == 0) launch(act_grad_kernel<0, 8>, 8);
-      else launch(act_grad_kernel<0, 1>, 1);
+      if (d.c_out % 8 == 0) SURGEON_ACT_GRAD(0, 8);
+      else SURGEON_ACT_GRAD(0, 1);
     } else {
-      if (d.c_out % 8 == 0) launch(act_grad_kernel<1, 8>, 8);
-      else launch(act_grad_kernel<1, 1>, 1);
+      if (d.c_out % 8 == 0) SURGEON_ACT_GRAD(1, 8);
+      else SURGEON_ACT_GRAD(1, 1);
     }
+#undef SURGEON_ACT_GRAD
   }
   ColumnSums sums = {};
   if (!copied && dbias && s.slabs > 1) sums = {partial, dbias, s.slabs, d.c_out, accumulate};

@@ -350,11 +350,13 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
       const int left = p.n - tn * p.tile_n;
       return ((left < p.tile_n ? left : p.tile_n) + kCols - 1) / kCols;
     };
+    // A warp's first piece of its it-th tile: the slots go round, so that two tiles of two pieces, or of six, keep all warps busy.
+    const auto first_of = [&](int it) { return (slot + it * (p.tile_n / kCols)) % kSlots; };
     // the warp's next piece whose residual is to be fetched
-    int ft = tile_first, fm = first_m, fn = first_n, fc = slot;
+    int ft = tile_first, fm = first_m, fn = first_n, fi = 0, fc = slot;
     uint32_t fetched = 0;
     const auto fetch_next = [&]() {              // (the leader)
-      while (ft < p.tiles && fc >= pieces_of(fm, fn)) { ft += tile_step; advance(fm, fn); fc = slot; }
+      while (ft < p.tiles && fc >= pieces_of(fm, fn)) { ft += tile_step; advance(fm, fn); fc = first_of(++fi); }
       if (ft >= p.tiles) return;
       const uint32_t buf = fetched & 1;
       mbar_arrive_expect_tx(my_res + 8 * buf, kPiece<DT>);
@@ -363,7 +365,7 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
       fc += kSlots;
     };
     if constexpr (B_MN && !COPY) {
-      if (p.sums.out && w < 4) add_columns<4>(p.sums, blockIdx.x, gridDim.x, w, s_slices);
+      if (p.sums.out) add_columns<kWarps>(p.sums, blockIdx.x, gridDim.x, w, s_slices);
     }
     if (tma_res && leader) fetch_next();
     int it = 0, tm = first_m, tn = first_n;
@@ -374,7 +376,7 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
       const int acc = it & 1;
       const uint32_t tmem_at = tmem_base + acc * (p.tmem_cols >> 1) + (static_cast<uint32_t>(quarter) << 21);
       bool waited = false;
-      for (int c = slot; c < pieces; c += kSlots) {
+      for (int c = first_of(it); c < pieces; c += kSlots) {
         const uint32_t buf = y_places == 2 ? piece & 1 : 0;
         unsigned char* mine = stage + buf * kPiece<DT>;
         const int x = n0 + c * kCols;
@@ -629,7 +631,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
     asm volatile("bar.sync 3, 256;" ::: "memory");
   }
   if constexpr (B_MN && !COPY) {
-    if (p.sums.out && warp >= 2 && warp < 6) add_columns<4>(p.sums, blockIdx.x, gridDim.x, warp - 2, s_slices);
+    if (p.sums.out && warp >= 2) add_columns<kSplitThreads / 32 - 2>(p.sums, blockIdx.x, gridDim.x, warp - 2, s_slices);
   }
   __syncwarp();
   // all MMAs of this CTA are done, and with them the ring: the sums take its place, rows of tile_n + 4
@@ -747,8 +749,8 @@ Shape choose_tile(const Product& p) {
     double step, tile, once;
   };
   static const Cost all[] = {{{1, 256, 0}, 0.42, 3.0, 2.3}, {{1, 128, 0}, 0.26, 2.0, 2.3}, {{0, 256, 0}, 0.50, 2.3, 1.5},
-                             {{0, 192, 0}, 0.37, 2.2, 1.5}, {{0, 128, 0}, 0.28, 1.25, 1.5}, {{0, 64, 0}, 0.19, 1.0, 1.5},
-                             {{1, 192, 0}, 0.36, 3.2, 2.3}};
+                             {{0, 192, 0}, 0.40, 2.0, 1.5}, {{0, 128, 0}, 0.28, 1.25, 1.5}, {{0, 64, 0}, 0.19, 0.75, 1.5},
+                             {{1, 192, 0}, 0.34, 3.0, 2.3}};
   constexpr int kKMajorOnly = 6;                 // half a tile's columns are no whole slabs of 64
   const int sms = sm_count();
   const int ktiles = (p.k + kTileK - 1) / kTileK;

@@ -23,7 +23,7 @@ PHI = 7.5e-8 + 8 * U
 SHAPES = [(1, 1, 1), (1, 2048, 1000), (2, 64, 33), (3, 100, 9), (4, 768, 257), (4, 65, 64), (5, 8, 8), (5, 1, 1), (7, 16, 24),
           (33, 72, 40), (64, 512, 1000), (65, 63, 64), (100, 64, 63), (127, 200, 100), (128, 128, 128), (129, 136, 130), (200, 768, 96),
           (257, 320, 1280), (300, 1000, 72), (513, 65, 513), (1030, 256, 264), (2050, 264, 1032)]
-LARGE = [(12608, 768, 768), (9000, 512, 2048), (37000, 64, 256)]
+LARGE = [(12608, 768, 768), (9000, 512, 2048), (37000, 64, 256), (5000, 1600, 384), (20000, 128, 192)]
 
 
 def weights(c_in, c_out, gen):
@@ -147,7 +147,8 @@ def check_backward(rows, c_in, c_out, act, gt, xt, seed=0):
     assert B.surgeon_linear_grad(desc, dy.cuda(), None, p, act, dz=dz2, want_dx=False) is None
     assert B.surgeon_linear_grad(desc, dy.cuda(), None, p, act, dbias=db2, accumulate=True, want_dx=False) is None
     assert torch.equal(dz2, dz)
-    if act == NONE and gt == BF16 and c_out % 8 == 0 and rows > 4:     # with dx, dz's sums come from the product's tiles: grouped otherwise
+    # with dx, dz's sums come from the product's tiles: grouped otherwise
+    if act == NONE and gt == BF16 and c_out % 8 == 0 and rows > 4 and c_in <= 1536:
         assert ((db2 - old.cuda()).double().cpu() - d.sum(0)).abs().le(k * d.abs().sum(0) + e_d.sum(0) + U * (db2.cpu().abs() + old.abs())).all()
         again = torch.full_like(db, 9.0)
         B.surgeon_linear_grad(desc, dy.cuda(), w.cuda(), p, act, dx=torch.empty_like(dx), dbias=again)
