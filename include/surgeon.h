@@ -297,7 +297,7 @@ surgeon_status surgeon_decompress(const surgeon_compressed* act, void* x_out, vo
  * stats: device, fp32, 2 * rows (the means, then the r) for surgeon_layer_norm_grad, or NULL.
  * A NaN or an infinity stays in its row.  rows = 0 is legal.  Asynchronous on cuda_stream.
  * Errors: INVALID_ARG (null or misaligned pointer, rows < 0, channels <= 0, bad dt, eps not a
- * positive fp32 number), UNSUPPORTED (more than SURGEON_MAX_N elements), CUDA.
+ * positive fp32 number), UNSUPPORTED (more than SURGEON_MAX_N elements, or 2^30 channels), CUDA.
  * ---------------------------------------------------------------------------------------- */
 surgeon_status surgeon_layer_norm(const void* x, int64_t rows, int32_t channels, surgeon_dtype dt,
                                   const float* gamma, const float* beta, double eps, void* y,
@@ -315,8 +315,9 @@ size_t surgeon_layer_norm_grad_workspace(int64_t rows, int32_t channels);
  * dx, dgamma, dbeta: any may be NULL (not wanted).  accumulate = 0 overwrites dgamma and dbeta,
  * 1 adds to them (dx is always overwritten).  workspace: scratch of the size that the query
  * gives (it may be NULL where neither dgamma nor dbeta is wanted), not shared with a call in flight.
- * Element types (dt, grad_dt): (F32, F32), (BF16, F32), (BF16, BF16).  Asynchronous.
- * Errors: INVALID_ARG, BUFFER_TOO_SMALL, UNSUPPORTED ((F32, BF16); size), CUDA.
+ * Element types (dt, grad_dt): (F32, F32), (BF16, F32), (BF16, BF16).  Asynchronous.  The waits for
+ * copies on their way are bounded: one that ran out, which no valid call does, shows as NaN.
+ * Errors: INVALID_ARG (also dx = x, dgamma = dbeta), BUFFER_TOO_SMALL, UNSUPPORTED ((F32, BF16); size), CUDA.
  * ---------------------------------------------------------------------------------------- */
 surgeon_status surgeon_layer_norm_grad(const void* x, const void* dy, int64_t rows, int32_t channels,
                                        surgeon_dtype dt, surgeon_dtype grad_dt, const float* gamma,
@@ -334,8 +335,9 @@ surgeon_status surgeon_layer_norm_grad(const void* x, const void* dy, int64_t ro
  * act: GELU is z Phi(z) with the error function (Phi to 8e-8), and 0 at -infinity.
  * workspace: scratch of the size that the query gives, not shared with a call in flight.  Its first
  * word holds a surgeon_status afterwards: SURGEON_ERR_TIMEOUT if a bounded wait ran out, which no
- * valid call does (calls of a few rows do not write it).  Asynchronous on cuda_stream.
- * Errors: INVALID_ARG, BUFFER_TOO_SMALL, UNSUPPORTED (path 1; sizes beyond 2^31-1), CUDA.
+ * valid call does (calls of up to 4 rows do not write it).  Asynchronous on cuda_stream.
+ * Errors: INVALID_ARG (also y or pre in the place of an operand), BUFFER_TOO_SMALL, UNSUPPORTED (path 1;
+ * more than 2^31-1 elements, or an extent above 2^30), CUDA.
  * ---------------------------------------------------------------------------------------- */
 typedef enum { SURGEON_ACT_NONE = 0, SURGEON_ACT_RELU = 1, SURGEON_ACT_GELU = 2 } surgeon_activation;
 size_t surgeon_linear_workspace(const surgeon_layer_desc* d);      /* 0 on a bad desc */
@@ -348,11 +350,12 @@ surgeon_status surgeon_linear(const surgeon_layer_desc* d, const void* x, const 
  * Backward pass of surgeon_linear but for the weights' gradient, which is surgeon_weight_grad's
  * from the stored activation and dz:
  *   dz = dy act'(z);  dbias = sum_t dz;  dx = dz W  (Eq. 2, first line)
- * d, weight, workspace: as above.  dy [rows, c_out]: grad_dt.  pre: z as the forward call stored it
+ * d, weight, workspace: as above (its first word is written where dx is wanted).  dy [rows, c_out]: grad_dt.  pre: z as the forward call stored it
  * (not read for SURGEON_ACT_NONE).  dz: fp32 [rows, c_out], the grad_out of surgeon_weight_grad.
  * dx [rows, c_in]: dx_dt, from dz rounded to bf16 (dy itself, without a rounding, where it is
  * bf16 and there is no activation; not rounded for up to 4 rows).  dbias: fp32 [c_out]; accumulate = 1 adds to it.
- * dx, dz, dbias: any may be NULL (not wanted), none may be dy.  The residual's gradient is dy.
+ * dx, dz, dbias: any may be NULL (not wanted), none may be an operand or another.  dbias is summed in a fixed
+ * order, another one where dx is wanted too and the sums come from its tiles.  The residual's gradient is dy.
  * ReLU's derivative at 0 is 0.  Asynchronous on cuda_stream.
  * Errors: as above.
  * ---------------------------------------------------------------------------------------- */

@@ -648,8 +648,8 @@ class GradientList:
     as the C array that the two calls below take.  The tensors are kept alive, and must not be reallocated."""
 
     def __init__(self, grads, outs=None):
-        self.grads = list(grads)
-        self.outs = self.grads if outs is None else list(outs)
+        self.grads = tuple(grads)                    # (as many as the array below has entries, for good)
+        self.outs = self.grads if outs is None else tuple(outs)
         if len(self.outs) != len(self.grads):
             raise ValueError("%d outputs for %d gradients" % (len(self.outs), len(self.grads)))
         self.device = self.grads[0].device if self.grads else None

@@ -106,9 +106,12 @@ bool desc_ok(const surgeon_layer_desc* d, surgeon_status* why) {
 
 inline bool known_dtype(int dt) { return dt == SURGEON_F32 || dt == SURGEON_BF16; }
 
+// Columns and rows are counted in 32 bits with a few CTAs' worth to spare.
+constexpr int32_t kMaxExtent = 1 << 30;
+
 surgeon_status rows_ok(int64_t rows, int32_t channels) {
   if (rows < 0 || channels <= 0) return SURGEON_ERR_INVALID_ARG;
-  if (rows > SURGEON_MAX_N / channels) return SURGEON_ERR_UNSUPPORTED;
+  if (rows > SURGEON_MAX_N / channels || channels > kMaxExtent) return SURGEON_ERR_UNSUPPORTED;
   return SURGEON_OK;
 }
 
@@ -116,6 +119,7 @@ surgeon_status linear_ok(const surgeon_layer_desc* d) {
   surgeon_status why;
   if (!desc_ok(d, &why)) return why;
   if (d->kind != 0) return SURGEON_ERR_INVALID_ARG;
+  if (d->batch > kMaxExtent || d->c_in > kMaxExtent || d->c_out > kMaxExtent) return SURGEON_ERR_UNSUPPORTED;
   return d->path == 0 ? SURGEON_OK : SURGEON_ERR_UNSUPPORTED;
 }
 inline bool known_activation(int act) { return act == SURGEON_ACT_NONE || act == SURGEON_ACT_RELU || act == SURGEON_ACT_GELU; }
@@ -373,6 +377,7 @@ surgeon_status surgeon_layer_norm_grad(const void* x, const void* dy, int64_t ro
     if (!workspace) return SURGEON_ERR_INVALID_ARG;
     if (workspace_bytes < layer_norm_grad_workspace(rows, channels)) return SURGEON_ERR_BUFFER_TOO_SMALL;
   }
+  if (rows > 0 && ((dx && dx == x) || (dgamma && dgamma == dbeta))) return SURGEON_ERR_INVALID_ARG;
   return launch_layer_norm_grad(x, dy, rows, channels, static_cast<int>(dt), static_cast<int>(grad_dt), gamma, stats,
                                 residual_grad, dx, dgamma, dbeta, accumulate ? 1 : 0, workspace,
                                 static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? SURGEON_OK : SURGEON_ERR_CUDA;
@@ -389,7 +394,7 @@ surgeon_status surgeon_linear(const surgeon_layer_desc* d, const void* x, const 
   const surgeon_status st = linear_ok(d);
   if (st != SURGEON_OK) return st;
   if (!x || !weight || !y || !workspace || !known_activation(act) || !known_dtype(out_dt)) return SURGEON_ERR_INVALID_ARG;
-  if (y == x || y == weight || pre == x || pre == weight || pre == y) return SURGEON_ERR_INVALID_ARG;
+  if (y == x || y == weight || pre == x || pre == weight || pre == y || (pre && pre == residual)) return SURGEON_ERR_INVALID_ARG;
   if (!aligned16(x) || !aligned16(weight) || !aligned16(bias) || !aligned16(residual) || !aligned16(y) || !aligned16(pre) ||
       !aligned16(workspace))
     return SURGEON_ERR_INVALID_ARG;
@@ -412,6 +417,8 @@ surgeon_status surgeon_linear_grad(const surgeon_layer_desc* d, const void* dy, 
   if (!dy || !workspace || !known_activation(act) || !known_dtype(grad_dt) || !known_dtype(dx_dt)) return SURGEON_ERR_INVALID_ARG;
   if ((dx && !weight) || (act != SURGEON_ACT_NONE && !pre)) return SURGEON_ERR_INVALID_ARG;
   if (dx == dy || static_cast<const void*>(dz) == dy) return SURGEON_ERR_INVALID_ARG;
+  const bool reads_pre = act != SURGEON_ACT_NONE;
+  if ((dx && (dx == weight || dx == dz || (reads_pre && dx == pre))) || (dz && reads_pre && dz == pre)) return SURGEON_ERR_INVALID_ARG;
   if (!aligned16(dy) || !aligned16(weight) || !aligned16(pre) || !aligned16(dx) || !aligned16(dz) || !aligned16(dbias) ||
       !aligned16(workspace))
     return SURGEON_ERR_INVALID_ARG;

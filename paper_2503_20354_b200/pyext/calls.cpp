@@ -76,6 +76,14 @@ struct Args {
     }
     return v;
   }
+  bool truth(PyObject* o) {                      // (as Python's `if`: any number, not True alone)
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) {
+      PyErr_Clear();
+      ok = false;
+    }
+    return v > 0;
+  }
   double number(PyObject* o) {
     const double v = PyFloat_AsDouble(o);
     if (PyErr_Occurred()) {
@@ -154,12 +162,13 @@ PyObject* layer_norm_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* dx = c.operand(a[5], g, x->sizes(), false);
     void* dgamma = c.operand(a[6], at::kFloat, {channels});
     void* dbeta = c.operand(a[7], at::kFloat, {channels});
+    const bool accumulate = c.truth(a[8]);
     size_t bytes = 0;
     void* ws = c.workspace(a[9], &bytes);
     if (!c.ok || channels > INT32_MAX) Py_RETURN_NONE;
     return answer(layer_norm_grad_fn(xp, dyp, rows, static_cast<int32_t>(channels), dt, gdt, static_cast<float*>(gamma),
                                      static_cast<float*>(stats), res, dx, static_cast<float*>(dgamma), static_cast<float*>(dbeta),
-                                     a[8] == Py_True, ws, bytes, c.stream()));
+                                     accumulate, ws, bytes, c.stream()));
   });
 }
 
@@ -206,11 +215,12 @@ PyObject* linear_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* dxp = c.operand(a[5], dx->scalar_type(), {rows, ci}, false);
     void* dz = c.operand(a[6], at::kFloat, {rows, co});
     void* dbias = c.operand(a[7], at::kFloat, {co});
+    const bool accumulate = c.truth(a[8]);
     size_t bytes = 0;
     void* ws = c.workspace(a[9], &bytes);
     if (!c.ok) Py_RETURN_NONE;
     return answer(linear_grad_fn(desc.d, dyp, gdt, w, pre, static_cast<surgeon_activation>(act), xdt, dxp, static_cast<float*>(dz),
-                                 static_cast<float*>(dbias), a[8] == Py_True, ws, bytes, c.stream()));
+                                 static_cast<float*>(dbias), accumulate, ws, bytes, c.stream()));
   });
 }
 

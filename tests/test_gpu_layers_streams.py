@@ -148,6 +148,22 @@ def test_short_calls_are_the_bindings_calls():
         B.surgeon_layer_norm(calls.x, eps=-1.0, out=calls.y)
 
 
+def test_accumulate_is_any_true_value():
+    """Sums are added to what is there for accumulate=1 as for accumulate=True, whichever way the call takes."""
+    calls = Calls(40, 64, 72, 7)
+    ws = torch.empty(calls.need, dtype=torch.uint8, device="cuda")
+    calls.run(ws)
+    first = [t.clone() for t in (calls.dg, calls.db, calls.dbl)]
+    for accumulate in (1, True):
+        for stream in (None, torch.cuda.current_stream()):
+            for t, v in zip((calls.dg, calls.db, calls.dbl), first):
+                t.copy_(v)
+            B.surgeon_layer_norm_grad(calls.x, calls.dy, calls.gamma, calls.stats, calls.skip, calls.dx, calls.dg, calls.db, accumulate,
+                                      ws, stream=stream)
+            B.surgeon_linear_grad(calls.d, calls.dh, calls.w, calls.pre, GELU, calls.dxl, calls.dz, calls.dbl, accumulate, ws, stream=stream)
+            assert same((calls.dg, calls.db, calls.dbl), [v + v for v in first])
+
+
 def test_many_calls_in_a_row():
     """Rings and accumulators pass many rounds; each call's bits are the first call's."""
     for rows, c in ((12608, 768), (4097, 1021), (3000, 2047), (20000, 64)):

@@ -83,6 +83,29 @@ def test_linear_grad_refusals():
     assert B.surgeon_linear_grad_workspace(d) >= 256 + 8 * 24 * 2
 
 
+def test_outputs_in_the_place_of_operands_are_refused():
+    assert norm_grad(dx=P, dg=3 * P, db=4 * P) == INVALID                        # dx over x
+    assert norm_grad(dx=2 * P, dg=3 * P, db=3 * P) == INVALID                    # dgamma over dbeta
+    assert linear(pre=5 * P, res=5 * P) == INVALID
+    for bad in (dict(dx=P), dict(dy=5 * P, dx=P), dict(dx=3 * P), dict(dy=5 * P, pre=6 * P, act=1, dx=6 * P),
+                dict(dy=5 * P, pre=6 * P, act=2, dz=6 * P)):
+        assert linear_grad(**bad) == INVALID, bad
+
+
+def test_extents_beyond_what_the_kernels_count_are_refused():
+    top = (1 << 30) + 1
+    assert norm(rows=1, channels=top) == UNSUPPORTED and norm(rows=1, channels=(1 << 31) - 1) == UNSUPPORTED
+    assert norm_grad(rows=1, channels=top) == UNSUPPORTED and B.surgeon_layer_norm_grad_workspace(1, top) == 0
+    for d in (B.linear_desc(top, 1, 1), B.linear_desc(1, top, 1), B.linear_desc(1, 1, top), B.linear_desc((1 << 31) - 1, 1, 1)):
+        assert linear(d=d) == UNSUPPORTED and linear_grad(d=d) == UNSUPPORTED
+        assert B.surgeon_linear_workspace(d) == 0 and B.surgeon_linear_grad_workspace(d) == 0
+    assert B.surgeon_linear_grad_workspace(B.linear_desc(1 << 30, 1, 1)) > 0
+
+
+def test_a_gradient_list_keeps_its_length():
+    assert B.GradientList([]).grads == () and len(B.GradientList([])) == 0
+
+
 def grads(*entries):
     """(address, output, n, dt) each."""
     return (B.Gradient * max(len(entries), 1))(*[(g, o, n, dt, 0) for g, o, n, dt in entries])
