@@ -663,7 +663,7 @@ void forward_as(const void* x, long long rows, int channels, const float* gamma,
                 float* stats, cudaStream_t stream) {
   constexpr int kRows = TPR > 32 ? 1 : kLnThreads / TPR;
   // (short fp32 rows are better off without: 65536 x 64 7.4 us against 8.2, 12608 x 384 8.4 against 8.7; 4096 x 1024 9.8 against 8.6)
-  if constexpr (TPR <= 32 && (DT == 1 || V >= 6)) {
+  if constexpr (E > 1 && TPR <= 32 && (DT == 1 || V >= 6)) {
     const long long most = static_cast<long long>(rows_ctas<DT, V, TPR>()) * sm_count();
     if (rows > most * kRows) {
       launch_kernel(ln_forward_rows_kernel<DT, V, TPR>, dim3(static_cast<unsigned>(most)), dim3(kLnThreads), 0, stream, true, x, rows,
@@ -760,8 +760,9 @@ int backward_ring_as(const void* x, const void* dy, long long rows, int channels
 }
 
 // E: elements of a vector, 1 where rows start at no 16-byte boundary; N elements per thread.  Whole vectors need no ring
-// (12608 x 768 bf16 13.0 us with one, 8.2 without); other widths go through it, which still reads them in wide pieces (3000 x 2047
-// bf16 16.7 us against 32.4).
+// (12608 x 768 bf16 13.0 us with one, 8.2 without), nor do odd widths of fp32, where a warp reads 128 bytes an element each (3000 x
+// 2047 15.7 us against 18.7, 12608 x 767 18.8 against 26.3); those of bf16 go through it, which reads them in wide pieces (3000 x
+// 2047 16.7 us against 32.4).
 template <int DT, int E>
 void forward_of(const void* x, long long rows, int channels, const float* gamma, const float* beta, float eps, void* y,
                 float* stats, cudaStream_t stream) {
@@ -777,6 +778,21 @@ void forward_of(const void* x, long long rows, int channels, const float* gamma,
     SURGEON_LN(128, 16);
     SURGEON_LN(256, 16);
     SURGEON_LN(512, 16);
+#undef SURGEON_LN
+  } else if constexpr (DT == 0) {
+#define SURGEON_LN(TPR, N)                                                                                \
+  if (channels <= TPR * N) return forward_as<DT, 1, N, TPR>(x, rows, channels, gamma, beta, eps, y, stats, stream)
+    SURGEON_LN(16, 4);
+    SURGEON_LN(16, 8);
+    SURGEON_LN(32, 8);
+    SURGEON_LN(32, 12);
+    SURGEON_LN(128, 6);
+    SURGEON_LN(256, 4);
+    SURGEON_LN(256, 8);
+    SURGEON_LN(512, 8);
+    SURGEON_LN(512, 12);
+    if (rows > 2 * sm_count()) SURGEON_LN(512, 16);              // (2000 x 7001 34.4 us, 51.7 by 1024 threads; 100 x 7001 10.4 against 6.9)
+    SURGEON_LN(1024, 8);
 #undef SURGEON_LN
   } else {
 #define SURGEON_LN(TPR, N)                                                                                            \
