@@ -6,7 +6,10 @@
 // in order, into one contiguous range per CTA.  A CTA leaves one sum per tensor that it meets, at slot (CTA + tensor): the
 // path through the list moves by one CTA or by one tensor at a time, so the slots are distinct.  The second kernel adds
 // the slots in a fixed order (every CTA for itself, some 5 KB from L2) and scales the same ranges, last unit first: what
-// the first kernel read last is still in L2.  Squares and sums are double (a product of two fp32 numbers is exact in double,
+// the first kernel read last is still in L2.  For that the first kernel reads all but the last 80 MB as data that leaves L2
+// first, and so does the second with all that it reads and writes: 86 million fp32 gradients clipped into other tensors 173 us, 181
+// without, in place the same 179 (48 MB: 174; the 80
+// MB asked for by a policy that keeps them: 175); three passes over HBM take 158, the norm alone 55 of 53.  Squares and sums are double (a product of two fp32 numbers is exact in double,
 // and no fp32 number's square overflows).  Both kernels are bound by HBM.
 #include "row_vectors.cuh"
 
@@ -19,7 +22,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kUnitBytes = 16384;            // of fp32 or bf16 elements: 64 bytes a thread
-constexpr int kMaxCtas = 592;                // four per SM
+constexpr int kMaxCtas = 592;                // four per SM (eight: 86 million fp32 gradients clipped in 181 us, four 179)
+constexpr uint32_t kKeptUnits = (80 << 20) / kUnitBytes;       // of the list's, that L2 is to hold from one kernel to the next
 constexpr double kClipEps = 1e-6;
 
 // One launch's part of the list, passed by value (a kernel's parameters hold up to 32764 bytes).
@@ -33,6 +37,7 @@ struct Table {
   int count;                                 // tensors
   uint32_t per;                              // units of a CTA
   int ctas;
+  uint32_t keep;                             // of a CTA's units, the last to be read and the first to be scaled
   long long slot;                            // this launch's first slot
   int index;                                 // this launch's first tensor in the whole list
 };
@@ -75,7 +80,7 @@ struct Unit {
 };
 
 template <int DT>
-__device__ __forceinline__ double unit_squares(const void* grad, long long n, uint32_t u) {
+__device__ __forceinline__ double unit_squares(const void* grad, long long n, uint32_t u, bool keep) {
   using T = typename Elem<DT>::type;
   const Unit<DT> unit(grad, n, u);
   constexpr int E = Unit<DT>::kElems;
@@ -83,7 +88,10 @@ __device__ __forceinline__ double unit_squares(const void* grad, long long n, ui
   if (unit.whole) {                          // (a branch around each load would let one load at a time be on its way)
     uint4 v[Unit<DT>::kVecs];
 #pragma unroll
-    for (int i = 0; i < Unit<DT>::kVecs; ++i) v[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(grad) + unit.vec(i));
+    for (int i = 0; i < Unit<DT>::kVecs; ++i) {
+      const uint4* from = reinterpret_cast<const uint4*>(static_cast<const T*>(grad) + unit.vec(i));
+      v[i] = keep ? *from : __ldcs(from);
+    }
 #pragma unroll
     for (int i = 0; i < Unit<DT>::kVecs; ++i) {
       float f[E];
@@ -120,8 +128,9 @@ list_squares_kernel(const __grid_constant__ Table<N> t, double* __restrict__ slo
   if (blockIdx.x > 0 && t.first[i] == begin && threadIdx.x == 0) slots[t.slot + blockIdx.x + i - 1] = 0.0;
   double acc = 0.0;
   for (uint32_t u = begin; u < end; ++u) {
-    acc += (t.types[i >> 5] >> (i & 31)) & 1 ? unit_squares<1>(t.grad[i], t.n[i], u - t.first[i])
-                                             : unit_squares<0>(t.grad[i], t.n[i], u - t.first[i]);
+    const bool keep = end - u <= t.keep;
+    acc += (t.types[i >> 5] >> (i & 31)) & 1 ? unit_squares<1>(t.grad[i], t.n[i], u - t.first[i], keep)
+                                             : unit_squares<0>(t.grad[i], t.n[i], u - t.first[i], keep);
     if (u + 1 == end || u + 1 == t.first[i + 1]) {
       acc = block_sum(acc, buf);
       if (threadIdx.x == 0) slots[t.slot + blockIdx.x + i] = acc;
@@ -187,7 +196,7 @@ __device__ __forceinline__ void scale_unit(const void* grad, void* out, long lon
   if (unit.whole && ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0) {
     uint4 v[Unit<DT>::kVecs];
 #pragma unroll
-    for (int i = 0; i < Unit<DT>::kVecs; ++i) v[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(grad) + unit.vec(i));
+    for (int i = 0; i < Unit<DT>::kVecs; ++i) v[i] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const T*>(grad) + unit.vec(i)));
 #pragma unroll
     for (int i = 0; i < Unit<DT>::kVecs; ++i) {
       if (!copy) {
@@ -279,6 +288,7 @@ cudaError_t launch_list_as(const surgeon_gradient* list, int count, int clip, do
         t.first[n] = units;
         t.count = n;
         t.ctas = ctas_for(units, &t.per);
+        t.keep = kKeptUnits / t.ctas;
         t.slot = slot;
         t.index = at;
       }

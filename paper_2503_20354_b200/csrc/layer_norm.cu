@@ -470,7 +470,7 @@ ln_forward_ring_kernel(const __grid_constant__ RingArgs a, const float* __restri
   const int l = static_cast<int>(threadIdx.x) % TPR, sub = static_cast<int>(threadIdx.x) % kGroupThreads / TPR;
   const float inv_c = 1.0f / static_cast<float>(a.channels);
   int turn = 0, i = 0;
-  uint32_t phases = 0;                           // of the group's barriers, a bit per stage
+    uint32_t phases = 0;                         // of the group's barriers, a bit per stage
   for (long long chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x, ++i) {
     if (i % kRingGroups != group) continue;
     const int s = i % a.stages;
@@ -559,7 +559,7 @@ ln_backward_ring_kernel(const __grid_constant__ RingArgs a, const float* __restr
     consumers_sync();
     const float inv_c = 1.0f / static_cast<float>(a.channels);
     int turn = 0, i = 0;
-  uint32_t phases = 0;                           // of the group's barriers, a bit per stage
+    uint32_t phases = 0;                         // of the group's barriers, a bit per stage
     for (long long chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x, ++i) {
       if (i % kRingGroups != group) continue;
       const int s = i % a.stages;
