@@ -8,9 +8,9 @@
 // the slots in a fixed order (every CTA for itself, some 5 KB from L2) and scales the same ranges, last unit first: what
 // the first kernel read last is still in L2.  For that the first kernel reads all but the last 80 MB as data that leaves L2
 // first, and so does the second with all that it reads and writes: 86 million fp32 gradients clipped into other tensors 173 us, 181
-// without, in place the same 179 (48 MB: 174; the 80
-// MB asked for by a policy that keeps them: 175); three passes over HBM take 158, the norm alone 55 of 53.  Squares and sums are double (a product of two fp32 numbers is exact in double,
-// and no fp32 number's square overflows).  Both kernels are bound by HBM.
+// without, in place the same 179 (48 MB: 174; the 80 MB asked for by a policy that keeps them: 175); three passes over HBM take
+// 158, the norm alone takes 55 of 53.  Squares and sums are double (a product of two fp32 numbers is exact in double, and no fp32
+// number's square overflows).  Both kernels are bound by HBM; a list of short tensors (106, 213 KB) by two launches, 8 us.
 #include "row_vectors.cuh"
 
 #include <algorithm>

@@ -7,6 +7,11 @@
 // in tensor memory, sixteen warps (eight for fp32 outputs) take the other one: lane = row, 32 columns at a time.  A piece of
 // 32 x 32 goes through shared memory, where the residual has been fetched by TMA before, and leaves by TMA.
 // b is K-major (weights [n, k], forward) or N-major (weights [k, n], the input's gradient): both are read as they lie.
+//
+// What bounds it: wide layers the tensor pipe (16384 x 2048 x 2048 with a residual 122 us, 1126 TFLOP/s, 0.82 of a library
+// product's sustained rate); few columns of reduction the epilogue (16384 x 128 -> 512 with GELU and z kept: 27 instructions an element,
+// 13 us for 38 MB); the input's gradient an SM's intake of operands (12608 x 768 <- 2304: 41 us, 1090 TFLOP/s; with dz written from the
+// tiles 64).
 #include <cuda.h>
 #include <string.h>
 
