@@ -4,14 +4,14 @@
 //
 // Persistent CTAs (or CTA pairs, cta_group::2: 256 rows, each CTA its 128 and half of the columns' operand) walk the output
 // tiles, columns fastest.  Warp 0 fetches operands by TMA into a ring, warp 1 issues the MMAs into one of two accumulators
-// in tensor memory, sixteen warps (eight for fp32 outputs) take the other one: lane = row, 32 columns at a time.  A piece of
+// in tensor memory, sixteen or eight warps (EPI) take the other one: lane = row, 32 columns at a time.  A piece of
 // 32 x 32 goes through shared memory, where the residual has been fetched by TMA before, and leaves by TMA.
 // b is K-major (weights [n, k], forward) or N-major (weights [k, n], the input's gradient): both are read as they lie.
 //
 // What bounds it: wide layers the tensor pipe (16384 x 2048 x 2048 with a residual 122 us, 1126 TFLOP/s, 0.82 of a library
 // product's sustained rate); few columns of reduction the epilogue (16384 x 128 -> 512 with GELU and z kept: 27 instructions an element,
-// 13 us for 38 MB); the input's gradient an SM's intake of operands (12608 x 768 <- 2304: 41 us, 1090 TFLOP/s; with dz written from the
-// tiles 64).
+// 13 us for 38 MB); the input's gradient an SM's intake of operands (12608 x 768 <- 2304: 39 us, 1150 TFLOP/s; with dz written from the
+// tiles 56).
 #include <cuda.h>
 #include <string.h>
 
@@ -30,9 +30,8 @@ constexpr int kABytes = kTileM * 128;
 constexpr int kMaxStages = 8;
 constexpr int kCols = 32;                        // columns (and rows) of a piece
 constexpr int kPrePiece = 32 * kCols * 2;
-template <int DT> constexpr int kEpiWarps = DT ? 16 : 8;
 constexpr int kCopyWarps = 4;
-template <int DT, int COPY> constexpr int kThreads = (2 + kEpiWarps<DT> + (COPY ? kCopyWarps : 0)) * 32;
+template <int COPY, int EPI> constexpr int kThreads = (2 + EPI + (COPY ? kCopyWarps : 0)) * 32;
 template <int DT> constexpr int kPiece = 32 * kCols * (DT ? 2 : 4);
 
 struct TileArgs {
@@ -178,12 +177,12 @@ __device__ __forceinline__ void copy_tile(const CopyOut& c, const unsigned char*
 // DT: type of y and of the residual.  An N-major b comes with no bias, activation or residual (the input's gradient); COPY (single
 // CTAs only: a pair's second CTA has no barrier that tells it of its tiles) passes a on as CopyOut says, each of its tiles
 // by one of the CTAs that read it.
-template <int PAIR, int B_MN, int DT, int ACT, int COPY>
-__global__ void __launch_bounds__(kThreads<DT, COPY>, 1)
+template <int PAIR, int B_MN, int DT, int ACT, int COPY, int EPI>
+__global__ void __launch_bounds__(kThreads<COPY, EPI>, 1)
 linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
               const __grid_constant__ CUtensorMap y_map, const __grid_constant__ CUtensorMap r_map,
               const __grid_constant__ CUtensorMap p_map, const __grid_constant__ TileArgs p) {
-  constexpr int kWarps = kEpiWarps<DT>, kSlots = kWarps / 4, kRow = kCols * (DT ? 2 : 4), kPreRow = kCols * 2;
+  constexpr int kWarps = EPI, kSlots = kWarps / 4, kRow = kCols * (DT ? 2 : 4), kPreRow = kCols * 2;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 4 + 2 * kWarps + (COPY ? kMaxStages : 0)];
@@ -791,7 +790,7 @@ Shape choose_tile(const Product& p) {
   return best;
 }
 
-template <int PAIR, int B_MN, int DT, int ACT, int COPY>
+template <int PAIR, int B_MN, int DT, int ACT, int COPY, int EPI>
 cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream_t stream) {
   TileArgs t = {};
   t.m = p.m; t.n = p.n; t.k = p.k;
@@ -802,7 +801,7 @@ cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream
   t.ktiles = (p.k + kTileK - 1) / kTileK;
   const int b_rows = PAIR ? tile_n / 2 : tile_n;
   t.stage_bytes = kABytes + b_rows * 128;
-  const int staging = kEpiWarps<DT> * ((p.residual ? 2 : 1) * kPiece<DT> + (p.pre ? kPrePiece : 0));
+  const int staging = EPI * ((p.residual ? 2 : 1) * kPiece<DT> + (p.pre ? kPrePiece : 0));
   t.stages = (227 * 1024 - 8192 - staging) / t.stage_bytes;       // (8 KB: alignment, and what is not dynamic)
   if (t.stages > kMaxStages) t.stages = kMaxStages;
   t.tmem_cols = 128;                             // two accumulators; an allocation is a power of two
@@ -828,7 +827,7 @@ cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream
   if (p.pre && t.vec_pre) ok = ok && encode(&maps[4], p.pre, 1, p.m, p.n, p.n, 32, kCols);
   if (!ok) return cudaErrorInvalidValue;
   const int smem = 1024 + t.stages * t.stage_bytes + staging;
-  const auto kernel = linear_kernel<PAIR, B_MN, DT, ACT, COPY>;
+  const auto kernel = linear_kernel<PAIR, B_MN, DT, ACT, COPY, EPI>;
   cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
   if (e != cudaSuccess) return e;
   const int at_once = PAIR ? sm_count() / 2 : sm_count();
@@ -837,7 +836,7 @@ cudaError_t launch_as(const Product& p, int tile_n, uint32_t* status, cudaStream
   t.step_n = groups % t.tiles_n;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(PAIR ? 2 * groups : groups);
-  cfg.blockDim = dim3(kThreads<DT, COPY>);
+  cfg.blockDim = dim3(kThreads<COPY, EPI>);
   cfg.dynamicSmemBytes = static_cast<size_t>(smem);
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
@@ -914,14 +913,24 @@ cudaError_t launch_product(const Product& p, uint32_t* status, cudaStream_t stre
            : p.b_mn ? launch_split<1, 0>(p, s.tile_n, s.splits, status, stream)
                     : launch_split<0, 0>(p, s.tile_n, s.splits, status, stream);
   if (p.copy_a)
-    return p.dt ? launch_as<0, 1, 1, kActNone, 1>(p, s.tile_n, status, stream) : launch_as<0, 1, 0, kActNone, 1>(p, s.tile_n, status, stream);
-#define SURGEON_PRODUCT(PAIR, DT)                                                                          \
-  (p.b_mn                  ? launch_as<PAIR, 1, DT, kActNone, 0>(p, s.tile_n, status, stream)               \
-   : p.act == kActNone     ? launch_as<PAIR, 0, DT, kActNone, 0>(p, s.tile_n, status, stream)               \
-   : p.act == kActRelu     ? launch_as<PAIR, 0, DT, kActRelu, 0>(p, s.tile_n, status, stream)               \
-                           : launch_as<PAIR, 0, DT, kActGelu, 0>(p, s.tile_n, status, stream))
-  if (s.pair) return p.dt ? SURGEON_PRODUCT(1, 1) : SURGEON_PRODUCT(1, 0);
-  return p.dt ? SURGEON_PRODUCT(0, 1) : SURGEON_PRODUCT(0, 0);
+    return p.dt ? launch_as<0, 1, 1, kActNone, 1, 8>(p, s.tile_n, status, stream) : launch_as<0, 1, 0, kActNone, 1, 8>(p, s.tile_n, status, stream);
+  // Sixteen epilogue warps where the epilogue counts, eight where their places in shared memory are better a stage of the ring (us, sixteen and
+  // eight: 16384 x 256 -> 1024 with GELU 21 and 27, 12608 x 768 -> 2304 36 and 41; 4096 x 1024 -> 1024 with all 18.5 and 15.4, 16384 x
+  // 2048 -> 2048 101 and 96; a residual doubles the places: 16384 x 512 -> 512 16.9 and 15.9).  The input's gradient has
+  // a light epilogue: 12608 x 768 <- 2304 41.7 and 38.9, with dz and its sums 65 and 56.5; 65536 x 64 <- 64 the same.
+  const bool wide = p.dt == 1 && !p.b_mn && p.k < (p.residual ? 512 : 1024);
+#define SURGEON_FORWARD(PAIR, DT, EPI)                                                                     \
+  (p.act == kActNone       ? launch_as<PAIR, 0, DT, kActNone, 0, EPI>(p, s.tile_n, status, stream)          \
+   : p.act == kActRelu     ? launch_as<PAIR, 0, DT, kActRelu, 0, EPI>(p, s.tile_n, status, stream)          \
+                           : launch_as<PAIR, 0, DT, kActGelu, 0, EPI>(p, s.tile_n, status, stream))
+#define SURGEON_PRODUCT(PAIR)                                                                              \
+  (p.b_mn   ? (p.dt ? launch_as<PAIR, 1, 1, kActNone, 0, 8>(p, s.tile_n, status, stream)                   \
+                    : launch_as<PAIR, 1, 0, kActNone, 0, 8>(p, s.tile_n, status, stream))                  \
+   : wide   ? SURGEON_FORWARD(PAIR, 1, 16)                                                                 \
+   : p.dt   ? SURGEON_FORWARD(PAIR, 1, 8)                                                                  \
+            : SURGEON_FORWARD(PAIR, 0, 8))
+  return s.pair ? SURGEON_PRODUCT(1) : SURGEON_PRODUCT(0);
+#undef SURGEON_FORWARD
 #undef SURGEON_PRODUCT
 }
 
