@@ -317,10 +317,9 @@ cudaError_t launch_linear_grad(const surgeon_layer_desc& d, const void* dy, int 
   const bool few = d.batch <= kFewRows;
   // the product's operand: dy itself where that is dz and lies as TMA reads it
   const bool direct = !few && !pre && grad_dt == SURGEON_BF16 && d.c_out % 8 == 0;
-  // Then dz and the column sums come from the product's tiles, without a pass over dy: 12608 x 768 x 2304 56.5 us against 80,
-  // 300 x 256 x 512 7.1 against 8.9.  Not for wide inputs, whose product is better off in pairs of CTAs: 16384 x 2048 x 2048 138
-  // us against 133.
-  const bool copied = direct && dx && (dz || dbias) && d.c_in <= 1536;
+  // Then dz and the column sums come from the product's tiles, without a pass over dy: 12608 x 768 <- 2304 56 us against 80, 16384 x
+  // 2048 <- 2048 119 against 128 (whose product by itself is the faster in pairs of CTAs), 300 x 256 <- 512 6.7 against 8.9.
+  const bool copied = direct && dx && (dz || dbias);
   float* dz32 = dz;
   if (few && dx && !dz) dz32 = reinterpret_cast<float*>(base + s.dz);
   void* dz16 = dx && !few && !direct ? base + s.dz : nullptr;

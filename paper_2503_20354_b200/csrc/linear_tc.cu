@@ -8,10 +8,10 @@
 // 32 x 32 goes through shared memory, where the residual has been fetched by TMA before, and leaves by TMA.
 // b is K-major (weights [n, k], forward) or N-major (weights [k, n], the input's gradient): both are read as they lie.
 //
-// What bounds it: wide layers the tensor pipe (16384 x 2048 x 2048 with a residual 122 us, 1126 TFLOP/s, 0.82 of a library
-// product's sustained rate); few columns of reduction the epilogue (16384 x 128 -> 512 with GELU and z kept: 27 instructions an element,
-// 13 us for 38 MB); the input's gradient an SM's intake of operands (12608 x 768 <- 2304: 39 us, 1150 TFLOP/s; with dz written from the
-// tiles 56).
+// What bounds it: wide layers the tensor pipe (16384 x 2048 x 2048 with a residual 113 us under the power cap, 1216 TFLOP/s, 0.88 of a
+// library product's sustained rate; 96 in short runs); few columns of reduction the epilogue (16384 x 128 -> 512 with GELU and z kept:
+// 27 instructions an element, 13 us for 38 MB); the input's gradient an SM's intake of operands (12608 x 768 <- 2304: 38 us, 1170
+// TFLOP/s; with dz and its sums written from the tiles 56).
 #include <cuda.h>
 #include <string.h>
 
@@ -134,7 +134,8 @@ __device__ __forceinline__ void mbar_arrive_many(uint32_t bar, uint32_t count) {
 
 // One of four warps' 32 rows of an operand tile (128 x 64 bf16 at `tile`, as TMA laid it out; rows m0 ..., columns k0 ... of [m, k],
 // whose tile row is `slab`): to fp32 in c.out, and the columns' sums of all 128 rows.  The rows are taken into registers and the
-// ring's stage given back at `bar` first: held until the copy was written, it kept the MMAs waiting (12608 x 768 x 2304 with both 77 us, now 67; a pass of its own over dy before the product 80).
+// ring's stage given back at `bar` first: held until the copy was written, it kept the MMAs waiting (12608 x 768 <- 2304 with both 77 us
+// against 67 with four stages; a pass of its own over dy before the product took 80).
 // `buf`: [4][64], another one than the call before had.
 __device__ __forceinline__ void copy_tile(const CopyOut& c, const unsigned char* tile, uint32_t bar, bool leader, int warp, int m0, int m,
                                           int k0, int k, int slab, float (&buf)[4][64]) {
