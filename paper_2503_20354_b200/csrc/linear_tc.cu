@@ -134,8 +134,11 @@ __device__ __forceinline__ void mbar_arrive_many(uint32_t bar, uint32_t count) {
 
 // One of four warps' 32 rows of an operand tile (128 x 64 bf16 at `tile`, as TMA laid it out; rows m0 ..., columns k0 ... of [m, k],
 // whose tile row is `slab`): to fp32 in c.out, and the columns' sums of all 128 rows.  The rows are taken into registers and the
-// ring's stage given back at `bar` first: held until the copy was written, it kept the MMAs waiting (12608 x 768 <- 2304 with both 77 us
-// against 67 with four stages; a pass of its own over dy before the product took 80).
+// ring's stage given back at `bar` before the copy is written: held until then, it kept the MMAs waiting (12608 x 768 <- 2304 with both
+// 77 us against 67 with four stages; a pass of its own over dy before the product took 80).  Given back only with all words arrived:
+// an issued load may stand behind the stores of the tile before for longer than the stage's next copy takes, and then
+// finds that copy.  Every lane's sum takes all of its words and is stored before the fence, which orders the reads before the
+// refill by TMA (another proxy).
 // `buf`: [4][64], another one than the call before had.
 __device__ __forceinline__ void copy_tile(const CopyOut& c, const unsigned char* tile, uint32_t bar, bool leader, int warp, int m0, int m,
                                           int k0, int k, int slab, float (&buf)[4][64]) {
@@ -144,6 +147,14 @@ __device__ __forceinline__ void copy_tile(const CopyOut& c, const unsigned char*
 #pragma unroll
   for (int i = 0; i < 32; ++i)                   // (row & 7 = i & 7)
     v[i] = *reinterpret_cast<const uint32_t*>(tile + (warp * 32 + i) * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4);
+  float2 sum = make_float2(0.0f, 0.0f);          // (rows and columns behind the last are zeros)
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    sum.x += bf16_lo(v[i]);
+    sum.y += bf16_hi(v[i]);
+  }
+  *reinterpret_cast<float2*>(&buf[warp][2 * lane]) = sum;
+  fence_proxy_async();
   __syncwarp();
   if (leader) mbar_arrive(bar);
   if (c.out && col < k) {
@@ -159,13 +170,6 @@ __device__ __forceinline__ void copy_tile(const CopyOut& c, const unsigned char*
     }
   }
   if (!c.partial && !c.sums) return;
-  float2 sum = make_float2(0.0f, 0.0f);          // (rows and columns behind the last are zeros)
-#pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    sum.x += bf16_lo(v[i]);
-    sum.y += bf16_hi(v[i]);
-  }
-  *reinterpret_cast<float2*>(&buf[warp][2 * lane]) = sum;
   asm volatile("bar.sync 2, 128;" ::: "memory");
   const int at = warp * 32 + lane;               // two warps finish the 64 columns
   if (at < 64 && k0 + at < k) {
