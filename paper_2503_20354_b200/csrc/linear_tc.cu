@@ -139,14 +139,15 @@ __device__ __forceinline__ void mbar_arrive_many(uint32_t bar, uint32_t count) {
 // an issued load may stand behind the stores of the tile before for longer than the stage's next copy takes, and then
 // finds that copy.  Every lane's sum takes all of its words and is stored before the fence, which orders the reads before the
 // refill by TMA (another proxy).
-// `buf`: [4][64], another one than the call before had.
-__device__ __forceinline__ void copy_tile(const CopyOut& c, const unsigned char* tile, uint32_t bar, bool leader, int warp, int m0, int m,
-                                          int k0, int k, int slab, float (&buf)[4][64]) {
+// `buf`: [4][64], another one than the call before had.  `there`: false once a wait of this warp ran out.  It goes on all the same, since
+// the other three wait for it at the barrier: its rows and their sums are NaN.
+__device__ __forceinline__ void copy_tile(const CopyOut& c, const unsigned char* tile, uint32_t bar, bool there, bool leader, int warp, int m0,
+                                          int m, int k0, int k, int slab, float (&buf)[4][64]) {
   const int lane = static_cast<int>(lane_id()), col = k0 + 2 * lane;
   uint32_t v[32];
 #pragma unroll
   for (int i = 0; i < 32; ++i)                   // (row & 7 = i & 7)
-    v[i] = *reinterpret_cast<const uint32_t*>(tile + (warp * 32 + i) * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4);
+    v[i] = there ? *reinterpret_cast<const uint32_t*>(tile + (warp * 32 + i) * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4) : 0x7FC07FC0u;
   float2 sum = make_float2(0.0f, 0.0f);          // (rows and columns behind the last are zeros)
 #pragma unroll
   for (int i = 0; i < 32; ++i) {
@@ -156,7 +157,7 @@ __device__ __forceinline__ void copy_tile(const CopyOut& c, const unsigned char*
   *reinterpret_cast<float2*>(&buf[warp][2 * lane]) = sum;
   fence_proxy_async();
   __syncwarp();
-  if (leader) mbar_arrive(bar);
+  if (leader && there) mbar_arrive(bar);
   if (c.out && col < k) {
     float* to = c.out + static_cast<long long>(m0 + warp * 32) * k + col;
     const int rows = m - m0 - warp * 32;
@@ -329,12 +330,12 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
       int at = 0, tm = first_m, tn = first_n, turn = 0;         // at: the stage of the tile's first step
       uint32_t phases = 0;                       // of each stage's copy_bar
       bool ok = true;
-      for (int t = tile_first; t < p.tiles && ok; t += tile_step, advance(tm, tn)) {
+      for (int t = tile_first; t < p.tiles; t += tile_step, advance(tm, tn)) {
         int s = (at + tn) % p.stages;
         for (int kt = tn; kt < p.ktiles; kt += p.tiles_n) {
-          if (!__all_sync(0xFFFFFFFFu, mbar_wait_suspend(copy_bar + 8 * s, (phases >> s) & 1))) { give_up(); ok = false; break; }
+          if (ok && !__all_sync(0xFFFFFFFFu, mbar_wait_suspend(copy_bar + 8 * s, (phases >> s) & 1))) { give_up(); ok = false; }
           phases ^= 1u << s;
-          copy_tile(p.copy, smem + s * p.stage_bytes, empty + 8 * s, leader, warp - 2 - kWarps, tm * kTileRows, p.m, kt * kTileK, p.k, tm,
+          copy_tile(p.copy, smem + s * p.stage_bytes, empty + 8 * s, ok, leader, warp - 2 - kWarps, tm * kTileRows, p.m, kt * kTileK, p.k, tm,
                     s_copy[turn]);
           turn ^= 1;
           s = (s + p.tiles_n) % p.stages;
@@ -627,12 +628,13 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
     if (warp >= 2 && warp < 2 + kCopyWarps) {
       int turn = 0;
       uint32_t phases = 0;
+      bool ok = true;
       for (int kt = kt_begin; kt < kt_end; ++kt) {
         if (kt % p.tiles_n != tn) continue;
         const int s = (kt - kt_begin) % p.stages;
-        if (!__all_sync(0xFFFFFFFFu, mbar_wait_suspend(copy_bar + 8 * s, (phases >> s) & 1))) { give_up(); break; }
+        if (ok && !__all_sync(0xFFFFFFFFu, mbar_wait_suspend(copy_bar + 8 * s, (phases >> s) & 1))) { give_up(); ok = false; }
         phases ^= 1u << s;
-        copy_tile(p.copy, smem + s * p.stage_bytes, empty + 8 * s, leader, warp - 2, m0, p.m, kt * kTileK, p.k, tile / p.tiles_n, s_copy[turn]);
+        copy_tile(p.copy, smem + s * p.stage_bytes, empty + 8 * s, ok, leader, warp - 2, m0, p.m, kt * kTileK, p.k, tile / p.tiles_n, s_copy[turn]);
         turn ^= 1;
       }
     }
