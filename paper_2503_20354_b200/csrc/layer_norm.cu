@@ -403,7 +403,7 @@ __device__ __forceinline__ float ring_sum(float v, float* buf, int& turn, int gr
   if constexpr (TPR > 32) {
     float* b = buf + (group * 2 + turn) * 8;
     if ((threadIdx.x & 31) == 0) b[(threadIdx.x >> 5) & 7] = v;
-    asm volatile("bar.sync %0, 256;" ::"r"(group + 1) : "memory");
+    named_barrier(group + 1, kGroupThreads);
     v = 0.0f;
 #pragma unroll
     for (int w = 0; w < 8; ++w) v += b[w];
@@ -420,7 +420,7 @@ __device__ __forceinline__ void ring_sums(float& u, float& v, float* buf, int& t
   if constexpr (TPR > 32) {
     float2* b = reinterpret_cast<float2*>(buf) + (group * 2 + turn) * 8;
     if ((threadIdx.x & 31) == 0) b[(threadIdx.x >> 5) & 7] = make_float2(u, v);
-    asm volatile("bar.sync %0, 256;" ::"r"(group + 1) : "memory");
+    named_barrier(group + 1, kGroupThreads);
     u = v = 0.0f;
 #pragma unroll
     for (int w = 0; w < 8; ++w) {
@@ -445,7 +445,7 @@ __device__ __forceinline__ void ring_begin(const RingArgs& a, uint32_t full, uin
   pdl_trigger();
 }
 
-__device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 3, 512;" ::: "memory"); }
+__device__ __forceinline__ void consumers_sync() { named_barrier(3, kRingGroups * kGroupThreads); }
 
 template <int DT, int E, int V, int TPR>
 __global__ void __launch_bounds__(kRingThreads, 1)

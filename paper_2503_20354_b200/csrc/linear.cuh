@@ -82,14 +82,14 @@ __device__ __forceinline__ void add_columns(const ColumnSums& s, int cta, int ct
       }
       buf[slice][lane] = t;
     }
-    asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory");
+    named_barrier(1, 32 * WARPS);
     if (warp == 0 && c < s.cols) {
       float t = 0.0f;
 #pragma unroll
       for (int i = 0; i < kSumSlices; ++i) t += buf[i][lane];
       s.out[c] = s.accumulate ? s.out[c] + t : t;
     }
-    asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory");
+    named_barrier(1, 32 * WARPS);
   }
 }
 

@@ -171,7 +171,7 @@ __device__ __forceinline__ void copy_tile(const CopyOut& c, const unsigned char*
     }
   }
   if (!c.partial && !c.sums) return;
-  asm volatile("bar.sync 2, 128;" ::: "memory");
+  named_barrier(2, 32 * kCopyWarps);
   const int at = warp * 32 + lane;               // two warps finish the 64 columns
   if (at < 64 && k0 + at < k) {
     const float t = buf[0][at] + buf[1][at] + buf[2][at] + buf[3][at];
@@ -639,7 +639,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
       }
     }
     // (the sums below take the place of the ring, which the copies have read)
-    asm volatile("bar.sync 3, 256;" ::: "memory");
+    named_barrier(3, kSplitThreads);
   }
   if constexpr (B_MN && !COPY) {
     if (p.sums.out && warp >= 2) add_columns<kSplitThreads / 32 - 2>(p.sums, blockIdx.x, gridDim.x, warp - 2, s_slices);

@@ -82,6 +82,13 @@ __device__ __forceinline__ void vector_elems(uint4 v, float (&f)[DT == 0 ? 4 : 8
   }
 }
 
+// Barrier `id` for `threads` threads, whole warps.  The instruction takes a warp's lanes together: they come together first, since
+// the code before may have sent them different ways.
+__device__ __forceinline__ void named_barrier(int id, int threads) {
+  __syncwarp();
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
 // Sum over groups of W lanes (W a power of two up to 32), the same bits in every lane of the group.
 template <int W, typename T>
 __device__ __forceinline__ T lanes_sum(T v) {
