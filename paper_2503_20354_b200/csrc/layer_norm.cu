@@ -391,7 +391,10 @@ __device__ __forceinline__ void ring_produce(const RingArgs& a, unsigned char* r
   }
 }
 
+// A chunk's place given back: every number of it has gone into a sum or a store by now, and the fence orders these reads before
+// the next bulk copy, which is of another proxy.
 __device__ __forceinline__ void ring_release(uint32_t bar) {
+  tc::fence_proxy_async();
   __syncwarp();
   if (lane_id() == 0) tc::mbar_arrive(bar);
 }
