@@ -6,6 +6,7 @@
 
 #include <atomic>
 
+#include "smem_table.h"
 #include "surgeon_internal.cuh"
 
 namespace surgeon {
@@ -27,30 +28,14 @@ void* tensor_map_encode_fn() {
 }
 
 cudaError_t allow_dynamic_smem(const void* kernel, int bytes) {
-  struct Seen { const void* fn; int dev; std::atomic<int> bytes; };
-  static Seen seen[256];
-  static std::atomic<int> n_seen{0};
+  static SmemTable table;
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) dev = 0;
-  const int n = n_seen.load(std::memory_order_acquire);
-  Seen* hit = nullptr;
-  for (int i = 0; i < n; ++i)
-    if (seen[i].fn == kernel && seen[i].dev == dev) { hit = &seen[i]; break; }
-  if (hit && hit->bytes.load(std::memory_order_relaxed) >= bytes) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  const cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  // two threads may both set the attribute (harmless: the larger value is set again by whoever
-  // needs it); the table only grows
-  if (hit) {
-    hit->bytes.store(bytes, std::memory_order_relaxed);
-  } else {
-    const int slot = n_seen.load(std::memory_order_relaxed);
-    if (slot < 256) {
-      seen[slot].fn = kernel; seen[slot].dev = dev; seen[slot].bytes.store(bytes, std::memory_order_relaxed);
-      n_seen.store(slot + 1, std::memory_order_release);
-    }
-  }
-  return cudaSuccess;
+  const int st = table.allow(kernel, dev, bytes, [kernel](int n) {
+    return static_cast<int>(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, n));
+  });
+  return st == SmemTable::kNoRoom ? cudaErrorNotSupported : static_cast<cudaError_t>(st);
 }
 
 int sm_count() {
