@@ -661,7 +661,7 @@ int resident_pairs() {
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = 1;
-    if (cudaFuncSetAttribute(dw_swap_kernel<1, 1, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+    if (allow_dynamic_smem(reinterpret_cast<const void*>(dw_swap_kernel<1, 1, 2>), smem) != cudaSuccess ||
         cudaOccupancyMaxActiveClusters(&n, dw_swap_kernel<1, 1, 2>, &cfg) != cudaSuccess || n <= 0) {
       cudaGetLastError();
       n = sm_count() / 2;
