@@ -285,7 +285,8 @@ surgeon_status surgeon_decompress(const surgeon_compressed* act, void* x_out, vo
  * layers (ViT, Segformer) also runs what produces the activations that are pruned (Eq. 1) and
  * what carries the gradient to the layer before (Eq. 2, first line).  Channels are the last,
  * contiguous dimension; parameters are fp32, sums are fp32 or wider and taken in a fixed order,
- * so results are bitwise reproducible from call to call.
+ * so results are bitwise reproducible from call to call.  An output (or the scratch) that overlaps an
+ * operand or another output, even in part, is INVALID_ARG, but for the places named at each call.
  * ======================================================================================== */
 
 /* ------------------------------------------------------------------------------------------
@@ -317,7 +318,7 @@ size_t surgeon_layer_norm_grad_workspace(int64_t rows, int32_t channels);
  * gives (it may be NULL where neither dgamma nor dbeta is wanted), not shared with a call in flight.
  * Element types (dt, grad_dt): (F32, F32), (BF16, F32), (BF16, BF16).  Asynchronous.  The waits for
  * copies on their way are bounded: one that ran out, which no valid call does, shows as NaN.
- * Errors: INVALID_ARG (also dx = x, dgamma = dbeta), BUFFER_TOO_SMALL, UNSUPPORTED ((F32, BF16); size), CUDA.
+ * Errors: INVALID_ARG, BUFFER_TOO_SMALL, UNSUPPORTED ((F32, BF16); size), CUDA.
  * ---------------------------------------------------------------------------------------- */
 surgeon_status surgeon_layer_norm_grad(const void* x, const void* dy, int64_t rows, int32_t channels,
                                        surgeon_dtype dt, surgeon_dtype grad_dt, const float* gamma,
@@ -330,13 +331,13 @@ surgeon_status surgeon_layer_norm_grad(const void* x, const void* dy, int64_t ro
  *   z = x W^T + bias;  y = act(z) + residual
  * d: kind 0 (batch = rows, c_in, c_out), path 0.  x [rows, c_in] and weight [c_out, c_in]: device,
  * bf16 (products and sums in fp32 on the tensor cores).  bias: device, fp32 [c_out], or NULL.
- * residual [rows, c_out] (NULL: none; the skip connection) and y: out_dt; y may be residual, not
- * x.  pre: bf16 [rows, c_out], receives z rounded, for surgeon_linear_grad; or NULL.
+ * residual [rows, c_out] (NULL: none; the skip connection) and y: out_dt; y may be residual.
+ * pre: bf16 [rows, c_out], receives z rounded, for surgeon_linear_grad; or NULL.
  * act: GELU is z Phi(z) with the error function (Phi to 8e-8), and 0 at -infinity.
  * workspace: scratch of the size that the query gives, not shared with a call in flight.  Its first
  * word holds a surgeon_status afterwards: SURGEON_ERR_TIMEOUT if a bounded wait ran out, which no
  * valid call does (calls of up to 4 rows do not write it).  Asynchronous on cuda_stream.
- * Errors: INVALID_ARG (also y or pre in the place of an operand), BUFFER_TOO_SMALL, UNSUPPORTED (path 1;
+ * Errors: INVALID_ARG, BUFFER_TOO_SMALL, UNSUPPORTED (path 1;
  * more than 2^31-1 elements, or an extent above 2^30), CUDA.
  * ---------------------------------------------------------------------------------------- */
 typedef enum { SURGEON_ACT_NONE = 0, SURGEON_ACT_RELU = 1, SURGEON_ACT_GELU = 2 } surgeon_activation;
@@ -354,7 +355,7 @@ surgeon_status surgeon_linear(const surgeon_layer_desc* d, const void* x, const 
  * (not read for SURGEON_ACT_NONE).  dz: fp32 [rows, c_out], the grad_out of surgeon_weight_grad.
  * dx [rows, c_in]: dx_dt, from dz rounded to bf16 (dy itself, without a rounding, where it is
  * bf16 and there is no activation; not rounded for up to 4 rows).  dbias: fp32 [c_out]; accumulate = 1 adds to it.
- * dx, dz, dbias: any may be NULL (not wanted), none may be an operand or another.  dbias is summed in a fixed
+ * dx, dz, dbias: any may be NULL (not wanted).  dbias is summed in a fixed
  * order, another one where dx is wanted too and the sums come from its tiles.  The residual's gradient is dy.
  * ReLU's derivative at 0 is 0.  Asynchronous on cuda_stream.
  * Errors: as above.

@@ -5,6 +5,7 @@
 #include <stdlib.h>
 
 #include <atomic>
+#include <initializer_list>
 
 #include "smem_table.h"
 #include "surgeon_internal.cuh"
@@ -108,6 +109,30 @@ surgeon_status linear_ok(const surgeon_layer_desc* d) {
   return d->path == 0 ? SURGEON_OK : SURGEON_ERR_UNSUPPORTED;
 }
 inline bool known_activation(int act) { return act == SURGEON_ACT_NONE || act == SURGEON_ACT_RELU || act == SURGEON_ACT_GELU; }
+
+// Memory that a call writes or reads (none where `at` is null).
+struct Span {
+  const void* at;
+  size_t bytes;
+};
+Span elems(const void* at, int64_t n, int dt) { return {at, static_cast<size_t>(n) * (dt == SURGEON_F32 ? 4 : 2)}; }
+Span floats(const float* at, int64_t n) { return elems(at, n, SURGEON_F32); }
+bool overlap(const Span& a, const Span& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+  return a.at && b.at && a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
+}
+// Whether something that is written overlaps something that is read, or another thing that is written.
+bool clash(std::initializer_list<Span> written, std::initializer_list<Span> read) {
+  for (const Span* a = written.begin(); a != written.end(); ++a) {
+    for (const Span* b = a + 1; b != written.end(); ++b)
+      if (overlap(*a, *b)) return true;
+    for (const Span& r : read)
+      if (overlap(*a, r)) return true;
+  }
+  return false;
+}
+// An operand in whose place `out` may be written: nothing to compare where it is.
+Span unless_place(Span operand, const void* out) { return operand.at == out ? Span{nullptr, 0} : operand; }
 
 surgeon_status gradients_ok(const surgeon_gradient* list, int32_t count, bool outputs, const double* norm_out,
                             const double* gi_out, const void* workspace, size_t workspace_bytes) {
@@ -337,6 +362,10 @@ surgeon_status surgeon_layer_norm(const void* x, int64_t rows, int32_t channels,
   if (rows > 0 && (!x || !y)) return SURGEON_ERR_INVALID_ARG;
   if (!aligned16(x) || !aligned16(y) || !aligned16(gamma) || !aligned16(beta) || !aligned16(stats))
     return SURGEON_ERR_INVALID_ARG;
+  const int64_t n = rows * channels;
+  if (rows > 0 && clash({elems(y, n, dt), floats(stats, 2 * rows)},
+                        {unless_place(elems(x, n, dt), y), floats(gamma, channels), floats(beta, channels)}))
+    return SURGEON_ERR_INVALID_ARG;
   return launch_layer_norm(x, rows, channels, static_cast<int>(dt), gamma, beta, e, y, stats,
                            static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? SURGEON_OK : SURGEON_ERR_CUDA;
 }
@@ -362,7 +391,12 @@ surgeon_status surgeon_layer_norm_grad(const void* x, const void* dy, int64_t ro
     if (!workspace) return SURGEON_ERR_INVALID_ARG;
     if (workspace_bytes < layer_norm_grad_workspace(rows, channels)) return SURGEON_ERR_BUFFER_TOO_SMALL;
   }
-  if (rows > 0 && ((dx && dx == x) || (dgamma && dgamma == dbeta))) return SURGEON_ERR_INVALID_ARG;
+  const int64_t n = rows * channels;
+  const size_t scratch = dgamma || dbeta ? layer_norm_grad_workspace(rows, channels) : 0;
+  if (rows > 0 && clash({elems(dx, n, grad_dt), floats(dgamma, channels), floats(dbeta, channels), {workspace, scratch}},
+                        {elems(x, n, dt), unless_place(elems(dy, n, grad_dt), dx), floats(gamma, channels), floats(stats, 2 * rows),
+                         unless_place(elems(dx ? residual_grad : nullptr, n, grad_dt), dx)}))
+    return SURGEON_ERR_INVALID_ARG;
   return launch_layer_norm_grad(x, dy, rows, channels, static_cast<int>(dt), static_cast<int>(grad_dt), gamma, stats,
                                 residual_grad, dx, dgamma, dbeta, accumulate ? 1 : 0, workspace,
                                 static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? SURGEON_OK : SURGEON_ERR_CUDA;
@@ -379,11 +413,16 @@ surgeon_status surgeon_linear(const surgeon_layer_desc* d, const void* x, const 
   const surgeon_status st = linear_ok(d);
   if (st != SURGEON_OK) return st;
   if (!x || !weight || !y || !workspace || !known_activation(act) || !known_dtype(out_dt)) return SURGEON_ERR_INVALID_ARG;
-  if (y == x || y == weight || pre == x || pre == weight || pre == y || (pre && pre == residual)) return SURGEON_ERR_INVALID_ARG;
   if (!aligned16(x) || !aligned16(weight) || !aligned16(bias) || !aligned16(residual) || !aligned16(y) || !aligned16(pre) ||
       !aligned16(workspace))
     return SURGEON_ERR_INVALID_ARG;
   if (workspace_bytes < linear_workspace(*d)) return SURGEON_ERR_BUFFER_TOO_SMALL;
+  const int64_t in = static_cast<int64_t>(d->batch) * d->c_in, out = static_cast<int64_t>(d->batch) * d->c_out;
+  const int64_t weights = static_cast<int64_t>(d->c_out) * d->c_in;
+  if (clash({elems(y, out, out_dt), elems(pre, out, SURGEON_BF16), {workspace, linear_workspace(*d)}},
+            {elems(x, in, SURGEON_BF16), elems(weight, weights, SURGEON_BF16), floats(bias, d->c_out),
+             unless_place(elems(residual, out, out_dt), y)}))
+    return SURGEON_ERR_INVALID_ARG;
   return launch_linear(*d, x, weight, bias, residual, static_cast<int>(act), static_cast<int>(out_dt), y, pre, workspace,
                        static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? SURGEON_OK : SURGEON_ERR_CUDA;
 }
@@ -401,13 +440,16 @@ surgeon_status surgeon_linear_grad(const surgeon_layer_desc* d, const void* dy, 
   if (st != SURGEON_OK) return st;
   if (!dy || !workspace || !known_activation(act) || !known_dtype(grad_dt) || !known_dtype(dx_dt)) return SURGEON_ERR_INVALID_ARG;
   if ((dx && !weight) || (act != SURGEON_ACT_NONE && !pre)) return SURGEON_ERR_INVALID_ARG;
-  if (dx == dy || static_cast<const void*>(dz) == dy) return SURGEON_ERR_INVALID_ARG;
-  const bool reads_pre = act != SURGEON_ACT_NONE;
-  if ((dx && (dx == weight || dx == dz || (reads_pre && dx == pre))) || (dz && reads_pre && dz == pre)) return SURGEON_ERR_INVALID_ARG;
   if (!aligned16(dy) || !aligned16(weight) || !aligned16(pre) || !aligned16(dx) || !aligned16(dz) || !aligned16(dbias) ||
       !aligned16(workspace))
     return SURGEON_ERR_INVALID_ARG;
   if (workspace_bytes < linear_grad_workspace(*d)) return SURGEON_ERR_BUFFER_TOO_SMALL;
+  const int64_t in = static_cast<int64_t>(d->batch) * d->c_in, out = static_cast<int64_t>(d->batch) * d->c_out;
+  const int64_t weights = static_cast<int64_t>(d->c_out) * d->c_in;
+  if (clash({elems(dx, in, dx_dt), floats(dz, out), floats(dbias, d->c_out), {workspace, linear_grad_workspace(*d)}},
+            {elems(dy, out, grad_dt), elems(dx ? weight : nullptr, weights, SURGEON_BF16),
+             elems(act != SURGEON_ACT_NONE ? pre : nullptr, out, SURGEON_BF16)}))
+    return SURGEON_ERR_INVALID_ARG;
   return launch_linear_grad(*d, dy, static_cast<int>(grad_dt), weight, pre, static_cast<int>(act), static_cast<int>(dx_dt), dx, dz,
                             dbias, accumulate ? 1 : 0, workspace, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
              ? SURGEON_OK : SURGEON_ERR_CUDA;
