@@ -315,7 +315,7 @@ size_t surgeon_layer_norm_grad_workspace(int64_t rows, int32_t channels);
  * passes the norm by, through the skip connection) and dx: grad_dt.  dx may be dy or residual_grad.
  * dx, dgamma, dbeta: any may be NULL (not wanted).  accumulate = 0 overwrites dgamma and dbeta,
  * 1 adds to them (dx is always overwritten).  workspace: scratch of the size that the query
- * gives (it may be NULL where neither dgamma nor dbeta is wanted), not shared with a call in flight.
+ * gives (it may be NULL where neither dgamma nor dbeta is wanted, or rows = 0), not shared with a call in flight.
  * Element types (dt, grad_dt): (F32, F32), (BF16, F32), (BF16, BF16).  Asynchronous.  The waits for
  * copies on their way are bounded: one that ran out, which no valid call does, shows as NaN.
  * Errors: INVALID_ARG, BUFFER_TOO_SMALL, UNSUPPORTED ((F32, BF16); size), CUDA.

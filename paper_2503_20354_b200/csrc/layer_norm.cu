@@ -877,7 +877,7 @@ cudaError_t launch_layer_norm_grad(const void* x, const void* dy, long long rows
     }
 #undef SURGEON_LN
   }
-  if (partial) {
+  if (dgamma || dbeta) {                         // (of no rows too, which need no scratch)
     launch_kernel(ln_final_kernel, dim3((channels + 31) / 32, 2), dim3(kFinalThreads), 0, stream, true, partial, n, channels, dgamma,
                   dbeta, accumulate);
     note_launches(1);
