@@ -336,7 +336,8 @@ surgeon_status surgeon_layer_norm_grad(const void* x, const void* dy, int64_t ro
  * act: GELU is z Phi(z) with the error function (Phi to 8e-8), and 0 at -infinity.
  * workspace: scratch of the size that the query gives, not shared with a call in flight.  Its first
  * word holds a surgeon_status afterwards: SURGEON_ERR_TIMEOUT if a bounded wait ran out, which no
- * valid call does (calls of up to 4 rows do not write it).  Asynchronous on cuda_stream.
+ * valid call does (calls of up to 4 rows do not write it); what had to wait for it is NaN in the
+ * outputs.  Asynchronous on cuda_stream.
  * Errors: INVALID_ARG, BUFFER_TOO_SMALL, UNSUPPORTED (path 1;
  * more than 2^31-1 elements, or an extent above 2^30), CUDA.
  * ---------------------------------------------------------------------------------------- */

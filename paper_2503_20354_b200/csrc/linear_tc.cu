@@ -481,7 +481,7 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
         ++piece;
       }
       if (ok && !waited) {                       // no piece of this tile: pass the accumulator on
-        if (!__all_sync(0xFFFFFFFFu, mbar_wait_suspend(acc_full + 8 * acc, (it >> 1) & 1))) { give_up(); break; }
+        if (!__all_sync(0xFFFFFFFFu, mbar_wait_suspend(acc_full + 8 * acc, (it >> 1) & 1))) { give_up(); ok = false; break; }
         if (leader) {
           if (PAIR) mbar_arrive_rank0(acc_empty + 8 * acc);
           else mbar_arrive(acc_empty + 8 * acc);
@@ -492,6 +492,24 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
       if (!ok)
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);       // copies in flight land
       bulk_wait_read<0>();                       // the pieces have left shared memory
+    }
+    __syncwarp();
+    if (!ok) {                                   // a wait ran out: all of this warp's part is NaN
+      using T = typename Elem<DT>::type;
+      it = 0; tm = first_m; tn = first_n;
+      for (int t = tile_first; t < p.tiles; t += tile_step, ++it, advance(tm, tn)) {
+        const int m0 = tm * kTileRows + row_in_tile, pieces = pieces_of(tm, tn);
+        for (int c = first_of(it); c < pieces; c += kSlots) {
+          const int x = tn * p.tile_n + c * kCols + r;
+          if (x >= p.n) continue;
+#pragma unroll 1
+          for (int q = m0; q < m0 + 32 && q < p.m; ++q) {
+            const long long at = static_cast<long long>(q) * p.n + x;
+            static_cast<T*>(p.y)[at] = static_cast<T>(DT ? 0x7FC0u : 0x7FC00000u);
+            if (keep) p.pre[at] = 0x7FC0u;
+          }
+        }
+      }
     }
   }
   tc_fence_before();
@@ -543,7 +561,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
   __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 1 + (COPY ? kMaxStages : 0)];
   __shared__ float s_slices[B_MN && !COPY ? kSumSlices : 1][32];
   __shared__ __align__(16) float s_copy[COPY ? 2 : 1][4][COPY ? 64 : 1];
-  __shared__ uint32_t tmem_slot;
+  __shared__ uint32_t tmem_slot, s_gave_up;
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
   const uint32_t lane = lane_id();
   const bool leader = elected();
@@ -555,6 +573,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
   const uint32_t full = smem_u32(bars), empty = full + 8 * kMaxStages, acc_full = full + 16 * kMaxStages, copy_bar = acc_full + 8;
   const int tn = tile % p.tiles_n;               // COPY: the steps kt with kt % tiles_n = tn are copied by this tile's CTAs
   if (tid == 0) {
+    s_gave_up = 0u;
     tma_prefetch_desc(&a_map);
     tma_prefetch_desc(&b_map);
     for (int s = 0; s < p.stages; ++s) {
@@ -574,7 +593,10 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
   pdl_wait();
   pdl_trigger();
   if (blockIdx.x == 0 && tid == 0) *p.status = 0u;              // (a wait gives up after seconds, long behind this)
-  const auto give_up = [&]() { atomicMax(p.status, static_cast<uint32_t>(SURGEON_ERR_TIMEOUT)); };
+  const auto give_up = [&]() {
+    atomicMax(p.status, static_cast<uint32_t>(SURGEON_ERR_TIMEOUT));
+    *static_cast<volatile uint32_t*>(&s_gave_up) = 1u;
+  };
   if (warp == 0) {
     if (leader) {
       int s = 0;
@@ -669,6 +691,10 @@ linear_split_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_cons
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(tmem_base, p.tile_n);
+  }
+  if (s_gave_up) {                               // a wait ran out: this CTA's share is NaN, and with it the cluster's tile
+#pragma unroll 1
+    for (int i = tid; i < kTileM * pitch; i += kSplitThreads) sums[i] = __int_as_float(0x7FC00000);
   }
   cluster_sync_all();
   const int rows = kTileM / p.splits, across = p.tile_n / 4;
