@@ -216,6 +216,7 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
     if (tn >= p.tiles_n) { tn -= p.tiles_n; ++tm; }
   };
 
+  if (PAIR) cluster_sync_all();                  // (both CTAs are there: tmem_alloc_pair)
   if (tid == 0) {
     tma_prefetch_desc(&a_map);
     tma_prefetch_desc(&b_map);

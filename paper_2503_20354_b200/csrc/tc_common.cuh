@@ -232,6 +232,9 @@ __device__ __forceinline__ uint32_t cluster_ctarank() {
 __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// The allocation of a pair is one of both CTAs: their warps have to find each other.  Both CTAs must be running by then (a
+// cluster_sync_all() before): a cluster's CTAs may start some time apart, and a warp whose partner asked before its own CTA had
+// started waited in the allocation for good (seen once in some 1500 launches behind a short kernel).
 __device__ __forceinline__ void tmem_alloc_pair(uint32_t smem_dst, uint32_t cols) {
   asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst),
                "r"(cols)
