@@ -167,6 +167,7 @@ dw_direct_kernel(const uint32_t* __restrict__ bitmap, const void* __restrict__ v
   const uint32_t full_b = smem_u32(bars + 2 * kMaxAStages);
   const uint32_t empty_b = smem_u32(bars + 2 * kMaxAStages + kMaxBStages);
   const uint32_t acc_bar = smem_u32(bars + 2 * kMaxAStages + 2 * kMaxBStages);
+  if (PAIR) cluster_sync_all();          // both CTAs are there (tmem_alloc_pair)
   if (tid == 0) {
     tma_prefetch_desc(&grad_map);
     for (int s = 0; s < p.a_stages; ++s) {

@@ -116,6 +116,7 @@ dw_swap_kernel(const uint32_t* __restrict__ bitmap, const void* __restrict__ val
   const uint32_t full_g = smem_u32(bars + 2 * kMaxAStages);
   const uint32_t empty_g = smem_u32(bars + 2 * kMaxAStages + kMaxGStages);
   const uint32_t acc_bar = smem_u32(bars + 2 * kMaxAStages + 2 * kMaxGStages);
+  cluster_sync_all();                    // both CTAs are there (tmem_alloc_pair)
   if (tid == 0) {
     tma_prefetch_desc(&grad_map);
     if (MODE != 0) tma_prefetch_desc(&rem_map);
