@@ -513,6 +513,7 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
       }
     }
   }
+  __syncwarp();                                  // (the roles of one lane end here; the barriers take whole warps)
   tc_fence_before();
   __syncthreads();
   if (PAIR) cluster_sync_all();
