@@ -5,12 +5,15 @@
 // A tensor is cut into units of kUnit elements whose places start at 16-byte boundaries, and the units of the whole list,
 // in order, into one contiguous range per CTA.  A CTA leaves one sum per tensor that it meets, at slot (CTA + tensor): the
 // path through the list moves by one CTA or by one tensor at a time, so the slots are distinct.  The second kernel adds
-// the slots in a fixed order (every CTA for itself, some 5 KB from L2) and scales the same ranges, last unit first: what
+// the slots in a fixed order (every CTA for itself, some 5 KB from L2 for a list of one launch; a list of several launches has all
+// its slots added by every CTA of each, which grows with the square of its length: 10000 tensors of 100 take 0.16 ms to clip, the
+// longest list, 65536 of them, 1.8, their norms alone 0.08 and 0.49) and scales the same ranges, last unit first: what
 // the first kernel read last is still in L2.  For that the first kernel reads all but the last 80 MB as data that leaves L2
 // first, and so does the second with all that it reads and writes: 86 million fp32 gradients clipped into other tensors 173 us, 181
 // without, in place the same 179 (48 MB: 174; the 80 MB asked for by a policy that keeps them: 175); three passes over HBM take
 // 158, the norm alone takes 55 of 53.  Squares and sums are double (a product of two fp32 numbers is exact in double, and no fp32
-// number's square overflows).  Both kernels are bound by HBM; a list of short tensors (106, 213 KB) by two launches, 8 us.
+// number's square overflows).  Both kernels are bound by HBM; a list of short tensors (106, 213 KB: 8-9 us) by two launches and
+// by the ends of its tensors: a unit that is not whole is read element by element, one load after the other.
 #include "row_vectors.cuh"
 
 #include <algorithm>

@@ -317,11 +317,14 @@ cudaError_t launch_linear_grad(const surgeon_layer_desc& d, const void* dy, int 
   const bool few = d.batch <= kFewRows;
   // the product's operand: dy itself where that is dz and lies as TMA reads it
   const bool direct = !few && !pre && grad_dt == SURGEON_BF16 && d.c_out % 8 == 0;
-  // Then dz and the column sums come from the product's tiles, without a pass over dy: 12608 x 768 <- 2304 56 us against 80, 16384 x
-  // 2048 <- 2048 119 against 128 (whose product by itself is the faster in pairs of CTAs), 300 x 256 <- 512 6.7 against 8.9.
+  // Then dz and the column sums come from the product's tiles, without a pass over dy: 12608 x 768 <- 2304 57 us against 82, 37000 x 64 <-
+  // 256 18 against 27, 64 x 320 <- 4096 8.3 against 10.5, 16384 x 2048 <- 2048 123 against 129 (whose product by itself is the faster in
+  // pairs of CTAs); 12608 x 3200 <- 768 62 against 60.5, 1000 x 768 <- 768 8.8 against 8.3.
   const bool copied = direct && dx && (dz || dbias);
   float* dz32 = dz;
   if (few && dx && !dz) dz32 = reinterpret_cast<float*>(base + s.dz);
+  // (dz in bf16, off by 2^-8 of itself at most: the tensor cores' operand.  In fp32 it would be two products, or one at half their rate of
+  // tf32 with a pass over the weights; dx errs by 0.0023 of its norm so, where its own rounding to bf16 alone gives 0.0017.)
   void* dz16 = dx && !few && !direct ? base + s.dz : nullptr;
   if (!copied && (dz32 || dz16 || dbias)) {
     const auto launch = [&](auto kernel, int elems) {

@@ -58,8 +58,6 @@ __device__ __forceinline__ float slope(float z) {
   return 1.0f;
 }
 
-// y = act(a b^T + bias) + residual, z = a b^T + bias.  a: bf16 [m, k], rows `lda` elements apart.  b: bf16, element (n, k)
-// at n * ldb + k, or (b_mn) at k * ldb + n.  y, residual: [m, n] of type dt; pre (z, bf16): [m, n].
 // Column sums that a kernel before left in `slabs` rows of partial sums, to be added in order into `out` (null: none).
 struct ColumnSums {
   const float* partial;
@@ -102,6 +100,8 @@ struct CopyOut {
   int accumulate;
 };
 
+// y = act(a b^T + bias) + residual, z = a b^T + bias.  a: bf16 [m, k], rows `lda` elements apart.  b: bf16, element (n, k)
+// at n * ldb + k, or (b_mn) at k * ldb + n.  y, residual: [m, n] of type dt; pre (z, bf16): [m, n].
 struct Product {
   const void* a;
   const void* b;

@@ -11,7 +11,7 @@
 // What bounds it: wide layers the tensor pipe (16384 x 2048 x 2048 with a residual 113 us under the power cap, 1216 TFLOP/s, 0.88 of a
 // library product's sustained rate; 96 in short runs); few columns of reduction the epilogue (16384 x 128 -> 512 with GELU and z kept:
 // 27 instructions an element, 13 us for 38 MB); the input's gradient an SM's intake of operands (12608 x 768 <- 2304: 38 us, 1170
-// TFLOP/s; with dz and its sums written from the tiles 56).
+// TFLOP/s; the call with dz and its sums written from the tiles 57, in long runs under the power cap 65).
 #include <cuda.h>
 #include <string.h>
 
@@ -526,7 +526,8 @@ linear_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
 
 // ---- few tiles: the reduction is split over the CTAs of a cluster ----
 //
-// An SM takes in some 85 GB/s of operands, whatever the tile, so a product of few tiles goes by how many SMs fetch them.  Each CTA
+// An SM takes in some 100 to 130 GB/s of operands (24 KB per 64 of k in 0.19 us for tiles of 64 columns, 48 KB in 0.50 for 256: the
+// steps of choose_tile), so a product of few tiles goes by how many SMs fetch them.  Each CTA
 // of a cluster of S sums its share of k for the same tile of 128 x tile_n, puts its sums into its shared memory, and after
 // a cluster barrier finishes 128 / S of the rows: the S sums of an element are added in the order of the CTAs' ranks.
 
@@ -952,7 +953,7 @@ cudaError_t launch_product(const Product& p, uint32_t* status, cudaStream_t stre
   // Sixteen epilogue warps where the epilogue counts, eight where their places in shared memory are better a stage of the ring (us, sixteen and
   // eight: 16384 x 256 -> 1024 with GELU 21 and 27, 12608 x 768 -> 2304 36 and 41; 4096 x 1024 -> 1024 with all 18.5 and 15.4, 16384 x
   // 2048 -> 2048 101 and 96; a residual doubles the places: 16384 x 512 -> 512 16.9 and 15.9).  The input's gradient has
-  // a light epilogue: 12608 x 768 <- 2304 41.7 and 38.9, with dz and its sums 65 and 56.5; 65536 x 64 <- 64 the same.
+  // a light epilogue: 12608 x 768 <- 2304 41.7 and 38.9, with dz and its sums 65 and 57; 65536 x 64 <- 64 the same.
   const bool wide = p.dt == 1 && !p.b_mn && p.k < (p.residual ? 512 : 1024);
 #define SURGEON_FORWARD(PAIR, DT, EPI)                                                                     \
   (p.act == kActNone       ? launch_as<PAIR, 0, DT, kActNone, 0, EPI>(p, s.tile_n, status, stream)          \
