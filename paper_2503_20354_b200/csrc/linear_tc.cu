@@ -8,10 +8,10 @@
 // 32 x 32 goes through shared memory, where the residual has been fetched by TMA before, and leaves by TMA.
 // b is K-major (weights [n, k], forward) or N-major (weights [k, n], the input's gradient): both are read as they lie.
 //
-// What bounds it: wide layers the tensor pipe (16384 x 2048 x 2048 with a residual 113 us under the power cap, 1216 TFLOP/s, 0.88 of a
-// library product's sustained rate; 96 in short runs); few columns of reduction the epilogue (16384 x 128 -> 512 with GELU and z kept:
+// What bounds it: wide layers the tensor pipe (16384 x 2048 x 2048 with a residual 112-116 us under the power cap, 1185-1225 TFLOP/s, 0.87 of
+// a library product's sustained rate; 98 in short runs); few columns of reduction the epilogue (16384 x 128 -> 512 with GELU and z kept:
 // 27 instructions an element, 13 us for 38 MB); the input's gradient an SM's intake of operands (12608 x 768 <- 2304: 38 us, 1170
-// TFLOP/s; the call with dz and its sums written from the tiles 57, in long runs under the power cap 65).
+// TFLOP/s; the call with dz and its sums written from the tiles 57, in long runs under the power cap 65-68).
 #include <cuda.h>
 #include <string.h>
 
