@@ -406,6 +406,101 @@ surgeon_status surgeon_clip_gradients(const surgeon_gradient* list, int32_t coun
                                       double* norm_out, double* gi_out, void* workspace,
                                       size_t workspace_bytes, void* cuda_stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Attention.  For every sequence b, head h and query i (k, v of the head h / (heads / kv_heads)):
+ *   s_ij = scale q_i . k_j for the keys j that i sees;  lse_i = log sum_j e^(s_ij);
+ *   o_i = sum_j e^(s_ij - lse_i) v_j
+ * Query i sees key j if i < q_len_b, j < kv_len_b and, with `causal`, j <= i + kv_len_b - q_len_b (the last query
+ * sees the last key).  A query that sees no key, or lies behind q_len_b, has o = 0 and lse = -infinity.
+ * All tensors bf16, the products' sums, lse and the sums of e^s fp32; e^(s - max) is rounded to bf16 for the product with v.
+ * What keys and values behind kv_len_b hold, NaN or infinity, reaches nothing; nor do, in the backward pass, queries
+ * and their gradients behind q_len_b.  (A NaN in a value that a causal query does not see yet can reach it.)
+ * ---------------------------------------------------------------------------------------- */
+typedef struct surgeon_heads { /* a tensor [batch, rows, heads, head_dim] of bf16 whose last dimension is dense               */
+  void* data;                  /* device, 16-byte aligned                                                                     */
+  int64_t batch_stride, row_stride, head_stride; /* elements; positive multiples of 8 (not looked at where the extent is 1);
+                                  an output's elements have places of their own                                               */
+} surgeon_heads;
+typedef struct surgeon_attention_desc {
+  int32_t batch, heads, kv_heads; /* kv_heads divides heads                                                                   */
+  int32_t q_len, kv_len;          /* rows of q and o, of k and v; 0 is legal                                                  */
+  int32_t head_dim;               /* a multiple of 8, at most 128                                                             */
+  int32_t causal;
+  int32_t reserved;               /* 0                                                                                        */
+  double scale;                   /* positive                                                                                 */
+} surgeon_attention_desc;
+
+/* q_lengths, kv_lengths: DEVICE pointers to `batch` int32, the rows of each sequence (clamped to 0 ... q_len or kv_len), or NULL:
+ * all.  lse: device, fp32 [batch, heads, q_len], or NULL.  workspace: scratch of the size that the query gives (which may be 0), not
+ * shared with a call in flight.  An output that overlaps an operand, the scratch or the other output is INVALID_ARG; views
+ * of one buffer are told apart if all their strides but those inside a row's span are multiples of one of them (a buffer [batch,
+ * row, 3, head, dim], for one).  Asynchronous on cuda_stream.  A bounded wait that ran out, which no valid call does,
+ * shows as NaN.  Errors: INVALID_ARG, BUFFER_TOO_SMALL, UNSUPPORTED (head_dim; more than 2^30 tiles of 64 queries or
+ * keys), CUDA. */
+size_t surgeon_attention_workspace(const surgeon_attention_desc* d);      /* 0 on a bad desc too */
+surgeon_status surgeon_attention(const surgeon_attention_desc* d, const surgeon_heads* q, const surgeon_heads* k,
+                                 const surgeon_heads* v, const int32_t* q_lengths, const int32_t* kv_lengths,
+                                 const surgeon_heads* o, float* lse, void* workspace, size_t workspace_bytes,
+                                 void* cuda_stream);
+
+/* Backward pass of surgeon_attention, which makes the probabilities again:
+ *   P_ij = e^(s_ij - lse_i);  delta_i = do_i . o_i;  dS_ij = P_ij (do_i . v_j - delta_i)
+ *   dq_i = scale sum_j dS_ij k_j;  dk_j = scale sum_i dS_ij q_i;  dv_j = sum_i P_ij do_i
+ * (dk, dv: summed over the heads that share them).  o, lse: as the forward call wrote them; dout: o's gradient.  dq, dk, dv
+ * (rows that see or are seen by nothing: 0) have a layout of their own each; dq may be NULL, and dk and dv together (not wanted).  P and dS are
+ * rounded to bf16 for the products.  Sums in a fixed order: results are bitwise reproducible.  Asynchronous.  Errors: as above. */
+size_t surgeon_attention_grad_workspace(const surgeon_attention_desc* d); /* 0 on a bad desc */
+surgeon_status surgeon_attention_grad(const surgeon_attention_desc* d, const surgeon_heads* q, const surgeon_heads* k,
+                                      const surgeon_heads* v, const surgeon_heads* o, const surgeon_heads* dout,
+                                      const float* lse, const int32_t* q_lengths, const int32_t* kv_lengths,
+                                      const surgeon_heads* dq, const surgeon_heads* dk, const surgeon_heads* dv,
+                                      void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Group norm with an activation over x [batch, positions, channels] (channels last); `groups` divides channels:
+ *   mean, r = 1 / sqrt(var + eps) over a group: all positions of an image, channels / groups channels
+ *   z = (x - mean) r gamma + beta;  y = act(z)
+ * act: NONE, RELU, GELU, or SURGEON_ACT_SILU, z / (1 + e^-z), 0 at -infinity (of the other calls none takes it).
+ * x, y: device, dt; y may be x.  gamma, beta: device, fp32, `channels` each; NULL: 1 and 0.  stats: device, fp32
+ * [2, batch, groups] (the means, then the r) for surgeon_group_norm_grad, or NULL.  A NaN or an infinity stays in its
+ * group.  batch = 0 or positions = 0 is legal: stats are then left as they were.  workspace: scratch of the size that the query gives, not shared with a call in
+ * flight.  Sums in a fixed order.  Asynchronous on cuda_stream.
+ * Errors: INVALID_ARG, BUFFER_TOO_SMALL, UNSUPPORTED (more than SURGEON_MAX_N elements, or 2^20 channels), CUDA.
+ * ---------------------------------------------------------------------------------------- */
+#define SURGEON_ACT_SILU 3
+size_t surgeon_group_norm_workspace(int64_t batch, int64_t positions, int32_t channels, int32_t groups); /* 0 on bad arguments */
+surgeon_status surgeon_group_norm(const void* x, int64_t batch, int64_t positions, int32_t channels,
+                                  int32_t groups, surgeon_dtype dt, const float* gamma, const float* beta,
+                                  double eps, int32_t act, void* y, float* stats, void* workspace,
+                                  size_t workspace_bytes, void* cuda_stream);
+
+/* Backward pass of surgeon_group_norm; z is made again from x, stats, gamma and beta (the forward call's), with its roundings:
+ *   dz = dy act'(z);  g = dz gamma;  xh = (x - mean) r;  dx = r (g - mean(g) - xh mean(g xh)), means over the group
+ *   dgamma = sum dz xh;  dbeta = sum dz, over images and positions
+ * dy and dx: grad_dt; dx may be dy.  dx, dgamma, dbeta: any may be NULL (not wanted).  accumulate = 0 overwrites dgamma and dbeta, 1
+ * adds to them.  Element types as for surgeon_layer_norm_grad.  Sums over a chunk fp32, over the chunks double, in a
+ * fixed order.  Asynchronous.  Errors: as above, UNSUPPORTED also for (F32, BF16). */
+size_t surgeon_group_norm_grad_workspace(int64_t batch, int64_t positions, int32_t channels, int32_t groups);
+surgeon_status surgeon_group_norm_grad(const void* x, const void* dy, int64_t batch, int64_t positions,
+                                       int32_t channels, int32_t groups, surgeon_dtype dt, surgeon_dtype grad_dt,
+                                       const float* gamma, const float* beta, const float* stats, int32_t act,
+                                       void* dx, float* dgamma, float* dbeta, int32_t accumulate,
+                                       void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Dropout whose mask is not stored:
+ *   y_i = (u_i >= t ? x_i * 65536 / (65536 - t) : 0) + residual_i,  t = floor(65536 p + 1/2)
+ * u_i: 16 random bits that are a function of (seed, offset, i) alone: word (i mod 8) / 2, its lower half for even i, of Philox 4x32 with ten
+ * rounds on the counter (i / 8, offset) (64 bits each, low words first) under the key seed.  The backward pass is the
+ * same call on dy with no residual (whose gradient is dy).  Calls whose bits have to be independent differ in seed or offset.
+ * x, residual (NULL: zero), y: device, dt, n elements; y may be x or residual.  What a dropped element held, NaN or infinity, is gone.
+ * device_offset: DEVICE pointer to a word that is added to offset when the kernel runs (for captured calls, which keep seed and
+ * offset), or NULL.  n = 0 is legal.  Asynchronous on cuda_stream.
+ * Errors: INVALID_ARG (p outside [0, 1]), UNSUPPORTED (n above SURGEON_MAX_N), CUDA.
+ * ---------------------------------------------------------------------------------------- */
+surgeon_status surgeon_dropout(const void* x, int64_t n, surgeon_dtype dt, double p, uint64_t seed, uint64_t offset,
+                               const uint64_t* device_offset, const void* residual, void* y, void* cuda_stream);
+
 /* Static text for a status code. */
 const char* surgeon_status_string(surgeon_status s);
 

@@ -53,6 +53,14 @@ class Gradient(C.Structure):
     _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dt", C.c_int32), ("reserved", C.c_int32)]
 
 
+class Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_int64), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class AttentionDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "heads", "kv_heads", "q_len", "kv_len", "head_dim", "causal", "reserved")] + [("scale", C.c_double)]
+
+
 class LayerDesc(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("kind", "batch", "c_in", "h", "w", "c_out", "kh", "kw",
                                          "stride", "pad", "path", "groups")]
@@ -134,6 +142,25 @@ def lib():
         l.surgeon_gradient_norm.argtypes = [P, I32, P, P, P, C.c_size_t, P]
         l.surgeon_clip_gradients.restype = C.c_int
         l.surgeon_clip_gradients.argtypes = [P, I32, F64, P, P, P, C.c_size_t, P]
+        A, H = C.POINTER(AttentionDesc), C.POINTER(Heads)
+        l.surgeon_attention_workspace.restype = C.c_size_t
+        l.surgeon_attention_workspace.argtypes = [A]
+        l.surgeon_attention.restype = C.c_int
+        l.surgeon_attention.argtypes = [A, H, H, H, P, P, H, P, P, C.c_size_t, P]
+        l.surgeon_attention_grad_workspace.restype = C.c_size_t
+        l.surgeon_attention_grad_workspace.argtypes = [A]
+        l.surgeon_attention_grad.restype = C.c_int
+        l.surgeon_attention_grad.argtypes = [A, H, H, H, H, H, P, P, P, H, H, H, P, C.c_size_t, P]
+        l.surgeon_group_norm_workspace.restype = C.c_size_t
+        l.surgeon_group_norm_workspace.argtypes = [I64, I64, I32, I32]
+        l.surgeon_group_norm.restype = C.c_int
+        l.surgeon_group_norm.argtypes = [P, I64, I64, I32, I32, C.c_int, P, P, F64, I32, P, P, P, C.c_size_t, P]
+        l.surgeon_group_norm_grad_workspace.restype = C.c_size_t
+        l.surgeon_group_norm_grad_workspace.argtypes = [I64, I64, I32, I32]
+        l.surgeon_group_norm_grad.restype = C.c_int
+        l.surgeon_group_norm_grad.argtypes = [P, P, I64, I64, I32, I32, C.c_int, C.c_int, P, P, P, I32, P, P, P, I32, P, C.c_size_t, P]
+        l.surgeon_dropout.restype = C.c_int
+        l.surgeon_dropout.argtypes = [P, I64, C.c_int, F64, C.c_uint64, C.c_uint64, P, P, P, P]
         l.surgeon_decompress.restype = C.c_int
         l.surgeon_decompress.argtypes = [C.POINTER(Compressed), C.c_void_p, C.c_void_p]
         l.surgeon_launch_count.restype = C.c_uint64
@@ -725,3 +752,186 @@ def surgeon_clip_gradients(grads, max_norm: float, norm: Optional[torch.Tensor] 
     if st != SURGEON_OK:
         _check(st, "surgeon_clip_gradients")
     return norm
+
+
+# ---------------------------------------------------------------------------------------------
+# Attention, group norm with an activation, dropout
+# ---------------------------------------------------------------------------------------------
+
+def attention_desc(batch: int, heads: int, q_len: int, kv_len: int, head_dim: int, kv_heads: Optional[int] = None,
+                   causal: bool = False, scale: Optional[float] = None) -> AttentionDesc:
+    """The descriptor of an attention: ``kv_heads`` (None: ``heads``) divides ``heads``, ``scale`` is head_dim^-1/2 if None."""
+    return AttentionDesc(int(batch), int(heads), int(heads if kv_heads is None else kv_heads), int(q_len), int(kv_len), int(head_dim),
+                         1 if causal else 0, 0, float(head_dim) ** -0.5 if scale is None else float(scale))
+
+
+def surgeon_attention_workspace(desc: AttentionDesc) -> int:
+    return int(lib().surgeon_attention_workspace(C.byref(desc)))
+
+
+def _heads(t: Optional[torch.Tensor], name: str, device: int, shape) -> Optional[Heads]:
+    """A tensor [batch, row, head, dim] with any strides but a dense last dimension."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError("%s must be a CUDA tensor" % name)
+    if t.get_device() != device:
+        raise ValueError("%s is on %s, which is not the current device" % (name, t.device))
+    if t.shape != shape:
+        raise ValueError("%s must have the shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if t.dtype is not torch.bfloat16:
+        raise ValueError("%s must be %s, got %s" % (name, torch.bfloat16, t.dtype))
+    b, r, h, e = t.stride()
+    if e != 1 and shape[3] != 1:
+        raise ValueError("the last dimension of %s must be dense" % name)
+    return Heads(t.data_ptr(), b, r, h)
+
+
+def _lengths(t: Optional[torch.Tensor], name: str, device: int, batch: int):
+    return _operand(t, name, device, (batch,), torch.int32)
+
+
+def _attention_shapes(desc: AttentionDesc):
+    return (desc.batch, desc.q_len, desc.heads, desc.head_dim), (desc.batch, desc.kv_len, desc.kv_heads, desc.head_dim)
+
+
+def surgeon_attention(desc: AttentionDesc, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                      q_lengths: Optional[torch.Tensor] = None, kv_lengths: Optional[torch.Tensor] = None,
+                      out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """softmax(scale q k^T) v per head; returns ``out`` (made here, contiguous, if None).  ``q`` and ``out`` [batch, q_len, heads, dim],
+    ``k`` and ``v`` [batch, kv_len, kv_heads, dim]: bf16, any strides (multiples of 8 elements) but a dense last dimension, so that
+    slices of a linear layer's output go as they are.  ``q_lengths``, ``kv_lengths``: int32 [batch], the rows of each sequence of
+    a padded batch.  ``lse``: an fp32 tensor [batch, heads, q_len] that receives what ``surgeon_attention_grad`` needs."""
+    dev, (qs, ks) = torch._C._cuda_getDevice(), _attention_shapes(desc)
+    if out is None:
+        out = _new(qs, torch.bfloat16, q.device, stream)
+    hq, hk, hv, ho = _heads(q, "q", dev, qs), _heads(k, "k", dev, ks), _heads(v, "v", dev, ks), _heads(out, "out", dev, qs)
+    ql, kl = _lengths(q_lengths, "q_lengths", dev, desc.batch), _lengths(kv_lengths, "kv_lengths", dev, desc.batch)
+    ls = _operand(lse, "lse", dev, (desc.batch, desc.heads, desc.q_len), torch.float32)
+    ws = _work(workspace, lambda: surgeon_attention_workspace(desc), dev, stream)
+    st = lib().surgeon_attention(desc, hq, hk, hv, ql, kl, ho, ls, *ws, _stream_ptr(stream))
+    if st != SURGEON_OK:
+        _check(st, "surgeon_attention")
+    return out
+
+
+def surgeon_attention_grad_workspace(desc: AttentionDesc) -> int:
+    return int(lib().surgeon_attention_grad_workspace(C.byref(desc)))
+
+
+def surgeon_attention_grad(desc: AttentionDesc, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                           dout: torch.Tensor, lse: torch.Tensor, q_lengths: Optional[torch.Tensor] = None,
+                           kv_lengths: Optional[torch.Tensor] = None, dq: Optional[torch.Tensor] = None,
+                           dk: Optional[torch.Tensor] = None, dv: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None,
+                           want_dq: bool = True, want_dkv: bool = True):
+    """Backward pass of ``surgeon_attention``; returns ``(dq, dk, dv)``, bf16, made here (contiguous) where None, None where not wanted.
+    ``out`` and ``lse`` are the forward call's, ``dout`` is the gradient of ``out``; each gradient has strides of its own."""
+    dev, (qs, ks) = torch._C._cuda_getDevice(), _attention_shapes(desc)
+    if (dq is not None and not want_dq) or ((dk is not None or dv is not None) and not want_dkv):
+        raise ValueError("a gradient given, but not wanted")
+    new = lambda t, shape: _new(shape, torch.bfloat16, q.device, stream) if t is None else t
+    if want_dq:
+        dq = new(dq, qs)
+    if want_dkv:
+        dk, dv = new(dk, ks), new(dv, ks)
+    ins = [_heads(t, n, dev, s) for t, n, s in ((q, "q", qs), (k, "k", ks), (v, "v", ks), (out, "out", qs), (dout, "dout", qs))]
+    outs = [_heads(t, n, dev, s) for t, n, s in ((dq, "dq", qs), (dk, "dk", ks), (dv, "dv", ks))]
+    ls = _operand(lse, "lse", dev, (desc.batch, desc.heads, desc.q_len), torch.float32)
+    ql, kl = _lengths(q_lengths, "q_lengths", dev, desc.batch), _lengths(kv_lengths, "kv_lengths", dev, desc.batch)
+    ws = _work(workspace, lambda: surgeon_attention_grad_workspace(desc), dev, stream)
+    st = lib().surgeon_attention_grad(desc, *ins, ls, ql, kl, *outs, *ws, _stream_ptr(stream))
+    if st != SURGEON_OK:
+        _check(st, "surgeon_attention_grad")
+    return dq, dk, dv
+
+
+SURGEON_ACT_SILU = 3                             # (of the group norm)
+
+
+def _positions(t: torch.Tensor, name: str):
+    """Shape, images, positions and channels of a channels-last tensor [batch, ..., channels]."""
+    shape = t.shape
+    if len(shape) < 2 or shape[-1] == 0:
+        raise ValueError("%s must be [batch, ..., channels]" % name)
+    positions = 1
+    for n in shape[1:-1]:
+        positions *= n
+    return shape, shape[0], positions, shape[-1]
+
+
+def surgeon_group_norm_workspace(batch: int, positions: int, channels: int, groups: int) -> int:
+    return int(lib().surgeon_group_norm_workspace(int(batch), int(positions), int(channels), int(groups)))
+
+
+def surgeon_group_norm(x: torch.Tensor, groups: int, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
+                       eps: float = 1e-5, act: int = SURGEON_ACT_NONE, out: Optional[torch.Tensor] = None,
+                       stats: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Group norm with an activation of ``x`` [batch, ..., channels] (channels last; fp32 or bf16); returns ``out``, which may be ``x``.
+    ``gamma``, ``beta``: fp32.  ``stats``: an fp32 tensor [2, batch, groups] that receives the means and the reciprocal standard
+    deviations for ``surgeon_group_norm_grad``."""
+    shape, batch, positions, channels = _positions(x, "x")
+    dev, dt, f32, vector = torch._C._cuda_getDevice(), x.dtype, torch.float32, (channels,)
+    code = dtype_code(dt)
+    if out is None:
+        out = _new(shape, dt, x.device, stream)
+    ws = _work(workspace, lambda: surgeon_group_norm_workspace(batch, positions, channels, groups), dev, stream)
+    st = lib().surgeon_group_norm(_operand(x, "x", dev, shape, dt), batch, positions, channels, groups, code,
+                                  _operand(gamma, "gamma", dev, vector, f32), _operand(beta, "beta", dev, vector, f32), eps, act,
+                                  _operand(out, "out", dev, shape, dt), _operand(stats, "stats", dev, (2, batch, groups), f32), *ws,
+                                  _stream_ptr(stream))
+    if st != SURGEON_OK:
+        _check(st, "surgeon_group_norm")
+    return out
+
+
+def surgeon_group_norm_grad_workspace(batch: int, positions: int, channels: int, groups: int) -> int:
+    return int(lib().surgeon_group_norm_grad_workspace(int(batch), int(positions), int(channels), int(groups)))
+
+
+def surgeon_group_norm_grad(x: torch.Tensor, dy: torch.Tensor, groups: int, gamma: Optional[torch.Tensor],
+                            beta: Optional[torch.Tensor], stats: torch.Tensor, act: int = SURGEON_ACT_NONE,
+                            dx: Optional[torch.Tensor] = None, dgamma: Optional[torch.Tensor] = None,
+                            dbeta: Optional[torch.Tensor] = None, accumulate: bool = False,
+                            workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None,
+                            want_dx: bool = True) -> Optional[torch.Tensor]:
+    """Backward pass of ``surgeon_group_norm``; returns ``dx`` (of dy's type, made here if None; None with ``want_dx=False``), which may
+    be ``dy``.  ``dgamma``, ``dbeta``: fp32, written (``accumulate=True``: added to) where given."""
+    shape, batch, positions, channels = _positions(x, "x")
+    dev, f32, vector, gt = torch._C._cuda_getDevice(), torch.float32, (channels,), dy.dtype
+    if not want_dx:
+        if dx is not None:
+            raise ValueError("dx given, but not wanted")
+    elif dx is None:
+        dx = _new(shape, gt, dy.device, stream)
+    ws = _work(workspace, lambda: surgeon_group_norm_grad_workspace(batch, positions, channels, groups), dev, stream)
+    st = lib().surgeon_group_norm_grad(_operand(x, "x", dev, shape, x.dtype), _operand(dy, "dy", dev, shape, gt), batch, positions, channels,
+                                       groups, dtype_code(x.dtype), dtype_code(gt), _operand(gamma, "gamma", dev, vector, f32),
+                                       _operand(beta, "beta", dev, vector, f32),
+                                       _operand(stats, "stats", dev, (2, batch, groups), f32), act, _operand(dx, "dx", dev, shape, gt),
+                                       _operand(dgamma, "dgamma", dev, vector, f32), _operand(dbeta, "dbeta", dev, vector, f32),
+                                       1 if accumulate else 0, *ws, _stream_ptr(stream))
+    if st != SURGEON_OK:
+        _check(st, "surgeon_group_norm_grad")
+    return dx
+
+
+def surgeon_dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, residual: Optional[torch.Tensor] = None,
+                    out: Optional[torch.Tensor] = None, device_offset: Optional[torch.Tensor] = None,
+                    stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Drops each element of ``x`` (fp32 or bf16) with probability ``p`` (a multiple of 2^-16), scales the others by 1 / (1 - p) and adds
+    ``residual``; returns ``out``, which may be ``x`` or ``residual``.  The mask is a function of ``seed``, ``offset`` (64 bits each) and the
+    element's index; the backward pass is the same call on dy.  ``device_offset``: an int64 tensor of one element that is added to
+    ``offset`` when the kernel runs, for captured calls."""
+    shape, dt, dev = x.shape, x.dtype, torch._C._cuda_getDevice()
+    code, low = dtype_code(dt), (1 << 64) - 1
+    if out is None:
+        out = _new(shape, dt, x.device, stream)
+    st = lib().surgeon_dropout(_operand(x, "x", dev, shape, dt), x.numel(), code, p, seed & low, offset & low,
+                               _operand(device_offset, "device_offset", dev, (1,), torch.int64),
+                               _operand(residual, "residual", dev, shape, dt), _operand(out, "out", dev, shape, dt), _stream_ptr(stream))
+    if st != SURGEON_OK:
+        _check(st, "surgeon_dropout")
+    return out

@@ -55,6 +55,7 @@ int sm_count() {
 namespace {
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // Algorithm 1: prune step: kept count for `ratio`; one double multiply, one floor.
 inline int64_t kept_count(int64_t n, double ratio) {
@@ -133,6 +134,110 @@ bool clash(std::initializer_list<Span> written, std::initializer_list<Span> read
 }
 // An operand in whose place `out` may be written: nothing to compare where it is.
 Span unless_place(Span operand, const void* out) { return operand.at == out ? Span{nullptr, 0} : operand; }
+
+surgeon_status group_norm_ok(int64_t batch, int64_t positions, int32_t channels, int32_t groups) {
+  if (batch < 0 || positions < 0 || channels <= 0 || groups <= 0 || channels % groups != 0) return SURGEON_ERR_INVALID_ARG;
+  if (channels > (1 << 20)) return SURGEON_ERR_UNSUPPORTED;
+  const int64_t most = SURGEON_MAX_N / channels;
+  if (batch > most || positions > most || (batch > 0 && positions > most / batch)) return SURGEON_ERR_UNSUPPORTED;
+  return SURGEON_OK;
+}
+inline bool known_norm_activation(int act) { return known_activation(act) || act == SURGEON_ACT_SILU; }
+
+surgeon_status attention_ok(const surgeon_attention_desc* d) {
+  if (!d || d->batch <= 0 || d->heads <= 0 || d->kv_heads <= 0 || d->heads % d->kv_heads != 0 || d->q_len < 0 || d->kv_len < 0 ||
+      d->head_dim <= 0 || d->reserved != 0)
+    return SURGEON_ERR_INVALID_ARG;
+  const float s = static_cast<float>(d->scale);
+  if (!(s > 0.0f) || !isfinite(s)) return SURGEON_ERR_INVALID_ARG;
+  if (d->head_dim % 8 != 0 || d->head_dim > 128) return SURGEON_ERR_UNSUPPORTED;
+  const int64_t tiles_q = d->q_len / 64 + 1, tiles_k = d->kv_len / 64 + 1, pairs = static_cast<int64_t>(d->batch) * d->heads;
+  constexpr int64_t kMost = 1 << 30;
+  if (d->q_len > kMost || d->kv_len > kMost || pairs > kMost / (tiles_q > tiles_k ? tiles_q : tiles_k)) return SURGEON_ERR_UNSUPPORTED;
+  return SURGEON_OK;
+}
+
+// A tensor of heads with its extents, for comparing places.
+struct View {
+  const void* at;
+  int64_t n[3], stride[3];                       // batch, rows, heads
+  int64_t dim;
+  int64_t span() const {                         // elements from the first to behind the last
+    int64_t s = dim;
+    for (int i = 0; i < 3; ++i) s += (n[i] - 1) * stride[i];
+    return s;
+  }
+  bool empty() const { return n[1] == 0; }
+};
+// Takes a tensor of a call over: false for a bad pointer or stride.
+bool view_of(const surgeon_heads* t, int64_t batch, int64_t rows, int64_t heads, int64_t dim, View* out) {
+  if (!t) return false;
+  *out = {t->data, {batch, rows, heads}, {t->batch_stride, t->row_stride, t->head_stride}, dim};
+  if (rows == 0) return true;
+  if (!t->data || !aligned16(t->data)) return false;
+  for (int i = 0; i < 3; ++i) {
+    if (out->n[i] == 1) out->stride[i] = 0;      // (not looked at)
+    else if (out->stride[i] <= 0 || out->stride[i] % 8 != 0 || out->stride[i] >= (1LL << 38)) return false;
+  }
+  return true;
+}
+// Whether every element has a place of its own.
+bool injective(const View& v) {
+  int64_t span = v.dim;
+  bool used[3] = {v.n[0] == 1, v.n[1] == 1, v.n[2] == 1};
+  for (;;) {
+    int next = -1;
+    for (int i = 0; i < 3; ++i)
+      if (!used[i] && (next < 0 || v.stride[i] < v.stride[next])) next = i;
+    if (next < 0) return true;
+    if (v.stride[next] < span) return false;
+    span += (v.n[next] - 1) * v.stride[next];
+    used[next] = true;
+  }
+}
+Span span_of(const View& v) { return {v.empty() ? nullptr : v.at, static_cast<size_t>(v.empty() ? 0 : v.span()) * 2}; }
+// Elements of both, modulo one of the strides: those dimensions whose strides are multiples of it drop out, the others span less.
+bool apart(const View& a, const View& b) {
+  if (!overlap(span_of(a), span_of(b))) return true;
+  const int64_t delta = (reinterpret_cast<intptr_t>(b.at) - reinterpret_cast<intptr_t>(a.at)) / 2;
+  for (const View* from : {&a, &b})
+    for (int64_t m : from->stride) {
+      if (m == 0) continue;
+      int64_t wide[2] = {a.dim, b.dim};
+      const View* both[2] = {&a, &b};
+      for (int w = 0; w < 2; ++w)
+        for (int i = 0; i < 3; ++i)
+          if (both[w]->n[i] > 1 && both[w]->stride[i] % m != 0) wide[w] += (both[w]->n[i] - 1) * both[w]->stride[i];
+      const int64_t at = ((delta % m) + m) % m;
+      if (at >= wide[0] && at + wide[1] <= m) return true;
+    }
+  return false;
+}
+// As clash(), of tensors of heads: `written` ones among themselves and against `read` ones, and all against `words`, which are written.
+bool heads_clash(std::initializer_list<const View*> written, std::initializer_list<const View*> read, std::initializer_list<Span> words) {
+  for (const View* const* a = written.begin(); a != written.end(); ++a) {
+    if (!*a) continue;
+    for (const View* const* b = a + 1; b != written.end(); ++b)
+      if (*b && !apart(**a, **b)) return true;
+    for (const View* r : read)
+      if (!apart(**a, *r)) return true;
+    for (const Span& w : words)
+      if (overlap(span_of(**a), w)) return true;
+  }
+  for (const View* r : read)
+    for (const Span& w : words)
+      if (overlap(span_of(*r), w)) return true;
+  return false;
+}
+// Strides that a tensor map takes, for extents of one too.
+surgeon_heads plain(const View& v) {
+  surgeon_heads t = {const_cast<void*>(v.at), v.stride[0], v.stride[1], v.stride[2]};
+  if (!t.head_stride) t.head_stride = (v.dim + 7) / 8 * 8;
+  if (!t.row_stride) t.row_stride = t.head_stride;
+  if (!t.batch_stride) t.batch_stride = t.row_stride;
+  return t;
+}
+Span ints(const int32_t* at, int64_t n) { return {at, static_cast<size_t>(n) * 4}; }
 
 surgeon_status gradients_ok(const surgeon_gradient* list, int32_t count, bool outputs, const double* norm_out,
                             const double* gi_out, const void* workspace, size_t workspace_bytes) {
@@ -478,6 +583,136 @@ surgeon_status surgeon_clip_gradients(const surgeon_gradient* list, int32_t coun
   if (gradient_list_overlaps(list, count)) return SURGEON_ERR_INVALID_ARG;
   return launch_gradient_list(list, count, 1, max_norm, norm_out, gi_out, workspace,
                               static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? SURGEON_OK : SURGEON_ERR_CUDA;
+}
+
+size_t surgeon_attention_workspace(const surgeon_attention_desc* d) { return attention_ok(d) == SURGEON_OK ? attention_workspace(*d) : 0; }
+
+surgeon_status surgeon_attention(const surgeon_attention_desc* d, const surgeon_heads* q, const surgeon_heads* k,
+                                 const surgeon_heads* v, const int32_t* q_lengths, const int32_t* kv_lengths,
+                                 const surgeon_heads* o, float* lse, void* workspace, size_t workspace_bytes,
+                                 void* cuda_stream) {
+  const surgeon_status st = attention_ok(d);
+  if (st != SURGEON_OK) return st;
+  View vq, vk, vv, vo;
+  if (!view_of(q, d->batch, d->q_len, d->heads, d->head_dim, &vq) || !view_of(k, d->batch, d->kv_len, d->kv_heads, d->head_dim, &vk) ||
+      !view_of(v, d->batch, d->kv_len, d->kv_heads, d->head_dim, &vv) || !view_of(o, d->batch, d->q_len, d->heads, d->head_dim, &vo) ||
+      !injective(vo))
+    return SURGEON_ERR_INVALID_ARG;
+  const size_t need = attention_workspace(*d);
+  if (!aligned16(lse) || !aligned16(workspace) || !aligned4(q_lengths) || !aligned4(kv_lengths) || (need && !workspace)) return SURGEON_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return SURGEON_ERR_BUFFER_TOO_SMALL;
+  if (d->q_len == 0) return SURGEON_OK;
+  const Span ls = floats(lse, static_cast<int64_t>(d->batch) * d->heads * d->q_len), ws = {workspace, need};
+  const Span ql = ints(q_lengths, d->batch), kl = ints(kv_lengths, d->batch);
+  if (heads_clash({&vo}, {&vq, &vk, &vv}, {ls, ws}) || clash({ls, ws, span_of(vo)}, {ql, kl})) return SURGEON_ERR_INVALID_ARG;
+  return launch_attention(*d, plain(vq), plain(vk), plain(vv), q_lengths, kv_lengths, plain(vo), lse, workspace,
+                          static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? SURGEON_OK : SURGEON_ERR_CUDA;
+}
+
+size_t surgeon_attention_grad_workspace(const surgeon_attention_desc* d) {
+  return attention_ok(d) == SURGEON_OK ? attention_grad_workspace(*d) : 0;
+}
+
+surgeon_status surgeon_attention_grad(const surgeon_attention_desc* d, const surgeon_heads* q, const surgeon_heads* k,
+                                      const surgeon_heads* v, const surgeon_heads* o, const surgeon_heads* dout,
+                                      const float* lse, const int32_t* q_lengths, const int32_t* kv_lengths,
+                                      const surgeon_heads* dq, const surgeon_heads* dk, const surgeon_heads* dv,
+                                      void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  const surgeon_status st = attention_ok(d);
+  if (st != SURGEON_OK) return st;
+  View vq, vk, vv, vo, vd, gq, gk, gv;
+  if (!view_of(q, d->batch, d->q_len, d->heads, d->head_dim, &vq) || !view_of(k, d->batch, d->kv_len, d->kv_heads, d->head_dim, &vk) ||
+      !view_of(v, d->batch, d->kv_len, d->kv_heads, d->head_dim, &vv) || !view_of(o, d->batch, d->q_len, d->heads, d->head_dim, &vo) ||
+      !view_of(dout, d->batch, d->q_len, d->heads, d->head_dim, &vd))
+    return SURGEON_ERR_INVALID_ARG;
+  if (dq && (!view_of(dq, d->batch, d->q_len, d->heads, d->head_dim, &gq) || !injective(gq))) return SURGEON_ERR_INVALID_ARG;
+  if ((dk != nullptr) != (dv != nullptr)) return SURGEON_ERR_INVALID_ARG;
+  if (dk && (!view_of(dk, d->batch, d->kv_len, d->kv_heads, d->head_dim, &gk) || !injective(gk) ||
+             !view_of(dv, d->batch, d->kv_len, d->kv_heads, d->head_dim, &gv) || !injective(gv)))
+    return SURGEON_ERR_INVALID_ARG;
+  if (!workspace || !aligned16(workspace) || !aligned16(lse) || (d->q_len > 0 && !lse) || !aligned4(q_lengths) || !aligned4(kv_lengths))
+    return SURGEON_ERR_INVALID_ARG;
+  const size_t need = attention_grad_workspace(*d);
+  if (workspace_bytes < need) return SURGEON_ERR_BUFFER_TOO_SMALL;
+  const Span ws = {workspace, need}, ls = floats(lse, static_cast<int64_t>(d->batch) * d->heads * d->q_len);
+  const Span ql = ints(q_lengths, d->batch), kl = ints(kv_lengths, d->batch);
+  if (heads_clash({dq ? &gq : nullptr, dk ? &gk : nullptr, dv ? &gv : nullptr}, {&vq, &vk, &vv, &vo, &vd}, {ws}) ||
+      clash({ws}, {ls, ql, kl}))
+    return SURGEON_ERR_INVALID_ARG;
+  for (const View* g : {dq ? &gq : nullptr, dk ? &gk : nullptr, dv ? &gv : nullptr})
+    if (g && clash({span_of(*g)}, {ls, ql, kl})) return SURGEON_ERR_INVALID_ARG;
+  surgeon_heads pq, pk, pv;
+  if (dq) pq = plain(gq);
+  if (dk) { pk = plain(gk); pv = plain(gv); }
+  return launch_attention_grad(*d, plain(vq), plain(vk), plain(vv), plain(vo), plain(vd), lse, q_lengths, kv_lengths, dq ? &pq : nullptr,
+                               dk ? &pk : nullptr, dk ? &pv : nullptr, workspace, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
+             ? SURGEON_OK : SURGEON_ERR_CUDA;
+}
+
+size_t surgeon_group_norm_workspace(int64_t batch, int64_t positions, int32_t channels, int32_t groups) {
+  return group_norm_ok(batch, positions, channels, groups) == SURGEON_OK ? group_norm_workspace(batch, positions, channels, groups) : 0;
+}
+
+surgeon_status surgeon_group_norm(const void* x, int64_t batch, int64_t positions, int32_t channels,
+                                  int32_t groups, surgeon_dtype dt, const float* gamma, const float* beta,
+                                  double eps, int32_t act, void* y, float* stats, void* workspace,
+                                  size_t workspace_bytes, void* cuda_stream) {
+  const surgeon_status st = group_norm_ok(batch, positions, channels, groups);
+  if (st != SURGEON_OK) return st;
+  const float e = static_cast<float>(eps);
+  if (!known_dtype(dt) || !known_norm_activation(act) || !(e > 0.0f) || !isfinite(e)) return SURGEON_ERR_INVALID_ARG;
+  const int64_t n = batch * positions * channels;
+  if (n > 0 && (!x || !y || !workspace)) return SURGEON_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(y) || !aligned16(gamma) || !aligned16(beta) || !aligned16(stats) || !aligned16(workspace))
+    return SURGEON_ERR_INVALID_ARG;
+  if (n == 0) return SURGEON_OK;
+  const size_t need = group_norm_workspace(batch, positions, channels, groups);
+  if (workspace_bytes < need) return SURGEON_ERR_BUFFER_TOO_SMALL;
+  if (clash({elems(y, n, dt), floats(stats, 2 * batch * groups), {workspace, need}},
+            {unless_place(elems(x, n, dt), y), floats(gamma, channels), floats(beta, channels)}))
+    return SURGEON_ERR_INVALID_ARG;
+  return launch_group_norm(x, batch, positions, channels, groups, static_cast<int>(dt), gamma, beta, e, act, y, stats, workspace,
+                           static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? SURGEON_OK : SURGEON_ERR_CUDA;
+}
+
+size_t surgeon_group_norm_grad_workspace(int64_t batch, int64_t positions, int32_t channels, int32_t groups) {
+  return group_norm_ok(batch, positions, channels, groups) == SURGEON_OK ? group_norm_grad_workspace(batch, positions, channels, groups) : 0;
+}
+
+surgeon_status surgeon_group_norm_grad(const void* x, const void* dy, int64_t batch, int64_t positions,
+                                       int32_t channels, int32_t groups, surgeon_dtype dt, surgeon_dtype grad_dt,
+                                       const float* gamma, const float* beta, const float* stats, int32_t act,
+                                       void* dx, float* dgamma, float* dbeta, int32_t accumulate,
+                                       void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  const surgeon_status st = group_norm_ok(batch, positions, channels, groups);
+  if (st != SURGEON_OK) return st;
+  if (!known_dtype(dt) || !known_dtype(grad_dt) || !known_norm_activation(act)) return SURGEON_ERR_INVALID_ARG;
+  const int64_t n = batch * positions * channels;
+  if (n > 0 && (!x || !dy || !stats || !workspace)) return SURGEON_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(dy) || !aligned16(gamma) || !aligned16(beta) || !aligned16(stats) || !aligned16(dx) || !aligned16(dgamma) ||
+      !aligned16(dbeta) || !aligned16(workspace))
+    return SURGEON_ERR_INVALID_ARG;
+  if (dt == SURGEON_F32 && grad_dt == SURGEON_BF16) return SURGEON_ERR_UNSUPPORTED;
+  const size_t need = n > 0 ? group_norm_grad_workspace(batch, positions, channels, groups) : 0;
+  if (workspace_bytes < need) return SURGEON_ERR_BUFFER_TOO_SMALL;
+  if (clash({elems(dx, n, grad_dt), floats(dgamma, channels), floats(dbeta, channels), {workspace, need}},
+            {elems(x, n, dt), unless_place(elems(dy, n, grad_dt), dx), floats(gamma, channels), floats(beta, channels),
+             floats(stats, 2 * batch * groups)}))
+    return SURGEON_ERR_INVALID_ARG;
+  return launch_group_norm_grad(x, dy, batch, positions, channels, groups, static_cast<int>(dt), static_cast<int>(grad_dt), gamma, beta, stats,
+                                act, dx, dgamma, dbeta, accumulate ? 1 : 0, workspace, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
+             ? SURGEON_OK : SURGEON_ERR_CUDA;
+}
+
+surgeon_status surgeon_dropout(const void* x, int64_t n, surgeon_dtype dt, double p, uint64_t seed, uint64_t offset,
+                               const uint64_t* device_offset, const void* residual, void* y, void* cuda_stream) {
+  if (n < 0 || !known_dtype(dt) || !(p >= 0.0 && p <= 1.0) || (n > 0 && (!x || !y))) return SURGEON_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(residual) || !aligned16(y) || (reinterpret_cast<uintptr_t>(device_offset) & 7u)) return SURGEON_ERR_INVALID_ARG;
+  if (n > SURGEON_MAX_N) return SURGEON_ERR_UNSUPPORTED;
+  if (clash({elems(y, n, dt)}, {unless_place(elems(x, n, dt), y), unless_place(elems(residual, n, dt), y), {device_offset, 8}}))
+    return SURGEON_ERR_INVALID_ARG;
+  return launch_dropout(x, n, static_cast<int>(dt), static_cast<uint32_t>(floor(p * 65536.0 + 0.5)), seed, offset, device_offset, residual, y,
+                        static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? SURGEON_OK : SURGEON_ERR_CUDA;
 }
 
 uint64_t surgeon_launch_count(void) { return launches_so_far(); }

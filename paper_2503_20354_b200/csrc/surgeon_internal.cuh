@@ -122,6 +122,28 @@ int gradient_list_overlaps(const surgeon_gradient* list, int count);
 cudaError_t launch_gradient_list(const surgeon_gradient* list, int count, int clip, double max_norm, double* norm_out,
                                  double* gi_out, void* workspace, cudaStream_t stream);
 
+size_t group_norm_workspace(long long batch, long long positions, int channels, int groups);
+cudaError_t launch_group_norm(const void* x, long long batch, long long positions, int channels, int groups, int dt, const float* gamma,
+                              const float* beta, float eps, int act, void* y, float* stats, void* workspace, cudaStream_t stream);
+size_t group_norm_grad_workspace(long long batch, long long positions, int channels, int groups);
+cudaError_t launch_group_norm_grad(const void* x, const void* dy, long long batch, long long positions, int channels, int groups, int dt,
+                                   int grad_dt, const float* gamma, const float* beta, const float* stats, int act, void* dx, float* dgamma,
+                                   float* dbeta, int accumulate, void* workspace, cudaStream_t stream);
+
+// A tensor of attention heads as the kernels take it: strides of dimensions of one element are valid ones too.
+size_t attention_workspace(const surgeon_attention_desc& d);
+cudaError_t launch_attention(const surgeon_attention_desc& d, const surgeon_heads& q, const surgeon_heads& k, const surgeon_heads& v,
+                             const int* q_lengths, const int* kv_lengths, const surgeon_heads& o, float* lse, void* workspace,
+                             cudaStream_t stream);
+size_t attention_grad_workspace(const surgeon_attention_desc& d);
+cudaError_t launch_attention_grad(const surgeon_attention_desc& d, const surgeon_heads& q, const surgeon_heads& k, const surgeon_heads& v,
+                                  const surgeon_heads& o, const surgeon_heads& dout, const float* lse, const int* q_lengths,
+                                  const int* kv_lengths, const surgeon_heads* dq, const surgeon_heads* dk, const surgeon_heads* dv,
+                                  void* workspace, cudaStream_t stream);
+
+cudaError_t launch_dropout(const void* x, long long n, int dt, uint32_t dropped, uint64_t seed, uint64_t offset,
+                           const uint64_t* device_offset, const void* residual, void* y, cudaStream_t stream);
+
 // The driver's cuTensorMapEncodeTiled, looked up through the runtime (the library carries no
 // link-time dependency on the driver library); nullptr if unavailable.
 void* tensor_map_encode_fn();
