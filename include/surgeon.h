@@ -435,8 +435,8 @@ typedef struct surgeon_attention_desc {
  * shared with a call in flight.  An output that overlaps an operand, the scratch or the other output is INVALID_ARG; views
  * of one buffer are told apart if all their strides but those inside a row's span are multiples of one of them (a buffer [batch,
  * row, 3, head, dim], for one).  Asynchronous on cuda_stream.  A bounded wait that ran out, which no valid call does,
- * shows as NaN.  Errors: INVALID_ARG, BUFFER_TOO_SMALL, UNSUPPORTED (head_dim; more than 2^30 tiles of 64 queries or
- * keys), CUDA. */
+ * shows as NaN.  Errors: INVALID_ARG, BUFFER_TOO_SMALL, UNSUPPORTED (head_dim; batch * heads * (the longer of q_len
+ * and kv_len + 256) above 2^30), CUDA. */
 size_t surgeon_attention_workspace(const surgeon_attention_desc* d);      /* 0 on a bad desc too */
 surgeon_status surgeon_attention(const surgeon_attention_desc* d, const surgeon_heads* q, const surgeon_heads* k,
                                  const surgeon_heads* v, const int32_t* q_lengths, const int32_t* kv_lengths,

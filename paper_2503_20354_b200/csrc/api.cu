@@ -151,9 +151,9 @@ surgeon_status attention_ok(const surgeon_attention_desc* d) {
   const float s = static_cast<float>(d->scale);
   if (!(s > 0.0f) || !isfinite(s)) return SURGEON_ERR_INVALID_ARG;
   if (d->head_dim % 8 != 0 || d->head_dim > 128) return SURGEON_ERR_UNSUPPORTED;
-  const int64_t tiles_q = d->q_len / 64 + 1, tiles_k = d->kv_len / 64 + 1, pairs = static_cast<int64_t>(d->batch) * d->heads;
-  constexpr int64_t kMost = 1 << 30;
-  if (d->q_len > kMost || d->kv_len > kMost || pairs > kMost / (tiles_q > tiles_k ? tiles_q : tiles_k)) return SURGEON_ERR_UNSUPPORTED;
+  // (rows of all heads are counted in 31 bits, a tile's worth to spare)
+  const int64_t most = (SURGEON_MAX_N / 2) / (static_cast<int64_t>(d->q_len > d->kv_len ? d->q_len : d->kv_len) + 256);
+  if (static_cast<int64_t>(d->batch) * d->heads > most) return SURGEON_ERR_UNSUPPORTED;
   return SURGEON_OK;
 }
 

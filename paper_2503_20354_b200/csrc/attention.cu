@@ -4,10 +4,10 @@
 //   c = scale log2(e);  in the end o / l and lse = scale m + log l
 //
 // A CTA takes 256 queries of a head, two tiles of 128, and walks the keys in blocks of 128.  s = q k^T goes to tensor memory (lane = query),
-// four warps a tile read it back, a thread a row, and leave 2^(c (s - m)) as bf16 in tensor memory, where it is the A operand
-// of the product with v: neither s nor p is ever in shared memory.  o stays in tensor memory over all blocks; it is multiplied by
-// 2^(c (m - m')) only when a row's maximum grew by more than 2^8, so hardly ever after the first block (p then is at most 2^8, as
-// exact in bf16 as below 1).  While the four warps of one tile compute, the products of the other run.
+// four warps a tile read it back, a thread a row, and leave 2^(c (s - m)) as bf16 in tensor memory, where it is the A
+// operand of the product with v: neither s nor p is ever in shared memory.  o stays in tensor memory over all blocks.
+// m is the first block's maximum, and set anew, o and l scaled, only where a later block's p add up to 2^64 or more: bf16 has fp32's
+// exponents, so a p above 1 is as exact as one below, and the other blocks need no maximum.
 // Persistent CTAs: the next item's queries, keys and values are on their way while this one's end.
 #include "attention.cuh"
 
@@ -19,22 +19,25 @@ using namespace tc;
 using namespace att;
 
 constexpr int kBlock = 128;                      // keys of a block
-constexpr int kThreads = 384;                    // 2 x 4 softmax warps, one that copies, one that issues products, two that idle
+constexpr int kCopyWarp = 8, kProductWarp = 9;
+constexpr int kThreads = 384;                    // (two warps idle: registers are dealt out by fours of warps)
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;               // 2 x 208 + 88 = 3 x 168, what 384 threads are launched with
 constexpr int kMaxStages = 8;
-constexpr float kGrowth = 8.0f;                  // log2 of what p may grow to before o is scaled
+constexpr float kMost = 18446744073709551616.0f;                 // 2^64: what a row's p of a block may add up to before m is set anew
 
 template <int DP> struct Shape {                 // DP: head_dim, padded to 64 or 128
-  static constexpr int kSlabs = DP / kSlabCols, kTileBytes = kTile * DP * 2;
-  static constexpr bool kOwnP = DP == 64;        // p has columns of its own, else it takes the place of s
+  static constexpr int kSlabs = DP / kSlabCols, kTileBytes = kTile * DP * 2, kBlockBytes = kBlock * DP * 2;
   static constexpr int kQStages = DP == 64 ? 2 : 1, kStages = DP == 64 ? 8 : 4;
-  static constexpr uint32_t kS = 0, kP = DP == 64 ? 256 : 0, kPStep = DP == 64 ? 64 : 128, kO = DP == 64 ? 384 : 256;  // columns; tile 1's s: + 128
-  static constexpr int kSmem = 1024 + (2 * kQStages + kStages) * kTileBytes;
+  static constexpr bool kOwnP = DP == 64;        // p has columns of its own, else it takes the place of s
+  // columns of tensor memory: s of tile t at 128 t
+  static constexpr uint32_t kP = DP == 64 ? 256 : 0, kPStep = DP == 64 ? 64 : 128, kO = DP == 64 ? 384 : 256;
+  static constexpr int kSmem = 1024 + 2 * kQStages * kTileBytes + kStages * kBlockBytes;
 };
 
 struct Args {
   int batch, heads, group, q_len, kv_len, head_dim, causal;     // group: heads that share keys
   int tiles, items;                              // pairs of tiles of a head
+  FastDiv by_tiles, by_heads, by_pairs, by_group;
   float scale;
   const int* q_lengths;
   const int* kv_lengths;
@@ -49,14 +52,15 @@ struct Item {
     const int pairs = p.batch * p.heads;
     int bh, qt;
     if (p.causal) {                              // the longest first
-      qt = p.tiles - 1 - item / pairs;
-      bh = item % pairs;
+      qt = static_cast<int>(divide(item, p.by_pairs));
+      bh = item - qt * pairs;
+      qt = p.tiles - 1 - qt;
     } else {
-      bh = item / p.tiles;
-      qt = item % p.tiles;
+      bh = static_cast<int>(divide(item, p.by_tiles));
+      qt = item - bh * p.tiles;
     }
-    b = bh / p.heads;
-    h = bh % p.heads;
+    b = static_cast<int>(divide(bh, p.by_heads));
+    h = bh - b * p.heads;
     row0 = qt * 2 * kTile;
     q_valid = length_of(p.q_lengths, b, p.q_len);
     kv_valid = length_of(p.kv_lengths, b, p.kv_len);
@@ -71,6 +75,48 @@ struct Item {
     }
   }
 };
+
+// Keys that this row does not see, of the 32 whose scores are in v: `limit` of them count.
+__device__ __forceinline__ void hide(uint32_t (&v)[32], int limit) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (i >= limit) v[i] = 0xFF800000u;
+}
+
+// The largest score of a row's block, and of m.
+__device__ __forceinline__ float largest(const uint32_t (&v)[32], float m) {
+  float a = m, b = m;
+#pragma unroll
+  for (int i = 0; i < 32; i += 4) {
+    a = max3(a, __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
+    b = max3(b, __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
+  }
+  return max3(a, b, b);
+}
+
+// p = 2^(c s - mc) of 32 keys of a row, as bf16; added to sums.
+__device__ __forceinline__ void exponentials(const uint32_t (&v)[32], uint32_t* w, uint64_t (&sums)[2], uint64_t c2, uint64_t mc2) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float2 e = exp2_unit(fma2(pair(v[2 * i], v[2 * i + 1]), c2, mc2));
+    sums[i & 1] = add2(sums[i & 1], pair(e.x, e.y));
+    w[i] = to_bf16x2(e.x, e.y);
+  }
+}
+
+// o of this row times f.
+template <int DP>
+__device__ __noinline__ void scale_row(uint32_t o_at, float f) {
+#pragma unroll 1
+  for (int q = 0; q < DP / 32; ++q) {
+    uint32_t o[32];
+    tmem_ld32(o_at + 32 * q, o);
+    tmem_wait_ld32(o);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+    tmem_st32(o_at + 32 * q, o);
+  }
+}
 
 template <int DP>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -108,7 +154,7 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
     mbar_init(fixed, 1);
     fence_barrier_init();
   }
-  if (warp == 9) tmem_alloc(smem_u32(&tmem_slot), 512);
+  if (warp == kProductWarp) tmem_alloc(smem_u32(&tmem_slot), 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -116,16 +162,16 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
   pdl_trigger();
   pdl_wait();
 
-  if (warp >= 8) {
+  if (warp >= kCopyWarp) {
   set_registers<false, kOtherRegs>();
-  if (warp == 8) {
+  if (warp == kCopyWarp) {
     // ---- copies ----
     int s = 0, it = 0;
     uint32_t phase = 1, fix_phase = 0;           // (a fresh barrier counts as passed in its phase before)
     bool ok = true;
     for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x, ++it) {
       const Item w(p, item);
-      const int qs = S::kQStages == 2 ? it & 1 : 0;
+      const int qs = S::kQStages == 2 ? it & 1 : 0, kv_head = static_cast<int>(divide(w.h, p.by_group));
       const uint32_t q_phase = (S::kQStages == 2 ? (it >> 1) & 1 : it & 1) ^ 1;
       for (int t = 0; t < 2 && ok; ++t) {
         const int at = 2 * qs + t;
@@ -141,40 +187,45 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
           }
         }
       }
-      for (int j = 0; j < 2 * w.most && ok; ++j) {               // k and v in turn
-        ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(empty + 8 * s, phase));
-        if (!ok) break;
-        const int row = (j >> 1) * kBlock, left = w.kv_valid - row;
+      const auto load = [&](bool is_v, int j) {
+        ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait_suspend(empty + 8 * s, phase));
+        if (!ok) return;
+        const int row = j * kBlock, left = w.kv_valid - row;
         // Rows of v behind the last key meet probabilities of zero: they must not hold a NaN.  Behind the tensor's end they are zeros anyway.
-        const bool fix = (j & 1) && left < kBlock && w.kv_valid < p.kv_len;
-        unsigned char* to = ring + s * S::kTileBytes;
+        const bool fix = is_v && left < kBlock && w.kv_valid < p.kv_len;
+        unsigned char* to = ring + s * S::kBlockBytes;
         if (leader) {
           const uint32_t bar = fix ? fixed : full + 8 * s;
-          mbar_arrive_expect_tx(bar, S::kTileBytes);
+          mbar_arrive_expect_tx(bar, S::kBlockBytes);
           for (int c = 0; c < S::kSlabs; ++c)
-            tma_load_4d(smem_u32(to) + c * kBlock * 128, j & 1 ? &v_map : &k_map, c * kSlabCols, row, w.h / p.group, w.b, bar);
+            tma_load_4d(smem_u32(to) + c * kBlock * 128, is_v ? &v_map : &k_map, c * kSlabCols, row, kv_head, w.b, bar);
         }
         if (fix) {
           ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(fixed, fix_phase));
           fix_phase ^= 1;
-          zero_rows<S::kSlabs>(to, kBlock, left, round_up(left, 16));
+          if (ok) zero_rows<S::kSlabs>(to, kBlock, left, round_up(left, 16));
           fence_proxy_async();
           __syncwarp();
-          if (leader) mbar_arrive(full + 8 * s);
+          if (leader && ok) mbar_arrive(full + 8 * s);
         }
         if (++s == S::kStages) { s = 0; phase ^= 1; }
+      };
+      for (int j = 0; j < w.most; ++j) {
+        load(false, j);
+        load(true, j);
       }
     }
     if (!ok)
       for (int i = 0; i < 1000; ++i) __nanosleep(1000);           // copies in flight land
-  } else if (warp == 9) {
+  } else if (warp == kProductWarp) {
     // ---- products ----
     if (leader) {
       const int k_steps = (p.head_dim + 15) / 16, n_o = round_up(p.head_dim, 16);
       const uint32_t idesc_o = make_idesc(kTile, n_o) | kRowsB;
+      const uint32_t q_desc = desc_low(smem_u32(smem)), k_desc = desc_low(smem_u32(ring)), v_desc = desc_low(smem_u32(ring), kBlock * 128);
       int s = 0, it = 0;                         // the ring's next tile
       uint32_t phase = 0;
-      uint32_t seen[2] = {0, 0};                 // blocks of each tile so far
+      uint32_t first[2] = {0, 0};                // number of each tile's first block of the item; a block's place and phases go by its number
       bool ok = true;
       for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x, ++it) {
         const Item w(p, item);
@@ -183,162 +234,165 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
         for (int t = 0; t < 2 && ok; ++t) ok = mbar_wait_suspend(q_full + 8 * (2 * qs + t), q_phase);
         if (!ok) break;
         if (!w.most) continue;
-        // s of tile t and block j from the keys in stage ks
-        const auto scores = [&](int t, int j, int ks) {
-          if (!mbar_wait_suspend((S::kOwnP ? s_free : o_done) + 8 * t, (seen[t] & 1) ^ 1)) return false;
+        const auto next = [&]() {
+          const int st = s;
+          if (++s == S::kStages) { s = 0; phase ^= 1; }
+          return st;
+        };
+        // s of tile t and block j, the t's block number n
+        const auto scores = [&](int t, int j, int st, uint32_t n) {
+          // (s has been read; where p takes its place, p has gone into o)
+          if (!mbar_wait_suspend((S::kOwnP ? s_free : o_done) + 8 * t, (n & 1) ^ 1)) return false;
           tc_fence_after();
           const uint32_t idesc = make_idesc(kTile, round_up(min(kBlock, w.keys[t] - j * kBlock), 16));
-          const uint64_t a = make_desc(smem_u32(smem) + (2 * qs + t) * S::kTileBytes), b = make_desc(smem_u32(ring) + ks * S::kTileBytes);
-          for (int k = 0; k < k_steps; ++k) {
-            const uint64_t step = static_cast<uint64_t>((k >> 2) * (kTile * 128 >> 4) + (k & 3) * 2);
-            umma_bf16(tmem + S::kS + 128 * t, a + step, b + step, idesc, k > 0);
-          }
+          const uint32_t a = q_desc + (2 * qs + t) * (S::kTileBytes >> 4), b = k_desc + st * (S::kBlockBytes >> 4);
+#pragma unroll
+          for (int k = 0; k < DP / 16; ++k)
+            if (k < k_steps) umma_ss(tmem + 128 * t, a + (k >> 2) * (kTile * 128 >> 4) + (k & 3) * 2, b + (k >> 2) * (kBlock * 128 >> 4) + (k & 3) * 2, idesc, k > 0);
           umma_commit(s_full + 8 * t);
           return true;
         };
-        const auto values = [&](int t, int j, int vs) {
-          if (!mbar_wait_suspend(p_full + 8 * t, seen[t] & 1)) return false;
+        const auto values = [&](int t, int j, int st, uint32_t n) {
+          if (!mbar_wait_suspend(p_full + 8 * t, n & 1)) return false;
           tc_fence_after();
           const int steps = (min(kBlock, w.keys[t] - j * kBlock) + 15) / 16;
-          const uint64_t b = make_desc_rows(smem_u32(ring) + vs * S::kTileBytes, kBlock * 128);
-          for (int k = 0; k < steps; ++k)
-            umma_bf16_ta(tmem + S::kO + DP * t, tmem + S::kP + S::kPStep * t + 8 * k, b + 128 * k, idesc_o, j > 0 || k > 0);
+          const uint32_t b = v_desc + st * (S::kBlockBytes >> 4);
+#pragma unroll
+          for (int k = 0; k < kBlock / 16; ++k)
+            if (k < steps) umma_ts(tmem + S::kO + DP * t, tmem + S::kP + S::kPStep * t + 8 * k, b + 128 * k, idesc_o, j > 0 || k > 0);
           umma_commit(o_done + 8 * t);
-          ++seen[t];
           return true;
         };
-        const auto next = [&](int& stage, uint32_t& ph) {
-          if (++stage == S::kStages) { stage = 0; ph ^= 1; }
-        };
-        // stage of k of block j: s; of v: the one behind it; of k of the block after: the one behind that
-        if (!mbar_wait_suspend(full + 8 * s, phase)) break;
+        ok = mbar_wait_suspend(full + 8 * s, phase);
+        int ks = next();                         // the place of the next block's keys
         for (int t = 0; t < 2 && ok; ++t)
-          if (w.blocks[t]) ok = scores(t, 0, s);
+          if (w.blocks[t]) ok = scores(t, 0, ks, first[t]);
         for (int j = 0; j < w.most && ok; ++j) {
-          const int ks = s;
-          next(s, phase);
-          umma_commit(empty + 8 * ks);           // (its products have been issued)
-          const int vs = s;
+          umma_commit(empty + 8 * ks);
+          const int v_at = s;
           const uint32_t v_phase = phase;
-          next(s, phase);
-          bool v_there = false, k_there = false;
-          for (int t = 0; t < 2 && ok; ++t) {
-            if (j >= w.blocks[t]) continue;
-            const bool more = j + 1 < w.blocks[t];
-            const auto ahead = [&]() {
-              if (!more) return true;
-              if (!k_there && !mbar_wait_suspend(full + 8 * s, phase)) return false;
-              k_there = true;
-              if (S::kOwnP) ++seen[t];           // (that block's number, for its own wait)
-              const bool fine = scores(t, j + 1, s);
-              if (S::kOwnP) --seen[t];
-              return fine;
-            };
-            if (S::kOwnP) ok = ahead();
-            if (ok && !v_there) ok = v_there = mbar_wait_suspend(full + 8 * vs, v_phase);
-            ok = ok && values(t, j, vs);
-            if (!S::kOwnP) ok = ok && ahead();
+          next();
+          const bool more = j + 1 < w.most;
+          if (more) {
+            ok = mbar_wait_suspend(full + 8 * s, phase);
+            ks = next();
           }
-          if (ok) umma_commit(empty + 8 * vs);
+          ok = ok && mbar_wait_suspend(full + 8 * v_at, v_phase);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const uint32_t n = first[t] + j;
+            const bool ahead = j + 1 < w.blocks[t];
+            if (S::kOwnP && ok && ahead) ok = scores(t, j + 1, ks, n + 1);
+            if (ok && j < w.blocks[t]) ok = values(t, j, v_at, n);
+            if (!S::kOwnP && ok && ahead) ok = scores(t, j + 1, ks, n + 1);
+          }
+          if (ok) umma_commit(empty + 8 * v_at);
         }
+        first[0] += w.blocks[0];
+        first[1] += w.blocks[1];
       }
     }
   }
   } else {
     // ---- softmax: a thread a row ----
     set_registers<true, kSoftmaxRegs>();
+
     const int t = warp >> 2, quarter = warp & 3, lane = static_cast<int>(lane_id()), row_in_tile = quarter * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(quarter) << 21;
-    const uint32_t s_at = tmem + S::kS + 128 * t + lanes, p_at = tmem + S::kP + S::kPStep * t + lanes, o_at = tmem + S::kO + DP * t + lanes;
-    const float c = p.scale * kLog2E, grown = kGrowth / c;
-    uint32_t seen = 0;
-    int it = 0;
+    const uint32_t s_at = tmem + 128 * t + lanes, p_at = tmem + S::kP + S::kPStep * t + lanes, o_at = tmem + S::kO + DP * t + lanes;
+    const float c = p.scale * kLog2E;
+    const uint64_t c2 = pair(c, c);
+    uint32_t seen = 0;                           // the next block's number
+    int it = 0, stored = -1;                     // stored: the place that outputs are leaving
     bool ok = true;
+    const auto release = [&]() {
+      if (leader && stored >= 0) {
+        bulk_wait_read();
+        mbar_arrive(q_empty + 8 * stored);
+      }
+      __syncwarp();
+      stored = -1;
+    };
     for (int item = blockIdx.x; item < p.items; item += gridDim.x, ++it) {
-      const Item w(p, item);
-      const int row = w.row0 + t * kTile + row_in_tile;
-      const int mine = p.causal ? min(w.kv_valid, row + w.off + 1) : w.kv_valid;         // keys that this row sees
-      const int all = p.causal ? min(w.kv_valid, w.row0 + t * kTile + w.off + 1) : w.kv_valid;    // that every row of the tile sees
+      int mine, all, keys, blocks;               // keys that this row sees; that every row of the tile sees; that any does
+      {
+        const Item w(p, item);
+        const int row = w.row0 + t * kTile + row_in_tile;
+        mine = p.causal ? min(w.kv_valid, row + w.off + 1) : w.kv_valid;
+        all = p.causal ? min(w.kv_valid, row - row_in_tile + w.off + 1) : w.kv_valid;
+        keys = w.keys[t];
+        blocks = w.blocks[t];
+      }
       float m = -INFINITY, l = 0.0f;
-      const int blocks = w.blocks[t], qs = S::kQStages == 2 ? it & 1 : 0;
-      for (int j = 0; j < blocks && ok; ++j, ++seen) {
+      const int qs = S::kQStages == 2 ? it & 1 : 0;
+      for (int j = 0; j < blocks; ++j, ++seen) {
         ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(s_full + 8 * t, seen & 1));
         if (!ok) break;
         tc_fence_after();
-        const int cols = min(kBlock, w.keys[t] - j * kBlock);
-        uint32_t v[kBlock];
+        const int cols = keys - j * kBlock, limit = mine - j * kBlock;
+        uint32_t v[4][32];
+        tmem_ld32(s_at, v[0]);
+        if (cols > 32) tmem_ld32(s_at + 32, v[1]);
+        if (cols > 64) tmem_ld32(s_at + 64, v[2]);
+        if (cols > 96) tmem_ld32(s_at + 96, v[3]);
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (q * 32 < cols) tmem_ld32(s_at + 32 * q, v + 32 * q);
-        tmem_wait_ld();
-        if (S::kOwnP) {
-          tc_fence_before();
-          __syncwarp();
-          if (leader) mbar_arrive(s_free + 8 * t);
+        for (int q = 0; q < 4; ++q) tmem_wait_ld32(v[q]);
+        tc_fence_before();
+        __syncwarp();
+        if (S::kOwnP && leader) mbar_arrive(s_free + 8 * t);
+        if ((j + 1) * kBlock > all) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) hide(v[q], limit - 32 * q);
         }
-        const bool masked = (j + 1) * kBlock > all;
-        const int limit = mine - j * kBlock;
-        float top = -INFINITY;
+        float sum;
+        bool arrived = j == 0;                   // the block before has gone into o, and p may be written
+        for (bool fresh = j == 0;; fresh = true) {
+          if (fresh) {
+            float to = m;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          if (q * 32 >= cols) break;
-          if (masked) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (q * 32 + i >= limit) v[q * 32 + i] = 0xFF800000u;
-          }
-          float a[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-          for (int i = 0; i < 32; ++i) a[i & 3] = fmaxf(a[i & 3], __uint_as_float(v[q * 32 + i]));
-          top = fmaxf(top, fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])));
-        }
-        if (j > 0) {
-          // the block before has gone into o, and p may be written
-          ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(o_done + 8 * t, (seen & 1) ^ 1));
-          if (!ok) break;
-          if (__any_sync(0xFFFFFFFFu, top > m + grown)) {
-            tc_fence_after();
-            const float to = fmaxf(m, top), f = m == to ? 1.0f : exp2_approx(c * (m - to));
-            m = to;
-            l *= f;
-#pragma unroll 1
-            for (int q = 0; q < DP / 32; ++q) {
-              uint32_t o[32];
-              tmem_ld32(o_at + 32 * q, o);
-              tmem_wait_ld();
-#pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-              tmem_st32(o_at + 32 * q, o);
+            for (int q = 0; q < 4; ++q)
+              if (cols > 32 * q) to = largest(v[q], to);
+            if (j > 0) {
+              const float f = m == to ? 1.0f : exp2_approx(c * (m - to));
+              l *= f;
+              scale_row<DP>(o_at, f);
             }
+            m = to;
           }
-        } else {
-          m = top;
-        }
-        const float mc = m == -INFINITY ? 0.0f : c * m;          // (no key so far: all p are 0)
-        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          const float mc = m == -INFINITY ? 0.0f : c * m;        // (no key so far: all p are 0)
+          const uint64_t mc2 = pair(-mc, -mc);
+          uint64_t sums[2] = {0, 0};
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          if (q * 32 >= cols) break;
-          uint32_t w16[16];
-#pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            const float x = exp2_approx(fmaf(c, __uint_as_float(v[q * 32 + i]), -mc)), y = exp2_approx(fmaf(c, __uint_as_float(v[q * 32 + i + 1]), -mc));
-            sum[i & 3] += x;
-            sum[(i & 3) + 1] += y;
-            w16[i >> 1] = to_bf16x2(x, y);
+          for (int q = 0; q < 4; ++q) {
+            if (q > 0 && cols <= 32 * q) break;
+            uint32_t w16[16];
+            exponentials(v[q], w16, sums, c2, mc2);
+            if (q == 0 && !arrived) {
+              ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(o_done + 8 * t, (seen & 1) ^ 1));
+              tc_fence_after();
+              arrived = true;
+            }
+            tmem_st16(p_at + 16 * q, w16);
           }
-          tmem_st16(p_at + 16 * q, w16);
+          const float2 both = unpair(add2(sums[0], sums[1]));
+          sum = both.x + both.y;
+          if (!ok || fresh || !__any_sync(0xFFFFFFFFu, m == -INFINITY || !(sum < kMost))) break;   // (a NaN too)
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        if (!ok) break;
+        l += sum;
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
         if (leader) mbar_arrive(p_full + 8 * t);
+        if (j == 0) release();
       }
+      const Item w(p, item);
+      const int row = w.row0 + t * kTile + row_in_tile;
       if (ok && blocks) ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(o_done + 8 * t, (seen & 1) ^ 1));
       // the queries' place takes the outputs: they are not read any more
       if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(q_full + 8 * (2 * qs + t), S::kQStages == 2 ? (it >> 1) & 1 : it & 1));
-      if (!ok) {                                 // a wait ran out: this warp's rows are NaN, here and from here on
+      if (stored >= 0) release();
+      if (!ok) {                                 // a wait ran out: the rows are NaN, here and from here on
         if (row < p.q_len) {
           unsigned short* to = static_cast<unsigned short*>(p.o.data) + w.b * p.o.batch_stride + static_cast<long long>(row) * p.o.row_stride + w.h * p.o.head_stride;
           for (int i = 0; i < p.head_dim; ++i) to[i] = 0x7FC0u;
@@ -346,7 +400,8 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
         }
         continue;
       }
-      const bool none = l == 0.0f || row >= w.q_valid;
+      if (!(m < INFINITY)) l = __uint_as_float(0x7FC00000u);     // an infinity or a NaN among the scores
+      const bool none = l == 0.0f || m == -INFINITY || row >= w.q_valid;
       const float inv = 1.0f / l;
       if (blocks) tc_fence_after();
       unsigned char* stage = smem + (2 * qs + t) * S::kTileBytes;
@@ -355,7 +410,7 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
         uint32_t o[32];
         if (blocks) {
           tmem_ld32(o_at + 32 * q, o);
-          tmem_wait_ld();
+          tmem_wait_ld32(o);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -378,16 +433,16 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
           for (int i = 0; i < S::kSlabs; ++i)
             tma_store_4d(&o_map, smem_u32(stage) + i * kTile * 128 + quarter * 32 * 128, i * kSlabCols, first, w.h, w.b);
         bulk_commit();
-        bulk_wait_read();
-        mbar_arrive(q_empty + 8 * (2 * qs + t));
       }
-      __syncwarp();
+      stored = 2 * qs + t;
+      if (S::kQStages == 1) release();           // (else behind the next item's first block)
     }
+    release();
   }
   __syncwarp();                                  // (the roles of one lane end here; the barriers take whole warps)
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == kProductWarp) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
@@ -420,6 +475,7 @@ cudaError_t launch_attention(const surgeon_attention_desc& d, const surgeon_head
   a.q_len = d.q_len; a.kv_len = d.kv_len; a.head_dim = d.head_dim; a.causal = d.causal != 0;
   a.tiles = (d.q_len + 2 * kTile - 1) / (2 * kTile);
   a.items = a.tiles * d.batch * d.heads;
+  a.by_tiles = make_div(a.tiles); a.by_heads = make_div(d.heads); a.by_pairs = make_div(d.batch * d.heads); a.by_group = make_div(a.group);
   a.scale = static_cast<float>(d.scale);
   a.q_lengths = q_lengths; a.kv_lengths = kv_lengths;
   a.o = o;

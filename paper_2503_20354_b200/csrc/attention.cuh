@@ -12,6 +12,7 @@ namespace att {
 
 constexpr int kTile = 128;                       // rows of a tile: lanes of tensor memory
 constexpr int kSlabCols = 64;                    // columns of a slab: 128 bytes, the swizzle's width
+template <bool V> struct Flag { static constexpr bool value = V; };
 constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const void* map, int x, int row, int head, int batch, uint32_t bar) {
@@ -28,12 +29,27 @@ __device__ __forceinline__ void tma_store_4d(const void* map, uint32_t src, int 
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 
-// D += A B^T, A (bf16, two to a column) in tensor memory.
-__device__ __forceinline__ void umma_bf16_ta(uint32_t tmem_d, uint32_t tmem_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
+// Operand descriptors in two words: the upper one is the same for all operands here, the lower one holds the address (16-byte units) and the
+// distance of slabs, and moves by additions of 32 bits.  Descriptors made anew for every MMA took the issuing thread 70 to 80 clocks each, where
+// the MMAs last 32 to 64.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_low(uint32_t saddr, uint32_t slab = 16) { return ((saddr & 0x3FFFFu) >> 4) | ((slab >> 4) << 16); }
+// D (+)= A B^T, both in shared memory.
+__device__ __forceinline__ void umma_ss(uint32_t tmem_d, uint32_t a_low, uint32_t b_low, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(tmem_d), "r"(tmem_a), "l"(desc_b), "r"(idesc), "r"(accumulate)
+      "mov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(tmem_d), "r"(a_low), "r"(b_low), "r"(idesc), "r"(accumulate), "r"(kDescHigh)
+      : "memory");
+}
+// D (+)= A B^T, A (bf16, two to a column) in tensor memory.
+__device__ __forceinline__ void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint32_t b_low, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "mov.b64 b, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(tmem_d), "r"(tmem_a), "r"(b_low), "r"(idesc), "r"(accumulate), "r"(kDescHigh)
       : "memory");
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
@@ -46,6 +62,16 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
         "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(taddr)
       : "memory");
+}
+// Waits for loads; r: the registers of the last of them, which are not to be read before.
+__device__ __forceinline__ void tmem_wait_ld32(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
+                 "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]),
+                 "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28])
+               :
+               : "memory");
+  asm volatile("" : "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
 }
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
   asm volatile(
@@ -71,6 +97,65 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
+// ---- pairs of fp32 numbers: one instruction for two ----
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ uint64_t pair(uint32_t lo, uint32_t hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t v) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+  return f;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// max(a, b, c), NaN if one is.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// 2^x of two numbers on the FMA pipe, for a part of the exponentials: the special function unit gives 16 a clock, an eighth of the FMA
+// rate, and would be the bound.  x = n + f with |f| <= 1/2; 2^f by the polynomial of degree 4 whose largest relative error on that interval
+// is least (2.6e-6; its coefficients by Remez' exchange algorithm); n goes into the exponent.  x outside [-126, 127] counts as its end
+// (an infinity too; what a NaN gives is no number to rely on).
+__device__ __forceinline__ float2 exp2_pair(uint64_t x) {
+  float2 v = unpair(x);
+  v.x = fminf(fmaxf(v.x, -126.0f), 127.0f);
+  v.y = fminf(fmaxf(v.y, -126.0f), 127.0f);
+  const uint64_t y = pair(v.x, v.y), shift = pair(12582912.0f, 12582912.0f);     // 1.5 * 2^23: what is added to it is rounded to an integer
+  const uint64_t n = add2(y, shift), f = fma2(add2(n, pair(-12582912.0f, -12582912.0f)), pair(-1.0f, -1.0f), y);
+  uint64_t r = fma2(pair(0.009570102207362652f, 0.009570102207362652f), f, pair(0.05591785907745361f, 0.05591785907745361f));
+  r = fma2(r, f, pair(0.240247443318367f, 0.240247443318367f));
+  r = fma2(r, f, pair(0.6931217908859253f, 0.6931217908859253f));
+  r = fma2(r, f, pair(0.9999992847442627f, 0.9999992847442627f));
+  const float2 m = unpair(r), e = unpair(n);
+  return make_float2(__int_as_float(__float_as_int(m.x) + (__float_as_int(e.x) << 23)), __int_as_float(__float_as_int(m.y) + (__float_as_int(e.y) << 23)));
+}
+__device__ __forceinline__ float2 exp2_unit(uint64_t x) {
+  const float2 v = unpair(x);
+  return make_float2(exp2_approx(v.x), exp2_approx(v.y));
+}
+
 // Registers of each thread of this warpgroup from here on: more or fewer than it was launched with.
 template <bool MORE, int N>
 __device__ __forceinline__ void set_registers() {
@@ -78,16 +163,6 @@ __device__ __forceinline__ void set_registers() {
   else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
 
-// Descriptor of an operand that is contiguous along its M or N: rows of 64 elements per k, slabs `slab` bytes apart.
-__device__ __forceinline__ uint64_t make_desc_rows(uint32_t saddr, uint32_t slab) {
-  uint64_t d = 0;
-  d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
-  d |= static_cast<uint64_t>(slab >> 4) << 16;
-  d |= static_cast<uint64_t>(1024 >> 4) << 32;
-  d |= static_cast<uint64_t>(1) << 46;
-  d |= static_cast<uint64_t>(2) << 61;
-  return d;
-}
 constexpr uint32_t kRowsB = 1u << 16;            // instruction descriptor: B is such an operand
 
 __host__ __device__ constexpr int round_up(int n, int m) { return (n + m - 1) / m * m; }

@@ -24,6 +24,13 @@ constexpr int kThreads = 384;                    // 2 x 4 warps with a thread a 
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;               // 2 x 208 + 88 = 3 x 168, what 384 threads are launched with
 constexpr int kMaxStages = 8;
 
+constexpr int kByFma = 4;                        // of sixteen pairs of exponentials, those that the FMA pipe computes
+
+// Four numbers of shared memory as two pairs.
+__device__ __forceinline__ void load_pairs(uint32_t at, uint64_t (&v)[2]) {
+  asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(v[0]), "=l"(v[1]) : "r"(at));
+}
+
 template <int DP, bool KV> struct Shape {
   static constexpr int kSlabs = DP / kSlabCols;
   static constexpr int kTiles = KV && DP == 128 ? 1 : 2;         // tiles that stay; the two halves of the warps have one each, or every other block of one
@@ -44,10 +51,11 @@ template <int DP, bool KV> struct Shape {
 struct Args {
   int batch, heads, kv_heads, group, q_len, kv_len, head_dim, causal;
   int tiles, items, splits, q_pad;
+  FastDiv by_tiles, by_heads, by_pairs, by_group, by_splits;
   float scale;
   const int* q_lengths;
   const int* kv_lengths;
-  const float2* rows;                            // lse2 and delta, [batch][heads][q_pad]
+  const float* rows;                             // [batch][heads][q_pad / 64][2][64]: -lse2, -delta of the queries of a block
   surgeon_heads out1, out2;                      // dq; or dk and dv
   float* partial;                                // [split][2][batch][kv_heads][kv_len][head_dim], where there are several
 };
@@ -63,19 +71,21 @@ struct Item {
     const int heads = KV ? p.kv_heads : p.heads, pairs = p.batch * heads;
     split = 0;
     if (KV && p.splits > 1) {
-      split = item % p.splits;
-      item /= p.splits;
+      const int whole = static_cast<int>(divide(item, p.by_splits));
+      split = item - whole * p.splits;
+      item = whole;
     }
     int bh, tile;
     if (p.causal) {                              // the longest first
-      tile = KV ? item / pairs : p.tiles - 1 - item / pairs;
-      bh = item % pairs;
+      tile = static_cast<int>(divide(item, p.by_pairs));
+      bh = item - tile * pairs;
+      if (!KV) tile = p.tiles - 1 - tile;
     } else {
-      bh = item / p.tiles;
-      tile = item % p.tiles;
+      bh = static_cast<int>(divide(item, p.by_tiles));
+      tile = item - bh * p.tiles;
     }
-    b = bh / heads;
-    h = bh % heads;
+    b = static_cast<int>(divide(bh, p.by_heads));
+    h = bh - b * heads;
     row0 = tile * S::kTiles * kTile;
     q_valid = length_of(p.q_lengths, b, p.q_len);
     kv_valid = length_of(p.kv_lengths, b, p.kv_len);
@@ -100,19 +110,29 @@ struct Item {
     active[0] = steps > 0;
     active[1] = steps > 0 && (S::kTiles == 1 || row0 + kTile < valid);
   }
-  // Head and first row of the n-th step's block, and how many rows of it count.
-  __device__ __forceinline__ void block(const Args& p, int n, int* head, int* row, int* left) const {
-    if (KV) {
-      const int at = from + n, g = at / blocks;
-      *head = h * p.group + g;
-      *row = (first + at - g * blocks) * kBlock;
-      *left = q_valid - *row;
-    } else {
-      *head = h / p.group;
-      *row = n * kBlock;
-      *left = kv_valid - *row;
-    }
-    if (*left > kBlock) *left = kBlock;
+};
+
+// The blocks of an item, one step after the other: head and first row of each, and how many rows of it count.
+template <int DP, bool KV>
+struct Walk {
+  int head, row, left, index;                    // index: of the block among its head's
+  __device__ __forceinline__ Walk(const Args& p, const Item<DP, KV>& w) {
+    head = KV ? w.h * p.group : static_cast<int>(divide(w.h, p.by_group));
+    index = w.from;
+    settle(w);
+  }
+  __device__ __forceinline__ void advance(const Item<DP, KV>& w, int steps) {
+    index += steps;
+    settle(w);
+  }
+  __device__ __forceinline__ void settle(const Item<DP, KV>& w) {
+    if (KV)
+      while (index >= w.blocks && w.blocks > 0) {
+        index -= w.blocks;
+        ++head;
+      }
+    row = (w.first + index) * kBlock;
+    left = min(kBlock, (KV ? w.q_valid : w.kv_valid) - row);
   }
 };
 
@@ -188,11 +208,11 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
             mbar_arrive(hold_full + 8 * hs);
           }
         }
-        for (int n = 0; n < w.steps && ok; ++n) {
+        Walk<DP, KV> at(p, w);
+        for (int n = 0; n < w.steps && ok; ++n, at.advance(w, 1)) {
           ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(empty + 8 * s, phase));
           if (!ok) break;
-          int head, row, left;
-          w.block(p, n, &head, &row, &left);
+          const int head = at.head, row = at.row, left = at.left;
           // Rows behind the last meet zeros in P and dS: they must not hold a NaN.  Behind the tensor's end they are zeros anyway.
           const bool fix = left < kBlock && row + left < (KV ? p.q_len : p.kv_len);
           unsigned char* to = ring + s * S::kStageBytes;
@@ -204,7 +224,7 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
               tma_load_4d(smem_u32(to) + S::kBlockBytes + c * kBlock * 128, &w_map, c * kSlabCols, row, head, w.b, bar);
             }
             if (KV)
-              bulk_load(smem_u32(row_ring) + s * S::kRowBytes, p.rows + (static_cast<long long>(w.b) * p.heads + head) * p.q_pad + row, S::kRowBytes, bar);
+              bulk_load(smem_u32(row_ring) + s * S::kRowBytes, p.rows + ((static_cast<long long>(w.b) * p.heads + head) * p.q_pad + row) * 2, S::kRowBytes, bar);
           }
           if (fix) {
             ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(fixed, fix_phase));
@@ -224,6 +244,7 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
       // ---- products ----
       if (leader) {
         const int k_steps = (p.head_dim + 15) / 16;
+        const uint32_t hold_desc = desc_low(smem_u32(smem)), ring_desc = desc_low(smem_u32(ring)), rows_desc = desc_low(smem_u32(ring), kBlock * 128);
         const uint32_t idesc_acc = make_idesc(kTile, round_up(p.head_dim, 16)) | kRowsB;
         int it = 0;
         int ss = 0, as = 0;                      // the ring's next place for s and do v^T, and for the sums
@@ -233,43 +254,38 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
           const Item<DP, KV> w(p, item);
           const int hs = S::kHold == 2 ? it & 1 : 0;
           if (!mbar_wait_suspend(hold_full + 8 * hs, S::kHold == 2 ? (it >> 1) & 1 : it & 1)) break;
-          if (!mbar_wait_suspend(acc_free, (it & 1) ^ 1)) break;
-          tc_fence_after();
-          const uint32_t hold = smem_u32(smem) + hs * S::kHoldBytes;
+          const uint32_t hold = hold_desc + hs * (S::kHoldBytes >> 4);
+          Walk<DP, KV> s_at(p, w), a_at(p, w);   // the next block for s and do v^T, and for the sums
           // s and do v^T of half t, the n-th step's block in stage st; number: of this block among the half's
-          const auto scores = [&](int t, int n, int st, uint32_t number) {
+          const auto scores = [&](int t, int st, uint32_t number) {
             if (!mbar_wait_suspend((S::kOwn ? s_free : acc_done) + 8 * t, (number & 1) ^ 1)) return false;
             tc_fence_after();
-            int head, row, left;
-            w.block(p, n, &head, &row, &left);
-            const uint32_t idesc = make_idesc(kTile, round_up(left, 16));
-            const uint32_t x = hold + (S::kTiles == 2 ? t * 2 * S::kTileBytes : 0), u = smem_u32(ring) + st * S::kStageBytes;
-            const uint64_t xd = make_desc(x), yd = make_desc(x + S::kTileBytes), ud = make_desc(u), wd = make_desc(u + S::kBlockBytes);
-            const uint32_t d = tmem + S::kStep * t;
-            for (int k = 0; k < k_steps; ++k) {
-              const uint64_t a = static_cast<uint64_t>((k >> 2) * (kTile * 128 >> 4) + (k & 3) * 2), b = static_cast<uint64_t>((k >> 2) * (kBlock * 128 >> 4) + (k & 3) * 2);
-              umma_bf16(d + S::kS, xd + a, ud + b, idesc, k > 0);
-            }
-            for (int k = 0; k < k_steps; ++k) {
-              const uint64_t a = static_cast<uint64_t>((k >> 2) * (kTile * 128 >> 4) + (k & 3) * 2), b = static_cast<uint64_t>((k >> 2) * (kBlock * 128 >> 4) + (k & 3) * 2);
-              umma_bf16(d + S::kD, yd + a, wd + b, idesc, k > 0);
-            }
+            const uint32_t idesc = make_idesc(kTile, round_up(s_at.left, 16));
+            const uint32_t x = hold + (S::kTiles == 2 ? t * (2 * S::kTileBytes >> 4) : 0), u = ring_desc + st * (S::kStageBytes >> 4), d = tmem + S::kStep * t;
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+              for (int k = 0; k < DP / 16; ++k)
+                if (k < k_steps)
+                  umma_ss(d + (half ? S::kD : S::kS), x + half * (S::kTileBytes >> 4) + (k >> 2) * (kTile * 128 >> 4) + (k & 3) * 2,
+                          u + half * (S::kBlockBytes >> 4) + (k >> 2) * (kBlock * 128 >> 4) + (k & 3) * 2, idesc, k > 0);
             umma_commit(s_full + 8 * t);
             return true;
           };
-          const auto sums = [&](int t, int n, int st, bool fresh) {
+          bool acc_ready = false;                // the sums of the item before have been taken out
+          const auto sums = [&](int t, int st, bool fresh) {
             if (!mbar_wait_suspend(p_full + 8 * t, seen[t] & 1)) return false;
+            if (fresh && !acc_ready && !(acc_ready = mbar_wait_suspend(acc_free, (it & 1) ^ 1))) return false;
             tc_fence_after();
-            int head, row, left;
-            w.block(p, n, &head, &row, &left);
-            const int steps = (left + 15) / 16;
-            const uint32_t u = smem_u32(ring) + st * S::kStageBytes, d = tmem + S::kStep * t;
-            const uint64_t ud = make_desc_rows(u, kBlock * 128), wd = make_desc_rows(u + S::kBlockBytes, kBlock * 128);
-            if (KV)
-              for (int k = 0; k < steps; ++k)
-                umma_bf16_ta(tmem + S::kAcc2 + S::kAccStep * t, d + S::kS + 8 * k, wd + 128 * k, idesc_acc, !fresh || k > 0);
-            for (int k = 0; k < steps; ++k)
-              umma_bf16_ta(tmem + S::kAcc1 + S::kAccStep * t, d + S::kDs + 8 * k, ud + 128 * k, idesc_acc, !fresh || k > 0);
+            const int steps = (a_at.left + 15) / 16;
+            const uint32_t u = rows_desc + st * (S::kStageBytes >> 4), d = tmem + S::kStep * t;
+#pragma unroll
+            for (int half = KV ? 1 : 0; half >= 0; --half)
+#pragma unroll
+              for (int k = 0; k < kBlock / 16; ++k)
+                if (k < steps)
+                  umma_ts(tmem + (half ? S::kAcc2 : S::kAcc1) + S::kAccStep * t, d + (half ? S::kS : S::kDs) + 8 * k,
+                          u + half * (S::kBlockBytes >> 4) + 128 * k, idesc_acc, !fresh || k > 0);
             umma_commit(acc_done + 8 * t);
             ++seen[t];
             return true;
@@ -281,8 +297,9 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
             // step n of both halves; s of the step after goes ahead of the sums where it has room
             const auto all_scores = [&](int n, int t) {          // (the first half waits for the block)
               if (t == 0 && !mbar_wait_suspend(full + 8 * ss, s_phase)) return false;
-              const bool fine = !w.active[t] || scores(t, n, ss, seen[t] + (S::kOwn && n > 0 ? 1 : 0));
+              const bool fine = !w.active[t] || scores(t, ss, seen[t] + (S::kOwn && n > 0 ? 1 : 0));
               if (t == 1) {
+                s_at.advance(w, 1);
                 forward(ss);
                 if (ss == 0) s_phase ^= 1;
               }
@@ -292,28 +309,32 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
             for (int n = 0; n < w.steps && ok; ++n) {
               for (int t = 0; t < 2 && ok; ++t) {
                 if (S::kOwn && n + 1 < w.steps) ok = all_scores(n + 1, t);
-                if (ok && w.active[t]) ok = sums(t, n, as, n == 0);
+                if (ok && w.active[t]) ok = sums(t, as, n == 0);
                 if (!S::kOwn && ok && n + 1 < w.steps) ok = all_scores(n + 1, t);
               }
               if (ok) umma_commit(empty + 8 * as);
               forward(as);
+              a_at.advance(w, 1);
             }
           } else {
             const auto next_scores = [&](int n) {
               if (!mbar_wait_suspend(full + 8 * ss, s_phase)) return false;
-              const bool fine = scores(n & 1, n, ss, seen[n & 1]);
+              const bool fine = scores(n & 1, ss, seen[n & 1]);
+              s_at.advance(w, 1);
               forward(ss);
               if (ss == 0) s_phase ^= 1;
               return fine;
             };
             for (int n = 0; n < 2 && n < w.steps && ok; ++n) ok = next_scores(n);
             for (int n = 0; n < w.steps && ok; ++n) {
-              ok = sums(n & 1, n, as, n == 0);
+              ok = sums(n & 1, as, n == 0);
               if (ok) umma_commit(empty + 8 * as);
               forward(as);
+              a_at.advance(w, 1);
               if (ok && n + 2 < w.steps) ok = next_scores(n + 2);
             }
           }
+          if (ok && !acc_ready) ok = mbar_wait_suspend(acc_free, (it & 1) ^ 1);  // (an item without steps)
           if (ok) umma_commit(item_done);
         }
       }
@@ -324,24 +345,28 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
     const int t = warp >> 2, quarter = warp & 3, lane = static_cast<int>(lane_id()), row_in_tile = quarter * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(quarter) << 21, mine_at = tmem + S::kStep * t + lanes;
     const float c = p.scale * kLog2E;
+    const uint64_t c2 = pair(c, c);
     uint32_t seen = 0, before = 0;               // before: steps of the items so far
     int it = 0;
     bool ok = true;
     for (int item = blockIdx.x; item < p.items; item += gridDim.x, ++it) {
       const Item<DP, KV> w(p, item);
       const int row = w.row0 + (S::kTiles == 2 ? t * kTile : 0) + row_in_tile;
-      float lse2 = 0.0f, delta = 0.0f;
+      float lse2 = -INFINITY, delta = 0.0f;      // (with their signs changed)
       if (!KV && w.active[t]) {
-        const float2 r = row < p.q_pad ? p.rows[(static_cast<long long>(w.b) * p.heads + w.h) * p.q_pad + row] : make_float2(INFINITY, 0.0f);
-        lse2 = r.x;
-        delta = r.y;
+        if (row < p.q_pad) {
+          const float* r = p.rows + ((static_cast<long long>(w.b) * p.heads + w.h) * p.q_pad + (row & ~(kBlock - 1))) * 2 + (row & (kBlock - 1));
+          lse2 = r[0];
+          delta = r[kBlock];
+        }
       }
       // columns [lo, hi) of a block count: Q: hi by the row; KV: lo by the row
       const int edge = KV ? (p.causal ? row - w.off : 0) : (p.causal ? min(w.kv_valid, row + w.off + 1) : w.kv_valid);
       const int tile0 = row - row_in_tile;
-      for (int n = S::kTiles == 2 ? 0 : t; n < w.steps && ok; n += S::kTiles == 2 ? 1 : 2) {
-        int head, col0, left;
-        w.block(p, n, &head, &col0, &left);
+      Walk<DP, KV> walk(p, w);
+      if (S::kTiles == 1) walk.advance(w, t);
+      for (int n = S::kTiles == 2 ? 0 : t; n < w.steps && ok; n += S::kTiles == 2 ? 1 : 2, walk.advance(w, S::kTiles == 2 ? 1 : 2)) {
+        const int col0 = walk.row, left = walk.left;
         const uint32_t turn = (before + n) / S::kStages, at = before + n - turn * S::kStages;     // this step's place in the ring
         if (KV && !w.active[t]) {                // the block's rows are given back all the same
           ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(full + 8 * at, turn & 1));
@@ -370,7 +395,7 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
           __syncwarp();
           if (leader) mbar_arrive(s_free + 8 * t);
         }
-        const float4* rows = reinterpret_cast<const float4*>(row_ring + at * S::kRowBytes);
+        const uint32_t rows = smem_u32(row_ring) + at * S::kRowBytes;
         int lo = 0, hi = kBlock;
         bool masked;
         if (KV) {
@@ -381,37 +406,50 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
           hi = edge - col0;
           masked = (p.causal ? min(w.kv_valid, tile0 + w.off + 1) : w.kv_valid) < col0 + kBlock;
         }
-        uint32_t pw[KV ? kBlock / 2 : 1], sw[kBlock / 2];
+        uint64_t nl = pair(lse2, lse2), nd = pair(delta, delta);
 #pragma unroll
-        for (int i = 0; i < kBlock; i += 2) {
-          if (i >= 32 && left <= 32) break;
-          float4 r = make_float4(lse2, delta, lse2, delta);
-          if (KV) r = rows[i >> 1];
-          float p0 = exp2_approx(fmaf(c, __uint_as_float(sv[i]), -r.x)), p1 = exp2_approx(fmaf(c, __uint_as_float(sv[i + 1]), -r.z));
-          float d0 = p0 * (__uint_as_float(dv[i]) - r.y), d1 = p1 * (__uint_as_float(dv[i + 1]) - r.w);
-          if (masked) {
-            const bool on0 = i >= lo && i < hi, on1 = i + 1 >= lo && i + 1 < hi;
-            p0 = on0 ? p0 : 0.0f;
-            d0 = on0 ? d0 : 0.0f;
-            p1 = on1 ? p1 : 0.0f;
-            d1 = on1 ? d1 : 0.0f;
+        for (int q = 0; q < 2; ++q) {
+          if (q == 1 && left <= 32) break;
+          uint32_t pw[16], sw[16];
+          const auto some = [&](auto masks) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+              uint64_t nl4[2] = {nl, nl}, nd4[2] = {nd, nd};
+              if (KV) {
+                load_pairs(rows + (q * 32 + i) * 4, nl4);
+                load_pairs(rows + (kBlock + q * 32 + i) * 4, nd4);
+              }
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const int e = q * 32 + i + 2 * k;
+                const uint64_t x = fma2(pair(sv[e], sv[e + 1]), c2, nl4[k]);
+                float2 f = !decltype(masks)::value && (i >> 2) < kByFma && k == 0 ? exp2_pair(x) : exp2_unit(x);
+                float2 g = unpair(mul2(pair(f.x, f.y), add2(pair(dv[e], dv[e + 1]), nd4[k])));
+                if (decltype(masks)::value) {
+                  const bool on0 = e >= lo && e < hi, on1 = e + 1 >= lo && e + 1 < hi;
+                  f.x = on0 ? f.x : 0.0f;
+                  g.x = on0 ? g.x : 0.0f;
+                  f.y = on1 ? f.y : 0.0f;
+                  g.y = on1 ? g.y : 0.0f;
+                }
+                if (KV) pw[(i >> 1) + k] = to_bf16x2(f.x, f.y);
+                sw[(i >> 1) + k] = to_bf16x2(g.x, g.y);
+              }
+            }
+          };
+          if (masked) some(Flag<true>());
+          else some(Flag<false>());
+          if (q == 0 && S::kOwn) {               // the sums before have read dS
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(acc_done + 8 * t, (seen & 1) ^ 1));
+            if (!ok) break;
           }
-          if (KV) pw[KV ? i >> 1 : 0] = to_bf16x2(p0, p1);
-          sw[i >> 1] = to_bf16x2(d0, d1);
+          if (KV) tmem_st16(mine_at + S::kS + 16 * q, pw);
+          tmem_st16(mine_at + S::kDs + 16 * q, sw);
         }
+        if (!ok) break;
         if (KV) {                                // (its rows have been read)
           __syncwarp();
           if (leader) mbar_arrive(empty + 8 * at);
-        }
-        if (S::kOwn) {                           // the sums before have read dS
-          ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(acc_done + 8 * t, (seen & 1) ^ 1));
-          if (!ok) break;
-        }
-        if (KV) tmem_st16(mine_at + S::kS, pw);
-        tmem_st16(mine_at + S::kDs, sw);
-        if (left > 32) {
-          if (KV) tmem_st16(mine_at + S::kS + 16, pw + (KV ? 16 : 0));
-          tmem_st16(mine_at + S::kDs + 16, sw + 16);
         }
         tmem_wait_st();
         tc_fence_before();
@@ -504,34 +542,44 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
   }
 }
 
-// lse2 and delta of every row; +infinity and 0 for rows that see nothing and for those that fill the last block up.
-// 16 lanes a row, 16 bytes each.
+// -lse2 and -delta of every row; -infinity and 0 for rows that see nothing and for those that fill the last block up.
+// LANES lanes a row, 16 bytes each; a CTA takes rows of one sequence, heads fastest: neighbours in memory where heads lie side by side.
+template <int LANES>
 __global__ void __launch_bounds__(256)
-attention_rows_kernel(const surgeon_heads o, const surgeon_heads dout, const float* lse, const int* q_lengths, int heads, int q_len, int q_pad,
-                      int head_dim, long long total, float2* rows) {
+attention_rows_kernel(const surgeon_heads o, const surgeon_heads dout, const float* lse, const int* q_lengths, int heads, FastDiv by_heads, int q_len,
+                      int q_pad, int head_dim, int ctas, float* rows) {
+  constexpr int kRows = 256 / LANES, kPasses = 4;
   pdl_trigger();
   pdl_wait();
-  const long long at = (static_cast<long long>(blockIdx.x) * 256 + threadIdx.x) >> 4;    // ((b * q_pad) + row) * heads + h: neighbours in memory
-  const int part = threadIdx.x & 15;
-  if (at >= total) return;                       // (sixteen lanes at a time)
-  const int h = static_cast<int>(at % heads);
-  const long long br = at / heads;
-  const int row = static_cast<int>(br % q_pad), b = static_cast<int>(br / q_pad);
-  const bool on = row < length_of(q_lengths, b, q_len);
-  float sum = 0.0f;
-  if (on && part * 8 < head_dim) {
-    float a[8], d[8];
-    load_elems<1, 8>(o.data, b * o.batch_stride + static_cast<long long>(row) * o.row_stride + h * o.head_stride + part * 8, a);
-    load_elems<1, 8>(dout.data, b * dout.batch_stride + static_cast<long long>(row) * dout.row_stride + h * dout.head_stride + part * 8, d);
+  const int b = static_cast<int>(blockIdx.x) / ctas, first = (static_cast<int>(blockIdx.x) - b * ctas) * kRows * kPasses;
+  const int part = threadIdx.x % LANES, q_valid = length_of(q_lengths, b, q_len);
+  const unsigned short* from_o = static_cast<const unsigned short*>(o.data) + b * o.batch_stride + part * 8;
+  const unsigned short* from_d = static_cast<const unsigned short*>(dout.data) + b * dout.batch_stride + part * 8;
+  float a[kPasses][8], d[kPasses][8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum = fmaf(a[i], d[i], sum);
+  for (int i = 0; i < kPasses; ++i) {
+    const int at = first + i * kRows + threadIdx.x / LANES, row = static_cast<int>(divide(at, by_heads)), h = at - row * heads;
+    if (row < q_valid && part * 8 < head_dim) {
+      load_elems<1, 8>(from_o, static_cast<long long>(row) * o.row_stride + h * o.head_stride, a[i]);
+      load_elems<1, 8>(from_d, static_cast<long long>(row) * dout.row_stride + h * dout.head_stride, d[i]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) a[i][k] = d[i][k] = 0.0f;
+    }
   }
-  const uint32_t mask = 0xFFFFu << (threadIdx.x & 16);
 #pragma unroll
-  for (int i = 8; i > 0; i >>= 1) sum += __shfl_xor_sync(mask, sum, i);
-  if (part == 0) {
-    const float l = on ? lse[(static_cast<long long>(b) * heads + h) * q_len + row] : -INFINITY;
-    rows[(static_cast<long long>(b) * heads + h) * q_pad + row] = l == -INFINITY ? make_float2(INFINITY, 0.0f) : make_float2(l * kLog2E, sum);
+  for (int i = 0; i < kPasses; ++i) {
+    const int at = first + i * kRows + threadIdx.x / LANES, row = static_cast<int>(divide(at, by_heads)), h = at - row * heads;
+    float sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum = fmaf(a[i][k], d[i][k], sum);
+    sum = lanes_sum<LANES>(sum);
+    if (part == 0 && row < q_pad) {
+      const float l = row < q_valid ? lse[(static_cast<long long>(b) * heads + h) * q_len + row] : -INFINITY;
+      float* to = rows + ((static_cast<long long>(b) * heads + h) * q_pad + (row & ~(kBlock - 1))) * 2 + (row & (kBlock - 1));
+      to[0] = l == -INFINITY ? -INFINITY : -l * kLog2E;
+      to[kBlock] = l == -INFINITY ? 0.0f : -sum;
+    }
   }
 }
 
@@ -572,7 +620,7 @@ int splits_of(const surgeon_attention_desc& d) {
 }
 int padded(int q_len) { return round_up(q_len, 128); }
 size_t rows_bytes(const surgeon_attention_desc& d) {
-  return (static_cast<size_t>(d.batch) * d.heads * padded(d.q_len) * sizeof(float2) + 255) & ~static_cast<size_t>(255);
+  return (static_cast<size_t>(d.batch) * d.heads * padded(d.q_len) * 2 * sizeof(float) + 255) & ~static_cast<size_t>(255);
 }
 size_t part_elems(const surgeon_attention_desc& d) { return static_cast<size_t>(d.batch) * d.kv_heads * d.kv_len * d.head_dim; }
 
@@ -586,6 +634,8 @@ cudaError_t launch_pass(const surgeon_attention_desc& d, const surgeon_heads& x,
   a.tiles = (stay + S::kTiles * kTile - 1) / (S::kTiles * kTile);
   if (!KV) a.splits = 1;
   a.items = a.tiles * d.batch * stay_heads * a.splits;
+  a.by_tiles = make_div(a.tiles); a.by_heads = make_div(stay_heads); a.by_pairs = make_div(d.batch * stay_heads);
+  a.by_group = make_div(a.group); a.by_splits = make_div(a.splits);
   CUtensorMap maps[6];
   memset(maps, 0, sizeof(maps));
   bool ok = encode(&maps[0], x, d.batch, stay, stay_heads, d.head_dim, kTile) && encode(&maps[1], y, d.batch, stay, stay_heads, d.head_dim, kTile) &&
@@ -636,12 +686,15 @@ cudaError_t launch_attention_grad(const surgeon_attention_desc& d, const surgeon
                                   const int* kv_lengths, const surgeon_heads* dq, const surgeon_heads* dk, const surgeon_heads* dv,
                                   void* workspace, cudaStream_t stream) {
   if (!dq && !dk) return cudaSuccess;
-  float2* rows = static_cast<float2*>(workspace);
+  float* rows = static_cast<float*>(workspace);
   const int q_pad = padded(d.q_len);
   if (d.q_len > 0) {
-    const long long total = static_cast<long long>(d.batch) * d.heads * q_pad;
-    const cudaError_t e = launch_kernel(attention_rows_kernel, dim3(static_cast<unsigned>((total + 15) / 16)), dim3(256), 0, stream, true, o, dout, lse,
-                                        q_lengths, d.heads, d.q_len, q_pad, d.head_dim, total, rows);
+    const bool narrow = d.head_dim <= 64;
+    const int rows_cta = (narrow ? 32 : 16) * 4;
+    const long long ctas = (static_cast<long long>(d.heads) * q_pad + rows_cta - 1) / rows_cta;
+    const cudaError_t e = launch_kernel(narrow ? attention_rows_kernel<8> : attention_rows_kernel<16>, dim3(static_cast<unsigned>(ctas * d.batch)), dim3(256), 0,
+                                        stream, true, o, dout, lse, q_lengths, d.heads, make_div(d.heads), d.q_len, q_pad, d.head_dim, static_cast<int>(ctas),
+                                        rows);
     note_launches(1);
     if (e != cudaSuccess) return e;
   }
