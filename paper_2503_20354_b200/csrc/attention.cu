@@ -37,7 +37,11 @@ template <int DP> struct Shape {                 // DP: head_dim, padded to 64 o
 struct Args {
   int batch, heads, group, q_len, kv_len, head_dim, causal;     // group: heads that share keys
   int tiles, items;                              // pairs of tiles of a head
-  FastDiv by_tiles, by_heads, by_pairs, by_group;
+  int pack, q_rows, item_heads;                  // pack: a tile holds q_rows rows of each head that shares keys, one head behind the other
+  int splits;                                    // parts of the keys that are summed by themselves
+  FastDiv by_tiles, by_heads, by_pairs, by_group, by_splits, by_rows;
+  float* partial;                                // [split][batch][heads][q_len][head_dim]: the parts' o, not divided by l
+  float2* marks;                                 // [split][batch][heads][q_len]: their m and l
   float scale;
   const int* q_lengths;
   const int* kv_lengths;
@@ -45,12 +49,21 @@ struct Args {
   float* lse;
 };
 
+// PARTS: heads may be packed and keys shared out (few queries); without, neither costs a register.
+template <bool PARTS>
 struct Item {
   int b, h, row0, q_valid, kv_valid, off;
-  int keys[2], blocks[2], most;                  // of each tile
+  int split, from;                               // of the keys' blocks this item's are from, ..., blocks - 1
+  int keys[2], blocks[2], most;                  // of each tile; h is a head of the keys where heads are packed
   __device__ __forceinline__ Item(const Args& p, int item) {
-    const int pairs = p.batch * p.heads;
+    const int heads = PARTS ? p.item_heads : p.heads, pairs = p.batch * heads;
     int bh, qt;
+    split = 0;
+    if (PARTS && p.splits > 1) {
+      const int whole = static_cast<int>(divide(item, p.by_splits));
+      split = item - whole * p.splits;
+      item = whole;
+    }
     if (p.causal) {                              // the longest first
       qt = static_cast<int>(divide(item, p.by_pairs));
       bh = item - qt * pairs;
@@ -60,7 +73,7 @@ struct Item {
       qt = item - bh * p.tiles;
     }
     b = static_cast<int>(divide(bh, p.by_heads));
-    h = bh - b * p.heads;
+    h = bh - b * heads;
     row0 = qt * 2 * kTile;
     q_valid = length_of(p.q_lengths, b, p.q_len);
     kv_valid = length_of(p.kv_lengths, b, p.kv_len);
@@ -72,6 +85,13 @@ struct Item {
       keys[t] = r0 >= q_valid ? 0 : p.causal ? max(0, min(kv_valid, last + off + 1)) : kv_valid;
       blocks[t] = (keys[t] + kBlock - 1) / kBlock;
       most = max(most, blocks[t]);
+    }
+    from = 0;
+    if (PARTS && p.splits > 1) {
+      from = static_cast<int>(static_cast<long long>(most) * split / p.splits);
+      most = static_cast<int>(static_cast<long long>(most) * (split + 1) / p.splits);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) blocks[t] = max(from, min(blocks[t], most));
     }
   }
 };
@@ -118,7 +138,7 @@ __device__ __noinline__ void scale_row(uint32_t o_at, float f) {
   }
 }
 
-template <int DP>
+template <int DP, bool PARTS>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                  const __grid_constant__ CUtensorMap o_map, const __grid_constant__ Args p) {
@@ -170,15 +190,21 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
     uint32_t phase = 1, fix_phase = 0;           // (a fresh barrier counts as passed in its phase before)
     bool ok = true;
     for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x, ++it) {
-      const Item w(p, item);
-      const int qs = S::kQStages == 2 ? it & 1 : 0, kv_head = static_cast<int>(divide(w.h, p.by_group));
+      const Item<PARTS> w(p, item);
+      const int qs = S::kQStages == 2 ? it & 1 : 0, kv_head = (PARTS && p.pack) ? w.h : static_cast<int>(divide(w.h, p.by_group));
       const uint32_t q_phase = (S::kQStages == 2 ? (it >> 1) & 1 : it & 1) ^ 1;
       for (int t = 0; t < 2 && ok; ++t) {
         const int at = 2 * qs + t;
         ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(q_empty + 8 * at, q_phase));
         if (!ok) break;
         if (leader) {
-          if (w.blocks[t]) {
+          if (w.blocks[t] > (PARTS ? w.from : 0) && (PARTS && p.pack)) {
+            mbar_arrive_expect_tx(q_full + 8 * at, p.group * p.q_rows * 128 * S::kSlabs);
+            for (int g = 0; g < p.group; ++g)
+              for (int c = 0; c < S::kSlabs; ++c)
+                tma_load_4d(smem_u32(smem) + at * S::kTileBytes + c * kTile * 128 + g * p.q_rows * 128, &q_map, c * kSlabCols, 0, w.h * p.group + g, w.b,
+                            q_full + 8 * at);
+          } else if (w.blocks[t] > (PARTS ? w.from : 0)) {
             mbar_arrive_expect_tx(q_full + 8 * at, S::kTileBytes);
             for (int c = 0; c < S::kSlabs; ++c)
               tma_load_4d(smem_u32(smem) + at * S::kTileBytes + c * kTile * 128, &q_map, c * kSlabCols, w.row0 + t * kTile, w.h, w.b, q_full + 8 * at);
@@ -210,7 +236,7 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
         }
         if (++s == S::kStages) { s = 0; phase ^= 1; }
       };
-      for (int j = 0; j < w.most; ++j) {
+      for (int j = (PARTS ? w.from : 0); j < w.most; ++j) {
         load(false, j);
         load(true, j);
       }
@@ -228,12 +254,12 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
       uint32_t first[2] = {0, 0};                // number of each tile's first block of the item; a block's place and phases go by its number
       bool ok = true;
       for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x, ++it) {
-        const Item w(p, item);
+        const Item<PARTS> w(p, item);
         const int qs = S::kQStages == 2 ? it & 1 : 0;
         const uint32_t q_phase = S::kQStages == 2 ? (it >> 1) & 1 : it & 1;
         for (int t = 0; t < 2 && ok; ++t) ok = mbar_wait_suspend(q_full + 8 * (2 * qs + t), q_phase);
         if (!ok) break;
-        if (!w.most) continue;
+        if (w.most <= (PARTS ? w.from : 0)) continue;
         const auto next = [&]() {
           const int st = s;
           if (++s == S::kStages) { s = 0; phase ^= 1; }
@@ -259,15 +285,15 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
           const uint32_t b = v_desc + st * (S::kBlockBytes >> 4);
 #pragma unroll
           for (int k = 0; k < kBlock / 16; ++k)
-            if (k < steps) umma_ts(tmem + S::kO + DP * t, tmem + S::kP + S::kPStep * t + 8 * k, b + 128 * k, idesc_o, j > 0 || k > 0);
+            if (k < steps) umma_ts(tmem + S::kO + DP * t, tmem + S::kP + S::kPStep * t + 8 * k, b + 128 * k, idesc_o, j > (PARTS ? w.from : 0) || k > 0);
           umma_commit(o_done + 8 * t);
           return true;
         };
         ok = mbar_wait_suspend(full + 8 * s, phase);
         int ks = next();                         // the place of the next block's keys
         for (int t = 0; t < 2 && ok; ++t)
-          if (w.blocks[t]) ok = scores(t, 0, ks, first[t]);
-        for (int j = 0; j < w.most && ok; ++j) {
+          if (w.blocks[t] > (PARTS ? w.from : 0)) ok = scores(t, (PARTS ? w.from : 0), ks, first[t]);
+        for (int j = (PARTS ? w.from : 0); j < w.most && ok; ++j) {
           umma_commit(empty + 8 * ks);
           const int v_at = s;
           const uint32_t v_phase = phase;
@@ -280,7 +306,7 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
           ok = ok && mbar_wait_suspend(full + 8 * v_at, v_phase);
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
-            const uint32_t n = first[t] + j;
+            const uint32_t n = first[t] + j - (PARTS ? w.from : 0);
             const bool ahead = j + 1 < w.blocks[t];
             if (S::kOwnP && ok && ahead) ok = scores(t, j + 1, ks, n + 1);
             if (ok && j < w.blocks[t]) ok = values(t, j, v_at, n);
@@ -288,8 +314,8 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
           }
           if (ok) umma_commit(empty + 8 * v_at);
         }
-        first[0] += w.blocks[0];
-        first[1] += w.blocks[1];
+        first[0] += w.blocks[0] - (PARTS ? w.from : 0);
+        first[1] += w.blocks[1] - (PARTS ? w.from : 0);
       }
     }
   }
@@ -313,19 +339,21 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
       __syncwarp();
       stored = -1;
     };
+    const int pack_head = (PARTS && p.pack) ? static_cast<int>(divide(row_in_tile, p.by_rows)) : 0;         // which of the heads in a packed tile
     for (int item = blockIdx.x; item < p.items; item += gridDim.x, ++it) {
-      int mine, all, keys, blocks;               // keys that this row sees; that every row of the tile sees; that any does
+      int mine, all, keys, from, blocks;         // keys that this row sees; that every row of the tile sees; that any does
       {
-        const Item w(p, item);
-        const int row = w.row0 + t * kTile + row_in_tile;
+        const Item<PARTS> w(p, item);
+        const int row = (PARTS && p.pack) ? row_in_tile - pack_head * p.q_rows : w.row0 + t * kTile + row_in_tile;
         mine = p.causal ? min(w.kv_valid, row + w.off + 1) : w.kv_valid;
-        all = p.causal ? min(w.kv_valid, row - row_in_tile + w.off + 1) : w.kv_valid;
+        all = p.causal ? min(w.kv_valid, w.row0 + t * kTile + w.off + 1) : w.kv_valid;
         keys = w.keys[t];
+        from = PARTS ? w.from : 0;
         blocks = w.blocks[t];
       }
       float m = -INFINITY, l = 0.0f;
       const int qs = S::kQStages == 2 ? it & 1 : 0;
-      for (int j = 0; j < blocks; ++j, ++seen) {
+      for (int j = from; j < blocks; ++j, ++seen) {
         ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(s_full + 8 * t, seen & 1));
         if (!ok) break;
         tc_fence_after();
@@ -345,14 +373,14 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
           for (int q = 0; q < 4; ++q) hide(v[q], limit - 32 * q);
         }
         float sum;
-        bool arrived = j == 0;                   // the block before has gone into o, and p may be written
-        for (bool fresh = j == 0;; fresh = true) {
+        bool arrived = j == from;                   // the block before has gone into o, and p may be written
+        for (bool fresh = j == from;; fresh = true) {
           if (fresh) {
             float to = m;
 #pragma unroll
             for (int q = 0; q < 4; ++q)
               if (cols > 32 * q) to = largest(v[q], to);
-            if (j > 0) {
+            if (j > from) {
               const float f = m == to ? 1.0f : exp2_approx(c * (m - to));
               l *= f;
               scale_row<DP>(o_at, f);
@@ -384,46 +412,87 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
         tc_fence_before();
         __syncwarp();
         if (leader) mbar_arrive(p_full + 8 * t);
-        if (j == 0) release();
+        if (j == from) release();
       }
-      const Item w(p, item);
-      const int row = w.row0 + t * kTile + row_in_tile;
-      if (ok && blocks) ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(o_done + 8 * t, (seen & 1) ^ 1));
+      const Item<PARTS> w(p, item);
+      const int row = (PARTS && p.pack) ? row_in_tile - pack_head * p.q_rows : w.row0 + t * kTile + row_in_tile, head = (PARTS && p.pack) ? w.h * p.group + pack_head : w.h;
+      const bool real = row < p.q_len && (!(PARTS && p.pack) || (t == 0 && pack_head < p.group)), any = blocks > from;
+      const long long at = (static_cast<long long>(w.b) * p.heads + head) * p.q_len + row;       // the row's number
+      if (ok && any) ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(o_done + 8 * t, (seen & 1) ^ 1));
       // the queries' place takes the outputs: they are not read any more
       if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(q_full + 8 * (2 * qs + t), S::kQStages == 2 ? (it >> 1) & 1 : it & 1));
       if (stored >= 0) release();
+      const long long all_rows = static_cast<long long>(p.batch) * p.heads * p.q_len;
+      unsigned short* const to = static_cast<unsigned short*>(p.o.data) + w.b * p.o.batch_stride + static_cast<long long>(row) * p.o.row_stride + head * p.o.head_stride;
       if (!ok) {                                 // a wait ran out: the rows are NaN, here and from here on
-        if (row < p.q_len) {
-          unsigned short* to = static_cast<unsigned short*>(p.o.data) + w.b * p.o.batch_stride + static_cast<long long>(row) * p.o.row_stride + w.h * p.o.head_stride;
-          for (int i = 0; i < p.head_dim; ++i) to[i] = 0x7FC0u;
-          if (p.lse) p.lse[(static_cast<long long>(w.b) * p.heads + w.h) * p.q_len + row] = __uint_as_float(0x7FC00000u);
+        if (real) {
+          if ((PARTS && p.splits > 1)) {
+            p.marks[w.split * all_rows + at] = make_float2(0.0f, __uint_as_float(0x7FC00000u));
+          } else {
+            for (int i = 0; i < p.head_dim; ++i) to[i] = 0x7FC0u;
+            if (p.lse) p.lse[at] = __uint_as_float(0x7FC00000u);
+          }
         }
         continue;
       }
       if (!(m < INFINITY)) l = __uint_as_float(0x7FC00000u);     // an infinity or a NaN among the scores
       const bool none = l == 0.0f || m == -INFINITY || row >= w.q_valid;
       const float inv = 1.0f / l;
-      if (blocks) tc_fence_after();
+      if (any) tc_fence_after();
+      if (PARTS) {                               // rows straight from the registers
+        if (real && (PARTS && p.splits > 1)) p.marks[w.split * all_rows + at] = none ? make_float2(-INFINITY, 0.0f) : make_float2(m, l);
+        if (real && p.splits == 1 && p.lse) p.lse[at] = none ? -INFINITY : fmaf(m, p.scale, logf(l));
+        float* const part = p.partial + (w.split * all_rows + at) * p.head_dim;
+#pragma unroll 1
+        for (int q = 0; q < DP / 32; ++q) {
+          uint32_t o[32];
+          if (any) {
+            tmem_ld32(o_at + 32 * q, o);
+            tmem_wait_ld32(o);
+          }
+          if (real) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if (32 * q + 8 * i >= p.head_dim) break;
+              if ((PARTS && p.splits > 1)) {
+                if (!none) {
+                  *reinterpret_cast<uint4*>(part + 32 * q + 8 * i) = make_uint4(o[8 * i], o[8 * i + 1], o[8 * i + 2], o[8 * i + 3]);
+                  *reinterpret_cast<uint4*>(part + 32 * q + 8 * i + 4) = make_uint4(o[8 * i + 4], o[8 * i + 5], o[8 * i + 6], o[8 * i + 7]);
+                }
+              } else {
+                uint4 u = make_uint4(0u, 0u, 0u, 0u);
+                const auto two = [&](int e) { return to_bf16x2(__uint_as_float(o[8 * i + e]) * inv, __uint_as_float(o[8 * i + e + 1]) * inv); };
+                if (!none) u = make_uint4(two(0), two(2), two(4), two(6));
+                *reinterpret_cast<uint4*>(to + 32 * q + 8 * i) = u;
+              }
+            }
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (leader) mbar_arrive(q_empty + 8 * (2 * qs + t));
+        __syncwarp();
+        continue;
+      }
       unsigned char* stage = smem + (2 * qs + t) * S::kTileBytes;
 #pragma unroll 1
       for (int q = 0; q < DP / 32; ++q) {
         uint32_t o[32];
-        if (blocks) {
+        if (any) {
           tmem_ld32(o_at + 32 * q, o);
           tmem_wait_ld32(o);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint4 u = make_uint4(0u, 0u, 0u, 0u);
-          if (blocks && !none) {
+          if (any && !none) {
             const auto two = [&](int e) { return to_bf16x2(__uint_as_float(o[8 * i + e]) * inv, __uint_as_float(o[8 * i + e + 1]) * inv); };
             u = make_uint4(two(0), two(2), two(4), two(6));
           }
           *reinterpret_cast<uint4*>(stage + (q >> 1) * kTile * 128 + tile_off(row_in_tile, (q & 1) * 4 + i)) = u;
         }
       }
-      if (p.lse && row < p.q_len)
-        p.lse[(static_cast<long long>(w.b) * p.heads + w.h) * p.q_len + row] = none ? -INFINITY : fmaf(m, p.scale, logf(l));
+      if (p.lse && real) p.lse[at] = none ? -INFINITY : fmaf(m, p.scale, logf(l));
       tc_fence_before();
       fence_proxy_async();
       __syncwarp();
@@ -448,14 +517,68 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
   }
 }
 
+// The parts' sums of a row, in their order: a warp a row.
+__global__ void __launch_bounds__(256)
+attention_join_parts_kernel(const float* partial, const float2* marks, const surgeon_heads o, float* lse, int splits, int heads, int q_len, int head_dim,
+                            float scale, int rows) {
+  pdl_trigger();
+  pdl_wait();
+  const int at = blockIdx.x * 8 + (threadIdx.x >> 5), d = static_cast<int>(lane_id()) * 4;
+  if (at >= rows) return;
+  float m = -INFINITY, l = 0.0f;
+  for (int s = 0; s < splits; ++s) m = fmaxf(m, marks[static_cast<long long>(s) * rows + at].x);
+  float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s) {
+    const long long r = static_cast<long long>(s) * rows + at;
+    const float2 k = marks[r];
+    if (k.x == -INFINITY) continue;              // (it sees none of this part's keys: nothing was written)
+    const float f = exp2_approx(scale * kLog2E * (k.x - m));
+    l = fmaf(k.y, f, l);
+    if (d < head_dim) {
+      const float4 v = *reinterpret_cast<const float4*>(partial + r * head_dim + d);
+      sum.x = fmaf(v.x, f, sum.x); sum.y = fmaf(v.y, f, sum.y); sum.z = fmaf(v.z, f, sum.z); sum.w = fmaf(v.w, f, sum.w);
+    }
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const int row = at % q_len, bh = at / q_len;
+  if (d < head_dim) {
+    unsigned short* to = static_cast<unsigned short*>(o.data) + bh / heads * o.batch_stride + row * o.row_stride + bh % heads * o.head_stride + d;
+    *reinterpret_cast<uint2*>(to) = l == 0.0f ? make_uint2(0u, 0u) : make_uint2(to_bf16x2(sum.x * inv, sum.y * inv), to_bf16x2(sum.z * inv, sum.w * inv));
+  }
+  if (d == 0 && lse) lse[at] = l == 0.0f ? -INFINITY : fmaf(m, scale, logf(l));
+}
+
+// How a call is cut.  Heads that share keys go into one tile where they fit (few queries): the keys are then read once for all of them.
+// Where that leaves SMs without an item, the keys are shared out in parts of two blocks at least, whose sums are joined by a kernel of its own.
+struct Plan {
+  int pack, q_rows, tiles, splits;
+};
+Plan plan_of(const surgeon_attention_desc& d) {
+  Plan p = {};
+  const int group = d.heads / d.kv_heads;
+  p.q_rows = round_up(d.q_len, 8);               // (whole groups of eight rows, as the operand's layout has them)
+  p.pack = group > 1 && static_cast<long long>(group) * p.q_rows <= kTile;
+  p.tiles = (d.q_len + 2 * kTile - 1) / (2 * kTile);
+  const long long items = static_cast<long long>(p.tiles) * d.batch * (p.pack ? d.kv_heads : d.heads);
+  const int blocks = (d.kv_len + kBlock - 1) / kBlock;
+  p.splits = items > 0 ? static_cast<int>(148 / items) : 1;
+  if (p.splits > blocks / 2) p.splits = blocks / 2;
+  if (p.splits < 1) p.splits = 1;
+  return p;
+}
+size_t marks_bytes(const surgeon_attention_desc& d, int splits) {
+  return (static_cast<size_t>(splits) * d.batch * d.heads * d.q_len * sizeof(float2) + 255) & ~static_cast<size_t>(255);
+}
+
 template <int DP>
 cudaError_t launch_as(const surgeon_attention_desc& d, const surgeon_heads& q, const surgeon_heads& k, const surgeon_heads& v, const surgeon_heads& o,
                       Args& a, cudaStream_t stream) {
   CUtensorMap maps[4];
-  if (!encode(&maps[0], q, d.batch, d.q_len, d.heads, d.head_dim, kTile) || !encode(&maps[1], k, d.batch, d.kv_len, d.kv_heads, d.head_dim, kBlock) ||
+  if (!encode(&maps[0], q, d.batch, d.q_len, d.heads, d.head_dim, a.pack ? a.q_rows : kTile) || !encode(&maps[1], k, d.batch, d.kv_len, d.kv_heads, d.head_dim, kBlock) ||
       !encode(&maps[2], v, d.batch, d.kv_len, d.kv_heads, d.head_dim, kBlock) || !encode(&maps[3], o, d.batch, d.q_len, d.heads, d.head_dim, 32))
     return cudaErrorInvalidValue;
-  const auto kernel = attention_kernel<DP>;
+  const auto kernel = a.pack || a.splits > 1 ? attention_kernel<DP, true> : attention_kernel<DP, false>;
   const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), Shape<DP>::kSmem);
   if (e != cudaSuccess) return e;
   const int grid = a.items < sm_count() ? a.items : sm_count();
@@ -466,21 +589,35 @@ cudaError_t launch_as(const surgeon_attention_desc& d, const surgeon_heads& q, c
 
 }  // namespace
 
-size_t attention_workspace(const surgeon_attention_desc&) { return 0; }
+size_t attention_workspace(const surgeon_attention_desc& d) {
+  const int splits = plan_of(d).splits;
+  return splits > 1 ? marks_bytes(d, splits) + static_cast<size_t>(splits) * d.batch * d.heads * d.q_len * d.head_dim * sizeof(float) : 0;
+}
 
 cudaError_t launch_attention(const surgeon_attention_desc& d, const surgeon_heads& q, const surgeon_heads& k, const surgeon_heads& v,
-                             const int* q_lengths, const int* kv_lengths, const surgeon_heads& o, float* lse, void*, cudaStream_t stream) {
+                             const int* q_lengths, const int* kv_lengths, const surgeon_heads& o, float* lse, void* workspace, cudaStream_t stream) {
+  const Plan plan = plan_of(d);
   Args a = {};
   a.batch = d.batch; a.heads = d.heads; a.group = d.heads / d.kv_heads;
   a.q_len = d.q_len; a.kv_len = d.kv_len; a.head_dim = d.head_dim; a.causal = d.causal != 0;
-  a.tiles = (d.q_len + 2 * kTile - 1) / (2 * kTile);
-  a.items = a.tiles * d.batch * d.heads;
-  a.by_tiles = make_div(a.tiles); a.by_heads = make_div(d.heads); a.by_pairs = make_div(d.batch * d.heads); a.by_group = make_div(a.group);
+  a.pack = plan.pack; a.q_rows = plan.q_rows; a.tiles = plan.tiles; a.splits = plan.splits;
+  a.item_heads = plan.pack ? d.kv_heads : d.heads;
+  a.items = a.tiles * d.batch * a.item_heads * a.splits;
+  a.by_tiles = make_div(a.tiles); a.by_heads = make_div(a.item_heads); a.by_pairs = make_div(d.batch * a.item_heads); a.by_group = make_div(a.group);
+  a.by_splits = make_div(a.splits); a.by_rows = make_div(a.q_rows);
   a.scale = static_cast<float>(d.scale);
   a.q_lengths = q_lengths; a.kv_lengths = kv_lengths;
   a.o = o;
   a.lse = lse;
-  return d.head_dim <= 64 ? launch_as<64>(d, q, k, v, o, a, stream) : launch_as<128>(d, q, k, v, o, a, stream);
+  a.marks = static_cast<float2*>(workspace);
+  a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + marks_bytes(d, plan.splits));
+  cudaError_t e = d.head_dim <= 64 ? launch_as<64>(d, q, k, v, o, a, stream) : launch_as<128>(d, q, k, v, o, a, stream);
+  if (e != cudaSuccess || a.splits == 1) return e;
+  const int rows = d.batch * d.heads * d.q_len;
+  e = launch_kernel(attention_join_parts_kernel, dim3((rows + 7) / 8), dim3(256), 0, stream, true, static_cast<const float*>(a.partial),
+                    static_cast<const float2*>(a.marks), o, lse, a.splits, d.heads, d.q_len, d.head_dim, a.scale, rows);
+  note_launches(1);
+  return e;
 }
 
 }  // namespace surgeon
