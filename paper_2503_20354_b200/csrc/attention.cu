@@ -38,7 +38,7 @@ struct Args {
   int batch, heads, group, q_len, kv_len, head_dim, causal;     // group: heads that share keys
   int tiles, items;                              // pairs of tiles of a head
   int pack, q_rows, item_heads;                  // pack: a tile holds q_rows rows of each head that shares keys, one head behind the other
-  int splits;                                    // parts of the keys that are summed by themselves
+  int splits, twin;                              // parts of the keys that are summed by themselves; twin: each by two tiles, which take the blocks in turn
   FastDiv by_tiles, by_heads, by_pairs, by_group, by_splits, by_rows;
   float* partial;                                // [split][batch][heads][q_len][head_dim]: the parts' o, not divided by l
   float2* marks;                                 // [split][batch][heads][q_len]: their m and l
@@ -81,7 +81,7 @@ struct Item {
     most = 0;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const int r0 = row0 + t * kTile, last = min(r0 + kTile, q_valid) - 1;
+      const int r0 = row0 + (PARTS && p.twin ? 0 : t * kTile), last = min(r0 + kTile, q_valid) - 1;
       keys[t] = r0 >= q_valid ? 0 : p.causal ? max(0, min(kv_valid, last + off + 1)) : kv_valid;
       blocks[t] = (keys[t] + kBlock - 1) / kBlock;
       most = max(most, blocks[t]);
@@ -198,13 +198,15 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
         ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(q_empty + 8 * at, q_phase));
         if (!ok) break;
         if (leader) {
-          if (w.blocks[t] > (PARTS ? w.from : 0) && (PARTS && p.pack)) {
+          if (PARTS && p.twin && t == 1) {       // (the first tile's queries serve both)
+            mbar_arrive(q_full + 8 * at);
+          } else if (w.blocks[t] > w.from && (PARTS && p.pack)) {
             mbar_arrive_expect_tx(q_full + 8 * at, p.group * p.q_rows * 128 * S::kSlabs);
             for (int g = 0; g < p.group; ++g)
               for (int c = 0; c < S::kSlabs; ++c)
                 tma_load_4d(smem_u32(smem) + at * S::kTileBytes + c * kTile * 128 + g * p.q_rows * 128, &q_map, c * kSlabCols, 0, w.h * p.group + g, w.b,
                             q_full + 8 * at);
-          } else if (w.blocks[t] > (PARTS ? w.from : 0)) {
+          } else if (w.blocks[t] > w.from) {
             mbar_arrive_expect_tx(q_full + 8 * at, S::kTileBytes);
             for (int c = 0; c < S::kSlabs; ++c)
               tma_load_4d(smem_u32(smem) + at * S::kTileBytes + c * kTile * 128, &q_map, c * kSlabCols, w.row0 + t * kTile, w.h, w.b, q_full + 8 * at);
@@ -236,7 +238,7 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
         }
         if (++s == S::kStages) { s = 0; phase ^= 1; }
       };
-      for (int j = (PARTS ? w.from : 0); j < w.most; ++j) {
+      for (int j = w.from; j < w.most; ++j) {
         load(false, j);
         load(true, j);
       }
@@ -259,7 +261,7 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
         const uint32_t q_phase = S::kQStages == 2 ? (it >> 1) & 1 : it & 1;
         for (int t = 0; t < 2 && ok; ++t) ok = mbar_wait_suspend(q_full + 8 * (2 * qs + t), q_phase);
         if (!ok) break;
-        if (w.most <= (PARTS ? w.from : 0)) continue;
+        if (w.most <= w.from) continue;
         const auto next = [&]() {
           const int st = s;
           if (++s == S::kStages) { s = 0; phase ^= 1; }
@@ -271,7 +273,7 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
           if (!mbar_wait_suspend((S::kOwnP ? s_free : o_done) + 8 * t, (n & 1) ^ 1)) return false;
           tc_fence_after();
           const uint32_t idesc = make_idesc(kTile, round_up(min(kBlock, w.keys[t] - j * kBlock), 16));
-          const uint32_t a = q_desc + (2 * qs + t) * (S::kTileBytes >> 4), b = k_desc + st * (S::kBlockBytes >> 4);
+          const uint32_t a = q_desc + (2 * qs + (PARTS && p.twin ? 0 : t)) * (S::kTileBytes >> 4), b = k_desc + st * (S::kBlockBytes >> 4);
 #pragma unroll
           for (int k = 0; k < DP / 16; ++k)
             if (k < k_steps) umma_ss(tmem + 128 * t, a + (k >> 2) * (kTile * 128 >> 4) + (k & 3) * 2, b + (k >> 2) * (kBlock * 128 >> 4) + (k & 3) * 2, idesc, k > 0);
@@ -285,15 +287,40 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
           const uint32_t b = v_desc + st * (S::kBlockBytes >> 4);
 #pragma unroll
           for (int k = 0; k < kBlock / 16; ++k)
-            if (k < steps) umma_ts(tmem + S::kO + DP * t, tmem + S::kP + S::kPStep * t + 8 * k, b + 128 * k, idesc_o, j > (PARTS ? w.from : 0) || k > 0);
+            if (k < steps) umma_ts(tmem + S::kO + DP * t, tmem + S::kP + S::kPStep * t + 8 * k, b + 128 * k, idesc_o, j > w.from + (PARTS && p.twin ? t : 0) || k > 0);
           umma_commit(o_done + 8 * t);
           return true;
         };
+        if (PARTS && p.twin) {
+          // one tile's block after the other's; k of block j is the 2 (j - from)-th tile of the ring from here, v the one behind it
+          const uint32_t base = s + (phase ? S::kStages : 0);
+          const auto there = [&](uint32_t at) { return mbar_wait_suspend(full + 8 * (at % S::kStages), (at / S::kStages) & 1); };
+          const auto turn = [&](int j) {
+            const uint32_t at = base + 2 * (j - w.from), st = at % S::kStages;
+            if (!there(at) || !scores((j - w.from) & 1, j, st, first[(j - w.from) & 1] + ((j - w.from) >> 1))) return false;
+            umma_commit(empty + 8 * st);
+            return true;
+          };
+          for (int j = w.from; j < w.from + 2 && j < w.most && ok; ++j) ok = turn(j);
+          for (int j = w.from; j < w.most && ok; ++j) {
+            const uint32_t at = base + 2 * (j - w.from) + 1, st = at % S::kStages;
+            ok = there(at) && values((j - w.from) & 1, j, st, first[(j - w.from) & 1] + ((j - w.from) >> 1));
+            if (!ok) break;
+            umma_commit(empty + 8 * st);
+            if (j + 2 < w.most) ok = turn(j + 2);
+          }
+          const uint32_t end = base + 2 * (w.most - w.from);
+          s = end % S::kStages;
+          phase = (end / S::kStages) & 1;
+          first[0] += (w.most - w.from + 1) >> 1;
+          first[1] += (w.most - w.from) >> 1;
+          continue;
+        }
         ok = mbar_wait_suspend(full + 8 * s, phase);
         int ks = next();                         // the place of the next block's keys
         for (int t = 0; t < 2 && ok; ++t)
-          if (w.blocks[t] > (PARTS ? w.from : 0)) ok = scores(t, (PARTS ? w.from : 0), ks, first[t]);
-        for (int j = (PARTS ? w.from : 0); j < w.most && ok; ++j) {
+          if (w.blocks[t] > w.from) ok = scores(t, w.from, ks, first[t]);
+        for (int j = w.from; j < w.most && ok; ++j) {
           umma_commit(empty + 8 * ks);
           const int v_at = s;
           const uint32_t v_phase = phase;
@@ -306,7 +333,7 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
           ok = ok && mbar_wait_suspend(full + 8 * v_at, v_phase);
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
-            const uint32_t n = first[t] + j - (PARTS ? w.from : 0);
+            const uint32_t n = first[t] + j - w.from;
             const bool ahead = j + 1 < w.blocks[t];
             if (S::kOwnP && ok && ahead) ok = scores(t, j + 1, ks, n + 1);
             if (ok && j < w.blocks[t]) ok = values(t, j, v_at, n);
@@ -314,8 +341,8 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
           }
           if (ok) umma_commit(empty + 8 * v_at);
         }
-        first[0] += w.blocks[0] - (PARTS ? w.from : 0);
-        first[1] += w.blocks[1] - (PARTS ? w.from : 0);
+        first[0] += w.blocks[0] - w.from;
+        first[1] += w.blocks[1] - w.from;
       }
     }
   }
@@ -339,21 +366,23 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
       __syncwarp();
       stored = -1;
     };
+    const int tile_row = PARTS && p.twin ? 0 : t * kTile;
     const int pack_head = (PARTS && p.pack) ? static_cast<int>(divide(row_in_tile, p.by_rows)) : 0;         // which of the heads in a packed tile
     for (int item = blockIdx.x; item < p.items; item += gridDim.x, ++it) {
       int mine, all, keys, from, blocks;         // keys that this row sees; that every row of the tile sees; that any does
       {
         const Item<PARTS> w(p, item);
-        const int row = (PARTS && p.pack) ? row_in_tile - pack_head * p.q_rows : w.row0 + t * kTile + row_in_tile;
+        const int row = (PARTS && p.pack) ? row_in_tile - pack_head * p.q_rows : w.row0 + tile_row + row_in_tile;
         mine = p.causal ? min(w.kv_valid, row + w.off + 1) : w.kv_valid;
-        all = p.causal ? min(w.kv_valid, w.row0 + t * kTile + w.off + 1) : w.kv_valid;
+        all = p.causal ? min(w.kv_valid, w.row0 + tile_row + w.off + 1) : w.kv_valid;
         keys = w.keys[t];
-        from = PARTS ? w.from : 0;
+        from = PARTS && p.twin ? w.from + t : w.from;
         blocks = w.blocks[t];
       }
       float m = -INFINITY, l = 0.0f;
       const int qs = S::kQStages == 2 ? it & 1 : 0;
-      for (int j = from; j < blocks; ++j, ++seen) {
+      const int step = PARTS && p.twin ? 2 : 1;
+      for (int j = from; j < blocks; j += step, ++seen) {
         ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(s_full + 8 * t, seen & 1));
         if (!ok) break;
         tc_fence_after();
@@ -415,8 +444,10 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
         if (j == from) release();
       }
       const Item<PARTS> w(p, item);
-      const int row = (PARTS && p.pack) ? row_in_tile - pack_head * p.q_rows : w.row0 + t * kTile + row_in_tile, head = (PARTS && p.pack) ? w.h * p.group + pack_head : w.h;
-      const bool real = row < p.q_len && (!(PARTS && p.pack) || (t == 0 && pack_head < p.group)), any = blocks > from;
+      const int row = (PARTS && p.pack) ? row_in_tile - pack_head * p.q_rows : w.row0 + tile_row + row_in_tile, head = (PARTS && p.pack) ? w.h * p.group + pack_head : w.h;
+      const bool real = row < p.q_len && (!PARTS || ((!p.pack || pack_head < p.group) && (!p.pack || p.twin || t == 0))), any = blocks > from;
+      const bool parts = PARTS && (p.splits > 1 || p.twin);
+      const long long part = PARTS ? (p.twin ? 2 * w.split + t : w.split) : 0;
       const long long at = (static_cast<long long>(w.b) * p.heads + head) * p.q_len + row;       // the row's number
       if (ok && any) ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(o_done + 8 * t, (seen & 1) ^ 1));
       // the queries' place takes the outputs: they are not read any more
@@ -426,8 +457,8 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
       unsigned short* const to = static_cast<unsigned short*>(p.o.data) + w.b * p.o.batch_stride + static_cast<long long>(row) * p.o.row_stride + head * p.o.head_stride;
       if (!ok) {                                 // a wait ran out: the rows are NaN, here and from here on
         if (real) {
-          if ((PARTS && p.splits > 1)) {
-            p.marks[w.split * all_rows + at] = make_float2(0.0f, __uint_as_float(0x7FC00000u));
+          if (PARTS && parts) {
+            p.marks[part * all_rows + at] = make_float2(0.0f, __uint_as_float(0x7FC00000u));
           } else {
             for (int i = 0; i < p.head_dim; ++i) to[i] = 0x7FC0u;
             if (p.lse) p.lse[at] = __uint_as_float(0x7FC00000u);
@@ -440,9 +471,9 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
       const float inv = 1.0f / l;
       if (any) tc_fence_after();
       if (PARTS) {                               // rows straight from the registers
-        if (real && (PARTS && p.splits > 1)) p.marks[w.split * all_rows + at] = none ? make_float2(-INFINITY, 0.0f) : make_float2(m, l);
-        if (real && p.splits == 1 && p.lse) p.lse[at] = none ? -INFINITY : fmaf(m, p.scale, logf(l));
-        float* const part = p.partial + (w.split * all_rows + at) * p.head_dim;
+        if (real && parts) p.marks[part * all_rows + at] = none ? make_float2(-INFINITY, 0.0f) : make_float2(m, l);
+        if (real && !parts && p.lse) p.lse[at] = none ? -INFINITY : fmaf(m, p.scale, logf(l));
+        float* const sums_to = p.partial + (part * all_rows + at) * p.head_dim;
 #pragma unroll 1
         for (int q = 0; q < DP / 32; ++q) {
           uint32_t o[32];
@@ -454,10 +485,10 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               if (32 * q + 8 * i >= p.head_dim) break;
-              if ((PARTS && p.splits > 1)) {
+              if (PARTS && parts) {
                 if (!none) {
-                  *reinterpret_cast<uint4*>(part + 32 * q + 8 * i) = make_uint4(o[8 * i], o[8 * i + 1], o[8 * i + 2], o[8 * i + 3]);
-                  *reinterpret_cast<uint4*>(part + 32 * q + 8 * i + 4) = make_uint4(o[8 * i + 4], o[8 * i + 5], o[8 * i + 6], o[8 * i + 7]);
+                  *reinterpret_cast<uint4*>(sums_to + 32 * q + 8 * i) = make_uint4(o[8 * i], o[8 * i + 1], o[8 * i + 2], o[8 * i + 3]);
+                  *reinterpret_cast<uint4*>(sums_to + 32 * q + 8 * i + 4) = make_uint4(o[8 * i + 4], o[8 * i + 5], o[8 * i + 6], o[8 * i + 7]);
                 }
               } else {
                 uint4 u = make_uint4(0u, 0u, 0u, 0u);
@@ -551,8 +582,10 @@ attention_join_parts_kernel(const float* partial, const float2* marks, const sur
 
 // How a call is cut.  Heads that share keys go into one tile where they fit (few queries): the keys are then read once for all of them.
 // Where that leaves SMs without an item, the keys are shared out in parts of two blocks at least, whose sums are joined by a kernel of its own.
+// A single tile of queries is taken by both halves of the warps, each with every other block of the keys, as two parts more: a half
+// alone would wait for its products and they for it.
 struct Plan {
-  int pack, q_rows, tiles, splits;
+  int pack, q_rows, tiles, splits, twin, parts;
 };
 Plan plan_of(const surgeon_attention_desc& d) {
   Plan p = {};
@@ -562,13 +595,15 @@ Plan plan_of(const surgeon_attention_desc& d) {
   p.tiles = (d.q_len + 2 * kTile - 1) / (2 * kTile);
   const long long items = static_cast<long long>(p.tiles) * d.batch * (p.pack ? d.kv_heads : d.heads);
   const int blocks = (d.kv_len + kBlock - 1) / kBlock;
+  p.twin = (p.pack || d.q_len <= kTile) && blocks >= 4;
   p.splits = items > 0 ? static_cast<int>(148 / items) : 1;
-  if (p.splits > blocks / 2) p.splits = blocks / 2;
+  if (p.splits > blocks / (p.twin ? 4 : 2)) p.splits = blocks / (p.twin ? 4 : 2);
   if (p.splits < 1) p.splits = 1;
+  p.parts = p.twin ? 2 * p.splits : p.splits;
   return p;
 }
-size_t marks_bytes(const surgeon_attention_desc& d, int splits) {
-  return (static_cast<size_t>(splits) * d.batch * d.heads * d.q_len * sizeof(float2) + 255) & ~static_cast<size_t>(255);
+size_t marks_bytes(const surgeon_attention_desc& d, int parts) {
+  return (static_cast<size_t>(parts) * d.batch * d.heads * d.q_len * sizeof(float2) + 255) & ~static_cast<size_t>(255);
 }
 
 template <int DP>
@@ -578,7 +613,7 @@ cudaError_t launch_as(const surgeon_attention_desc& d, const surgeon_heads& q, c
   if (!encode(&maps[0], q, d.batch, d.q_len, d.heads, d.head_dim, a.pack ? a.q_rows : kTile) || !encode(&maps[1], k, d.batch, d.kv_len, d.kv_heads, d.head_dim, kBlock) ||
       !encode(&maps[2], v, d.batch, d.kv_len, d.kv_heads, d.head_dim, kBlock) || !encode(&maps[3], o, d.batch, d.q_len, d.heads, d.head_dim, 32))
     return cudaErrorInvalidValue;
-  const auto kernel = a.pack || a.splits > 1 ? attention_kernel<DP, true> : attention_kernel<DP, false>;
+  const auto kernel = a.pack || a.splits > 1 || a.twin ? attention_kernel<DP, true> : attention_kernel<DP, false>;
   const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), Shape<DP>::kSmem);
   if (e != cudaSuccess) return e;
   const int grid = a.items < sm_count() ? a.items : sm_count();
@@ -590,8 +625,8 @@ cudaError_t launch_as(const surgeon_attention_desc& d, const surgeon_heads& q, c
 }  // namespace
 
 size_t attention_workspace(const surgeon_attention_desc& d) {
-  const int splits = plan_of(d).splits;
-  return splits > 1 ? marks_bytes(d, splits) + static_cast<size_t>(splits) * d.batch * d.heads * d.q_len * d.head_dim * sizeof(float) : 0;
+  const int parts = plan_of(d).parts;
+  return parts > 1 ? marks_bytes(d, parts) + static_cast<size_t>(parts) * d.batch * d.heads * d.q_len * d.head_dim * sizeof(float) : 0;
 }
 
 cudaError_t launch_attention(const surgeon_attention_desc& d, const surgeon_heads& q, const surgeon_heads& k, const surgeon_heads& v,
@@ -600,7 +635,7 @@ cudaError_t launch_attention(const surgeon_attention_desc& d, const surgeon_head
   Args a = {};
   a.batch = d.batch; a.heads = d.heads; a.group = d.heads / d.kv_heads;
   a.q_len = d.q_len; a.kv_len = d.kv_len; a.head_dim = d.head_dim; a.causal = d.causal != 0;
-  a.pack = plan.pack; a.q_rows = plan.q_rows; a.tiles = plan.tiles; a.splits = plan.splits;
+  a.pack = plan.pack; a.q_rows = plan.q_rows; a.tiles = plan.tiles; a.splits = plan.splits; a.twin = plan.twin;
   a.item_heads = plan.pack ? d.kv_heads : d.heads;
   a.items = a.tiles * d.batch * a.item_heads * a.splits;
   a.by_tiles = make_div(a.tiles); a.by_heads = make_div(a.item_heads); a.by_pairs = make_div(d.batch * a.item_heads); a.by_group = make_div(a.group);
@@ -610,12 +645,12 @@ cudaError_t launch_attention(const surgeon_attention_desc& d, const surgeon_head
   a.o = o;
   a.lse = lse;
   a.marks = static_cast<float2*>(workspace);
-  a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + marks_bytes(d, plan.splits));
+  a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + marks_bytes(d, plan.parts));
   cudaError_t e = d.head_dim <= 64 ? launch_as<64>(d, q, k, v, o, a, stream) : launch_as<128>(d, q, k, v, o, a, stream);
-  if (e != cudaSuccess || a.splits == 1) return e;
+  if (e != cudaSuccess || plan.parts == 1) return e;
   const int rows = d.batch * d.heads * d.q_len;
   e = launch_kernel(attention_join_parts_kernel, dim3((rows + 7) / 8), dim3(256), 0, stream, true, static_cast<const float*>(a.partial),
-                    static_cast<const float2*>(a.marks), o, lse, a.splits, d.heads, d.q_len, d.head_dim, a.scale, rows);
+                    static_cast<const float2*>(a.marks), o, lse, plan.parts, d.heads, d.q_len, d.head_dim, a.scale, rows);
   note_launches(1);
   return e;
 }
