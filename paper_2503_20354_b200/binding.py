@@ -79,7 +79,9 @@ def _bind_calls(l):
     except ImportError:
         return
     module.bind(*(C.cast(f, C.c_void_p).value for f in (l.surgeon_layer_norm, l.surgeon_layer_norm_grad, l.surgeon_linear,
-                                                        l.surgeon_linear_grad, l.surgeon_gradient_norm, l.surgeon_clip_gradients)))
+                                                        l.surgeon_linear_grad, l.surgeon_gradient_norm, l.surgeon_clip_gradients,
+                                                        l.surgeon_attention, l.surgeon_attention_grad, l.surgeon_group_norm,
+                                                        l.surgeon_group_norm_grad, l.surgeon_dropout)))
     _calls = module
 
 
@@ -803,6 +805,12 @@ def surgeon_attention(desc: AttentionDesc, q: torch.Tensor, k: torch.Tensor, v: 
     ``k`` and ``v`` [batch, kv_len, kv_heads, dim]: bf16, any strides (multiples of 8 elements) but a dense last dimension, so that
     slices of a linear layer's output go as they are.  ``q_lengths``, ``kv_lengths``: int32 [batch], the rows of each sequence of
     a padded batch.  ``lse``: an fp32 tensor [batch, heads, q_len] that receives what ``surgeon_attention_grad`` needs."""
+    if _calls is not None and stream is None and out is not None and workspace is not None:
+        st = _calls.attention(desc, q, k, v, q_lengths, kv_lengths, out, lse, workspace)
+        if st is not None:
+            if st != SURGEON_OK:
+                _check(st, "surgeon_attention")
+            return out
     dev, (qs, ks) = torch._C._cuda_getDevice(), _attention_shapes(desc)
     if out is None:
         out = _new(qs, torch.bfloat16, q.device, stream)
@@ -828,6 +836,12 @@ def surgeon_attention_grad(desc: AttentionDesc, q: torch.Tensor, k: torch.Tensor
                            want_dq: bool = True, want_dkv: bool = True):
     """Backward pass of ``surgeon_attention``; returns ``(dq, dk, dv)``, bf16, made here (contiguous) where None, None where not wanted.
     ``out`` and ``lse`` are the forward call's, ``dout`` is the gradient of ``out``; each gradient has strides of its own."""
+    if _calls is not None and stream is None and dq is not None and dk is not None and dv is not None and workspace is not None and want_dq and want_dkv:
+        st = _calls.attention_grad(desc, q, k, v, out, dout, lse, q_lengths, kv_lengths, dq, dk, dv, workspace)
+        if st is not None:
+            if st != SURGEON_OK:
+                _check(st, "surgeon_attention_grad")
+            return dq, dk, dv
     dev, (qs, ks) = torch._C._cuda_getDevice(), _attention_shapes(desc)
     if (dq is not None and not want_dq) or ((dk is not None or dv is not None) and not want_dkv):
         raise ValueError("a gradient given, but not wanted")
@@ -872,6 +886,12 @@ def surgeon_group_norm(x: torch.Tensor, groups: int, gamma: Optional[torch.Tenso
     """Group norm with an activation of ``x`` [batch, ..., channels] (channels last; fp32 or bf16); returns ``out``, which may be ``x``.
     ``gamma``, ``beta``: fp32.  ``stats``: an fp32 tensor [2, batch, groups] that receives the means and the reciprocal standard
     deviations for ``surgeon_group_norm_grad``."""
+    if _calls is not None and stream is None and out is not None and workspace is not None:
+        st = _calls.group_norm(x, groups, gamma, beta, eps, act, out, stats, workspace)
+        if st is not None:
+            if st != SURGEON_OK:
+                _check(st, "surgeon_group_norm")
+            return out
     shape, batch, positions, channels = _positions(x, "x")
     dev, dt, f32, vector = torch._C._cuda_getDevice(), x.dtype, torch.float32, (channels,)
     code = dtype_code(dt)
@@ -899,6 +919,12 @@ def surgeon_group_norm_grad(x: torch.Tensor, dy: torch.Tensor, groups: int, gamm
                             want_dx: bool = True) -> Optional[torch.Tensor]:
     """Backward pass of ``surgeon_group_norm``; returns ``dx`` (of dy's type, made here if None; None with ``want_dx=False``), which may
     be ``dy``.  ``dgamma``, ``dbeta``: fp32, written (``accumulate=True``: added to) where given."""
+    if _calls is not None and stream is None and dx is not None and workspace is not None and want_dx:
+        st = _calls.group_norm_grad(x, dy, groups, gamma, beta, stats, act, dx, dgamma, dbeta, accumulate, workspace)
+        if st is not None:
+            if st != SURGEON_OK:
+                _check(st, "surgeon_group_norm_grad")
+            return dx
     shape, batch, positions, channels = _positions(x, "x")
     dev, f32, vector, gt = torch._C._cuda_getDevice(), torch.float32, (channels,), dy.dtype
     if not want_dx:
@@ -925,6 +951,12 @@ def surgeon_dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, resid
     ``residual``; returns ``out``, which may be ``x`` or ``residual``.  The mask is a function of ``seed``, ``offset`` (64 bits each) and the
     element's index; the backward pass is the same call on dy.  ``device_offset``: an int64 tensor of one element that is added to
     ``offset`` when the kernel runs, for captured calls."""
+    if _calls is not None and stream is None and out is not None:
+        st = _calls.dropout(x, p, seed, offset, residual, out, device_offset)
+        if st is not None:
+            if st != SURGEON_OK:
+                _check(st, "surgeon_dropout")
+            return out
     shape, dt, dev = x.shape, x.dtype, torch._C._cuda_getDevice()
     code, low = dtype_code(dt), (1 << 64) - 1
     if out is None:

@@ -19,6 +19,50 @@ namespace {
 constexpr int kActSilu = 3;
 constexpr int kMaxThreads = 256;                 // vectors of channels a CTA takes at once
 constexpr int kUnroll = 4;                       // rows on their way
+constexpr int kGradUnroll = 4;
+constexpr int kResident = 3, kGradResident = 2;  // CTAs of an SM in the first and the last step
+
+// A vector as it lies in memory: E elements of type DT, 16 bytes of the narrower type of a call.
+template <int DT, int E> struct Raw {
+  uint4 v[E == 1 ? 1 : E * (DT ? 2 : 4) / 16];
+  __device__ __forceinline__ void load(const void* __restrict__ base, long long at) {
+    if constexpr (E == 1) {
+      v[0].x = DT ? static_cast<const unsigned short*>(base)[at] : static_cast<const uint32_t*>(base)[at];
+    } else {
+      const uint4* from = reinterpret_cast<const uint4*>(static_cast<const char*>(base) + at * (DT ? 2 : 4));
+#pragma unroll
+      for (int i = 0; i < static_cast<int>(sizeof(v) / 16); ++i) v[i] = from[i];
+    }
+  }
+  __device__ __forceinline__ void numbers(float (&f)[E]) const {
+    if constexpr (E == 1) {
+      f[0] = __uint_as_float(DT ? v[0].x << 16 : v[0].x);
+    } else {
+      constexpr int kPer = DT ? 8 : 4;
+#pragma unroll
+      for (int i = 0; i < E / kPer; ++i) {
+        float g[kPer];
+        vector_elems<DT>(v[i], g);
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) f[i * kPer + k] = g[k];
+      }
+    }
+  }
+};
+// Outputs are written past what the caches hold: the next reader of x and dy shares L2 with them.
+template <int DT, int E>
+__device__ __forceinline__ void store_stream(void* __restrict__ base, long long at, const float (&f)[E]) {
+  if constexpr (E == 1) {
+    store_elems<DT, 1>(base, at, f);
+  } else if constexpr (DT == 0) {
+#pragma unroll
+    for (int i = 0; i < E / 4; ++i)
+      __stcs(reinterpret_cast<float4*>(static_cast<float*>(base) + at) + i, make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]));
+  } else {
+    __stcs(reinterpret_cast<uint4*>(static_cast<unsigned short*>(base) + at),
+           make_uint4(to_bf16x2(f[0], f[1]), to_bf16x2(f[2], f[3]), to_bf16x2(f[4], f[5]), to_bf16x2(f[6], f[7])));
+  }
+}
 
 template <int ACT>
 __device__ __forceinline__ float gn_activate(float z) {
@@ -50,26 +94,55 @@ struct Geometry {
   long long image;                               // elements of an image
 };
 
-// xh and z of one element, a rounding per operation
-__device__ __forceinline__ float normal(float x, float mean, float r) { return __fmul_rn(__fsub_rn(x, mean), r); }
-__device__ __forceinline__ float affine(float xh, float gamma, float beta) { return __fadd_rn(__fmul_rn(xh, gamma), beta); }
+// Numbers of a vector in pairs (a vector of one: a pair whose second is 0).
+template <int E> constexpr int kPairs = E == 1 ? 1 : E / 2;
+template <int E>
+__device__ __forceinline__ void to_pairs(const float (&f)[E], uint64_t (&v)[kPairs<E>]) {
+#pragma unroll
+  for (int i = 0; i < kPairs<E>; ++i) v[i] = pair(f[2 * i], E == 1 ? 0.0f : f[E == 1 ? 0 : 2 * i + 1]);
+}
+template <int E>
+__device__ __forceinline__ void from_pairs(const uint64_t (&v)[kPairs<E>], float (&f)[E]) {
+#pragma unroll
+  for (int i = 0; i < kPairs<E>; ++i) {
+    const float2 g = unpair(v[i]);
+    f[2 * i] = g.x;
+    if (E > 1) f[E == 1 ? 0 : 2 * i + 1] = g.y;
+  }
+}
 
+// What a thread keeps of its vector's channels.
 template <int E>
 struct Params {
-  float mean[E], r[E], gamma[E], beta[E];
-};
-// The parameters of channels c, ..., c + E - 1 of image b.
-template <int E>
-__device__ __forceinline__ void load_params(Params<E>& p, const Geometry& g, int b, int c, const float* stats, int images, const float* gamma,
-                                            const float* beta) {
+  uint64_t minus_mean[kPairs<E>], r[kPairs<E>], gamma[kPairs<E>], beta[kPairs<E>];
+  // The parameters of channels c, ..., c + E - 1 of image b.
+  __device__ __forceinline__ Params(const Geometry& g, int b, int c, const float* stats, int images, const float* gammas, const float* betas) {
+    float m[E], s[E], w[E], o[E];
 #pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const int at = b * g.groups + (c + i) / g.per_group;
-    p.mean[i] = stats[at];
-    p.r[i] = stats[images * g.groups + at];
-    p.gamma[i] = gamma ? gamma[c + i] : 1.0f;
-    p.beta[i] = beta ? beta[c + i] : 0.0f;
+    for (int i = 0; i < E; ++i) {
+      const int at = b * g.groups + (c + i) / g.per_group;
+      m[i] = -stats[at];
+      s[i] = stats[images * g.groups + at];
+      w[i] = gammas ? gammas[c + i] : 1.0f;
+      o[i] = betas ? betas[c + i] : 0.0f;
+    }
+    to_pairs<E>(m, minus_mean);
+    to_pairs<E>(s, r);
+    to_pairs<E>(w, gamma);
+    to_pairs<E>(o, beta);
   }
+  // xh and z of the i-th pair, a rounding per operation
+  __device__ __forceinline__ uint64_t normal(int i, uint64_t x) const { return mul2(add2(x, minus_mean[i]), r[i]); }
+  __device__ __forceinline__ uint64_t affine(int i, uint64_t xh) const { return add2(mul2(xh, gamma[i]), beta[i]); }
+};
+
+// dy act'(z) of a pair
+template <int ACT>
+__device__ __forceinline__ uint64_t through(uint64_t z, uint64_t dy) {
+  if constexpr (ACT == kActNone) return dy;
+  const float2 a = unpair(z), d = unpair(dy);
+  if constexpr (ACT == kActRelu) return pair(a.x > 0.0f ? d.x : 0.0f, a.y > 0.0f ? d.y : 0.0f);
+  return mul2(dy, pair(gn_slope<ACT>(a.x), gn_slope<ACT>(a.y)));
 }
 
 // Rows of a chunk that lane `lane` takes: lane, lane + lanes, ...
@@ -100,7 +173,7 @@ struct Place {
 // A thread sums x - s and (x - s)^2, s its first number of the channel.  What the difference of the n squares and their mean's loses is
 // below n roundings of the result, wherever s lies.
 template <int DT, int E>
-__global__ void __launch_bounds__(kMaxThreads)
+__global__ void __launch_bounds__(kMaxThreads, kResident)
 group_sums_kernel(const void* x, float2* partial, const Geometry g) {
   extern __shared__ float2 s_pairs[];            // [lanes - 1][E][cols]
   pdl_trigger();
@@ -123,11 +196,15 @@ group_sums_kernel(const void* x, float2* partial, const Geometry g) {
     long long at = p.at;
     int t = 0;
     for (; t + kUnroll <= p.mine; t += kUnroll, at += kUnroll * p.step) {
-      float f[kUnroll][E];
+      Raw<DT, E> raw[kUnroll];
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) load_elems<DT, E>(x, at + u * p.step, f[u]);
+      for (int u = 0; u < kUnroll; ++u) raw[u].load(x, at + u * p.step);
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) add(f[u]);
+      for (int u = 0; u < kUnroll; ++u) {
+        float f[E];
+        raw[u].numbers(f);
+        add(f);
+      }
     }
     for (; t < p.mine; ++t, at += p.step) {
       float f[E];
@@ -170,6 +247,8 @@ group_sums_kernel(const void* x, float2* partial, const Geometry g) {
   }
 }
 
+constexpr int kTermThreads = 1024;              // at most
+
 // Sum of a double over a CTA's threads in a fixed order, in every thread.
 __device__ __forceinline__ double cta_sum(double v, double* buf) {
   v = lanes_sum<32>(v);
@@ -177,27 +256,30 @@ __device__ __forceinline__ double cta_sum(double v, double* buf) {
   if (lane_id() == 0) buf[threadIdx.x >> 5] = v;
   __syncthreads();
   double t = 0.0;
+#pragma unroll 8
   for (int i = 0; i < static_cast<int>(blockDim.x >> 5); ++i) t += buf[i];
   return t;
 }
 
 // ---- step 2, forward: a group's mean and r from the chunks', in double ----
-__global__ void __launch_bounds__(256)
-group_stats_kernel(const float2* partial, float* stats, int images, float eps, const Geometry g) {
-  __shared__ double buf[8];
+// `width` threads side by side on channels, the others' rows of them on the chunks.
+__global__ void __launch_bounds__(kTermThreads)
+group_stats_kernel(const float2* partial, float* stats, int images, float eps, int width, const Geometry g) {
+  __shared__ double buf[kTermThreads / 32];
   pdl_trigger();
   pdl_wait();
   const int b = blockIdx.x / g.groups, group = blockIdx.x % g.groups;
+  const int col = threadIdx.x % width, row = threadIdx.x / width, rows = static_cast<int>(blockDim.x) / width;
   double s = 0.0, q = 0.0;
-  const long long total = static_cast<long long>(g.chunks) * g.per_group;
   const float2* from = partial + static_cast<long long>(b) * g.chunks * g.channels + group * g.per_group;
-  for (long long i = threadIdx.x; i < total; i += blockDim.x) {
-    const int chunk = static_cast<int>(i / g.per_group), c = static_cast<int>(i % g.per_group);
-    const float2 v = from[static_cast<long long>(chunk) * g.channels + c];
-    const double n = min(g.chunk, g.positions - chunk * g.chunk), m = v.x;
-    s += n * m;
-    q += v.y + n * m * m;
-  }
+  for (int c = col; c < g.per_group; c += width)
+#pragma unroll 4
+    for (int i = row; i < g.chunks; i += rows) {
+      const float2 v = from[static_cast<long long>(i) * g.channels + c];
+      const double n = min(g.chunk, g.positions - i * g.chunk), m = v.x;
+      s += n * m;
+      q += v.y + n * m * m;
+    }
   s = cta_sum(s, buf);
   q = cta_sum(q, buf);
   if (threadIdx.x == 0) {
@@ -211,27 +293,35 @@ group_stats_kernel(const float2* partial, float* stats, int images, float eps, c
 
 // ---- step 3, forward ----
 template <int DT, int E, int ACT>
-__global__ void __launch_bounds__(kMaxThreads)
+__global__ void __launch_bounds__(kMaxThreads, kResident)
 group_apply_kernel(const void* x, void* y, const float* stats, int images, const float* gamma, const float* beta, const Geometry g) {
   pdl_trigger();
   pdl_wait();
   const Place<E> p(g, gridDim.x - 1 - blockIdx.x);
   if (p.mine == 0) return;
-  Params<E> k;
-  load_params<E>(k, g, p.b, p.v * E, stats, images, gamma, beta);
+  const Params<E> k(g, p.b, p.v * E, stats, images, gamma, beta);
   const auto finish = [&](long long at, float (&f)[E]) {
+    uint64_t v[kPairs<E>];
+    to_pairs<E>(f, v);
 #pragma unroll
-    for (int i = 0; i < E; ++i) f[i] = gn_activate<ACT>(affine(normal(f[i], k.mean[i], k.r[i]), k.gamma[i], k.beta[i]));
-    store_elems<DT, E>(y, at, f);
+    for (int i = 0; i < kPairs<E>; ++i) v[i] = k.affine(i, k.normal(i, v[i]));
+    from_pairs<E>(v, f);
+#pragma unroll
+    for (int i = 0; i < E; ++i) f[i] = gn_activate<ACT>(f[i]);
+    store_stream<DT, E>(y, at, f);
   };
   long long at = p.at;
   int t = 0;
   for (; t + kUnroll <= p.mine; t += kUnroll, at += kUnroll * p.step) {
-    float f[kUnroll][E];
+    Raw<DT, E> raw[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) load_elems<DT, E>(x, at + u * p.step, f[u]);
+    for (int u = 0; u < kUnroll; ++u) raw[u].load(x, at + u * p.step);
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) finish(at + u * p.step, f[u]);
+    for (int u = 0; u < kUnroll; ++u) {
+      float f[E];
+      raw[u].numbers(f);
+      finish(at + u * p.step, f);
+    }
   }
   for (; t < p.mine; ++t, at += p.step) {
     float f[E];
@@ -242,7 +332,7 @@ group_apply_kernel(const void* x, void* y, const float* stats, int images, const
 
 // ---- step 1, backward: A and B of every channel of a chunk ----
 template <int DT, int GDT, int E, int ACT>
-__global__ void __launch_bounds__(kMaxThreads)
+__global__ void __launch_bounds__(kMaxThreads, kGradResident)
 group_grad_sums_kernel(const void* x, const void* dy, float2* partial, const float* stats, int images, const float* gamma, const float* beta,
                        const Geometry g) {
   extern __shared__ float2 s_pairs[];
@@ -253,35 +343,48 @@ group_grad_sums_kernel(const void* x, const void* dy, float2* partial, const flo
 #pragma unroll
   for (int i = 0; i < E; ++i) sum[i] = make_float2(0.0f, 0.0f);
   if (p.mine > 0) {
-    Params<E> k;
-    load_params<E>(k, g, p.b, p.v * E, stats, images, gamma, beta);
+    const Params<E> k(g, p.b, p.v * E, stats, images, gamma, beta);
+    uint64_t a[kPairs<E>] = {}, b[kPairs<E>] = {};
     const auto add = [&](const float (&f)[E], const float (&d)[E]) {
+      uint64_t fx[kPairs<E>], fd[kPairs<E>];
+      to_pairs<E>(f, fx);
+      to_pairs<E>(d, fd);
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        const float xh = normal(f[i], k.mean[i], k.r[i]);
-        const float dz = ACT == kActNone ? d[i] : d[i] * gn_slope<ACT>(affine(xh, k.gamma[i], k.beta[i]));
-        sum[i].x += dz;
-        sum[i].y = fmaf(dz, xh, sum[i].y);
+      for (int i = 0; i < kPairs<E>; ++i) {
+        const uint64_t xh = k.normal(i, fx[i]), dz = through<ACT>(k.affine(i, xh), fd[i]);
+        a[i] = add2(a[i], dz);
+        b[i] = fma2(dz, xh, b[i]);
       }
     };
     long long at = p.at;
     int t = 0;
-    for (; t + 2 <= p.mine; t += 2, at += 2 * p.step) {
-      float f[2][E], d[2][E];
+    for (; t + kGradUnroll <= p.mine; t += kGradUnroll, at += kGradUnroll * p.step) {
+      Raw<DT, E> rx[kGradUnroll];
+      Raw<GDT, E> rd[kGradUnroll];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        load_elems<DT, E>(x, at + u * p.step, f[u]);
-        load_elems<GDT, E>(dy, at + u * p.step, d[u]);
+      for (int u = 0; u < kGradUnroll; ++u) {
+        rx[u].load(x, at + u * p.step);
+        rd[u].load(dy, at + u * p.step);
       }
 #pragma unroll
-      for (int u = 0; u < 2; ++u) add(f[u], d[u]);
+      for (int u = 0; u < kGradUnroll; ++u) {
+        float f[E], d[E];
+        rx[u].numbers(f);
+        rd[u].numbers(d);
+        add(f, d);
+      }
     }
-    if (t < p.mine) {
+    for (; t < p.mine; ++t, at += p.step) {
       float f[E], d[E];
       load_elems<DT, E>(x, at, f);
       load_elems<GDT, E>(dy, at, d);
       add(f, d);
     }
+    float fa[E], fb[E];
+    from_pairs<E>(a, fa);
+    from_pairs<E>(b, fb);
+#pragma unroll
+    for (int i = 0; i < E; ++i) sum[i] = make_float2(fa[i], fb[i]);
   }
   if (g.lanes > 1) {
     if (p.on && p.lane > 0)
@@ -305,20 +408,20 @@ group_grad_sums_kernel(const void* x, const void* dy, float2* partial, const flo
 }
 
 // ---- step 2, backward: A and B of every channel of an image, c1 and c2 of every group ----
-// `width` threads side by side on channels, 256 / width on the chunks.
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kTermThreads)
 group_grad_terms_kernel(const float2* partial, double2* sums, float2* terms, const float* gamma, int width, const Geometry g) {
-  __shared__ double2 buf[256];
-  __shared__ double total[8];
+  __shared__ double2 buf[kTermThreads];
+  __shared__ double total[kTermThreads / 32];
   pdl_trigger();
   pdl_wait();
   const int b = blockIdx.x / g.groups, group = blockIdx.x % g.groups;
-  const int col = threadIdx.x % width, row = threadIdx.x / width, rows = 256 / width;
+  const int col = threadIdx.x % width, row = threadIdx.x / width, rows = static_cast<int>(blockDim.x) / width;
   double c1 = 0.0, c2 = 0.0;
   for (int c0 = 0; c0 < g.per_group; c0 += width) {
     const int c = c0 + col, channel = group * g.per_group + c;
     double2 s = make_double2(0.0, 0.0);
     if (c < g.per_group)
+#pragma unroll 4
       for (int i = row; i < g.chunks; i += rows) {
         const float2 v = partial[(static_cast<long long>(b) * g.chunks + i) * g.channels + channel];
         s.x += v.x;
@@ -327,11 +430,15 @@ group_grad_terms_kernel(const float2* partial, double2* sums, float2* terms, con
     __syncthreads();
     buf[threadIdx.x] = s;
     __syncthreads();
-    if (row == 0 && c < g.per_group) {
-      for (int i = 1; i < rows; ++i) {
-        s.x += buf[i * width + col].x;
-        s.y += buf[i * width + col].y;
+    for (int half = rows / 2; half > 0; half /= 2) {             // (rows is a power of two)
+      if (row < half) {
+        buf[threadIdx.x].x += buf[threadIdx.x + half * width].x;
+        buf[threadIdx.x].y += buf[threadIdx.x + half * width].y;
       }
+      __syncthreads();
+    }
+    if (row == 0 && c < g.per_group) {
+      s = buf[threadIdx.x];
       sums[static_cast<long long>(b) * g.channels + channel] = s;
       const double w = gamma ? gamma[channel] : 1.0;
       c1 += w * s.x;
@@ -353,7 +460,7 @@ struct Columns {
 };
 
 template <int DT, int GDT, int E, int ACT>
-__global__ void __launch_bounds__(kMaxThreads)
+__global__ void __launch_bounds__(kMaxThreads, kGradResident)
 group_grad_apply_kernel(const void* x, const void* dy, void* dx, const float* stats, const float2* terms, int images, const float* gamma,
                         const float* beta, const Columns cols, int items, const Geometry g) {
   pdl_trigger();
@@ -374,37 +481,57 @@ group_grad_apply_kernel(const void* x, const void* dy, void* dx, const float* st
   if (static_cast<int>(blockIdx.x) >= items) return;
   const Place<E> p(g, items - 1 - blockIdx.x);
   if (p.mine == 0) return;
-  Params<E> k;
-  load_params<E>(k, g, p.b, p.v * E, stats, images, gamma, beta);
-  float c1[E], c2[E];
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const float2 v = terms[p.b * g.groups + (p.v * E + i) / g.per_group];
-    c1[i] = v.x;
-    c2[i] = v.y;
-  }
-  const auto finish = [&](long long at, const float (&f)[E], float (&d)[E]) {
+  const Params<E> k(g, p.b, p.v * E, stats, images, gamma, beta);
+  // dx = dz (r gamma) - r c1 - xh (r c2)
+  uint64_t scale[kPairs<E>], c1[kPairs<E>], c2[kPairs<E>];
+  {
+    float f1[E], f2[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      const float xh = normal(f[i], k.mean[i], k.r[i]);
-      const float dz = ACT == kActNone ? d[i] : d[i] * gn_slope<ACT>(affine(xh, k.gamma[i], k.beta[i]));
-      d[i] = k.r[i] * (__fmul_rn(dz, k.gamma[i]) - c1[i] - xh * c2[i]);
+      const float2 v = terms[p.b * g.groups + (p.v * E + i) / g.per_group];
+      f1[i] = -v.x;
+      f2[i] = -v.y;
     }
-    store_elems<GDT, E>(dx, at, d);
+    to_pairs<E>(f1, c1);
+    to_pairs<E>(f2, c2);
+#pragma unroll
+    for (int i = 0; i < kPairs<E>; ++i) {
+      scale[i] = mul2(k.r[i], k.gamma[i]);
+      c1[i] = mul2(k.r[i], c1[i]);
+      c2[i] = mul2(k.r[i], c2[i]);
+    }
+  }
+  const auto finish = [&](long long at, const float (&f)[E], float (&d)[E]) {
+    uint64_t fx[kPairs<E>], fd[kPairs<E>];
+    to_pairs<E>(f, fx);
+    to_pairs<E>(d, fd);
+#pragma unroll
+    for (int i = 0; i < kPairs<E>; ++i) {
+      const uint64_t xh = k.normal(i, fx[i]);
+      fd[i] = fma2(through<ACT>(ACT == kActNone ? 0 : k.affine(i, xh), fd[i]), scale[i], fma2(xh, c2[i], c1[i]));
+    }
+    from_pairs<E>(fd, d);
+    store_stream<GDT, E>(dx, at, d);
   };
   long long at = p.at;
   int t = 0;
-  for (; t + 2 <= p.mine; t += 2, at += 2 * p.step) {
-    float f[2][E], d[2][E];
+  for (; t + kGradUnroll <= p.mine; t += kGradUnroll, at += kGradUnroll * p.step) {
+    Raw<DT, E> rx[kGradUnroll];
+    Raw<GDT, E> rd[kGradUnroll];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      load_elems<DT, E>(x, at + u * p.step, f[u]);
-      load_elems<GDT, E>(dy, at + u * p.step, d[u]);
+    for (int u = 0; u < kGradUnroll; ++u) {
+      rx[u].load(x, at + u * p.step);
+      rd[u].load(dy, at + u * p.step);
     }
 #pragma unroll
-    for (int u = 0; u < 2; ++u) finish(at + u * p.step, f[u], d[u]);
+    for (int u = 0; u < kGradUnroll; ++u) {
+      float f[E], d[E];
+      rx[u].numbers(f);
+      rd[u].numbers(d);
+      finish(at + u * p.step, f, d);
+    }
   }
-  if (t < p.mine) {
+  for (; t < p.mine; ++t, at += p.step) {
     float f[E], d[E];
     load_elems<DT, E>(x, at, f);
     load_elems<GDT, E>(dy, at, d);
@@ -413,9 +540,8 @@ group_grad_apply_kernel(const void* x, const void* dy, void* dx, const float* st
 }
 
 // ---- host ----
-constexpr int kPartials = 148 * 6;               // CTAs of the first step, about: enough for two or three on every SM to take turns
-
-Geometry geometry(long long batch, long long positions, int channels, int groups, int vec) {
+constexpr int kRounds = 4;
+Geometry geometry(long long batch, long long positions, int channels, int groups, int vec, bool grad) {
   Geometry g = {};
   g.positions = static_cast<int>(positions);
   g.channels = channels;
@@ -427,15 +553,33 @@ Geometry geometry(long long batch, long long positions, int channels, int groups
   g.lanes = kMaxThreads / g.cols;
   if (g.lanes > positions) g.lanes = static_cast<int>(positions > 0 ? positions : 1);
   g.image = positions * channels;
-  const long long items = batch * blocks;
-  long long chunks = items > 0 ? (kPartials + items - 1) / items : 1;
-  const long long most = (positions + 2 * g.lanes - 1) / (2 * g.lanes);      // two rows a thread at least
-  if (chunks > most) chunks = most;
-  if (chunks < 1) chunks = 1;
-  g.chunk = static_cast<int>((positions + chunks - 1) / chunks);
-  g.chunk = (g.chunk + g.lanes - 1) / g.lanes * g.lanes;
+  // One to four rounds of CTAs, the number that takes the least: a round is as long as a chunk and the start of a CTA (some eight rows a thread).
+  const long long items = batch * blocks, at_once = 148LL * (grad ? kGradResident : kResident), steps = (positions + g.lanes - 1) / g.lanes;
+  long long best = -1;
+  g.chunk = g.lanes;
+  for (int rounds = 1; rounds <= kRounds && items > 0; ++rounds) {
+    long long n = rounds * at_once / items;
+    n = n < 1 ? 1 : n > steps ? steps : n;
+    const long long rows = (steps + n - 1) / n, cost = (n * items + at_once - 1) / at_once * (rows + 8);
+    if (best < 0 || cost < best) {
+      best = cost;
+      g.chunk = static_cast<int>(rows * g.lanes);
+    }
+  }
   g.chunks = static_cast<int>((positions + g.chunk - 1) / g.chunk);
+  if (g.chunks < 1) g.chunks = 1;
   return g;
+}
+int width_of(const Geometry& g) {                 // threads side by side on a group's channels: a power of two
+  int width = 1;
+  while (width < g.per_group && width < 32) width *= 2;
+  return width;
+}
+// Threads of a group's CTA in the second step: about four chunks a thread.
+int term_threads(const Geometry& g) {
+  int n = 64;
+  while (n < kTermThreads && n * 4 < g.chunks * width_of(g)) n *= 2;
+  return n;
 }
 int vector_of(int channels, int dt, int grad_dt) {               // elements of a thread's vector: 16 bytes of the narrower type
   const int e = dt || grad_dt ? 8 : 4;
@@ -452,13 +596,10 @@ struct Scratch {
 };
 size_t up(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 Scratch scratch_of(long long batch, long long positions, int channels, int groups, bool grad) {
-  // (the most of either width of vectors)
-  long long chunks = 0;
-  for (int e : {1, 4, 8})
-    if (channels % e == 0) {
-      const Geometry g = geometry(batch, positions, channels, groups, e);
-      if (g.chunks > chunks) chunks = g.chunks;
-    }
+  // (the most that geometry() takes, whatever the width of vectors)
+  long long chunks = batch > 0 ? kRounds * 148LL * kResident / batch : 1;
+  if (chunks > positions) chunks = positions;
+  if (chunks < 1) chunks = 1;
   Scratch s = {};
   s.second = up(static_cast<size_t>(batch) * chunks * channels * 8);
   s.terms = s.second + (grad ? up(static_cast<size_t>(batch) * channels * 16) : up(static_cast<size_t>(batch) * groups * 8));
@@ -479,7 +620,7 @@ cudaError_t launch_group_norm(const void* x, long long batch, long long position
                               const float* beta, float eps, int act, void* y, float* stats, void* workspace, cudaStream_t stream) {
   if (batch == 0 || positions == 0) return cudaSuccess;
   const int e = vector_of(channels, dt, dt), images = static_cast<int>(batch);
-  const Geometry g = geometry(batch, positions, channels, groups, e);
+  const Geometry g = geometry(batch, positions, channels, groups, e, false);
   const Scratch s = scratch_of(batch, positions, channels, groups, false);
   char* ws = static_cast<char*>(workspace);
   float2* partial = reinterpret_cast<float2*>(ws);
@@ -488,8 +629,8 @@ cudaError_t launch_group_norm(const void* x, long long batch, long long position
   const auto sums = dt ? (e == 8 ? group_sums_kernel<1, 8> : group_sums_kernel<1, 1>) : (e == 4 ? group_sums_kernel<0, 4> : group_sums_kernel<0, 1>);
   cudaError_t st = launch_kernel(sums, grid_of(g, batch), block_of(g), smem, stream, true, x, partial, g);
   if (st != cudaSuccess) return st;
-  st = launch_kernel(group_stats_kernel, dim3(static_cast<unsigned>(batch * groups)), dim3(256), 0, stream, true,
-                     static_cast<const float2*>(partial), stats, images, eps, g);
+  st = launch_kernel(group_stats_kernel, dim3(static_cast<unsigned>(batch * groups)), dim3(term_threads(g)), 0, stream, true,
+                     static_cast<const float2*>(partial), stats, images, eps, width_of(g), g);
   if (st != cudaSuccess) return st;
 #define SURGEON_APPLY(ACT)                                                                      \
   (dt ? (e == 8 ? group_apply_kernel<1, 8, ACT> : group_apply_kernel<1, 1, ACT>)                \
@@ -515,10 +656,8 @@ cudaError_t launch_grad(const void* x, const void* dy, long long batch, const Ge
   cudaError_t st = launch_kernel(group_grad_sums_kernel<DT, GDT, E, ACT>, grid_of(g, batch), block_of(g), smem, stream, true, x, dy, partial,
                                  stats, images, gamma, beta, g);
   if (st != cudaSuccess) return st;
-  int width = 1;
-  while (width < g.per_group && width < 32) width *= 2;
-  st = launch_kernel(group_grad_terms_kernel, dim3(static_cast<unsigned>(batch * g.groups)), dim3(256), 0, stream, true,
-                     static_cast<const float2*>(partial), sums, terms, gamma, width, g);
+  st = launch_kernel(group_grad_terms_kernel, dim3(static_cast<unsigned>(batch * g.groups)), dim3(term_threads(g)), 0, stream, true,
+                     static_cast<const float2*>(partial), sums, terms, gamma, width_of(g), g);
   if (st != cudaSuccess) return st;
   dim3 grid = grid_of(g, batch);
   const int items = dx ? static_cast<int>(grid.x) : 0;
@@ -559,7 +698,7 @@ cudaError_t launch_group_norm_grad(const void* x, const void* dy, long long batc
     return cudaGetLastError();
   }
   const int e = vector_of(channels, dt, grad_dt);
-  const Geometry g = geometry(batch, positions, channels, groups, e);
+  const Geometry g = geometry(batch, positions, channels, groups, e, true);
   const Scratch s = scratch_of(batch, positions, channels, groups, true);
   const Columns cols = {nullptr, dgamma, dbeta, accumulate, static_cast<int>(batch)};
   char* ws = static_cast<char*>(workspace);

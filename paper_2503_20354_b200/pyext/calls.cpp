@@ -22,6 +22,11 @@ decltype(&surgeon_linear) linear_fn = nullptr;
 decltype(&surgeon_linear_grad) linear_grad_fn = nullptr;
 decltype(&surgeon_gradient_norm) gradient_norm_fn = nullptr;
 decltype(&surgeon_clip_gradients) clip_gradients_fn = nullptr;
+decltype(&surgeon_attention) attention_fn = nullptr;
+decltype(&surgeon_attention_grad) attention_grad_fn = nullptr;
+decltype(&surgeon_group_norm) group_norm_fn = nullptr;
+decltype(&surgeon_group_norm_grad) group_norm_grad_fn = nullptr;
+decltype(&surgeon_dropout) dropout_fn = nullptr;
 
 using Shape = std::initializer_list<int64_t>;
 
@@ -57,6 +62,16 @@ struct Args {
   void* operand(PyObject* o, at::ScalarType type, Shape shape, bool optional = true) {
     return operand(o, type, at::IntArrayRef(shape.begin(), shape.size()), optional);
   }
+  // A tensor of heads: bf16, of this shape, on this device, with any strides but a dense last dimension.
+  surgeon_heads heads(PyObject* o, Shape shape) {
+    const at::Tensor* t = tensor(o);
+    if (!t || t->scalar_type() != at::kBFloat16 || t->sizes() != at::IntArrayRef(shape.begin(), shape.size()) || !t->is_cuda() ||
+        t->get_device() != device || (t->stride(3) != 1 && t->size(3) != 1)) {
+      ok = false;
+      return {};
+    }
+    return {t->data_ptr(), t->stride(0), t->stride(1), t->stride(2)};
+  }
   void* workspace(PyObject* o, size_t* bytes) {
     const at::Tensor* t = tensor(o);
     if (!t) return nullptr;
@@ -70,6 +85,18 @@ struct Args {
   }
   int64_t integer(PyObject* o) {
     const int64_t v = PyLong_Check(o) ? PyLong_AsLongLong(o) : (ok = false, 0);
+    if (PyErr_Occurred()) {
+      PyErr_Clear();
+      ok = false;
+    }
+    return v;
+  }
+  uint64_t word(PyObject* o) {                   // (modulo 2^64)
+    if (!PyLong_Check(o)) {
+      ok = false;
+      return 0;
+    }
+    const uint64_t v = PyLong_AsUnsignedLongLongMask(o);
     if (PyErr_Occurred()) {
       PyErr_Clear();
       ok = false;
@@ -97,19 +124,21 @@ struct Args {
 
 PyObject* answer(surgeon_status s) { return PyLong_FromLong(s); }
 
-// A linear layer's descriptor: a ctypes structure of the binding's.
-struct Desc {
+// A descriptor (of a linear layer, of an attention): a ctypes structure of the binding's.
+template <typename T>
+struct DescOf {
   Py_buffer view;
-  const surgeon_layer_desc* d = nullptr;
-  explicit Desc(PyObject* o) {
+  const T* d = nullptr;
+  explicit DescOf(PyObject* o) {
     if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) PyErr_Clear();
-    else if (view.len == static_cast<Py_ssize_t>(sizeof(surgeon_layer_desc))) d = static_cast<const surgeon_layer_desc*>(view.buf);
+    else if (view.len == static_cast<Py_ssize_t>(sizeof(T))) d = static_cast<const T*>(view.buf);
     else PyBuffer_Release(&view);
   }
-  ~Desc() {
+  ~DescOf() {
     if (d) PyBuffer_Release(&view);
   }
 };
+using Desc = DescOf<surgeon_layer_desc>;
 
 // The body of a call: no exception of the tensor library's leaves it.
 template <typename F>
@@ -246,6 +275,131 @@ PyObject* gradients(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// desc, q, k, v, q_lengths, kv_lengths, out, lse, workspace
+PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    Args c;
+    if (n != 9 || !attention_fn) Py_RETURN_NONE;
+    const DescOf<surgeon_attention_desc> desc(a[0]);
+    if (!desc.d) Py_RETURN_NONE;
+    const int64_t b = desc.d->batch, h = desc.d->heads, hk = desc.d->kv_heads, nq = desc.d->q_len, nk = desc.d->kv_len, d = desc.d->head_dim;
+    const surgeon_heads q = c.heads(a[1], {b, nq, h, d}), k = c.heads(a[2], {b, nk, hk, d}), v = c.heads(a[3], {b, nk, hk, d});
+    void* ql = c.operand(a[4], at::kInt, {b});
+    void* kl = c.operand(a[5], at::kInt, {b});
+    const surgeon_heads o = c.heads(a[6], {b, nq, h, d});
+    void* lse = c.operand(a[7], at::kFloat, {b, h, nq});
+    size_t bytes = 0;
+    void* ws = c.workspace(a[8], &bytes);
+    if (!c.ok) Py_RETURN_NONE;
+    return answer(attention_fn(desc.d, &q, &k, &v, static_cast<int32_t*>(ql), static_cast<int32_t*>(kl), &o, static_cast<float*>(lse), ws, bytes,
+                               c.stream()));
+  });
+}
+
+// desc, q, k, v, out, dout, lse, q_lengths, kv_lengths, dq, dk, dv, workspace
+PyObject* attention_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    Args c;
+    if (n != 13 || !attention_grad_fn) Py_RETURN_NONE;
+    const DescOf<surgeon_attention_desc> desc(a[0]);
+    if (!desc.d) Py_RETURN_NONE;
+    const int64_t b = desc.d->batch, h = desc.d->heads, hk = desc.d->kv_heads, nq = desc.d->q_len, nk = desc.d->kv_len, d = desc.d->head_dim;
+    const surgeon_heads q = c.heads(a[1], {b, nq, h, d}), k = c.heads(a[2], {b, nk, hk, d}), v = c.heads(a[3], {b, nk, hk, d});
+    const surgeon_heads o = c.heads(a[4], {b, nq, h, d}), dout = c.heads(a[5], {b, nq, h, d});
+    void* lse = c.operand(a[6], at::kFloat, {b, h, nq}, false);
+    void* ql = c.operand(a[7], at::kInt, {b});
+    void* kl = c.operand(a[8], at::kInt, {b});
+    const surgeon_heads dq = c.heads(a[9], {b, nq, h, d}), dk = c.heads(a[10], {b, nk, hk, d}), dv = c.heads(a[11], {b, nk, hk, d});
+    size_t bytes = 0;
+    void* ws = c.workspace(a[12], &bytes);
+    if (!c.ok) Py_RETURN_NONE;
+    return answer(attention_grad_fn(desc.d, &q, &k, &v, &o, &dout, static_cast<float*>(lse), static_cast<int32_t*>(ql), static_cast<int32_t*>(kl), &dq,
+                                    &dk, &dv, ws, bytes, c.stream()));
+  });
+}
+
+// A channels-last tensor [batch, ..., channels].
+bool positions_of(const at::Tensor& x, int64_t* batch, int64_t* positions, int64_t* channels) {
+  if (x.dim() < 2 || x.size(-1) == 0 || x.size(-1) > INT32_MAX) return false;
+  *batch = x.size(0);
+  *channels = x.size(-1);
+  *positions = 1;
+  for (int64_t i = 1; i + 1 < x.dim(); ++i) *positions *= x.size(i);
+  return true;
+}
+
+// x, groups, gamma, beta, eps, act, out, stats, workspace
+PyObject* group_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    Args c;
+    if (n != 9 || !group_norm_fn) Py_RETURN_NONE;
+    const at::Tensor* x = c.tensor(a[0]);
+    int64_t batch = 0, positions = 0, channels = 0;
+    if (!x || !positions_of(*x, &batch, &positions, &channels)) Py_RETURN_NONE;
+    const surgeon_dtype dt = c.type(*x);
+    void* xp = c.plain(*x);
+    const int64_t groups = c.integer(a[1]), act = c.integer(a[5]);
+    void* gamma = c.operand(a[2], at::kFloat, {channels});
+    void* beta = c.operand(a[3], at::kFloat, {channels});
+    const double eps = c.number(a[4]);
+    void* out = c.operand(a[6], x->scalar_type(), x->sizes(), false);
+    void* stats = c.operand(a[7], at::kFloat, {2, batch, groups});
+    size_t bytes = 0;
+    void* ws = c.workspace(a[8], &bytes);
+    if (!c.ok || groups < 1 || groups > channels || act < 0 || act > 255) Py_RETURN_NONE;
+    return answer(group_norm_fn(xp, batch, positions, static_cast<int32_t>(channels), static_cast<int32_t>(groups), dt, static_cast<float*>(gamma),
+                                static_cast<float*>(beta), eps, static_cast<int32_t>(act), out, static_cast<float*>(stats), ws, bytes, c.stream()));
+  });
+}
+
+// x, dy, groups, gamma, beta, stats, act, dx, dgamma, dbeta, accumulate, workspace
+PyObject* group_norm_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    Args c;
+    if (n != 12 || !group_norm_grad_fn) Py_RETURN_NONE;
+    const at::Tensor* x = c.tensor(a[0]);
+    const at::Tensor* dy = c.tensor(a[1]);
+    int64_t batch = 0, positions = 0, channels = 0;
+    if (!x || !dy || !positions_of(*x, &batch, &positions, &channels)) Py_RETURN_NONE;
+    const surgeon_dtype dt = c.type(*x), gdt = c.type(*dy);
+    void* xp = c.plain(*x);
+    void* dyp = c.operand(a[1], dy->scalar_type(), x->sizes(), false);
+    const int64_t groups = c.integer(a[2]), act = c.integer(a[6]);
+    void* gamma = c.operand(a[3], at::kFloat, {channels});
+    void* beta = c.operand(a[4], at::kFloat, {channels});
+    void* stats = c.operand(a[5], at::kFloat, {2, batch, groups}, false);
+    void* dx = c.operand(a[7], dy->scalar_type(), x->sizes(), false);
+    void* dgamma = c.operand(a[8], at::kFloat, {channels});
+    void* dbeta = c.operand(a[9], at::kFloat, {channels});
+    const bool accumulate = c.truth(a[10]);
+    size_t bytes = 0;
+    void* ws = c.workspace(a[11], &bytes);
+    if (!c.ok || groups < 1 || groups > channels || act < 0 || act > 255) Py_RETURN_NONE;
+    return answer(group_norm_grad_fn(xp, dyp, batch, positions, static_cast<int32_t>(channels), static_cast<int32_t>(groups), dt, gdt,
+                                     static_cast<float*>(gamma), static_cast<float*>(beta), static_cast<float*>(stats), static_cast<int32_t>(act), dx,
+                                     static_cast<float*>(dgamma), static_cast<float*>(dbeta), accumulate, ws, bytes, c.stream()));
+  });
+}
+
+// x, p, seed, offset, residual, out, device_offset
+PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    Args c;
+    if (n != 7 || !dropout_fn) Py_RETURN_NONE;
+    const at::Tensor* x = c.tensor(a[0]);
+    if (!x) Py_RETURN_NONE;
+    const surgeon_dtype dt = c.type(*x);
+    void* xp = c.plain(*x);
+    const double p = c.number(a[1]);
+    const uint64_t seed = c.word(a[2]), offset = c.word(a[3]);
+    void* res = c.operand(a[4], x->scalar_type(), x->sizes());
+    void* out = c.operand(a[5], x->scalar_type(), x->sizes(), false);
+    void* later = c.operand(a[6], at::kLong, {1});
+    if (!c.ok) Py_RETURN_NONE;
+    return answer(dropout_fn(xp, x->numel(), dt, p, seed, offset, static_cast<uint64_t*>(later), res, out, c.stream()));
+  });
+}
+
 template <typename F>
 bool address(PyObject* o, F* to) {
   void* p = PyLong_AsVoidPtr(o);
@@ -255,12 +409,14 @@ bool address(PyObject* o, F* to) {
 
 // The entry points' addresses, in the order of their declarations above.
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 6) {
-    PyErr_SetString(PyExc_TypeError, "bind takes six addresses");
+  if (n != 11) {
+    PyErr_SetString(PyExc_TypeError, "bind takes eleven addresses");
     return nullptr;
   }
   if (!address(a[0], &layer_norm_fn) || !address(a[1], &layer_norm_grad_fn) || !address(a[2], &linear_fn) ||
-      !address(a[3], &linear_grad_fn) || !address(a[4], &gradient_norm_fn) || !address(a[5], &clip_gradients_fn)) {
+      !address(a[3], &linear_grad_fn) || !address(a[4], &gradient_norm_fn) || !address(a[5], &clip_gradients_fn) ||
+      !address(a[6], &attention_fn) || !address(a[7], &attention_grad_fn) || !address(a[8], &group_norm_fn) ||
+      !address(a[9], &group_norm_grad_fn) || !address(a[10], &dropout_fn)) {
     if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a null address");
     return nullptr;
   }
@@ -269,7 +425,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define SURGEON_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SURGEON_METHOD(bind),        SURGEON_METHOD(layer_norm), SURGEON_METHOD(layer_norm_grad), SURGEON_METHOD(linear),
-                         SURGEON_METHOD(linear_grad), SURGEON_METHOD(gradients),  {nullptr, nullptr, 0, nullptr}};
+                         SURGEON_METHOD(linear_grad), SURGEON_METHOD(gradients),  SURGEON_METHOD(attention), SURGEON_METHOD(attention_grad),
+                         SURGEON_METHOD(group_norm),  SURGEON_METHOD(group_norm_grad), SURGEON_METHOD(dropout), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
