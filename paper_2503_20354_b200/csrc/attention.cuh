@@ -10,6 +10,8 @@
 namespace surgeon {
 namespace att {
 
+using namespace tc;
+
 constexpr int kTile = 128;                       // rows of a tile: lanes of tensor memory
 constexpr int kSlabCols = 64;                    // columns of a slab: 128 bytes, the swizzle's width
 template <bool V> struct Flag { static constexpr bool value = V; };
@@ -124,6 +126,9 @@ __device__ __forceinline__ float2 exp2_unit(uint64_t x) {
   const float2 v = unpair(x);
   return make_float2(exp2_approx(v.x), exp2_approx(v.y));
 }
+
+// mbar_wait_suspend, asked once without a wait first: where the phase is over already, as it mostly is, that takes 62 clocks instead of 113.
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity) { return mbar_test(bar, parity) || mbar_wait_suspend(bar, parity); }
 
 // Registers of each thread of this warpgroup from here on: more or fewer than it was launched with.
 template <bool MORE, int N>

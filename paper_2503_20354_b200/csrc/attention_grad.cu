@@ -24,7 +24,7 @@ constexpr int kThreads = 384;                    // 2 x 4 warps with a thread a 
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;               // 2 x 208 + 88 = 3 x 168, what 384 threads are launched with
 constexpr int kMaxStages = 8;
 
-constexpr int kByFma = 4;                        // of sixteen pairs of exponentials, those that the FMA pipe computes
+constexpr int kByFma = 0;                        // of sixteen pairs of exponentials, those that the FMA pipe computes
 
 // Four numbers of shared memory as two pairs.
 __device__ __forceinline__ void load_pairs(uint32_t at, uint64_t (&v)[2]) {
@@ -41,10 +41,10 @@ template <int DP, bool KV> struct Shape {
   static constexpr int kStageBytes = 2 * kBlockBytes;
   static constexpr int kHoldBytes = kTiles * 2 * kTileBytes;     // [tile][first, second]
   static constexpr int kSmem = 1024 + kHold * kHoldBytes + kStages * (kStageBytes + kRowBytes);
-  static constexpr bool kOwn = !KV && DP == 64;  // dS has columns of its own, else P and dS take the places of s and do v^T
+  static constexpr bool kOwn = !KV && DP == 64;  // dS has columns of its own, else it takes the place of do v^T, and P that of s
   // columns of tensor memory
   static constexpr uint32_t kStep = KV && DP == 128 ? 128 : 256; // from one half's to the other's
-  static constexpr uint32_t kS = 0, kD = 64, kDs = kOwn ? 128 : KV ? 64 : 0, kAcc1 = KV ? (DP == 64 ? 128 : 256) : (DP == 64 ? 192 : 128),
+  static constexpr uint32_t kS = 0, kD = 64, kDs = kOwn ? 128 : 64, kAcc1 = KV ? (DP == 64 ? 128 : 256) : (DP == 64 ? 192 : 128),
                             kAcc2 = DP == 64 ? 192 : 384, kAccStep = KV && DP == 128 ? 0 : 256;
 };
 
@@ -55,6 +55,7 @@ struct Args {
   float scale;
   const int* q_lengths;
   const int* kv_lengths;
+  int* claims;                                   // how many items have been taken (null: one round over the CTAs after another)
   const float* rows;                             // [batch][heads][q_pad / 64][2][64]: -lse2, -delta of the queries of a block
   surgeon_heads out1, out2;                      // dq; or dk and dv
   float* partial;                                // [split][2][batch][kv_heads][kv_len][head_dim], where there are several
@@ -146,15 +147,17 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   unsigned char* ring = smem + S::kHold * S::kHoldBytes;
   unsigned char* row_ring = ring + S::kStages * S::kStageBytes;
-  __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 4 + 8 + 3];
+  __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 4 + 10 + 3 + 4];
   __shared__ uint32_t tmem_slot;
+  __shared__ int s_items[2];
 
   const int warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x) >> 5, 0);
   const bool leader = elected();
   const uint32_t full = smem_u32(bars), empty = full + 8 * kMaxStages;
   const uint32_t hold_full = empty + 8 * kMaxStages, hold_empty = hold_full + 16;
-  const uint32_t s_full = hold_empty + 16, s_free = s_full + 16, p_full = s_free + 16, acc_done = p_full + 16;     // of each half
+  const uint32_t s_full = hold_empty + 16, s_free = s_full + 16, p_full = s_free + 16, p_done = p_full + 16, acc_done = p_done + 16;     // of each half
   const uint32_t item_done = acc_done + 16, acc_free = item_done + 8, fixed = acc_free + 8;
+  const uint32_t item_full = fixed + 8, item_empty = item_full + 16;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S::kStages; ++s) {
@@ -167,7 +170,10 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
       mbar_init(s_full + 8 * i, 1);
       mbar_init(s_free + 8 * i, 4);
       mbar_init(p_full + 8 * i, 4);
+      mbar_init(p_done + 8 * i, 1);
       mbar_init(acc_done + 8 * i, 1);
+      mbar_init(item_full + 8 * i, 1);
+      mbar_init(item_empty + 8 * i, 9);
     }
     mbar_init(item_done, 1);
     mbar_init(acc_free, 8);
@@ -181,6 +187,18 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
   const uint32_t tmem = tmem_slot;
   pdl_trigger();
   pdl_wait();
+  // The it-th item of this CTA, as the copying warp has taken it: items differ in length by masks and by the sequences' lengths, so a CTA
+  // takes the next one when it has room for it.  Called by whole warps, or by one thread that says so.
+  const auto item_of = [&](int it, bool alone) {
+    const uint32_t at = 8 * (it & 1);
+    bool there = wait_for(item_full + at, (it >> 1) & 1);
+    if (!alone) there = __all_sync(0xFFFFFFFFu, there);
+    if (!there) return p.items;
+    const int item = *static_cast<volatile int*>(&s_items[it & 1]);
+    if (!alone) __syncwarp();
+    if (leader) mbar_arrive(item_empty + at);
+    return item;
+  };
 
   if (warp >= 8) {
     set_registers<false, kOtherRegs>();
@@ -189,10 +207,20 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
       int s = 0, it = 0;
       uint32_t phase = 1, fix_phase = 0;         // (a fresh barrier counts as passed in its phase before)
       bool ok = true;
-      for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x, ++it) {
+      for (;; ++it) {
+        ok = __all_sync(0xFFFFFFFFu, wait_for(item_empty + 8 * (it & 1), ((it >> 1) & 1) ^ 1));
+        if (!ok) break;
+        int item = it * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x);
+        if (p.claims && lane_id() == 0) item = atomicAdd(p.claims, 1);
+        item = min(__shfl_sync(0xFFFFFFFFu, item, 0), p.items);
+        if (leader) {
+          *static_cast<volatile int*>(&s_items[it & 1]) = item;
+          mbar_arrive(item_full + 8 * (it & 1));
+        }
+        if (item >= p.items) break;
         const Item<DP, KV> w(p, item);
         const int hs = S::kHold == 2 ? it & 1 : 0;
-        ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(hold_empty + 8 * hs, (S::kHold == 2 ? (it >> 1) & 1 : it & 1) ^ 1));
+        ok = __all_sync(0xFFFFFFFFu, wait_for(hold_empty + 8 * hs, (S::kHold == 2 ? (it >> 1) & 1 : it & 1) ^ 1));
         if (!ok) break;
         if (leader) {
           if (w.steps) {
@@ -210,7 +238,7 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
         }
         Walk<DP, KV> at(p, w);
         for (int n = 0; n < w.steps && ok; ++n, at.advance(w, 1)) {
-          ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(empty + 8 * s, phase));
+          ok = __all_sync(0xFFFFFFFFu, wait_for(empty + 8 * s, phase));
           if (!ok) break;
           const int head = at.head, row = at.row, left = at.left;
           // Rows behind the last meet zeros in P and dS: they must not hold a NaN.  Behind the tensor's end they are zeros anyway.
@@ -227,7 +255,7 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
               bulk_load(smem_u32(row_ring) + s * S::kRowBytes, p.rows + ((static_cast<long long>(w.b) * p.heads + head) * p.q_pad + row) * 2, S::kRowBytes, bar);
           }
           if (fix) {
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(fixed, fix_phase));
+            ok = __all_sync(0xFFFFFFFFu, wait_for(fixed, fix_phase));
             fix_phase ^= 1;
             zero_rows<S::kSlabs>(to, kBlock, left, round_up(left, 16));
             zero_rows<S::kSlabs>(to + S::kBlockBytes, kBlock, left, round_up(left, 16));
@@ -237,6 +265,7 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
           }
           if (++s == S::kStages) { s = 0; phase ^= 1; }
         }
+        if (!ok) break;
       }
       if (!ok)
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);         // copies in flight land
@@ -250,42 +279,51 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
         int ss = 0, as = 0;                      // the ring's next place for s and do v^T, and for the sums
         uint32_t s_phase = 0, seen[2] = {0, 0};  // seen: blocks of each half that have gone into the sums
         bool ok = true;
-        for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x, ++it) {
+        for (int item; ok && (item = item_of(it, true)) < p.items; ++it) {
           const Item<DP, KV> w(p, item);
           const int hs = S::kHold == 2 ? it & 1 : 0;
-          if (!mbar_wait_suspend(hold_full + 8 * hs, S::kHold == 2 ? (it >> 1) & 1 : it & 1)) break;
+          if (!wait_for(hold_full + 8 * hs, S::kHold == 2 ? (it >> 1) & 1 : it & 1)) break;
           const uint32_t hold = hold_desc + hs * (S::kHoldBytes >> 4);
           Walk<DP, KV> s_at(p, w), a_at(p, w);   // the next block for s and do v^T, and for the sums
           // s and do v^T of half t, the n-th step's block in stage st; number: of this block among the half's
           const auto scores = [&](int t, int st, uint32_t number) {
-            if (!mbar_wait_suspend((S::kOwn ? s_free : acc_done) + 8 * t, (number & 1) ^ 1)) return false;
+            if (S::kOwn && !wait_for(s_free + 8 * t, (number & 1) ^ 1)) return false;
+            // (P of this half's block before has gone into the sums; dS will have by the time that s is done)
+            if (KV && !wait_for(p_done + 8 * t, (number & 1) ^ 1)) return false;
             tc_fence_after();
             const uint32_t idesc = make_idesc(kTile, round_up(s_at.left, 16));
             const uint32_t x = hold + (S::kTiles == 2 ? t * (2 * S::kTileBytes >> 4) : 0), u = ring_desc + st * (S::kStageBytes >> 4), d = tmem + S::kStep * t;
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+            for (int half = 0; half < 2; ++half) {
+              if (half && !S::kOwn) {
+                if (!wait_for(acc_done + 8 * t, (number & 1) ^ 1)) return false;
+                tc_fence_after();
+              }
 #pragma unroll
               for (int k = 0; k < DP / 16; ++k)
                 if (k < k_steps)
                   umma_ss(d + (half ? S::kD : S::kS), x + half * (S::kTileBytes >> 4) + (k >> 2) * (kTile * 128 >> 4) + (k & 3) * 2,
                           u + half * (S::kBlockBytes >> 4) + (k >> 2) * (kBlock * 128 >> 4) + (k & 3) * 2, idesc, k > 0);
+            }
             umma_commit(s_full + 8 * t);
             return true;
           };
           bool acc_ready = false;                // the sums of the item before have been taken out
           const auto sums = [&](int t, int st, bool fresh) {
-            if (!mbar_wait_suspend(p_full + 8 * t, seen[t] & 1)) return false;
-            if (fresh && !acc_ready && !(acc_ready = mbar_wait_suspend(acc_free, (it & 1) ^ 1))) return false;
+            if (!wait_for(p_full + 8 * t, seen[t] & 1)) return false;
+            if (fresh && !acc_ready && !(acc_ready = wait_for(acc_free, (it & 1) ^ 1))) return false;
             tc_fence_after();
             const int steps = (a_at.left + 15) / 16;
             const uint32_t u = rows_desc + st * (S::kStageBytes >> 4), d = tmem + S::kStep * t;
 #pragma unroll
-            for (int half = KV ? 1 : 0; half >= 0; --half)
+            for (int half = KV ? 1 : 0; half >= 0; --half) {
 #pragma unroll
               for (int k = 0; k < kBlock / 16; ++k)
                 if (k < steps)
                   umma_ts(tmem + (half ? S::kAcc2 : S::kAcc1) + S::kAccStep * t, d + (half ? S::kS : S::kDs) + 8 * k,
                           u + half * (S::kBlockBytes >> 4) + 128 * k, idesc_acc, !fresh || k > 0);
+              if (half) umma_commit(p_done + 8 * t);
+            }
             umma_commit(acc_done + 8 * t);
             ++seen[t];
             return true;
@@ -296,7 +334,7 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
           if (S::kTiles == 2) {
             // step n of both halves; s of the step after goes ahead of the sums where it has room
             const auto all_scores = [&](int n, int t) {          // (the first half waits for the block)
-              if (t == 0 && !mbar_wait_suspend(full + 8 * ss, s_phase)) return false;
+              if (t == 0 && !wait_for(full + 8 * ss, s_phase)) return false;
               const bool fine = !w.active[t] || scores(t, ss, seen[t] + (S::kOwn && n > 0 ? 1 : 0));
               if (t == 1) {
                 s_at.advance(w, 1);
@@ -307,8 +345,8 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
             };
             for (int t = 0; t < 2 && ok && w.steps; ++t) ok = all_scores(0, t);
             for (int n = 0; n < w.steps && ok; ++n) {
+              for (int t = 0; t < 2 && ok && S::kOwn && n + 1 < w.steps; ++t) ok = all_scores(n + 1, t);
               for (int t = 0; t < 2 && ok; ++t) {
-                if (S::kOwn && n + 1 < w.steps) ok = all_scores(n + 1, t);
                 if (ok && w.active[t]) ok = sums(t, as, n == 0);
                 if (!S::kOwn && ok && n + 1 < w.steps) ok = all_scores(n + 1, t);
               }
@@ -318,7 +356,7 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
             }
           } else {
             const auto next_scores = [&](int n) {
-              if (!mbar_wait_suspend(full + 8 * ss, s_phase)) return false;
+              if (!wait_for(full + 8 * ss, s_phase)) return false;
               const bool fine = scores(n & 1, ss, seen[n & 1]);
               s_at.advance(w, 1);
               forward(ss);
@@ -334,7 +372,7 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
               if (ok && n + 2 < w.steps) ok = next_scores(n + 2);
             }
           }
-          if (ok && !acc_ready) ok = mbar_wait_suspend(acc_free, (it & 1) ^ 1);  // (an item without steps)
+          if (ok && !acc_ready) ok = wait_for(acc_free, (it & 1) ^ 1);  // (an item without steps)
           if (ok) umma_commit(item_done);
         }
       }
@@ -349,7 +387,7 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
     uint32_t seen = 0, before = 0;               // before: steps of the items so far
     int it = 0;
     bool ok = true;
-    for (int item = blockIdx.x; item < p.items; item += gridDim.x, ++it) {
+    for (int item; (item = item_of(it, false)) < p.items; ++it) {
       const Item<DP, KV> w(p, item);
       const int row = w.row0 + (S::kTiles == 2 ? t * kTile : 0) + row_in_tile;
       float lse2 = -INFINITY, delta = 0.0f;      // (with their signs changed)
@@ -369,17 +407,17 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
         const int col0 = walk.row, left = walk.left;
         const uint32_t turn = (before + n) / S::kStages, at = before + n - turn * S::kStages;     // this step's place in the ring
         if (KV && !w.active[t]) {                // the block's rows are given back all the same
-          ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(full + 8 * at, turn & 1));
+          ok = __all_sync(0xFFFFFFFFu, wait_for(full + 8 * at, turn & 1));
           if (!ok) break;
           if (leader) mbar_arrive(empty + 8 * at);
           __syncwarp();
           continue;
         }
         if (!w.active[t]) break;
-        ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(s_full + 8 * t, seen & 1));
+        ok = __all_sync(0xFFFFFFFFu, wait_for(s_full + 8 * t, seen & 1));
         // (its lse2 and delta are there: the products have waited for them.  With a single tile this half sees every other block alone; behind
         // s_full the parity is that of this block all the same, whose place is not given back before this warp says so)
-        if (KV) ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait_suspend(full + 8 * at, turn & 1));
+        if (KV) ok = ok && __all_sync(0xFFFFFFFFu, wait_for(full + 8 * at, turn & 1));
         if (!ok) break;
         tc_fence_after();
         uint32_t sv[kBlock], dv[kBlock];
@@ -440,7 +478,7 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
           if (masked) some(Flag<true>());
           else some(Flag<false>());
           if (q == 0 && S::kOwn) {               // the sums before have read dS
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(acc_done + 8 * t, (seen & 1) ^ 1));
+            ok = __all_sync(0xFFFFFFFFu, wait_for(acc_done + 8 * t, (seen & 1) ^ 1));
             if (!ok) break;
           }
           if (KV) tmem_st16(mine_at + S::kS + 16 * q, pw);
@@ -458,8 +496,8 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
         ++seen;
       }
       before += w.steps;
-      if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(hold_full + 8 * (S::kHold == 2 ? it & 1 : 0), S::kHold == 2 ? (it >> 1) & 1 : it & 1));
-      if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(item_done, it & 1));
+      if (ok) ok = __all_sync(0xFFFFFFFFu, wait_for(hold_full + 8 * (S::kHold == 2 ? it & 1 : 0), S::kHold == 2 ? (it >> 1) & 1 : it & 1));
+      if (ok) ok = __all_sync(0xFFFFFFFFu, wait_for(item_done, it & 1));
       // ---- the sums of this half's tile; of a single tile the first half takes the first sums, the second the others ----
       const int hs = S::kHold == 2 ? it & 1 : 0;
       const bool live = S::kTiles == 1 ? w.steps > 0 : w.active[t];
@@ -543,42 +581,48 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
 }
 
 // -lse2 and -delta of every row; -infinity and 0 for rows that see nothing and for those that fill the last block up.
-// LANES lanes a row, 16 bytes each; a CTA takes rows of one sequence, heads fastest: neighbours in memory where heads lie side by side.
+// LANES lanes a row, 16 bytes each; a CTA takes 128 rows of one head, heads fastest: neighbours in memory where heads lie side by side.
 template <int LANES>
 __global__ void __launch_bounds__(256)
-attention_rows_kernel(const surgeon_heads o, const surgeon_heads dout, const float* lse, const int* q_lengths, int heads, FastDiv by_heads, int q_len,
-                      int q_pad, int head_dim, int ctas, float* rows) {
-  constexpr int kRows = 256 / LANES, kPasses = 4;
+attention_rows_kernel(const surgeon_heads o, const surgeon_heads dout, const float* lse, const int* q_lengths, int heads, int q_len, int q_pad,
+                      int head_dim, int tiles, float* rows, int* claims) {
+  constexpr int kRows = 256 / LANES, kPasses = 128 / kRows;
   pdl_trigger();
   pdl_wait();
-  const int b = static_cast<int>(blockIdx.x) / ctas, first = (static_cast<int>(blockIdx.x) - b * ctas) * kRows * kPasses;
+  if (blockIdx.x == 0 && threadIdx.x < 2) claims[threadIdx.x] = 0;
+  const int h = static_cast<int>(blockIdx.x) % heads, bt = static_cast<int>(blockIdx.x) / heads, b = bt / tiles, first = (bt - b * tiles) * 128;
   const int part = threadIdx.x % LANES, q_valid = length_of(q_lengths, b, q_len);
-  const unsigned short* from_o = static_cast<const unsigned short*>(o.data) + b * o.batch_stride + part * 8;
-  const unsigned short* from_d = static_cast<const unsigned short*>(dout.data) + b * dout.batch_stride + part * 8;
-  float a[kPasses][8], d[kPasses][8];
+  const unsigned short* from_o = static_cast<const unsigned short*>(o.data) + b * o.batch_stride + h * o.head_stride + part * 8;
+  const unsigned short* from_d = static_cast<const unsigned short*>(dout.data) + b * dout.batch_stride + h * dout.head_stride + part * 8;
+  const long long bh = static_cast<long long>(b) * heads + h;
+  uint4 a[kPasses], d[kPasses];
+  float l[kPasses];
 #pragma unroll
   for (int i = 0; i < kPasses; ++i) {
-    const int at = first + i * kRows + threadIdx.x / LANES, row = static_cast<int>(divide(at, by_heads)), h = at - row * heads;
-    if (row < q_valid && part * 8 < head_dim) {
-      load_elems<1, 8>(from_o, static_cast<long long>(row) * o.row_stride + h * o.head_stride, a[i]);
-      load_elems<1, 8>(from_d, static_cast<long long>(row) * dout.row_stride + h * dout.head_stride, d[i]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) a[i][k] = d[i][k] = 0.0f;
+    const int row = first + i * kRows + threadIdx.x / LANES;
+    a[i] = d[i] = make_uint4(0u, 0u, 0u, 0u);
+    l[i] = -INFINITY;
+    if (row < q_valid) {
+      if (part * 8 < head_dim) {
+        a[i] = *reinterpret_cast<const uint4*>(from_o + static_cast<long long>(row) * o.row_stride);
+        d[i] = *reinterpret_cast<const uint4*>(from_d + static_cast<long long>(row) * dout.row_stride);
+      }
+      if (part == 0) l[i] = lse[bh * q_len + row];
     }
   }
 #pragma unroll
   for (int i = 0; i < kPasses; ++i) {
-    const int at = first + i * kRows + threadIdx.x / LANES, row = static_cast<int>(divide(at, by_heads)), h = at - row * heads;
-    float sum = 0.0f;
+    const int row = first + i * kRows + threadIdx.x / LANES;
+    float f[8], g[8], sum = 0.0f;
+    vector_elems<1>(a[i], f);
+    vector_elems<1>(d[i], g);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sum = fmaf(a[i][k], d[i][k], sum);
+    for (int k = 0; k < 8; ++k) sum = fmaf(f[k], g[k], sum);
     sum = lanes_sum<LANES>(sum);
-    if (part == 0 && row < q_pad) {
-      const float l = row < q_valid ? lse[(static_cast<long long>(b) * heads + h) * q_len + row] : -INFINITY;
-      float* to = rows + ((static_cast<long long>(b) * heads + h) * q_pad + (row & ~(kBlock - 1))) * 2 + (row & (kBlock - 1));
-      to[0] = l == -INFINITY ? -INFINITY : -l * kLog2E;
-      to[kBlock] = l == -INFINITY ? 0.0f : -sum;
+    if (part == 0) {
+      float* to = rows + (bh * q_pad + (row & ~(kBlock - 1))) * 2 + (row & (kBlock - 1));
+      to[0] = l[i] == -INFINITY ? -INFINITY : -l[i] * kLog2E;
+      to[kBlock] = l[i] == -INFINITY ? 0.0f : -sum;
     }
   }
 }
@@ -619,6 +663,7 @@ int splits_of(const surgeon_attention_desc& d) {
   return splits < 1 ? 1 : static_cast<int>(splits);
 }
 int padded(int q_len) { return round_up(q_len, 128); }
+constexpr size_t kClaimBytes = 256;              // the passes' counters of items
 size_t rows_bytes(const surgeon_attention_desc& d) {
   return (static_cast<size_t>(d.batch) * d.heads * padded(d.q_len) * 2 * sizeof(float) + 255) & ~static_cast<size_t>(255);
 }
@@ -663,6 +708,7 @@ cudaError_t launch_as(const surgeon_attention_desc& d, const surgeon_heads& q, c
   }
   if (!dk || d.kv_len == 0) return e;
   a.out1 = *dk;
+  if (a.claims) ++a.claims;
   a.out2 = *dv;
   e = launch_pass<DP, true>(d, k, v, q, dout, a, stream);
   if (e != cudaSuccess || a.splits == 1) return e;
@@ -677,8 +723,7 @@ cudaError_t launch_as(const surgeon_attention_desc& d, const surgeon_heads& q, c
 
 size_t attention_grad_workspace(const surgeon_attention_desc& d) {
   const int splits = splits_of(d);
-  const size_t n = rows_bytes(d) + (splits > 1 ? splits * 2 * part_elems(d) * sizeof(float) : 0);
-  return n < 16 ? 16 : n;
+  return kClaimBytes + rows_bytes(d) + (splits > 1 ? splits * 2 * part_elems(d) * sizeof(float) : 0);
 }
 
 cudaError_t launch_attention_grad(const surgeon_attention_desc& d, const surgeon_heads& q, const surgeon_heads& k, const surgeon_heads& v,
@@ -686,15 +731,14 @@ cudaError_t launch_attention_grad(const surgeon_attention_desc& d, const surgeon
                                   const int* kv_lengths, const surgeon_heads* dq, const surgeon_heads* dk, const surgeon_heads* dv,
                                   void* workspace, cudaStream_t stream) {
   if (!dq && !dk) return cudaSuccess;
-  float* rows = static_cast<float*>(workspace);
+  int* claims = static_cast<int*>(workspace);
+  float* rows = reinterpret_cast<float*>(static_cast<char*>(workspace) + kClaimBytes);
   const int q_pad = padded(d.q_len);
   if (d.q_len > 0) {
-    const bool narrow = d.head_dim <= 64;
-    const int rows_cta = (narrow ? 32 : 16) * 4;
-    const long long ctas = (static_cast<long long>(d.heads) * q_pad + rows_cta - 1) / rows_cta;
-    const cudaError_t e = launch_kernel(narrow ? attention_rows_kernel<8> : attention_rows_kernel<16>, dim3(static_cast<unsigned>(ctas * d.batch)), dim3(256), 0,
-                                        stream, true, o, dout, lse, q_lengths, d.heads, make_div(d.heads), d.q_len, q_pad, d.head_dim, static_cast<int>(ctas),
-                                        rows);
+    const int tiles = q_pad / 128;
+    const cudaError_t e = launch_kernel(d.head_dim <= 64 ? attention_rows_kernel<8> : attention_rows_kernel<16>,
+                                        dim3(static_cast<unsigned>(tiles) * d.batch * d.heads), dim3(256), 0, stream, true, o, dout, lse, q_lengths, d.heads,
+                                        d.q_len, q_pad, d.head_dim, tiles, rows, claims);
     note_launches(1);
     if (e != cudaSuccess) return e;
   }
@@ -705,8 +749,9 @@ cudaError_t launch_attention_grad(const surgeon_attention_desc& d, const surgeon
   a.splits = splits_of(d);
   a.scale = static_cast<float>(d.scale);
   a.q_lengths = q_lengths; a.kv_lengths = kv_lengths;
+  a.claims = d.q_len > 0 ? claims : nullptr;
   a.rows = rows;
-  a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + rows_bytes(d));
+  a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + kClaimBytes + rows_bytes(d));
   return d.head_dim <= 64 ? launch_as<64>(d, q, k, v, dout, dq, dk, dv, a, stream) : launch_as<128>(d, q, k, v, dout, dq, dk, dv, a, stream);
 }
 
