@@ -21,7 +21,7 @@ using namespace att;
 constexpr int kBlock = 128;                      // keys of a block
 constexpr int kCopyWarp = 8, kProductWarp = 9;
 constexpr int kThreads = 384;                    // (two warps idle: registers are dealt out by fours of warps)
-constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;               // 2 x 208 + 88 = 3 x 168, what 384 threads are launched with
+constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;               // 2 x 216 + 72 = 3 x 168, what 384 threads are launched with
 constexpr int kMaxStages = 8;
 constexpr float kMost = 18446744073709551616.0f;                 // 2^64: what a row's p of a block may add up to before m is set anew
 
@@ -259,7 +259,7 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
         const Item<PARTS> w(p, item);
         const int qs = S::kQStages == 2 ? it & 1 : 0;
         const uint32_t q_phase = S::kQStages == 2 ? (it >> 1) & 1 : it & 1;
-        for (int t = 0; t < 2 && ok; ++t) ok = mbar_wait_suspend(q_full + 8 * (2 * qs + t), q_phase);
+        for (int t = 0; t < 2 && ok; ++t) ok = wait_for(q_full + 8 * (2 * qs + t), q_phase);
         if (!ok) break;
         if (w.most <= w.from) continue;
         const auto next = [&]() {
@@ -270,7 +270,7 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
         // s of tile t and block j, the t's block number n
         const auto scores = [&](int t, int j, int st, uint32_t n) {
           // (s has been read; where p takes its place, p has gone into o)
-          if (!mbar_wait_suspend((S::kOwnP ? s_free : o_done) + 8 * t, (n & 1) ^ 1)) return false;
+          if (!wait_for((S::kOwnP ? s_free : o_done) + 8 * t, (n & 1) ^ 1)) return false;
           tc_fence_after();
           const uint32_t idesc = make_idesc(kTile, round_up(min(kBlock, w.keys[t] - j * kBlock), 16));
           const uint32_t a = q_desc + (2 * qs + (PARTS && p.twin ? 0 : t)) * (S::kTileBytes >> 4), b = k_desc + st * (S::kBlockBytes >> 4);
@@ -281,7 +281,7 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
           return true;
         };
         const auto values = [&](int t, int j, int st, uint32_t n) {
-          if (!mbar_wait_suspend(p_full + 8 * t, n & 1)) return false;
+          if (!wait_for(p_full + 8 * t, n & 1)) return false;
           tc_fence_after();
           const int steps = (min(kBlock, w.keys[t] - j * kBlock) + 15) / 16;
           const uint32_t b = v_desc + st * (S::kBlockBytes >> 4);
@@ -294,7 +294,7 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
         if (PARTS && p.twin) {
           // one tile's block after the other's; k of block j is the 2 (j - from)-th tile of the ring from here, v the one behind it
           const uint32_t base = s + (phase ? S::kStages : 0);
-          const auto there = [&](uint32_t at) { return mbar_wait_suspend(full + 8 * (at % S::kStages), (at / S::kStages) & 1); };
+          const auto there = [&](uint32_t at) { return wait_for(full + 8 * (at % S::kStages), (at / S::kStages) & 1); };
           const auto turn = [&](int j) {
             const uint32_t at = base + 2 * (j - w.from), st = at % S::kStages;
             if (!there(at) || !scores((j - w.from) & 1, j, st, first[(j - w.from) & 1] + ((j - w.from) >> 1))) return false;
@@ -316,7 +316,7 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
           first[1] += (w.most - w.from) >> 1;
           continue;
         }
-        ok = mbar_wait_suspend(full + 8 * s, phase);
+        ok = wait_for(full + 8 * s, phase);
         int ks = next();                         // the place of the next block's keys
         for (int t = 0; t < 2 && ok; ++t)
           if (w.blocks[t] > w.from) ok = scores(t, w.from, ks, first[t]);
@@ -327,10 +327,10 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
           next();
           const bool more = j + 1 < w.most;
           if (more) {
-            ok = mbar_wait_suspend(full + 8 * s, phase);
+            ok = wait_for(full + 8 * s, phase);
             ks = next();
           }
-          ok = ok && mbar_wait_suspend(full + 8 * v_at, v_phase);
+          ok = ok && wait_for(full + 8 * v_at, v_phase);
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             const uint32_t n = first[t] + j - w.from;
@@ -399,7 +399,8 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
         if (S::kOwnP && leader) mbar_arrive(s_free + 8 * t);
         if ((j + 1) * kBlock > all) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) hide(v[q], limit - 32 * q);
+          for (int q = 0; q < 4; ++q)
+            if (all - j * kBlock < 32 * q + 32) hide(v[q], limit - 32 * q);
         }
         float sum;
         bool arrived = j == from;                   // the block before has gone into o, and p may be written
