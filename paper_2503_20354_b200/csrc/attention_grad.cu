@@ -33,19 +33,19 @@ __device__ __forceinline__ void load_pairs(uint32_t at, uint64_t (&v)[2]) {
 
 template <int DP, bool KV> struct Shape {
   static constexpr int kSlabs = DP / kSlabCols;
-  static constexpr int kTiles = KV && DP == 128 ? 1 : 2;         // tiles that stay; the two halves of the warps have one each, or every other block of one
+  static constexpr int kTiles = KV ? 1 : 2;      // tiles that stay; the two halves of the warps have one each, or every other block of one
   static constexpr int kTileBytes = kTile * DP * 2, kBlockBytes = kBlock * DP * 2;
   static constexpr int kHold = DP == 64 ? 2 : 1;                 // places for what stays
-  static constexpr int kStages = DP == 64 ? 5 : KV ? 4 : 3;
+  static constexpr int kStages = DP == 64 ? (KV ? 8 : 5) : KV ? 4 : 3;
   static constexpr int kRowBytes = KV ? kBlock * 8 : 0;          // lse2 and delta of a block
   static constexpr int kStageBytes = 2 * kBlockBytes;
   static constexpr int kHoldBytes = kTiles * 2 * kTileBytes;     // [tile][first, second]
   static constexpr int kSmem = 1024 + kHold * kHoldBytes + kStages * (kStageBytes + kRowBytes);
-  static constexpr bool kOwn = !KV && DP == 64;  // dS has columns of its own, else it takes the place of do v^T, and P that of s
-  // columns of tensor memory
-  static constexpr uint32_t kStep = KV && DP == 128 ? 128 : 256; // from one half's to the other's
-  static constexpr uint32_t kS = 0, kD = 64, kDs = kOwn ? 128 : 64, kAcc1 = KV ? (DP == 64 ? 128 : 256) : (DP == 64 ? 192 : 128),
-                            kAcc2 = DP == 64 ? 192 : 384, kAccStep = KV && DP == 128 ? 0 : 256;
+  static constexpr bool kOwn = DP == 64;         // P and dS have columns of their own, else they take the places of s and do v^T
+  // columns of tensor memory, and from one half's to the other's
+  static constexpr uint32_t kS = 0, kD = 64, kStep = KV ? 128 : 256;
+  static constexpr uint32_t kP = KV && DP == 64 ? 256 : 0, kDs = DP == 64 ? (KV ? 288 : 128) : 64, kPStep = KV ? (DP == 64 ? 64 : 128) : 256;
+  static constexpr uint32_t kAcc1 = DP == 64 ? (KV ? 384 : 192) : (KV ? 256 : 128), kAcc2 = DP == 64 ? 448 : 384, kAccStep = KV ? 0 : 256;
 };
 
 struct Args {
@@ -289,7 +289,7 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
           const auto scores = [&](int t, int st, uint32_t number) {
             if (S::kOwn && !wait_for(s_free + 8 * t, (number & 1) ^ 1)) return false;
             // (P of this half's block before has gone into the sums; dS will have by the time that s is done)
-            if (KV && !wait_for(p_done + 8 * t, (number & 1) ^ 1)) return false;
+            if (KV && !S::kOwn && !wait_for(p_done + 8 * t, (number & 1) ^ 1)) return false;
             tc_fence_after();
             const uint32_t idesc = make_idesc(kTile, round_up(s_at.left, 16));
             const uint32_t x = hold + (S::kTiles == 2 ? t * (2 * S::kTileBytes >> 4) : 0), u = ring_desc + st * (S::kStageBytes >> 4), d = tmem + S::kStep * t;
@@ -314,13 +314,13 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
             if (fresh && !acc_ready && !(acc_ready = wait_for(acc_free, (it & 1) ^ 1))) return false;
             tc_fence_after();
             const int steps = (a_at.left + 15) / 16;
-            const uint32_t u = rows_desc + st * (S::kStageBytes >> 4), d = tmem + S::kStep * t;
+            const uint32_t u = rows_desc + st * (S::kStageBytes >> 4), d = tmem + S::kPStep * t;
 #pragma unroll
             for (int half = KV ? 1 : 0; half >= 0; --half) {
 #pragma unroll
               for (int k = 0; k < kBlock / 16; ++k)
                 if (k < steps)
-                  umma_ts(tmem + (half ? S::kAcc2 : S::kAcc1) + S::kAccStep * t, d + (half ? S::kS : S::kDs) + 8 * k,
+                  umma_ts(tmem + (half ? S::kAcc2 : S::kAcc1) + S::kAccStep * t, d + (half ? S::kP : S::kDs) + 8 * k,
                           u + half * (S::kBlockBytes >> 4) + 128 * k, idesc_acc, !fresh || k > 0);
               if (half) umma_commit(p_done + 8 * t);
             }
@@ -357,7 +357,7 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
           } else {
             const auto next_scores = [&](int n) {
               if (!wait_for(full + 8 * ss, s_phase)) return false;
-              const bool fine = scores(n & 1, ss, seen[n & 1]);
+              const bool fine = scores(n & 1, ss, seen[n & 1] + (S::kOwn && n > 1 ? 1 : 0));
               s_at.advance(w, 1);
               forward(ss);
               if (ss == 0) s_phase ^= 1;
@@ -365,11 +365,12 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
             };
             for (int n = 0; n < 2 && n < w.steps && ok; ++n) ok = next_scores(n);
             for (int n = 0; n < w.steps && ok; ++n) {
-              ok = sums(n & 1, as, n == 0);
+              if (S::kOwn && n + 2 < w.steps) ok = next_scores(n + 2);
+              ok = ok && sums(n & 1, as, n == 0);
               if (ok) umma_commit(empty + 8 * as);
               forward(as);
               a_at.advance(w, 1);
-              if (ok && n + 2 < w.steps) ok = next_scores(n + 2);
+              if (!S::kOwn && ok && n + 2 < w.steps) ok = next_scores(n + 2);
             }
           }
           if (ok && !acc_ready) ok = wait_for(acc_free, (it & 1) ^ 1);  // (an item without steps)
@@ -381,7 +382,7 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
     // ---- a thread a row of s ----
     set_registers<true, kSoftmaxRegs>();
     const int t = warp >> 2, quarter = warp & 3, lane = static_cast<int>(lane_id()), row_in_tile = quarter * 32 + lane;
-    const uint32_t lanes = static_cast<uint32_t>(quarter) << 21, mine_at = tmem + S::kStep * t + lanes;
+    const uint32_t lanes = static_cast<uint32_t>(quarter) << 21, mine_at = tmem + S::kStep * t + lanes, p_at = tmem + S::kPStep * t + lanes;
     const float c = p.scale * kLog2E;
     const uint64_t c2 = pair(c, c);
     uint32_t seen = 0, before = 0;               // before: steps of the items so far
@@ -481,8 +482,8 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
             ok = __all_sync(0xFFFFFFFFu, wait_for(acc_done + 8 * t, (seen & 1) ^ 1));
             if (!ok) break;
           }
-          if (KV) tmem_st16(mine_at + S::kS + 16 * q, pw);
-          tmem_st16(mine_at + S::kDs + 16 * q, sw);
+          if (KV) tmem_st16(p_at + S::kP + 16 * q, pw);
+          tmem_st16(p_at + S::kDs + 16 * q, sw);
         }
         if (!ok) break;
         if (KV) {                                // (its rows have been read)
@@ -654,8 +655,7 @@ attention_join_kernel(const float* partial, const surgeon_heads dk, const surgeo
 
 // Parts of the queries that the keys' tiles are shared out in: enough for two items an SM (they differ in length), eight blocks each at least.
 int splits_of(const surgeon_attention_desc& d) {
-  const int rows = kTile * (d.head_dim <= 64 ? 2 : 1);
-  const long long items = static_cast<long long>(d.batch) * d.kv_heads * ((d.kv_len + rows - 1) / rows);
+  const long long items = static_cast<long long>(d.batch) * d.kv_heads * ((d.kv_len + kTile - 1) / kTile);
   const long long steps = static_cast<long long>(d.heads / d.kv_heads) * ((d.q_len + kBlock - 1) / kBlock);
   if (items <= 0 || items >= 2 * 148) return 1;
   long long splits = (2 * 148 + items - 1) / items;
