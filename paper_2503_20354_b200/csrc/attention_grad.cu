@@ -20,8 +20,10 @@ using namespace tc;
 using namespace att;
 
 constexpr int kBlock = 64;                       // rows that stream by at a time
-constexpr int kThreads = 384;                    // 2 x 4 warps with a thread a row, one that copies, one that issues products, two that idle
-constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;               // 2 x 208 + 88 = 3 x 168, what 384 threads are launched with
+// 2 x 4 warps with a thread a row, one that copies, one that issues products, two that idle, four that write the sums of an item
+// while the others are at the next one.
+constexpr int kCopyWarp = 8, kProductWarp = 9, kWriteWarp = 12, kThreads = 512;
+constexpr int kRowRegs = 160, kOtherRegs = 96;                   // 2 x 160 + 2 x 96 = 4 x 128, what 512 threads are launched with
 constexpr int kMaxStages = 8;
 
 constexpr int kByFma = 0;                        // of sixteen pairs of exponentials, those that the FMA pipe computes
@@ -99,8 +101,13 @@ struct Item {
       first = min(start, q_valid) / kBlock;
       blocks = start >= q_valid ? 0 : (q_valid + kBlock - 1) / kBlock - first;
       const int total = blocks * p.group;
-      from = static_cast<int>(static_cast<long long>(total) * split / p.splits);
-      steps = static_cast<int>(static_cast<long long>(total) * (split + 1) / p.splits) - from;
+      from = 0;
+      steps = total;
+      if (p.splits > 1) {
+        from = static_cast<int>(divide(total, p.by_splits)) * split;
+        if (split + 1 < p.splits) steps = static_cast<int>(divide(total, p.by_splits));
+        else steps = total - from;
+      }
     } else {
       const int last = min(row0 + S::kTiles * kTile, q_valid) - 1;
       const int keys = row0 >= q_valid ? 0 : p.causal ? max(0, min(kv_valid, last + off + 1)) : kv_valid;
@@ -166,21 +173,21 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(hold_full + 8 * i, 1);
-      mbar_init(hold_empty + 8 * i, 8);
+      mbar_init(hold_empty + 8 * i, 4);
       mbar_init(s_full + 8 * i, 1);
       mbar_init(s_free + 8 * i, 4);
       mbar_init(p_full + 8 * i, 4);
       mbar_init(p_done + 8 * i, 1);
       mbar_init(acc_done + 8 * i, 1);
       mbar_init(item_full + 8 * i, 1);
-      mbar_init(item_empty + 8 * i, 9);
+      mbar_init(item_empty + 8 * i, 13);
     }
     mbar_init(item_done, 1);
-    mbar_init(acc_free, 8);
+    mbar_init(acc_free, 4);
     mbar_init(fixed, 1);
     fence_barrier_init();
   }
-  if (warp == 9) tmem_alloc(smem_u32(&tmem_slot), 512);
+  if (warp == kProductWarp) tmem_alloc(smem_u32(&tmem_slot), 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -200,9 +207,9 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
     return item;
   };
 
-  if (warp >= 8) {
+  if (warp >= kCopyWarp && warp < kWriteWarp) {
     set_registers<false, kOtherRegs>();
-    if (warp == 8) {
+    if (warp == kCopyWarp) {
       // ---- copies ----
       int s = 0, it = 0;
       uint32_t phase = 1, fix_phase = 0;         // (a fresh barrier counts as passed in its phase before)
@@ -269,7 +276,7 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
       }
       if (!ok)
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);         // copies in flight land
-    } else if (warp == 9) {
+    } else if (warp == kProductWarp) {
       // ---- products ----
       if (leader) {
         const int k_steps = (p.head_dim + 15) / 16;
@@ -378,9 +385,9 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
         }
       }
     }
-  } else {
+  } else if (warp < kCopyWarp) {
     // ---- a thread a row of s ----
-    set_registers<true, kSoftmaxRegs>();
+    set_registers<true, kRowRegs>();
     const int t = warp >> 2, quarter = warp & 3, lane = static_cast<int>(lane_id()), row_in_tile = quarter * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(quarter) << 21, mine_at = tmem + S::kStep * t + lanes, p_at = tmem + S::kPStep * t + lanes;
     const float c = p.scale * kLog2E;
@@ -388,7 +395,7 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
     uint32_t seen = 0, before = 0;               // before: steps of the items so far
     int it = 0;
     bool ok = true;
-    for (int item; (item = item_of(it, false)) < p.items; ++it) {
+    for (int item; ok && (item = item_of(it, false)) < p.items; ++it) {
       const Item<DP, KV> w(p, item);
       const int row = w.row0 + (S::kTiles == 2 ? t * kTile : 0) + row_in_tile;
       float lse2 = -INFINITY, delta = 0.0f;      // (with their signs changed)
@@ -421,19 +428,6 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
         if (KV) ok = ok && __all_sync(0xFFFFFFFFu, wait_for(full + 8 * at, turn & 1));
         if (!ok) break;
         tc_fence_after();
-        uint32_t sv[kBlock], dv[kBlock];
-        tmem_ld32(mine_at + S::kS, sv);
-        tmem_ld32(mine_at + S::kD, dv);
-        if (left > 32) {
-          tmem_ld32(mine_at + S::kS + 32, sv + 32);
-          tmem_ld32(mine_at + S::kD + 32, dv + 32);
-        }
-        tmem_wait_ld();
-        if (S::kOwn) {
-          tc_fence_before();
-          __syncwarp();
-          if (leader) mbar_arrive(s_free + 8 * t);
-        }
         const uint32_t rows = smem_u32(row_ring) + at * S::kRowBytes;
         int lo = 0, hi = kBlock;
         bool masked;
@@ -448,8 +442,21 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
         uint64_t nl = pair(lse2, lse2), nd = pair(delta, delta);
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-          if (q == 1 && left <= 32) break;
-          uint32_t pw[16], sw[16];
+          uint32_t sv[32], dv[32], pw[16], sw[16];
+          if (q == 0 || left > 32) {
+            tmem_ld32(mine_at + S::kS + 32 * q, sv);
+            tmem_ld32(mine_at + S::kD + 32 * q, dv);
+            tmem_wait_ld32(sv);
+            tmem_wait_ld32(dv);
+          }
+          if (q == 1) {                          // s and do v^T have been read
+            if (S::kOwn) {
+              tc_fence_before();
+              __syncwarp();
+              if (leader) mbar_arrive(s_free + 8 * t);
+            }
+            if (left <= 32) break;
+          }
           const auto some = [&](auto masks) {
 #pragma unroll
             for (int i = 0; i < 32; i += 4) {
@@ -460,10 +467,10 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
               }
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
-                const int e = q * 32 + i + 2 * k;
-                const uint64_t x = fma2(pair(sv[e], sv[e + 1]), c2, nl4[k]);
+                const int v = i + 2 * k, e = q * 32 + v;
+                const uint64_t x = fma2(pair(sv[v], sv[v + 1]), c2, nl4[k]);
                 float2 f = !decltype(masks)::value && (i >> 2) < kByFma && k == 0 ? exp2_pair(x) : exp2_unit(x);
-                float2 g = unpair(mul2(pair(f.x, f.y), add2(pair(dv[e], dv[e + 1]), nd4[k])));
+                float2 g = unpair(mul2(pair(f.x, f.y), add2(pair(dv[v], dv[v + 1]), nd4[k])));
                 if (decltype(masks)::value) {
                   const bool on0 = e >= lo && e < hi, on1 = e + 1 >= lo && e + 1 < hi;
                   f.x = on0 ? f.x : 0.0f;
@@ -497,49 +504,60 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
         ++seen;
       }
       before += w.steps;
-      if (ok) ok = __all_sync(0xFFFFFFFFu, wait_for(hold_full + 8 * (S::kHold == 2 ? it & 1 : 0), S::kHold == 2 ? (it >> 1) & 1 : it & 1));
-      if (ok) ok = __all_sync(0xFFFFFFFFu, wait_for(item_done, it & 1));
-      // ---- the sums of this half's tile; of a single tile the first half takes the first sums, the second the others ----
+    }
+  } else {
+    // ---- the sums of an item, out of tensor memory: two tiles' dq, or a tile's dk and dv ----
+    set_registers<false, kOtherRegs>();
+    const int quarter = warp & 3, row_in_tile = quarter * 32 + static_cast<int>(lane_id());
+    const bool parts = KV && p.splits > 1;
+    int it = 0;
+    bool ok = true;
+    for (int item; (item = item_of(it, false)) < p.items; ++it) {
+      const Item<DP, KV> w(p, item);
       const int hs = S::kHold == 2 ? it & 1 : 0;
-      const bool live = S::kTiles == 1 ? w.steps > 0 : w.active[t];
-      const int rows_all = KV ? p.kv_len : p.q_len;
-      if (ok && live) tc_fence_after();
+      // the place of what stayed takes the outputs: it is not read any more
+      if (ok) ok = __all_sync(0xFFFFFFFFu, wait_for(hold_full + 8 * hs, S::kHold == 2 ? (it >> 1) & 1 : it & 1));
+      if (ok) ok = __all_sync(0xFFFFFFFFu, wait_for(item_done, it & 1));
+      tc_fence_after();
+#pragma unroll 1
       for (int part = 0; part < 2; ++part) {
-        if (S::kTiles == 1 ? part != t : !KV && part == 1) continue;
-        const surgeon_heads& out = part ? p.out2 : p.out1;
-        const uint32_t acc = tmem + (part ? S::kAcc2 : S::kAcc1) + S::kAccStep * t + lanes;
-        const float f = part ? 1.0f : p.scale;
-        if (!ok) {                               // a wait ran out: this warp's rows are NaN, here and from here on
+        const int row = w.row0 + (KV ? 0 : part * kTile) + row_in_tile, rows_all = KV ? p.kv_len : p.q_len;
+        const bool second = KV && part;          // dv
+        const surgeon_heads& out = second ? p.out2 : p.out1;
+        float* const sums_to = p.partial + ((((static_cast<long long>(w.split) * 2 + part) * p.batch + w.b) * p.kv_heads + w.h) * p.kv_len + row) * p.head_dim;
+        if (!ok) {                               // a wait ran out: the rows are NaN, here and from here on
           if (row < rows_all) {
-            if (KV && p.splits > 1) {
-              float* to = p.partial + (((static_cast<long long>(w.split) * 2 + part) * p.batch + w.b) * p.kv_heads + w.h) * static_cast<long long>(p.kv_len) * p.head_dim +
-                          static_cast<long long>(row) * p.head_dim;
-              for (int i = 0; i < p.head_dim; ++i) to[i] = __uint_as_float(0x7FC00000u);
-            } else {
-              unsigned short* to = static_cast<unsigned short*>(out.data) + w.b * out.batch_stride + static_cast<long long>(row) * out.row_stride + w.h * out.head_stride;
-              for (int i = 0; i < p.head_dim; ++i) to[i] = 0x7FC0u;
+            unsigned short* to = static_cast<unsigned short*>(out.data) + w.b * out.batch_stride + static_cast<long long>(row) * out.row_stride + w.h * out.head_stride;
+            for (int i = 0; i < p.head_dim; ++i) {
+              if (parts) sums_to[i] = __uint_as_float(0x7FC00000u);
+              else to[i] = 0x7FC0u;
             }
           }
           continue;
         }
-        const bool some = live && row < w.valid;
-        unsigned char* stage = smem + hs * S::kHoldBytes + (S::kTiles == 2 ? t * 2 + part : part) * S::kTileBytes;
+        const bool live = KV ? w.steps > 0 : w.active[part], some = live && row < w.valid;
+        const uint32_t acc = tmem + (second ? S::kAcc2 : S::kAcc1) + (KV ? 0 : S::kAccStep * part) + (static_cast<uint32_t>(quarter) << 21);
+        const float f = second ? 1.0f : p.scale;
+        unsigned char* stage = smem + hs * S::kHoldBytes + (KV ? part : 2 * part) * S::kTileBytes;
 #pragma unroll 1
         for (int q = 0; q < DP / 32; ++q) {
           uint32_t o[32];
           if (live) {
             tmem_ld32(acc + 32 * q, o);
-            tmem_wait_ld();
+            tmem_wait_ld32(o);
+          }
+          if (part == 1 && q == DP / 32 - 1) {   // all sums have been read
+            tc_fence_before();
+            __syncwarp();
+            if (leader) mbar_arrive(acc_free);
           }
 #pragma unroll
           for (int i = 0; i < 32; ++i) o[i] = some ? __float_as_uint(__uint_as_float(o[i]) * f) : 0u;
-          if (KV && p.splits > 1) {
+          if (parts) {
             if (row < p.kv_len) {
-              float* to = p.partial + (((static_cast<long long>(w.split) * 2 + part) * p.batch + w.b) * p.kv_heads + w.h) * static_cast<long long>(p.kv_len) * p.head_dim +
-                          static_cast<long long>(row) * p.head_dim + 32 * q;
 #pragma unroll
               for (int i = 0; i < 8; ++i)
-                if (32 * q + 4 * i < p.head_dim) *reinterpret_cast<uint4*>(to + 4 * i) = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                if (32 * q + 4 * i < p.head_dim) *reinterpret_cast<uint4*>(sums_to + 32 * q + 4 * i) = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
             }
           } else {
 #pragma unroll
@@ -549,23 +567,19 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
             }
           }
         }
-        if (!(KV && p.splits > 1)) {
+        if (!parts) {
           fence_proxy_async();
           __syncwarp();
-          if (leader) {
-            const int first = tile0 + quarter * 32;
-            if (first < rows_all)
-              for (int i = 0; i < S::kSlabs; ++i)
-                tma_store_4d(part ? &o2_map : &o1_map, smem_u32(stage) + i * kTile * 128 + quarter * 32 * 128, i * kSlabCols, first, w.h, w.b);
+          const int first = row - static_cast<int>(lane_id());
+          if (leader && first < rows_all) {
+            for (int i = 0; i < S::kSlabs; ++i)
+              tma_store_4d(second ? &o2_map : &o1_map, smem_u32(stage) + i * kTile * 128 + quarter * 32 * 128, i * kSlabCols, first, w.h, w.b);
             bulk_commit();
           }
           __syncwarp();
         }
       }
-      tc_fence_before();
-      __syncwarp();
       if (leader && ok) {
-        mbar_arrive(acc_free);
         bulk_wait_read();
         mbar_arrive(hold_empty + 8 * hs);
       }
@@ -575,7 +589,7 @@ attention_grad_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_co
   __syncwarp();                                  // (the roles of one lane end here; the barriers take whole warps)
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == kProductWarp) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
