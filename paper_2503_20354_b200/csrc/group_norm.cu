@@ -7,7 +7,8 @@
 // z is computed with the same roundings in both directions, a rounding per operation, so that ReLU's slope is that of the sign the
 // forward pass saw.
 //
-// Three steps: sums of a chunk of positions per channel, sums of the chunks per group, the outputs.  In the first and the last a
+// Images of which a CTA holds whole groups in registers (up to 4096 vectors of 16 bytes): one kernel, x is read once.
+// Others in three steps: sums of a chunk of positions per channel, sums of the chunks per group, the outputs.  In the first and the last a
 // thread keeps its vector of channels, so that their parameters stay in registers, and walks down the positions.
 // The last step takes the chunks in the opposite order: what the first read last is still in L2.
 #include "linear.cuh"
@@ -539,6 +540,117 @@ group_grad_apply_kernel(const void* x, const void* dy, void* dx, const float* st
   }
 }
 
+// ---- forward in one kernel: a CTA holds all positions of some groups of an image, kHeld vectors a thread ----
+constexpr int kHeld = 8, kHeldThreads = 512;
+struct Held {
+  int sets, channels, vectors, lanes;            // sets of groups of an image; channels and vectors of a set; positions that a CTA takes at once
+  int in_set, team;                              // groups of a set, and threads that add up one of them (a power of two)
+  FastDiv by_group;                              // per_group
+};
+
+// Sums of every group of the set, of a number for each channel and lane that is in buf [lanes][channels]; thread i gets the i-th group's, in a
+// fixed order.
+__device__ __forceinline__ double held_sum(const float* buf, double* part, const Held& s, int per_group) {
+  const int team = static_cast<int>(threadIdx.x) / s.team, in_team = static_cast<int>(threadIdx.x) - team * s.team;
+  double sum = 0.0;
+  if (team < s.in_set) {
+    float f = 0.0f;
+    for (int i = in_team; i < s.lanes * per_group; i += s.team) {
+      const int l = static_cast<int>(divide(i, s.by_group));
+      f += buf[l * s.channels + team * per_group + (i - l * per_group)];
+    }
+    sum = f;
+  }
+  const int width = s.team < 32 ? s.team : 32;
+  for (int o = width / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+  if (in_team % width == 0) part[threadIdx.x / width] = sum;
+  __syncthreads();
+  sum = 0.0;
+  const int i = static_cast<int>(threadIdx.x);
+  if (i < s.in_set)
+    for (int k = 0; k < s.team / width; ++k) sum += part[i * (s.team / width) + k];
+  return sum;
+}
+
+template <int DT, int E, int ACT>
+__global__ void __launch_bounds__(kHeldThreads)
+group_held_kernel(const void* x, void* y, float* stats, int images, const float* gamma, const float* beta, float eps, const Held s, const Geometry g) {
+  extern __shared__ float s_held[];              // [lanes][channels] numbers, then means and r of the groups
+  __shared__ double s_part[kHeldThreads / 4];
+  pdl_trigger();
+  pdl_wait();
+  const int b = static_cast<int>(blockIdx.x) / s.sets, set = static_cast<int>(blockIdx.x) - b * s.sets;
+  const int col = threadIdx.x % s.vectors, lane = threadIdx.x / s.vectors;
+  const bool on = lane < s.lanes;
+  const long long first = b * g.image + static_cast<long long>(set) * s.channels + static_cast<long long>(col) * E;
+  float* const s_mean = s_held + s.lanes * s.channels;
+  float* const s_r = s_mean + s.in_set;
+  Raw<DT, E> raw[kHeld];
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k)
+    if (on && lane + k * s.lanes < g.positions) raw[k].load(x, first + static_cast<long long>(lane + k * s.lanes) * g.channels);
+  const double n = static_cast<double>(g.positions) * g.per_group;
+  float mean[E], r[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) mean[i] = r[i] = 0.0f;
+  // the mean, then the squares about it
+#pragma unroll 1
+  for (int turn = 0; turn < 2; ++turn) {
+    float sum[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) sum[i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+      if (on && lane + k * s.lanes < g.positions) {
+        float f[E];
+        raw[k].numbers(f);
+#pragma unroll
+        for (int i = 0; i < E; ++i) sum[i] += turn ? (f[i] - mean[i]) * (f[i] - mean[i]) : f[i];
+      }
+    if (on)
+#pragma unroll
+      for (int i = 0; i < E; ++i) s_held[lane * s.channels + col * E + i] = sum[i];
+    __syncthreads();
+    const double total = held_sum(s_held, s_part, s, g.per_group);
+    if (static_cast<int>(threadIdx.x) < s.in_set) {
+      if (turn) s_r[threadIdx.x] = static_cast<float>(1.0 / sqrt(total / n + eps));
+      else s_mean[threadIdx.x] = static_cast<float>(total / n);
+    }
+    __syncthreads();
+    if (on)
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const int at = (col * E + i) / g.per_group;
+        if (turn) r[i] = s_r[at];
+        else mean[i] = s_mean[at];
+      }
+  }
+  if (stats)
+    for (int i = threadIdx.x; i < s.in_set; i += blockDim.x) {
+      const int at = b * g.groups + set * s.in_set + i;
+      stats[at] = s_mean[i];
+      stats[images * g.groups + at] = s_r[i];
+    }
+  if (!on) return;
+  float w[E], o[E];
+  const int channel = set * s.channels + col * E;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    w[i] = gamma ? gamma[channel + i] : 1.0f;
+    o[i] = beta ? beta[channel + i] : 0.0f;
+  }
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k)
+    if (lane + k * s.lanes < g.positions) {
+      float f[E];
+      raw[k].numbers(f);
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        f[i] = gn_activate<ACT>(__fadd_rn(__fmul_rn(__fmul_rn(__fsub_rn(f[i], mean[i]), r[i]), w[i]), o[i]));
+      store_elems<DT, E>(y, first + static_cast<long long>(lane + k * s.lanes) * g.channels, f);
+    }
+}
+
 // ---- host ----
 constexpr int kRounds = 4;
 Geometry geometry(long long batch, long long positions, int channels, int groups, int vec, bool grad) {
@@ -607,6 +719,35 @@ Scratch scratch_of(long long batch, long long positions, int channels, int group
   return s;
 }
 
+// Whether a CTA can hold whole groups, and which: as few as are whole vectors and 64 bytes of a row at least (less makes the memory read
+// lines for nothing), more where they do not fill 512 threads and the SMs have CTAs enough.
+bool held_of(const Geometry& g, long long batch, int vec, Held* out) {
+  Held best = {};
+  for (int n = 1; n <= g.groups && n <= 64; ++n) {
+    if (g.groups % n != 0 || n * g.per_group % vec != 0) continue;
+    Held s = {};
+    s.in_set = n;
+    s.sets = g.groups / n;
+    s.channels = n * g.per_group;
+    s.vectors = s.channels / vec;
+    if (s.vectors > kHeldThreads) break;
+    s.lanes = kHeldThreads / s.vectors;
+    if (s.lanes > g.positions) s.lanes = g.positions;
+    if (static_cast<long long>(s.lanes) * kHeld < g.positions) break;
+    if (best.sets && (best.vectors >= 4 && (best.vectors * best.lanes >= kHeldThreads / 2 || batch * s.sets < 148))) break;
+    best = s;
+  }
+  if (best.sets) {
+    const int threads = (best.vectors * best.lanes + 31) / 32 * 32;
+    best.team = 4;
+    while (best.team * 2 * best.in_set <= threads) best.team *= 2;
+    best.by_group = make_div(static_cast<uint32_t>(g.per_group));
+    if (best.team * best.in_set > threads) best.sets = 0;        // (more groups than threads for them)
+  }
+  *out = best;
+  return best.sets > 0;
+}
+
 }  // namespace
 
 size_t group_norm_workspace(long long batch, long long positions, int channels, int groups) {
@@ -622,6 +763,20 @@ cudaError_t launch_group_norm(const void* x, long long batch, long long position
   const int e = vector_of(channels, dt, dt), images = static_cast<int>(batch);
   const Geometry g = geometry(batch, positions, channels, groups, e, false);
   const Scratch s = scratch_of(batch, positions, channels, groups, false);
+  Held held;
+  if (held_of(g, batch, e, &held)) {
+#define SURGEON_HELD(ACT)                                                                     \
+  (dt ? (e == 8 ? group_held_kernel<1, 8, ACT> : group_held_kernel<1, 1, ACT>)                \
+      : (e == 4 ? group_held_kernel<0, 4, ACT> : group_held_kernel<0, 1, ACT>))
+    const auto kernel = act == kActNone ? SURGEON_HELD(kActNone) : act == kActRelu ? SURGEON_HELD(kActRelu)
+                        : act == kActGelu ? SURGEON_HELD(kActGelu) : SURGEON_HELD(kActSilu);
+#undef SURGEON_HELD
+    const size_t smem = (static_cast<size_t>(held.lanes) * held.channels + 2 * held.in_set) * sizeof(float);
+    const cudaError_t st = launch_kernel(kernel, dim3(static_cast<unsigned>(batch * held.sets)), dim3((held.vectors * held.lanes + 31) / 32 * 32), smem, stream,
+                                         true, x, y, stats, images, gamma, beta, eps, held, g);
+    note_launches(1);
+    return st;
+  }
   char* ws = static_cast<char*>(workspace);
   float2* partial = reinterpret_cast<float2*>(ws);
   if (!stats) stats = reinterpret_cast<float*>(ws + s.second);
