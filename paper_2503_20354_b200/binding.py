@@ -764,7 +764,7 @@ def attention_desc(batch: int, heads: int, q_len: int, kv_len: int, head_dim: in
                    causal: bool = False, scale: Optional[float] = None) -> AttentionDesc:
     """The descriptor of an attention: ``kv_heads`` (None: ``heads``) divides ``heads``, ``scale`` is head_dim^-1/2 if None."""
     return AttentionDesc(int(batch), int(heads), int(heads if kv_heads is None else kv_heads), int(q_len), int(kv_len), int(head_dim),
-                         1 if causal else 0, 0, float(head_dim) ** -0.5 if scale is None else float(scale))
+                         1 if causal else 0, 0, max(float(head_dim), 1.0) ** -0.5 if scale is None else float(scale))
 
 
 def surgeon_attention_workspace(desc: AttentionDesc) -> int:

@@ -183,6 +183,7 @@ bool view_of(const surgeon_heads* t, int64_t batch, int64_t rows, int64_t heads,
 }
 // Whether every element has a place of its own.
 bool injective(const View& v) {
+  if (v.empty()) return true;
   int64_t span = v.dim;
   bool used[3] = {v.n[0] == 1, v.n[1] == 1, v.n[2] == 1};
   for (;;) {
