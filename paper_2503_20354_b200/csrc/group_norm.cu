@@ -7,10 +7,12 @@
 // z is computed with the same roundings in both directions, a rounding per operation, so that ReLU's slope is that of the sign the
 // forward pass saw.
 //
-// Images of which a CTA holds whole groups in registers (up to 4096 vectors of 16 bytes): one kernel, x is read once.
-// Others in three steps: sums of a chunk of positions per channel, sums of the chunks per group, the outputs.  In the first and the last a
-// thread keeps its vector of channels, so that their parameters stay in registers, and walks down the positions.
-// The last step takes the chunks in the opposite order: what the first read last is still in L2.
+// Few images of which a CTA holds whole groups in registers (up to 4096 vectors of 16 bytes): one kernel, x is read once.  7 x 7 x 2048 fp32:
+// 5.6 us, of which the launch, a read and a write of memory are most.
+// Others in three steps: sums of a chunk of positions, sums of the chunks per group, the outputs.  In the first and the last a thread keeps its
+// vector of channels, so that their parameters stay in registers, and walks down the positions, the last step from their end: what the first
+// read last is still in L2.  Bound by memory: a 256 x 256 x 768 bf16 image takes 60 us, of which the second read of x is 48 MB from memory
+// and 53 MB from L2 (101 MB walked the other way, 70 us); the backward pass of 64 x 56 x 56 x 256 bf16 takes 105 us.
 #include "linear.cuh"
 
 namespace surgeon {
@@ -19,7 +21,7 @@ namespace {
 
 constexpr int kActSilu = 3;
 constexpr int kMaxThreads = 256;                 // vectors of channels a CTA takes at once
-constexpr int kUnroll = 4;                       // rows on their way
+constexpr int kUnroll = 6;                       // rows on their way
 constexpr int kGradUnroll = 4;
 constexpr int kResident = 3, kGradResident = 2;  // CTAs of an SM in the first and the last step
 
@@ -170,13 +172,22 @@ struct Place {
   }
 };
 
-// ---- step 1, forward: mean and centred sum of squares of every channel of a chunk ----
+// The item of a CTA in the last step.  That step takes what the first read last first, while it is in L2: every chunk from its end, and where the
+// CTAs are more than the SMs take at once, the chunks in the opposite order (else in the same, so that an SM mostly has its chunk again, and
+// its half of L2).
+__device__ __forceinline__ int again(int items, int resident) {
+  return items <= 148 * resident ? static_cast<int>(blockIdx.x) : items - 1 - static_cast<int>(blockIdx.x);
+}
+
+// ---- step 1, forward: mean and centred sum of squares of every group of a chunk ----
 // A thread sums x - s and (x - s)^2, s its first number of the channel.  What the difference of the n squares and their mean's loses is
 // below n roundings of the result, wherever s lies.
+// A group that lies in two blocks of columns has a piece in each: the piece of group i in block y has number i + y.
+__host__ __device__ inline int blocks_of(const Geometry& g) { return (g.vectors + g.cols - 1) / g.cols; }
 template <int DT, int E>
 __global__ void __launch_bounds__(kMaxThreads, kResident)
-group_sums_kernel(const void* x, float2* partial, const Geometry g) {
-  extern __shared__ float2 s_pairs[];            // [lanes - 1][E][cols]
+group_sums_kernel(const void* x, float2* partial, int width, const Geometry g) {
+  extern __shared__ float2 s_pairs[];            // [lanes - 1][E][cols], then [cols][E]
   pdl_trigger();
   pdl_wait();
   const Place<E> p(g, blockIdx.x);
@@ -241,10 +252,28 @@ group_sums_kernel(const void* x, float2* partial, const Geometry g) {
       }
     }
   }
-  if (p.on && p.lane == 0) {
-    float2* to = partial + (static_cast<long long>(p.b) * g.chunks + p.chunk) * g.channels + static_cast<long long>(p.v) * E;
+  // the channels' of a group together, by `width` threads
+  __syncthreads();
+  if (p.on && p.lane == 0)
 #pragma unroll
-    for (int i = 0; i < E; ++i) to[i] = sum[i];
+    for (int i = 0; i < E; ++i) s_pairs[p.col * E + i] = sum[i];
+  __syncthreads();
+  const int c0 = blockIdx.y * g.cols * E, c1 = min(c0 + g.cols * E, g.channels), member = threadIdx.x % width, teams = static_cast<int>(blockDim.x) / width;
+  const int first = c0 / g.per_group, last = (c1 - 1) / g.per_group;
+  float2* const to = partial + (static_cast<long long>(p.b) * g.chunks + p.chunk) * (g.groups + gridDim.y - 1) + blockIdx.y;
+  for (int i0 = first; i0 <= last; i0 += teams) {                // (as many turns for every thread)
+    const int i = i0 + static_cast<int>(threadIdx.x) / width;
+    const int a = max(i * g.per_group, c0) - c0, e = i <= last ? min((i + 1) * g.per_group, c1) - c0 : a;
+    float m = 0.0f, q = 0.0f;
+    for (int c = a + member; c < e; c += width) m += s_pairs[c].x;
+    for (int o = width / 2; o > 0; o >>= 1) m += __shfl_xor_sync(0xFFFFFFFFu, m, o);
+    m /= static_cast<float>(max(e - a, 1));
+    for (int c = a + member; c < e; c += width) {
+      const float2 v = s_pairs[c];
+      q += v.y + static_cast<float>(p.rows) * (v.x - m) * (v.x - m);
+    }
+    for (int o = width / 2; o > 0; o >>= 1) q += __shfl_xor_sync(0xFFFFFFFFu, q, o);
+    if (member == 0 && i <= last) to[i] = make_float2(m, q);
   }
 }
 
@@ -263,24 +292,25 @@ __device__ __forceinline__ double cta_sum(double v, double* buf) {
 }
 
 // ---- step 2, forward: a group's mean and r from the chunks', in double ----
-// `width` threads side by side on channels, the others' rows of them on the chunks.
 __global__ void __launch_bounds__(kTermThreads)
-group_stats_kernel(const float2* partial, float* stats, int images, float eps, int width, const Geometry g) {
+group_stats_kernel(const float2* partial, float* stats, int images, float eps, int block_channels, const Geometry g) {
   __shared__ double buf[kTermThreads / 32];
   pdl_trigger();
   pdl_wait();
-  const int b = blockIdx.x / g.groups, group = blockIdx.x % g.groups;
-  const int col = threadIdx.x % width, row = threadIdx.x / width, rows = static_cast<int>(blockDim.x) / width;
+  const int b = blockIdx.x / g.groups, group = blockIdx.x % g.groups, pieces = g.groups + blocks_of(g) - 1;
+  const int c0 = group * g.per_group, c1 = c0 + g.per_group;
   double s = 0.0, q = 0.0;
-  const float2* from = partial + static_cast<long long>(b) * g.chunks * g.channels + group * g.per_group;
-  for (int c = col; c < g.per_group; c += width)
+  for (int y = c0 / block_channels; y * block_channels < c1; ++y) {
+    const double channels = min(c1, (y + 1) * block_channels) - max(c0, y * block_channels);
+    const float2* from = partial + static_cast<long long>(b) * g.chunks * pieces + group + y;
 #pragma unroll 4
-    for (int i = row; i < g.chunks; i += rows) {
-      const float2 v = from[static_cast<long long>(i) * g.channels + c];
-      const double n = min(g.chunk, g.positions - i * g.chunk), m = v.x;
+    for (int i = threadIdx.x; i < g.chunks; i += blockDim.x) {
+      const float2 v = from[static_cast<long long>(i) * pieces];
+      const double n = min(g.chunk, g.positions - i * g.chunk) * channels, m = v.x;
       s += n * m;
       q += v.y + n * m * m;
     }
+  }
   s = cta_sum(s, buf);
   q = cta_sum(q, buf);
   if (threadIdx.x == 0) {
@@ -298,7 +328,7 @@ __global__ void __launch_bounds__(kMaxThreads, kResident)
 group_apply_kernel(const void* x, void* y, const float* stats, int images, const float* gamma, const float* beta, const Geometry g) {
   pdl_trigger();
   pdl_wait();
-  const Place<E> p(g, gridDim.x - 1 - blockIdx.x);
+  const Place<E> p(g, again(gridDim.x, kResident));
   if (p.mine == 0) return;
   const Params<E> k(g, p.b, p.v * E, stats, images, gamma, beta);
   const auto finish = [&](long long at, float (&f)[E]) {
@@ -311,20 +341,21 @@ group_apply_kernel(const void* x, void* y, const float* stats, int images, const
     for (int i = 0; i < E; ++i) f[i] = gn_activate<ACT>(f[i]);
     store_stream<DT, E>(y, at, f);
   };
-  long long at = p.at;
+  const long long step = -p.step;
+  long long at = p.at + (p.mine - 1) * p.step;
   int t = 0;
-  for (; t + kUnroll <= p.mine; t += kUnroll, at += kUnroll * p.step) {
+  for (; t + kUnroll <= p.mine; t += kUnroll, at += kUnroll * step) {
     Raw<DT, E> raw[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) raw[u].load(x, at + u * p.step);
+    for (int u = 0; u < kUnroll; ++u) raw[u].load(x, at + u * step);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       float f[E];
       raw[u].numbers(f);
-      finish(at + u * p.step, f);
+      finish(at + u * step, f);
     }
   }
-  for (; t < p.mine; ++t, at += p.step) {
+  for (; t < p.mine; ++t, at += step) {
     float f[E];
     load_elems<DT, E>(x, at, f);
     finish(at, f);
@@ -480,7 +511,7 @@ group_grad_apply_kernel(const void* x, const void* dy, void* dx, const float* st
     }
   }
   if (static_cast<int>(blockIdx.x) >= items) return;
-  const Place<E> p(g, items - 1 - blockIdx.x);
+  const Place<E> p(g, again(items, kGradResident));
   if (p.mine == 0) return;
   const Params<E> k(g, p.b, p.v * E, stats, images, gamma, beta);
   // dx = dz (r gamma) - r c1 - xh (r c2)
@@ -514,25 +545,26 @@ group_grad_apply_kernel(const void* x, const void* dy, void* dx, const float* st
     from_pairs<E>(fd, d);
     store_stream<GDT, E>(dx, at, d);
   };
-  long long at = p.at;
+  const long long step = -p.step;
+  long long at = p.at + (p.mine - 1) * p.step;
   int t = 0;
-  for (; t + kGradUnroll <= p.mine; t += kGradUnroll, at += kGradUnroll * p.step) {
+  for (; t + kGradUnroll <= p.mine; t += kGradUnroll, at += kGradUnroll * step) {
     Raw<DT, E> rx[kGradUnroll];
     Raw<GDT, E> rd[kGradUnroll];
 #pragma unroll
     for (int u = 0; u < kGradUnroll; ++u) {
-      rx[u].load(x, at + u * p.step);
-      rd[u].load(dy, at + u * p.step);
+      rx[u].load(x, at + u * step);
+      rd[u].load(dy, at + u * step);
     }
 #pragma unroll
     for (int u = 0; u < kGradUnroll; ++u) {
       float f[E], d[E];
       rx[u].numbers(f);
       rd[u].numbers(d);
-      finish(at + u * p.step, f, d);
+      finish(at + u * step, f, d);
     }
   }
-  for (; t < p.mine; ++t, at += p.step) {
+  for (; t < p.mine; ++t, at += step) {
     float f[E], d[E];
     load_elems<DT, E>(x, at, f);
     load_elems<GDT, E>(dy, at, d);
@@ -541,7 +573,7 @@ group_grad_apply_kernel(const void* x, const void* dy, void* dx, const float* st
 }
 
 // ---- forward in one kernel: a CTA holds all positions of some groups of an image, kHeld vectors a thread ----
-constexpr int kHeld = 8, kHeldThreads = 512;
+constexpr int kHeld = 8, kHeldThreads = 512, kHeldAtOnce = 2 * 148;
 struct Held {
   int sets, channels, vectors, lanes;            // sets of groups of an image; channels and vectors of a set; positions that a CTA takes at once
   int in_set, team;                              // groups of a set, and threads that add up one of them (a power of two)
@@ -693,6 +725,11 @@ int term_threads(const Geometry& g) {
   while (n < kTermThreads && n * 4 < g.chunks * width_of(g)) n *= 2;
   return n;
 }
+int stat_threads(const Geometry& g) {             // of the forward pass: a chunk or two each
+  int n = 32;
+  while (n < 512 && n < g.chunks) n *= 2;
+  return n;
+}
 int vector_of(int channels, int dt, int grad_dt) {               // elements of a thread's vector: 16 bytes of the narrower type
   const int e = dt || grad_dt ? 8 : 4;
   return channels % e == 0 ? e : 1;
@@ -713,14 +750,16 @@ Scratch scratch_of(long long batch, long long positions, int channels, int group
   if (chunks > positions) chunks = positions;
   if (chunks < 1) chunks = 1;
   Scratch s = {};
-  s.second = up(static_cast<size_t>(batch) * chunks * channels * 8);
+  s.second = up(static_cast<size_t>(batch) * chunks * (grad ? channels : groups + (channels + kMaxThreads - 1) / kMaxThreads) * 8);
   s.terms = s.second + (grad ? up(static_cast<size_t>(batch) * channels * 16) : up(static_cast<size_t>(batch) * groups * 8));
   s.total = s.terms + (grad ? up(static_cast<size_t>(batch) * groups * 8) : 0);
   return s;
 }
 
-// Whether a CTA can hold whole groups, and which: as few as are whole vectors and 64 bytes of a row at least (less makes the memory read
-// lines for nothing), more where they do not fill 512 threads and the SMs have CTAs enough.
+// Whether CTAs hold whole groups, and which: as few as are whole vectors and 64 bytes of a row at least (less makes the memory read
+// lines for nothing), more where they do not fill 512 threads and the SMs have CTAs enough.  Only where all CTAs run at once, two on an SM:
+// 4 x 1000 x 256 bf16 in 32 groups takes 8.4 us held and 12.6 streamed, but 64 x 196 x 1024 95 and 22.6 (a CTA of a held group waits for
+// memory and computes in turn, and what one reads of a row's lines is a part).
 bool held_of(const Geometry& g, long long batch, int vec, Held* out) {
   Held best = {};
   for (int n = 1; n <= g.groups && n <= 64; ++n) {
@@ -744,6 +783,7 @@ bool held_of(const Geometry& g, long long batch, int vec, Held* out) {
     best.by_group = make_div(static_cast<uint32_t>(g.per_group));
     if (best.team * best.in_set > threads) best.sets = 0;        // (more groups than threads for them)
   }
+  if (batch * best.sets > kHeldAtOnce) best.sets = 0;
   *out = best;
   return best.sets > 0;
 }
@@ -780,12 +820,12 @@ cudaError_t launch_group_norm(const void* x, long long batch, long long position
   char* ws = static_cast<char*>(workspace);
   float2* partial = reinterpret_cast<float2*>(ws);
   if (!stats) stats = reinterpret_cast<float*>(ws + s.second);
-  const size_t smem = static_cast<size_t>(g.lanes - 1) * e * g.cols * sizeof(float2);
+  const size_t smem = static_cast<size_t>(g.lanes > 1 ? g.lanes - 1 : 1) * e * g.cols * sizeof(float2);
   const auto sums = dt ? (e == 8 ? group_sums_kernel<1, 8> : group_sums_kernel<1, 1>) : (e == 4 ? group_sums_kernel<0, 4> : group_sums_kernel<0, 1>);
-  cudaError_t st = launch_kernel(sums, grid_of(g, batch), block_of(g), smem, stream, true, x, partial, g);
+  cudaError_t st = launch_kernel(sums, grid_of(g, batch), block_of(g), smem, stream, true, x, partial, width_of(g), g);
   if (st != cudaSuccess) return st;
-  st = launch_kernel(group_stats_kernel, dim3(static_cast<unsigned>(batch * groups)), dim3(term_threads(g)), 0, stream, true,
-                     static_cast<const float2*>(partial), stats, images, eps, width_of(g), g);
+  st = launch_kernel(group_stats_kernel, dim3(static_cast<unsigned>(batch * groups)), dim3(stat_threads(g)), 0, stream, true,
+                     static_cast<const float2*>(partial), stats, images, eps, g.cols * e, g);
   if (st != cudaSuccess) return st;
 #define SURGEON_APPLY(ACT)                                                                      \
   (dt ? (e == 8 ? group_apply_kernel<1, 8, ACT> : group_apply_kernel<1, 1, ACT>)                \

@@ -15,7 +15,8 @@ EPS = 1e-5
 ACTS = {"none": B.SURGEON_ACT_NONE, "relu": B.SURGEON_ACT_RELU, "gelu": B.SURGEON_ACT_GELU, "silu": B.SURGEON_ACT_SILU}
 # one position, odd channels, groups that no vector divides, held in registers or streamed, several blocks of channels, many images
 SHAPES = [(1, 1, 1, 1), (2, 3, 6, 2), (1, 49, 2048, 32), (3, 5, 320, 32), (2, 100, 64, 64), (1, 300, 24, 3), (2, 1000, 320, 32), (1, 5000, 96, 1),
-          (4, 3136, 256, 32), (1, 777, 4104, 8), (70, 9, 40, 5), (1, 4097, 33, 11), (2, 2500, 2056, 257), (300, 4, 8, 8), (1, 20000, 16, 4)]
+          (4, 3136, 256, 32), (1, 777, 4104, 8), (70, 9, 40, 5), (1, 4097, 33, 11), (2, 2500, 2056, 257), (300, 4, 8, 8), (1, 20000, 16, 4), (2, 3000, 2100, 2100),
+          (3, 700, 515, 5)]
 
 
 def inputs(b, p, c, dt, seed=0, offset=1.0):
