@@ -10,9 +10,9 @@
 // Few images of which a CTA holds whole groups in registers (up to 4096 vectors of 16 bytes): one kernel, x is read once.  7 x 7 x 2048 fp32:
 // 5.6 us, of which the launch, a read and a write of memory are most.
 // Others in three steps: sums of a chunk of positions, sums of the chunks per group, the outputs.  In the first and the last a thread keeps its
-// vector of channels, so that their parameters stay in registers, and walks down the positions, the last step from their end: what the first
+// vector of channels, so that their parameters stay in registers, and walks down the positions, copies of five rows ahead, the last step from their end: what the first
 // read last is still in L2.  Bound by memory: a 256 x 256 x 768 bf16 image takes 60 us, of which the second read of x is 48 MB from memory
-// and 53 MB from L2 (101 MB walked the other way, 70 us); the backward pass of 64 x 56 x 56 x 256 bf16 takes 105 us.
+// and 53 MB from L2 (101 MB walked the other way, 70 us); the backward pass of 64 x 56 x 56 x 256 bf16 takes 87 us (105 with four rows on their way to registers).
 #include "linear.cuh"
 
 namespace surgeon {
@@ -21,9 +21,9 @@ namespace {
 
 constexpr int kActSilu = 3;
 constexpr int kMaxThreads = 256;                 // vectors of channels a CTA takes at once
-constexpr int kUnroll = 6;                       // rows on their way
-constexpr int kGradUnroll = 4;
-constexpr int kResident = 3, kGradResident = 2;  // CTAs of an SM in the first and the last step
+constexpr int kAhead = 6;                        // places of shared memory for a thread's rows
+constexpr int kUnroll = 4;                       // rows on their way to registers, where vectors are of one element
+constexpr int kResident = 4, kGradResident = 2;  // CTAs of an SM in the first and the last step
 
 // A vector as it lies in memory: E elements of type DT, 16 bytes of the narrower type of a call.
 template <int DT, int E> struct Raw {
@@ -172,6 +172,104 @@ struct Place {
   }
 };
 
+// A thread's walk over its rows of x, and of dy (TWO): copies of kAhead - 1 rows are on their way to places of shared memory that are the
+// thread's own, so that nothing but its own copies is waited for, and no register holds what has not arrived.
+template <int DT, int GDT, int E, bool TWO>
+struct Walk {
+  static constexpr int kX = sizeof(Raw<DT, E>) / 16, kD = TWO ? sizeof(Raw<GDT, E>) / 16 : 0;
+  static constexpr uint32_t kVector = kMaxThreads * 16, kRow = (kX + kD) * kVector;                // bytes of a CTA's vectors, of its rows
+  static constexpr size_t kPlaces = E == 1 ? 0 : kAhead * kRow;
+  const char *x, *dy;
+  long long at, step;
+  int mine;
+  uint32_t place;
+  __device__ __forceinline__ void issue(int t, uint32_t to) {
+    if (t < mine) {
+#pragma unroll
+      for (int i = 0; i < kX; ++i) copy(to + i * kVector, x + 16 * i);
+      x += step * (DT ? 2 : 4);
+      if constexpr (TWO) {
+#pragma unroll
+        for (int i = 0; i < kD; ++i) copy(to + (kX + i) * kVector, dy + 16 * i);
+        dy += step * (GDT ? 2 : 4);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  static __device__ __forceinline__ void copy(uint32_t to, const char* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+  }
+  // From element `from` in steps of `by`, `rows` times.
+  __device__ __forceinline__ Walk(const void* x_, const void* dy_, long long from, long long by, int rows, void* ring)
+      : x(static_cast<const char*>(x_)), dy(static_cast<const char*>(dy_)), at(from), step(by), mine(rows) {
+    if constexpr (E > 1) {
+      x += at * (DT ? 2 : 4);
+      if constexpr (TWO) dy += at * (GDT ? 2 : 4);
+      place = static_cast<uint32_t>(__cvta_generic_to_shared(ring)) + threadIdx.x * 16;
+#pragma unroll 1
+      for (int t = 0; t < kAhead - 1; ++t) issue(t, place + t * kRow);
+    }
+  }
+  // f(the row's first element, numbers of x, of dy)
+  template <class F>
+  __device__ __forceinline__ void run(F&& f) {
+    if constexpr (E > 1) {
+      constexpr int kHalf = kAhead / 2;
+      uint32_t half = 0;
+#pragma unroll 1
+      for (int t = 0; t < mine; t += kHalf, half = kHalf * kRow - half)
+#pragma unroll
+        for (int u = 0; u < kHalf; ++u) {
+          if (t + u >= mine) break;
+          asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 2) : "memory");
+          Raw<DT, E> rx;
+          Raw<GDT, E> rd;
+          const uint32_t from = place + half + u * kRow;
+#pragma unroll
+          for (int i = 0; i < kX; ++i) rx.v[i] = held(from + i * kVector);
+#pragma unroll
+          for (int i = 0; i < kD; ++i) rd.v[i] = held(from + (kX + i) * kVector);
+          // (into the place whose numbers have been read a row ago)
+          issue(t + u + kAhead - 1, u ? from - kRow : place + (kHalf * kRow - half) + (kHalf - 1) * kRow);
+          float a[E], d[E];
+          rx.numbers(a);
+          if constexpr (TWO) rd.numbers(d);
+          f(at, a, d);
+          at += step;
+        }
+    } else {
+      int t = 0;
+      for (; t + kUnroll <= mine; t += kUnroll, at += kUnroll * step) {
+        Raw<DT, E> rx[kUnroll];
+        Raw<GDT, E> rd[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+          rx[u].load(x, at + u * step);
+          if constexpr (TWO) rd[u].load(dy, at + u * step);
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+          float a[E], d[E];
+          rx[u].numbers(a);
+          if constexpr (TWO) rd[u].numbers(d);
+          f(at + u * step, a, d);
+        }
+      }
+      for (; t < mine; ++t, at += step) {
+        float a[E], d[E];
+        load_elems<DT, E>(x, at, a);
+        if constexpr (TWO) load_elems<GDT, E>(dy, at, d);
+        f(at, a, d);
+      }
+    }
+  }
+  static __device__ __forceinline__ uint4 held(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+  }
+};
+
 // The item of a CTA in the last step.  That step takes what the first read last first, while it is in L2: every chunk from its end, and where the
 // CTAs are more than the SMs take at once, the chunks in the opposite order (else in the same, so that an SM mostly has its chunk again, and
 // its half of L2).
@@ -187,42 +285,26 @@ __host__ __device__ inline int blocks_of(const Geometry& g) { return (g.vectors 
 template <int DT, int E>
 __global__ void __launch_bounds__(kMaxThreads, kResident)
 group_sums_kernel(const void* x, float2* partial, int width, const Geometry g) {
-  extern __shared__ float2 s_pairs[];            // [lanes - 1][E][cols], then [cols][E]
-  pdl_trigger();
+  extern __shared__ __align__(16) unsigned char s_rows[];        // the walk's places, behind it [lanes - 1][E][cols], then [cols][E]
+  float2* const s_pairs = reinterpret_cast<float2*>(s_rows);
   pdl_wait();
+  pdl_trigger();                                 // (here, so that the last step may read x before this one ends)
   const Place<E> p(g, blockIdx.x);
   float2 sum[E];
 #pragma unroll
   for (int i = 0; i < E; ++i) sum[i] = make_float2(0.0f, 0.0f);
   if (p.mine > 0) {
+    Walk<DT, 0, E, false> walk(x, nullptr, p.at, p.step, p.mine, s_rows);
     float shift[E];
     load_elems<DT, E>(x, p.at, shift);
-    const auto add = [&](const float (&f)[E]) {
+    walk.run([&](long long, const float (&f)[E], const float (&)[E]) {
 #pragma unroll
       for (int i = 0; i < E; ++i) {
         const float d = f[i] - shift[i];
         sum[i].x += d;
         sum[i].y = fmaf(d, d, sum[i].y);
       }
-    };
-    long long at = p.at;
-    int t = 0;
-    for (; t + kUnroll <= p.mine; t += kUnroll, at += kUnroll * p.step) {
-      Raw<DT, E> raw[kUnroll];
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) raw[u].load(x, at + u * p.step);
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        float f[E];
-        raw[u].numbers(f);
-        add(f);
-      }
-    }
-    for (; t < p.mine; ++t, at += p.step) {
-      float f[E];
-      load_elems<DT, E>(x, at, f);
-      add(f);
-    }
+    });
     const float inv = 1.0f / static_cast<float>(p.mine);
 #pragma unroll
     for (int i = 0; i < E; ++i) {
@@ -230,6 +312,7 @@ group_sums_kernel(const void* x, float2* partial, int width, const Geometry g) {
       sum[i] = make_float2(shift[i] + m, sum[i].y - sum[i].x * m);
     }
   }
+  __syncthreads();
   if (g.lanes > 1) {                             // (Chan, Golub and LeVeque's update, lane by lane)
     if (p.on && p.lane > 0)
 #pragma unroll
@@ -326,12 +409,14 @@ group_stats_kernel(const float2* partial, float* stats, int images, float eps, i
 template <int DT, int E, int ACT>
 __global__ void __launch_bounds__(kMaxThreads, kResident)
 group_apply_kernel(const void* x, void* y, const float* stats, int images, const float* gamma, const float* beta, const Geometry g) {
+  extern __shared__ __align__(16) unsigned char s_rows[];
+  const Place<E> p(g, again(gridDim.x, kResident));
+  Walk<DT, 0, E, false> walk(x, nullptr, p.at + (p.mine - 1) * p.step, -p.step, p.mine, s_rows);
   pdl_trigger();
   pdl_wait();
-  const Place<E> p(g, again(gridDim.x, kResident));
   if (p.mine == 0) return;
   const Params<E> k(g, p.b, p.v * E, stats, images, gamma, beta);
-  const auto finish = [&](long long at, float (&f)[E]) {
+  walk.run([&](long long at, float (&f)[E], const float (&)[E]) {
     uint64_t v[kPairs<E>];
     to_pairs<E>(f, v);
 #pragma unroll
@@ -340,26 +425,7 @@ group_apply_kernel(const void* x, void* y, const float* stats, int images, const
 #pragma unroll
     for (int i = 0; i < E; ++i) f[i] = gn_activate<ACT>(f[i]);
     store_stream<DT, E>(y, at, f);
-  };
-  const long long step = -p.step;
-  long long at = p.at + (p.mine - 1) * p.step;
-  int t = 0;
-  for (; t + kUnroll <= p.mine; t += kUnroll, at += kUnroll * step) {
-    Raw<DT, E> raw[kUnroll];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) raw[u].load(x, at + u * step);
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      float f[E];
-      raw[u].numbers(f);
-      finish(at + u * step, f);
-    }
-  }
-  for (; t < p.mine; ++t, at += step) {
-    float f[E];
-    load_elems<DT, E>(x, at, f);
-    finish(at, f);
-  }
+  });
 }
 
 // ---- step 1, backward: A and B of every channel of a chunk ----
@@ -367,17 +433,19 @@ template <int DT, int GDT, int E, int ACT>
 __global__ void __launch_bounds__(kMaxThreads, kGradResident)
 group_grad_sums_kernel(const void* x, const void* dy, float2* partial, const float* stats, int images, const float* gamma, const float* beta,
                        const Geometry g) {
-  extern __shared__ float2 s_pairs[];
-  pdl_trigger();
+  extern __shared__ __align__(16) unsigned char s_rows[];        // the walk's places, behind it [lanes - 1][E][cols]
+  float2* const s_pairs = reinterpret_cast<float2*>(s_rows);
   pdl_wait();
+  pdl_trigger();                                 // (here, so that the last step may read x and dy before this one ends)
   const Place<E> p(g, blockIdx.x);
   float2 sum[E];
 #pragma unroll
   for (int i = 0; i < E; ++i) sum[i] = make_float2(0.0f, 0.0f);
   if (p.mine > 0) {
+    Walk<DT, GDT, E, true> walk(x, dy, p.at, p.step, p.mine, s_rows);
     const Params<E> k(g, p.b, p.v * E, stats, images, gamma, beta);
     uint64_t a[kPairs<E>] = {}, b[kPairs<E>] = {};
-    const auto add = [&](const float (&f)[E], const float (&d)[E]) {
+    walk.run([&](long long, const float (&f)[E], const float (&d)[E]) {
       uint64_t fx[kPairs<E>], fd[kPairs<E>];
       to_pairs<E>(f, fx);
       to_pairs<E>(d, fd);
@@ -387,37 +455,14 @@ group_grad_sums_kernel(const void* x, const void* dy, float2* partial, const flo
         a[i] = add2(a[i], dz);
         b[i] = fma2(dz, xh, b[i]);
       }
-    };
-    long long at = p.at;
-    int t = 0;
-    for (; t + kGradUnroll <= p.mine; t += kGradUnroll, at += kGradUnroll * p.step) {
-      Raw<DT, E> rx[kGradUnroll];
-      Raw<GDT, E> rd[kGradUnroll];
-#pragma unroll
-      for (int u = 0; u < kGradUnroll; ++u) {
-        rx[u].load(x, at + u * p.step);
-        rd[u].load(dy, at + u * p.step);
-      }
-#pragma unroll
-      for (int u = 0; u < kGradUnroll; ++u) {
-        float f[E], d[E];
-        rx[u].numbers(f);
-        rd[u].numbers(d);
-        add(f, d);
-      }
-    }
-    for (; t < p.mine; ++t, at += p.step) {
-      float f[E], d[E];
-      load_elems<DT, E>(x, at, f);
-      load_elems<GDT, E>(dy, at, d);
-      add(f, d);
-    }
+    });
     float fa[E], fb[E];
     from_pairs<E>(a, fa);
     from_pairs<E>(b, fb);
 #pragma unroll
     for (int i = 0; i < E; ++i) sum[i] = make_float2(fa[i], fb[i]);
   }
+  __syncthreads();
   if (g.lanes > 1) {
     if (p.on && p.lane > 0)
 #pragma unroll
@@ -495,6 +540,10 @@ template <int DT, int GDT, int E, int ACT>
 __global__ void __launch_bounds__(kMaxThreads, kGradResident)
 group_grad_apply_kernel(const void* x, const void* dy, void* dx, const float* stats, const float2* terms, int images, const float* gamma,
                         const float* beta, const Columns cols, int items, const Geometry g) {
+  extern __shared__ __align__(16) unsigned char s_rows[];
+  const bool work = static_cast<int>(blockIdx.x) < items;
+  const Place<E> p(g, work ? again(items, kGradResident) : 0);
+  Walk<DT, GDT, E, true> walk(x, dy, p.at + (p.mine - 1) * p.step, -p.step, work ? p.mine : 0, s_rows);
   pdl_trigger();
   pdl_wait();
   if (blockIdx.y == 0) {
@@ -510,9 +559,7 @@ group_grad_apply_kernel(const void* x, const void* dy, void* dx, const float* st
       if (cols.dgamma) cols.dgamma[c] = static_cast<float>(cols.accumulate ? cols.dgamma[c] + s : s);
     }
   }
-  if (static_cast<int>(blockIdx.x) >= items) return;
-  const Place<E> p(g, again(items, kGradResident));
-  if (p.mine == 0) return;
+  if (!work || p.mine == 0) return;
   const Params<E> k(g, p.b, p.v * E, stats, images, gamma, beta);
   // dx = dz (r gamma) - r c1 - xh (r c2)
   uint64_t scale[kPairs<E>], c1[kPairs<E>], c2[kPairs<E>];
@@ -533,7 +580,7 @@ group_grad_apply_kernel(const void* x, const void* dy, void* dx, const float* st
       c2[i] = mul2(k.r[i], c2[i]);
     }
   }
-  const auto finish = [&](long long at, const float (&f)[E], float (&d)[E]) {
+  walk.run([&](long long at, const float (&f)[E], float (&d)[E]) {
     uint64_t fx[kPairs<E>], fd[kPairs<E>];
     to_pairs<E>(f, fx);
     to_pairs<E>(d, fd);
@@ -544,32 +591,7 @@ group_grad_apply_kernel(const void* x, const void* dy, void* dx, const float* st
     }
     from_pairs<E>(fd, d);
     store_stream<GDT, E>(dx, at, d);
-  };
-  const long long step = -p.step;
-  long long at = p.at + (p.mine - 1) * p.step;
-  int t = 0;
-  for (; t + kGradUnroll <= p.mine; t += kGradUnroll, at += kGradUnroll * step) {
-    Raw<DT, E> rx[kGradUnroll];
-    Raw<GDT, E> rd[kGradUnroll];
-#pragma unroll
-    for (int u = 0; u < kGradUnroll; ++u) {
-      rx[u].load(x, at + u * step);
-      rd[u].load(dy, at + u * step);
-    }
-#pragma unroll
-    for (int u = 0; u < kGradUnroll; ++u) {
-      float f[E], d[E];
-      rx[u].numbers(f);
-      rd[u].numbers(d);
-      finish(at + u * step, f, d);
-    }
-  }
-  for (; t < p.mine; ++t, at += step) {
-    float f[E], d[E];
-    load_elems<DT, E>(x, at, f);
-    load_elems<GDT, E>(dy, at, d);
-    finish(at, f, d);
-  }
+  });
 }
 
 // ---- forward in one kernel: a CTA holds all positions of some groups of an image, kHeld vectors a thread ----
@@ -820,7 +842,8 @@ cudaError_t launch_group_norm(const void* x, long long batch, long long position
   char* ws = static_cast<char*>(workspace);
   float2* partial = reinterpret_cast<float2*>(ws);
   if (!stats) stats = reinterpret_cast<float*>(ws + s.second);
-  const size_t smem = static_cast<size_t>(g.lanes > 1 ? g.lanes - 1 : 1) * e * g.cols * sizeof(float2);
+  const size_t pairs = static_cast<size_t>(g.lanes > 1 ? g.lanes - 1 : 1) * e * g.cols * sizeof(float2);
+  const size_t places = e == 1 ? 0 : static_cast<size_t>(kAhead) * kMaxThreads * 16, smem = pairs > places ? pairs : places;
   const auto sums = dt ? (e == 8 ? group_sums_kernel<1, 8> : group_sums_kernel<1, 1>) : (e == 4 ? group_sums_kernel<0, 4> : group_sums_kernel<0, 1>);
   cudaError_t st = launch_kernel(sums, grid_of(g, batch), block_of(g), smem, stream, true, x, partial, width_of(g), g);
   if (st != cudaSuccess) return st;
@@ -833,7 +856,7 @@ cudaError_t launch_group_norm(const void* x, long long batch, long long position
   const auto apply = act == kActNone ? SURGEON_APPLY(kActNone) : act == kActRelu ? SURGEON_APPLY(kActRelu)
                      : act == kActGelu ? SURGEON_APPLY(kActGelu) : SURGEON_APPLY(kActSilu);
 #undef SURGEON_APPLY
-  st = launch_kernel(apply, grid_of(g, batch), block_of(g), 0, stream, true, x, y, static_cast<const float*>(stats), images, gamma, beta, g);
+  st = launch_kernel(apply, grid_of(g, batch), block_of(g), places, stream, true, x, y, static_cast<const float*>(stats), images, gamma, beta, g);
   note_launches(3);
   return st;
 }
@@ -847,8 +870,12 @@ cudaError_t launch_grad(const void* x, const void* dy, long long batch, const Ge
   double2* sums = reinterpret_cast<double2*>(ws + s.second);
   float2* terms = reinterpret_cast<float2*>(ws + s.terms);
   const int images = static_cast<int>(batch);
-  const size_t smem = static_cast<size_t>(g.lanes - 1) * E * g.cols * sizeof(float2);
-  cudaError_t st = launch_kernel(group_grad_sums_kernel<DT, GDT, E, ACT>, grid_of(g, batch), block_of(g), smem, stream, true, x, dy, partial,
+  const size_t pairs = static_cast<size_t>(g.lanes - 1) * E * g.cols * sizeof(float2);
+  const size_t places = Walk<DT, GDT, E, true>::kPlaces, smem = pairs > places ? pairs : places;
+  cudaError_t st = allow_dynamic_smem(reinterpret_cast<const void*>(group_grad_sums_kernel<DT, GDT, E, ACT>), static_cast<int>(smem));
+  if (st == cudaSuccess) st = allow_dynamic_smem(reinterpret_cast<const void*>(group_grad_apply_kernel<DT, GDT, E, ACT>), static_cast<int>(places));
+  if (st != cudaSuccess) return st;
+  st = launch_kernel(group_grad_sums_kernel<DT, GDT, E, ACT>, grid_of(g, batch), block_of(g), smem, stream, true, x, dy, partial,
                                  stats, images, gamma, beta, g);
   if (st != cudaSuccess) return st;
   st = launch_kernel(group_grad_terms_kernel, dim3(static_cast<unsigned>(batch * g.groups)), dim3(term_threads(g)), 0, stream, true,
@@ -859,7 +886,7 @@ cudaError_t launch_grad(const void* x, const void* dy, long long batch, const Ge
   if (!dx) grid = dim3((g.channels + block_of(g).x - 1) / block_of(g).x);
   Columns c = cols;
   c.sums = sums;
-  st = launch_kernel(group_grad_apply_kernel<DT, GDT, E, ACT>, grid, block_of(g), 0, stream, true, x, dy, dx, stats,
+  st = launch_kernel(group_grad_apply_kernel<DT, GDT, E, ACT>, grid, block_of(g), places, stream, true, x, dy, dx, stats,
                      static_cast<const float2*>(terms), images, gamma, beta, c, items, g);
   note_launches(3);
   return st;
