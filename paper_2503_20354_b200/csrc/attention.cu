@@ -27,7 +27,7 @@ constexpr float kMost = 18446744073709551616.0f;                 // 2^64: what a
 
 template <int DP> struct Shape {                 // DP: head_dim, padded to 64 or 128
   static constexpr int kSlabs = DP / kSlabCols, kTileBytes = kTile * DP * 2, kBlockBytes = kBlock * DP * 2;
-  static constexpr int kQStages = DP == 64 ? 2 : 1, kStages = DP == 64 ? 8 : 4;
+  static constexpr int kQStages = DP == 64 ? 2 : 1, kStages = DP == 64 ? 8 : 5;
   static constexpr bool kOwnP = DP == 64;        // p has columns of its own, else it takes the place of s
   // columns of tensor memory: s of tile t at 128 t
   static constexpr uint32_t kP = DP == 64 ? 256 : 0, kPStep = DP == 64 ? 64 : 128, kO = DP == 64 ? 384 : 256;
@@ -49,7 +49,10 @@ struct Args {
   float* lse;
 };
 
-// PARTS: heads may be packed and keys shared out (few queries); without, neither costs a register.
+// How a kernel takes its rows.  kWhole: a tile of queries of one head, all keys.  kParts: heads may be packed and keys shared out (few queries);
+// the other kernel has no register for either.  kSpread: at most 32 rows (a single token and its heads), four times in the tile, and each
+// quarter of the warps has a quarter of a block's keys: its p of the others' are 0, so that its rows of o are the sums over its own.
+enum { kWhole, kParts, kSpread };
 template <bool PARTS>
 struct Item {
   int b, h, row0, q_valid, kv_valid, off;
@@ -138,11 +141,12 @@ __device__ __noinline__ void scale_row(uint32_t o_at, float f) {
   }
 }
 
-template <int DP, bool PARTS>
+template <int DP, int MODE>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                  const __grid_constant__ CUtensorMap o_map, const __grid_constant__ Args p) {
   using S = Shape<DP>;
+  constexpr bool PARTS = MODE != kWhole, SPREAD = MODE == kSpread;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   unsigned char* ring = smem + 2 * S::kQStages * S::kTileBytes;
@@ -201,11 +205,13 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
           if (PARTS && p.twin && t == 1) {       // (the first tile's queries serve both)
             mbar_arrive(q_full + 8 * at);
           } else if (w.blocks[t] > w.from && (PARTS && p.pack)) {
-            mbar_arrive_expect_tx(q_full + 8 * at, p.group * p.q_rows * 128 * S::kSlabs);
-            for (int g = 0; g < p.group; ++g)
-              for (int c = 0; c < S::kSlabs; ++c)
-                tma_load_4d(smem_u32(smem) + at * S::kTileBytes + c * kTile * 128 + g * p.q_rows * 128, &q_map, c * kSlabCols, 0, w.h * p.group + g, w.b,
-                            q_full + 8 * at);
+            constexpr int kTimes = SPREAD ? 4 : 1;
+            mbar_arrive_expect_tx(q_full + 8 * at, kTimes * p.group * p.q_rows * 128 * S::kSlabs);
+            for (int i = 0; i < kTimes; ++i)
+              for (int g = 0; g < p.group; ++g)
+                for (int c = 0; c < S::kSlabs; ++c)
+                  tma_load_4d(smem_u32(smem) + at * S::kTileBytes + c * kTile * 128 + (32 * i + g * p.q_rows) * 128, &q_map, c * kSlabCols, 0,
+                              w.h * p.group + g, w.b, q_full + 8 * at);
           } else if (w.blocks[t] > w.from) {
             mbar_arrive_expect_tx(q_full + 8 * at, S::kTileBytes);
             for (int c = 0; c < S::kSlabs; ++c)
@@ -350,7 +356,9 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
     // ---- softmax: a thread a row ----
     set_registers<true, kSoftmaxRegs>();
 
-    const int t = warp >> 2, quarter = warp & 3, lane = static_cast<int>(lane_id()), row_in_tile = quarter * 32 + lane;
+    const int t = warp >> 2, quarter = warp & 3, lane = static_cast<int>(lane_id()), row_in_tile = SPREAD ? lane : quarter * 32 + lane;
+    constexpr int kQ = SPREAD ? 1 : 4;           // of the four times 32 keys of a block, those this row takes, from the first-th on
+    const int q0 = SPREAD ? quarter : 0;
     const uint32_t lanes = static_cast<uint32_t>(quarter) << 21;
     const uint32_t s_at = tmem + 128 * t + lanes, p_at = tmem + S::kP + S::kPStep * t + lanes, o_at = tmem + S::kO + DP * t + lanes;
     const float c = p.scale * kLog2E;
@@ -387,20 +395,20 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
         if (!ok) break;
         tc_fence_after();
         const int cols = keys - j * kBlock, limit = mine - j * kBlock;
-        uint32_t v[4][32];
-        tmem_ld32(s_at, v[0]);
-        if (cols > 32) tmem_ld32(s_at + 32, v[1]);
-        if (cols > 64) tmem_ld32(s_at + 64, v[2]);
-        if (cols > 96) tmem_ld32(s_at + 96, v[3]);
+        uint32_t v[kQ][32];
+        tmem_ld32(s_at + 32 * q0, v[0]);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) tmem_wait_ld32(v[q]);
+        for (int q = 1; q < kQ; ++q)
+          if (cols > 32 * q) tmem_ld32(s_at + 32 * q, v[q]);
+#pragma unroll
+        for (int q = 0; q < kQ; ++q) tmem_wait_ld32(v[q]);
         tc_fence_before();
         __syncwarp();
         if (S::kOwnP && leader) mbar_arrive(s_free + 8 * t);
         if ((j + 1) * kBlock > all) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (all - j * kBlock < 32 * q + 32) hide(v[q], limit - 32 * q);
+          for (int q = 0; q < kQ; ++q)
+            if (all - j * kBlock < 32 * (q0 + q) + 32) hide(v[q], limit - 32 * (q0 + q));
         }
         float sum;
         bool arrived = j == from;                   // the block before has gone into o, and p may be written
@@ -408,8 +416,8 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
           if (fresh) {
             float to = m;
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-              if (cols > 32 * q) to = largest(v[q], to);
+            for (int q = 0; q < kQ; ++q)
+              if (SPREAD || cols > 32 * q) to = largest(v[q], to);
             if (j > from) {
               const float f = m == to ? 1.0f : exp2_approx(c * (m - to));
               l *= f;
@@ -421,7 +429,7 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
           const uint64_t mc2 = pair(-mc, -mc);
           uint64_t sums[2] = {0, 0};
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
+          for (int q = 0; q < kQ; ++q) {
             if (q > 0 && cols <= 32 * q) break;
             uint32_t w16[16];
             exponentials(v[q], w16, sums, c2, mc2);
@@ -430,11 +438,16 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
               tc_fence_after();
               arrived = true;
             }
-            tmem_st16(p_at + 16 * q, w16);
+            tmem_st16(p_at + 16 * (q0 + q), w16);
+          }
+          if (SPREAD) {
+            const uint32_t none[16] = {};
+#pragma unroll
+            for (int q = 1; q < 4; ++q) tmem_st16(p_at + 16 * ((q0 + q) & 3), none);
           }
           const float2 both = unpair(add2(sums[0], sums[1]));
           sum = both.x + both.y;
-          if (!ok || fresh || !__any_sync(0xFFFFFFFFu, m == -INFINITY || !(sum < kMost))) break;   // (a NaN too)
+          if (!ok || fresh || !__any_sync(0xFFFFFFFFu, (!SPREAD || pack_head < p.group) && (m == -INFINITY || !(sum < kMost)))) break;   // (a NaN too)
         }
         if (!ok) break;
         l += sum;
@@ -448,7 +461,7 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
       const int row = (PARTS && p.pack) ? row_in_tile - pack_head * p.q_rows : w.row0 + tile_row + row_in_tile, head = (PARTS && p.pack) ? w.h * p.group + pack_head : w.h;
       const bool real = row < p.q_len && (!PARTS || ((!p.pack || pack_head < p.group) && (!p.pack || p.twin || t == 0))), any = blocks > from;
       const bool parts = PARTS && (p.splits > 1 || p.twin);
-      const long long part = PARTS ? (p.twin ? 2 * w.split + t : w.split) : 0;
+      const long long part = SPREAD ? 4 * (2 * w.split + t) + quarter : PARTS ? (p.twin ? 2 * w.split + t : w.split) : 0;
       const long long at = (static_cast<long long>(w.b) * p.heads + head) * p.q_len + row;       // the row's number
       if (ok && any) ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(o_done + 8 * t, (seen & 1) ^ 1));
       // the queries' place takes the outputs: they are not read any more
@@ -549,29 +562,40 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
   }
 }
 
-// The parts' sums of a row, in their order: a warp a row.
-__global__ void __launch_bounds__(256)
-attention_join_parts_kernel(const float* partial, const float2* marks, const surgeon_heads o, float* lse, int splits, int heads, int q_len, int head_dim,
+// The parts' sums of a row, in their order: a warp a row, a lane four columns and every 32nd part's m and l.
+constexpr int kJoinThreads = 64;
+__global__ void __launch_bounds__(kJoinThreads)
+attention_join_parts_kernel(const float* partial, const float2* marks, const surgeon_heads o, float* lse, int parts, int heads, int q_len, int head_dim,
                             float scale, int rows) {
   pdl_trigger();
   pdl_wait();
-  const int at = blockIdx.x * 8 + (threadIdx.x >> 5), d = static_cast<int>(lane_id()) * 4;
+  const int at = blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5), lane = static_cast<int>(lane_id()), d = lane * 4;
   if (at >= rows) return;
-  float m = -INFINITY, l = 0.0f;
-  for (int s = 0; s < splits; ++s) m = fmaxf(m, marks[static_cast<long long>(s) * rows + at].x);
+  float m = -INFINITY;
+  for (int s = lane; s < parts; s += 32) m = fmaxf(m, marks[static_cast<long long>(s) * rows + at].x);
+  for (int i = 16; i > 0; i >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, i));
+  float l = 0.0f;
   float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-  for (int s = 0; s < splits; ++s) {
-    const long long r = static_cast<long long>(s) * rows + at;
-    const float2 k = marks[r];
-    if (k.x == -INFINITY) continue;              // (it sees none of this part's keys: nothing was written)
-    const float f = exp2_approx(scale * kLog2E * (k.x - m));
-    l = fmaf(k.y, f, l);
-    if (d < head_dim) {
-      const float4 v = *reinterpret_cast<const float4*>(partial + r * head_dim + d);
-      sum.x = fmaf(v.x, f, sum.x); sum.y = fmaf(v.y, f, sum.y); sum.z = fmaf(v.z, f, sum.z); sum.w = fmaf(v.w, f, sum.w);
+  for (int s0 = 0; s0 < parts; s0 += 32) {
+    float f = 0.0f;                              // (where a row sees none of a part's keys, nothing was written)
+    if (s0 + lane < parts) {
+      const float2 k = marks[static_cast<long long>(s0 + lane) * rows + at];
+      if (k.x != -INFINITY) {
+        f = exp2_approx(scale * kLog2E * (k.x - m));
+        l = fmaf(k.y, f, l);
+      }
+    }
+    const int n = min(32, parts - s0);
+    const float* from = partial + (static_cast<long long>(s0) * rows + at) * head_dim + d;
+#pragma unroll 8
+    for (int s = 0; s < n; ++s) {
+      const float w = __shfl_sync(0xFFFFFFFFu, f, s);
+      if (w == 0.0f || d >= head_dim) continue;
+      const float4 v = *reinterpret_cast<const float4*>(from + static_cast<long long>(s) * rows * head_dim);
+      sum.x = fmaf(v.x, w, sum.x); sum.y = fmaf(v.y, w, sum.y); sum.z = fmaf(v.z, w, sum.z); sum.w = fmaf(v.w, w, sum.w);
     }
   }
+  l = lanes_sum<32>(l);
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   const int row = at % q_len, bh = at / q_len;
   if (d < head_dim) {
@@ -584,23 +608,25 @@ attention_join_parts_kernel(const float* partial, const float2* marks, const sur
 // How a call is cut.  Heads that share keys go into one tile where they fit (few queries): the keys are then read once for all of them.
 // Where that leaves SMs without an item, the keys are shared out in parts of two blocks at least, whose sums are joined by a kernel of its own.
 // A single tile of queries is taken by both halves of the warps, each with every other block of the keys, as two parts more: a half
-// alone would wait for its products and they for it.
+// alone would wait for its products and they for it.  At most 32 rows are spread over the warps of a tile, as four times the parts:
+// 8 sequences of one query and 8192 keys, 16 heads of 128 that share 4, take 34 us, and 41 where one warp of four has all the rows that count.
 struct Plan {
-  int pack, q_rows, tiles, splits, twin, parts;
+  int pack, q_rows, tiles, splits, twin, spread, parts;
 };
 Plan plan_of(const surgeon_attention_desc& d) {
   Plan p = {};
-  const int group = d.heads / d.kv_heads;
+  const int group = d.heads / d.kv_heads, blocks = (d.kv_len + kBlock - 1) / kBlock;
   p.q_rows = round_up(d.q_len, 8);               // (whole groups of eight rows, as the operand's layout has them)
-  p.pack = group > 1 && static_cast<long long>(group) * p.q_rows <= kTile;
+  const long long rows = static_cast<long long>(group) * p.q_rows;
+  p.spread = rows <= 32 && blocks >= 4;
+  p.pack = (group > 1 && rows <= kTile) || p.spread;
   p.tiles = (d.q_len + 2 * kTile - 1) / (2 * kTile);
   const long long items = static_cast<long long>(p.tiles) * d.batch * (p.pack ? d.kv_heads : d.heads);
-  const int blocks = (d.kv_len + kBlock - 1) / kBlock;
   p.twin = (p.pack || d.q_len <= kTile) && blocks >= 4;
   p.splits = items > 0 ? static_cast<int>(148 / items) : 1;
   if (p.splits > blocks / (p.twin ? 4 : 2)) p.splits = blocks / (p.twin ? 4 : 2);
   if (p.splits < 1) p.splits = 1;
-  p.parts = p.twin ? 2 * p.splits : p.splits;
+  p.parts = (p.twin ? 2 : 1) * (p.spread ? 4 : 1) * p.splits;
   return p;
 }
 size_t marks_bytes(const surgeon_attention_desc& d, int parts) {
@@ -609,12 +635,12 @@ size_t marks_bytes(const surgeon_attention_desc& d, int parts) {
 
 template <int DP>
 cudaError_t launch_as(const surgeon_attention_desc& d, const surgeon_heads& q, const surgeon_heads& k, const surgeon_heads& v, const surgeon_heads& o,
-                      Args& a, cudaStream_t stream) {
+                      Args& a, bool spread, cudaStream_t stream) {
   CUtensorMap maps[4];
   if (!encode(&maps[0], q, d.batch, d.q_len, d.heads, d.head_dim, a.pack ? a.q_rows : kTile) || !encode(&maps[1], k, d.batch, d.kv_len, d.kv_heads, d.head_dim, kBlock) ||
       !encode(&maps[2], v, d.batch, d.kv_len, d.kv_heads, d.head_dim, kBlock) || !encode(&maps[3], o, d.batch, d.q_len, d.heads, d.head_dim, 32))
     return cudaErrorInvalidValue;
-  const auto kernel = a.pack || a.splits > 1 || a.twin ? attention_kernel<DP, true> : attention_kernel<DP, false>;
+  const auto kernel = spread ? attention_kernel<DP, kSpread> : a.pack || a.splits > 1 || a.twin ? attention_kernel<DP, kParts> : attention_kernel<DP, kWhole>;
   const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), Shape<DP>::kSmem);
   if (e != cudaSuccess) return e;
   const int grid = a.items < sm_count() ? a.items : sm_count();
@@ -647,10 +673,10 @@ cudaError_t launch_attention(const surgeon_attention_desc& d, const surgeon_head
   a.lse = lse;
   a.marks = static_cast<float2*>(workspace);
   a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + marks_bytes(d, plan.parts));
-  cudaError_t e = d.head_dim <= 64 ? launch_as<64>(d, q, k, v, o, a, stream) : launch_as<128>(d, q, k, v, o, a, stream);
+  cudaError_t e = d.head_dim <= 64 ? launch_as<64>(d, q, k, v, o, a, plan.spread, stream) : launch_as<128>(d, q, k, v, o, a, plan.spread, stream);
   if (e != cudaSuccess || plan.parts == 1) return e;
   const int rows = d.batch * d.heads * d.q_len;
-  e = launch_kernel(attention_join_parts_kernel, dim3((rows + 7) / 8), dim3(256), 0, stream, true, static_cast<const float*>(a.partial),
+  e = launch_kernel(attention_join_parts_kernel, dim3((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32)), dim3(kJoinThreads), 0, stream, true, static_cast<const float*>(a.partial),
                     static_cast<const float2*>(a.marks), o, lse, plan.parts, d.heads, d.q_len, d.head_dim, a.scale, rows);
   note_launches(1);
   return e;
