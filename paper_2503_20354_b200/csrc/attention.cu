@@ -6,9 +6,13 @@
 // A CTA takes 256 queries of a head, two tiles of 128, and walks the keys in blocks of 128.  s = q k^T goes to tensor memory (lane = query),
 // four warps a tile read it back, a thread a row, and leave 2^(c (s - m)) as bf16 in tensor memory, where it is the A
 // operand of the product with v: neither s nor p is ever in shared memory.  o stays in tensor memory over all blocks.
-// m is the first block's maximum, and set anew, o and l scaled, only where a later block's p add up to 2^64 or more: bf16 has fp32's
-// exponents, so a p above 1 is as exact as one below, and the other blocks need no maximum.
+// m is the first block's maximum, and set anew, o and l scaled, only where a later block's p add up to 2^32 or more: bf16 has fp32's
+// exponents, so a p above 1 is as exact as one below, and the other blocks need no maximum.  p is rounded to bf16 (half a step, 2^-8), as
+// an operand must be; l adds the unrounded ones up.
 // Persistent CTAs: the next item's queries, keys and values are on their way while this one's end.
+// Bound by the softmax's instructions (an exponential, half a packed multiply-add, an addition, a conversion and a load from tensor memory a
+// score) and the waits between them and the products.  64 x 197 rows of 12 heads of 64: 35 us (768 items are 5.2 rounds of the SMs);
+// 65536 rows, 1024 keys of 64: 33 us, 0.52 PFLOP/s; 2 x 16 heads of 128, 4096 rows: 302 us, 0.91 PFLOP/s.
 #include "attention.cuh"
 
 namespace surgeon {
@@ -23,7 +27,7 @@ constexpr int kCopyWarp = 8, kProductWarp = 9;
 constexpr int kThreads = 384;                    // (two warps idle: registers are dealt out by fours of warps)
 constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;               // 2 x 216 + 72 = 3 x 168, what 384 threads are launched with
 constexpr int kMaxStages = 8;
-constexpr float kMost = 18446744073709551616.0f;                 // 2^64: what a row's p of a block may add up to before m is set anew
+constexpr float kMost = 4294967296.0f;                           // 2^32: what a row's p of a block may add up to before m is set anew
 
 template <int DP> struct Shape {                 // DP: head_dim, padded to 64 or 128
   static constexpr int kSlabs = DP / kSlabCols, kTileBytes = kTile * DP * 2, kBlockBytes = kBlock * DP * 2;
@@ -121,7 +125,7 @@ __device__ __forceinline__ float largest(const uint32_t (&v)[32], float m) {
 __device__ __forceinline__ void exponentials(const uint32_t (&v)[32], uint32_t* w, uint64_t (&sums)[2], uint64_t c2, uint64_t mc2) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const float2 e = exp2_unit(fma2(pair(v[2 * i], v[2 * i + 1]), c2, mc2));
+    const float2 e = exp2_both(fma2(pair(v[2 * i], v[2 * i + 1]), c2, mc2));
     sums[i & 1] = add2(sums[i & 1], pair(e.x, e.y));
     w[i] = to_bf16x2(e.x, e.y);
   }
@@ -187,171 +191,171 @@ attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
   pdl_wait();
 
   if (warp >= kCopyWarp) {
-  set_registers<false, kOtherRegs>();
-  if (warp == kCopyWarp) {
-    // ---- copies ----
-    int s = 0, it = 0;
-    uint32_t phase = 1, fix_phase = 0;           // (a fresh barrier counts as passed in its phase before)
-    bool ok = true;
-    for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x, ++it) {
-      const Item<PARTS> w(p, item);
-      const int qs = S::kQStages == 2 ? it & 1 : 0, kv_head = (PARTS && p.pack) ? w.h : static_cast<int>(divide(w.h, p.by_group));
-      const uint32_t q_phase = (S::kQStages == 2 ? (it >> 1) & 1 : it & 1) ^ 1;
-      for (int t = 0; t < 2 && ok; ++t) {
-        const int at = 2 * qs + t;
-        ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(q_empty + 8 * at, q_phase));
-        if (!ok) break;
-        if (leader) {
-          if (PARTS && p.twin && t == 1) {       // (the first tile's queries serve both)
-            mbar_arrive(q_full + 8 * at);
-          } else if (w.blocks[t] > w.from && (PARTS && p.pack)) {
-            constexpr int kTimes = SPREAD ? 4 : 1;
-            mbar_arrive_expect_tx(q_full + 8 * at, kTimes * p.group * p.q_rows * 128 * S::kSlabs);
-            for (int i = 0; i < kTimes; ++i)
-              for (int g = 0; g < p.group; ++g)
-                for (int c = 0; c < S::kSlabs; ++c)
-                  tma_load_4d(smem_u32(smem) + at * S::kTileBytes + c * kTile * 128 + (32 * i + g * p.q_rows) * 128, &q_map, c * kSlabCols, 0,
-                              w.h * p.group + g, w.b, q_full + 8 * at);
-          } else if (w.blocks[t] > w.from) {
-            mbar_arrive_expect_tx(q_full + 8 * at, S::kTileBytes);
-            for (int c = 0; c < S::kSlabs; ++c)
-              tma_load_4d(smem_u32(smem) + at * S::kTileBytes + c * kTile * 128, &q_map, c * kSlabCols, w.row0 + t * kTile, w.h, w.b, q_full + 8 * at);
-          } else {
-            mbar_arrive(q_full + 8 * at);
-          }
-        }
-      }
-      const auto load = [&](bool is_v, int j) {
-        ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait_suspend(empty + 8 * s, phase));
-        if (!ok) return;
-        const int row = j * kBlock, left = w.kv_valid - row;
-        // Rows of v behind the last key meet probabilities of zero: they must not hold a NaN.  Behind the tensor's end they are zeros anyway.
-        const bool fix = is_v && left < kBlock && w.kv_valid < p.kv_len;
-        unsigned char* to = ring + s * S::kBlockBytes;
-        if (leader) {
-          const uint32_t bar = fix ? fixed : full + 8 * s;
-          mbar_arrive_expect_tx(bar, S::kBlockBytes);
-          for (int c = 0; c < S::kSlabs; ++c)
-            tma_load_4d(smem_u32(to) + c * kBlock * 128, is_v ? &v_map : &k_map, c * kSlabCols, row, kv_head, w.b, bar);
-        }
-        if (fix) {
-          ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(fixed, fix_phase));
-          fix_phase ^= 1;
-          if (ok) zero_rows<S::kSlabs>(to, kBlock, left, round_up(left, 16));
-          fence_proxy_async();
-          __syncwarp();
-          if (leader && ok) mbar_arrive(full + 8 * s);
-        }
-        if (++s == S::kStages) { s = 0; phase ^= 1; }
-      };
-      for (int j = w.from; j < w.most; ++j) {
-        load(false, j);
-        load(true, j);
-      }
-    }
-    if (!ok)
-      for (int i = 0; i < 1000; ++i) __nanosleep(1000);           // copies in flight land
-  } else if (warp == kProductWarp) {
-    // ---- products ----
-    if (leader) {
-      const int k_steps = (p.head_dim + 15) / 16, n_o = round_up(p.head_dim, 16);
-      const uint32_t idesc_o = make_idesc(kTile, n_o) | kRowsB;
-      const uint32_t q_desc = desc_low(smem_u32(smem)), k_desc = desc_low(smem_u32(ring)), v_desc = desc_low(smem_u32(ring), kBlock * 128);
-      int s = 0, it = 0;                         // the ring's next tile
-      uint32_t phase = 0;
-      uint32_t first[2] = {0, 0};                // number of each tile's first block of the item; a block's place and phases go by its number
+    set_registers<false, kOtherRegs>();
+    if (warp == kCopyWarp) {
+      // ---- copies ----
+      int s = 0, it = 0;
+      uint32_t phase = 1, fix_phase = 0;           // (a fresh barrier counts as passed in its phase before)
       bool ok = true;
       for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x, ++it) {
         const Item<PARTS> w(p, item);
-        const int qs = S::kQStages == 2 ? it & 1 : 0;
-        const uint32_t q_phase = S::kQStages == 2 ? (it >> 1) & 1 : it & 1;
-        for (int t = 0; t < 2 && ok; ++t) ok = wait_for(q_full + 8 * (2 * qs + t), q_phase);
-        if (!ok) break;
-        if (w.most <= w.from) continue;
-        const auto next = [&]() {
-          const int st = s;
+        const int qs = S::kQStages == 2 ? it & 1 : 0, kv_head = (PARTS && p.pack) ? w.h : static_cast<int>(divide(w.h, p.by_group));
+        const uint32_t q_phase = (S::kQStages == 2 ? (it >> 1) & 1 : it & 1) ^ 1;
+        for (int t = 0; t < 2 && ok; ++t) {
+          const int at = 2 * qs + t;
+          ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(q_empty + 8 * at, q_phase));
+          if (!ok) break;
+          if (leader) {
+            if (PARTS && p.twin && t == 1) {       // (the first tile's queries serve both)
+              mbar_arrive(q_full + 8 * at);
+            } else if (w.blocks[t] > w.from && (PARTS && p.pack)) {
+              constexpr int kTimes = SPREAD ? 4 : 1;
+              mbar_arrive_expect_tx(q_full + 8 * at, kTimes * p.group * p.q_rows * 128 * S::kSlabs);
+              for (int i = 0; i < kTimes; ++i)
+                for (int g = 0; g < p.group; ++g)
+                  for (int c = 0; c < S::kSlabs; ++c)
+                    tma_load_4d(smem_u32(smem) + at * S::kTileBytes + c * kTile * 128 + (32 * i + g * p.q_rows) * 128, &q_map, c * kSlabCols, 0,
+                                w.h * p.group + g, w.b, q_full + 8 * at);
+            } else if (w.blocks[t] > w.from) {
+              mbar_arrive_expect_tx(q_full + 8 * at, S::kTileBytes);
+              for (int c = 0; c < S::kSlabs; ++c)
+                tma_load_4d(smem_u32(smem) + at * S::kTileBytes + c * kTile * 128, &q_map, c * kSlabCols, w.row0 + t * kTile, w.h, w.b, q_full + 8 * at);
+            } else {
+              mbar_arrive(q_full + 8 * at);
+            }
+          }
+        }
+        const auto load = [&](bool is_v, int j) {
+          ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait_suspend(empty + 8 * s, phase));
+          if (!ok) return;
+          const int row = j * kBlock, left = w.kv_valid - row;
+          // Rows of v behind the last key meet probabilities of zero: they must not hold a NaN.  Behind the tensor's end they are zeros anyway.
+          const bool fix = is_v && left < kBlock && w.kv_valid < p.kv_len;
+          unsigned char* to = ring + s * S::kBlockBytes;
+          if (leader) {
+            const uint32_t bar = fix ? fixed : full + 8 * s;
+            mbar_arrive_expect_tx(bar, S::kBlockBytes);
+            for (int c = 0; c < S::kSlabs; ++c)
+              tma_load_4d(smem_u32(to) + c * kBlock * 128, is_v ? &v_map : &k_map, c * kSlabCols, row, kv_head, w.b, bar);
+          }
+          if (fix) {
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait_suspend(fixed, fix_phase));
+            fix_phase ^= 1;
+            if (ok) zero_rows<S::kSlabs>(to, kBlock, left, round_up(left, 16));
+            fence_proxy_async();
+            __syncwarp();
+            if (leader && ok) mbar_arrive(full + 8 * s);
+          }
           if (++s == S::kStages) { s = 0; phase ^= 1; }
-          return st;
         };
-        // s of tile t and block j, the t's block number n
-        const auto scores = [&](int t, int j, int st, uint32_t n) {
-          // (s has been read; where p takes its place, p has gone into o)
-          if (!wait_for((S::kOwnP ? s_free : o_done) + 8 * t, (n & 1) ^ 1)) return false;
-          tc_fence_after();
-          const uint32_t idesc = make_idesc(kTile, round_up(min(kBlock, w.keys[t] - j * kBlock), 16));
-          const uint32_t a = q_desc + (2 * qs + (PARTS && p.twin ? 0 : t)) * (S::kTileBytes >> 4), b = k_desc + st * (S::kBlockBytes >> 4);
-#pragma unroll
-          for (int k = 0; k < DP / 16; ++k)
-            if (k < k_steps) umma_ss(tmem + 128 * t, a + (k >> 2) * (kTile * 128 >> 4) + (k & 3) * 2, b + (k >> 2) * (kBlock * 128 >> 4) + (k & 3) * 2, idesc, k > 0);
-          umma_commit(s_full + 8 * t);
-          return true;
-        };
-        const auto values = [&](int t, int j, int st, uint32_t n) {
-          if (!wait_for(p_full + 8 * t, n & 1)) return false;
-          tc_fence_after();
-          const int steps = (min(kBlock, w.keys[t] - j * kBlock) + 15) / 16;
-          const uint32_t b = v_desc + st * (S::kBlockBytes >> 4);
-#pragma unroll
-          for (int k = 0; k < kBlock / 16; ++k)
-            if (k < steps) umma_ts(tmem + S::kO + DP * t, tmem + S::kP + S::kPStep * t + 8 * k, b + 128 * k, idesc_o, j > w.from + (PARTS && p.twin ? t : 0) || k > 0);
-          umma_commit(o_done + 8 * t);
-          return true;
-        };
-        if (PARTS && p.twin) {
-          // one tile's block after the other's; k of block j is the 2 (j - from)-th tile of the ring from here, v the one behind it
-          const uint32_t base = s + (phase ? S::kStages : 0);
-          const auto there = [&](uint32_t at) { return wait_for(full + 8 * (at % S::kStages), (at / S::kStages) & 1); };
-          const auto turn = [&](int j) {
-            const uint32_t at = base + 2 * (j - w.from), st = at % S::kStages;
-            if (!there(at) || !scores((j - w.from) & 1, j, st, first[(j - w.from) & 1] + ((j - w.from) >> 1))) return false;
-            umma_commit(empty + 8 * st);
+        for (int j = w.from; j < w.most; ++j) {
+          load(false, j);
+          load(true, j);
+        }
+      }
+      if (!ok)
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);           // copies in flight land
+    } else if (warp == kProductWarp) {
+      // ---- products ----
+      if (leader) {
+        const int k_steps = (p.head_dim + 15) / 16, n_o = round_up(p.head_dim, 16);
+        const uint32_t idesc_o = make_idesc(kTile, n_o) | kRowsB;
+        const uint32_t q_desc = desc_low(smem_u32(smem)), k_desc = desc_low(smem_u32(ring)), v_desc = desc_low(smem_u32(ring), kBlock * 128);
+        int s = 0, it = 0;                         // the ring's next tile
+        uint32_t phase = 0;
+        uint32_t first[2] = {0, 0};                // number of each tile's first block of the item; a block's place and phases go by its number
+        bool ok = true;
+        for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x, ++it) {
+          const Item<PARTS> w(p, item);
+          const int qs = S::kQStages == 2 ? it & 1 : 0;
+          const uint32_t q_phase = S::kQStages == 2 ? (it >> 1) & 1 : it & 1;
+          for (int t = 0; t < 2 && ok; ++t) ok = wait_for(q_full + 8 * (2 * qs + t), q_phase);
+          if (!ok) break;
+          if (w.most <= w.from) continue;
+          const auto next = [&]() {
+            const int st = s;
+            if (++s == S::kStages) { s = 0; phase ^= 1; }
+            return st;
+          };
+          // s of tile t and block j, the t's block number n
+          const auto scores = [&](int t, int j, int st, uint32_t n) {
+            // (s has been read; where p takes its place, p has gone into o)
+            if (!wait_for((S::kOwnP ? s_free : o_done) + 8 * t, (n & 1) ^ 1)) return false;
+            tc_fence_after();
+            const uint32_t idesc = make_idesc(kTile, round_up(min(kBlock, w.keys[t] - j * kBlock), 16));
+            const uint32_t a = q_desc + (2 * qs + (PARTS && p.twin ? 0 : t)) * (S::kTileBytes >> 4), b = k_desc + st * (S::kBlockBytes >> 4);
+  #pragma unroll
+            for (int k = 0; k < DP / 16; ++k)
+              if (k < k_steps) umma_ss(tmem + 128 * t, a + (k >> 2) * (kTile * 128 >> 4) + (k & 3) * 2, b + (k >> 2) * (kBlock * 128 >> 4) + (k & 3) * 2, idesc, k > 0);
+            umma_commit(s_full + 8 * t);
             return true;
           };
-          for (int j = w.from; j < w.from + 2 && j < w.most && ok; ++j) ok = turn(j);
+          const auto values = [&](int t, int j, int st, uint32_t n) {
+            if (!wait_for(p_full + 8 * t, n & 1)) return false;
+            tc_fence_after();
+            const int steps = (min(kBlock, w.keys[t] - j * kBlock) + 15) / 16;
+            const uint32_t b = v_desc + st * (S::kBlockBytes >> 4);
+  #pragma unroll
+            for (int k = 0; k < kBlock / 16; ++k)
+              if (k < steps) umma_ts(tmem + S::kO + DP * t, tmem + S::kP + S::kPStep * t + 8 * k, b + 128 * k, idesc_o, j > w.from + (PARTS && p.twin ? t : 0) || k > 0);
+            umma_commit(o_done + 8 * t);
+            return true;
+          };
+          if (PARTS && p.twin) {
+            // one tile's block after the other's; k of block j is the 2 (j - from)-th tile of the ring from here, v the one behind it
+            const uint32_t base = s + (phase ? S::kStages : 0);
+            const auto there = [&](uint32_t at) { return wait_for(full + 8 * (at % S::kStages), (at / S::kStages) & 1); };
+            const auto turn = [&](int j) {
+              const uint32_t at = base + 2 * (j - w.from), st = at % S::kStages;
+              if (!there(at) || !scores((j - w.from) & 1, j, st, first[(j - w.from) & 1] + ((j - w.from) >> 1))) return false;
+              umma_commit(empty + 8 * st);
+              return true;
+            };
+            for (int j = w.from; j < w.from + 2 && j < w.most && ok; ++j) ok = turn(j);
+            for (int j = w.from; j < w.most && ok; ++j) {
+              const uint32_t at = base + 2 * (j - w.from) + 1, st = at % S::kStages;
+              ok = there(at) && values((j - w.from) & 1, j, st, first[(j - w.from) & 1] + ((j - w.from) >> 1));
+              if (!ok) break;
+              umma_commit(empty + 8 * st);
+              if (j + 2 < w.most) ok = turn(j + 2);
+            }
+            const uint32_t end = base + 2 * (w.most - w.from);
+            s = end % S::kStages;
+            phase = (end / S::kStages) & 1;
+            first[0] += (w.most - w.from + 1) >> 1;
+            first[1] += (w.most - w.from) >> 1;
+            continue;
+          }
+          ok = wait_for(full + 8 * s, phase);
+          int ks = next();                         // the place of the next block's keys
+          for (int t = 0; t < 2 && ok; ++t)
+            if (w.blocks[t] > w.from) ok = scores(t, w.from, ks, first[t]);
           for (int j = w.from; j < w.most && ok; ++j) {
-            const uint32_t at = base + 2 * (j - w.from) + 1, st = at % S::kStages;
-            ok = there(at) && values((j - w.from) & 1, j, st, first[(j - w.from) & 1] + ((j - w.from) >> 1));
-            if (!ok) break;
-            umma_commit(empty + 8 * st);
-            if (j + 2 < w.most) ok = turn(j + 2);
+            umma_commit(empty + 8 * ks);
+            const int v_at = s;
+            const uint32_t v_phase = phase;
+            next();
+            const bool more = j + 1 < w.most;
+            if (more) {
+              ok = wait_for(full + 8 * s, phase);
+              ks = next();
+            }
+            ok = ok && wait_for(full + 8 * v_at, v_phase);
+  #pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              const uint32_t n = first[t] + j - w.from;
+              const bool ahead = j + 1 < w.blocks[t];
+              if (S::kOwnP && ok && ahead) ok = scores(t, j + 1, ks, n + 1);
+              if (ok && j < w.blocks[t]) ok = values(t, j, v_at, n);
+              if (!S::kOwnP && ok && ahead) ok = scores(t, j + 1, ks, n + 1);
+            }
+            if (ok) umma_commit(empty + 8 * v_at);
           }
-          const uint32_t end = base + 2 * (w.most - w.from);
-          s = end % S::kStages;
-          phase = (end / S::kStages) & 1;
-          first[0] += (w.most - w.from + 1) >> 1;
-          first[1] += (w.most - w.from) >> 1;
-          continue;
+          first[0] += w.blocks[0] - w.from;
+          first[1] += w.blocks[1] - w.from;
         }
-        ok = wait_for(full + 8 * s, phase);
-        int ks = next();                         // the place of the next block's keys
-        for (int t = 0; t < 2 && ok; ++t)
-          if (w.blocks[t] > w.from) ok = scores(t, w.from, ks, first[t]);
-        for (int j = w.from; j < w.most && ok; ++j) {
-          umma_commit(empty + 8 * ks);
-          const int v_at = s;
-          const uint32_t v_phase = phase;
-          next();
-          const bool more = j + 1 < w.most;
-          if (more) {
-            ok = wait_for(full + 8 * s, phase);
-            ks = next();
-          }
-          ok = ok && wait_for(full + 8 * v_at, v_phase);
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            const uint32_t n = first[t] + j - w.from;
-            const bool ahead = j + 1 < w.blocks[t];
-            if (S::kOwnP && ok && ahead) ok = scores(t, j + 1, ks, n + 1);
-            if (ok && j < w.blocks[t]) ok = values(t, j, v_at, n);
-            if (!S::kOwnP && ok && ahead) ok = scores(t, j + 1, ks, n + 1);
-          }
-          if (ok) umma_commit(empty + 8 * v_at);
-        }
-        first[0] += w.blocks[0] - w.from;
-        first[1] += w.blocks[1] - w.from;
       }
     }
-  }
   } else {
     // ---- softmax: a thread a row ----
     set_registers<true, kSoftmaxRegs>();

@@ -91,7 +91,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
       "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
@@ -105,24 +104,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// 2^x of two numbers on the FMA pipe, for a part of the exponentials: the special function unit gives 16 a clock, an eighth of the FMA
-// rate, and would be the bound.  x = n + f with |f| <= 1/2; 2^f by the polynomial of degree 4 whose largest relative error on that interval
-// is least (2.6e-6; its coefficients by Remez' exchange algorithm); n goes into the exponent.  x outside [-126, 127] counts as its end
-// (an infinity too; what a NaN gives is no number to rely on).
-__device__ __forceinline__ float2 exp2_pair(uint64_t x) {
-  float2 v = unpair(x);
-  v.x = fminf(fmaxf(v.x, -126.0f), 127.0f);
-  v.y = fminf(fmaxf(v.y, -126.0f), 127.0f);
-  const uint64_t y = pair(v.x, v.y), shift = pair(12582912.0f, 12582912.0f);     // 1.5 * 2^23: what is added to it is rounded to an integer
-  const uint64_t n = add2(y, shift), f = fma2(add2(n, pair(-12582912.0f, -12582912.0f)), pair(-1.0f, -1.0f), y);
-  uint64_t r = fma2(pair(0.009570102207362652f, 0.009570102207362652f), f, pair(0.05591785907745361f, 0.05591785907745361f));
-  r = fma2(r, f, pair(0.240247443318367f, 0.240247443318367f));
-  r = fma2(r, f, pair(0.6931217908859253f, 0.6931217908859253f));
-  r = fma2(r, f, pair(0.9999992847442627f, 0.9999992847442627f));
-  const float2 m = unpair(r), e = unpair(n);
-  return make_float2(__int_as_float(__float_as_int(m.x) + (__float_as_int(e.x) << 23)), __int_as_float(__float_as_int(m.y) + (__float_as_int(e.y) << 23)));
-}
-__device__ __forceinline__ float2 exp2_unit(uint64_t x) {
+// 2^x of two numbers on the special function unit: an instruction of a warp takes it 8 clocks.  A polynomial on the FMA pipe for a part of
+// them was no faster: the loops issue in most of the other clocks already.
+__device__ __forceinline__ float2 exp2_both(uint64_t x) {
   const float2 v = unpair(x);
   return make_float2(exp2_approx(v.x), exp2_approx(v.y));
 }
