@@ -611,7 +611,7 @@ attention_join_parts_kernel(const float* partial, const float2* marks, const sur
 
 // How a call is cut.  Heads that share keys go into one tile where they fit (few queries): the keys are then read once for all of them.
 // Where that leaves SMs without an item, the keys are shared out in parts of two blocks at least, whose sums are joined by a kernel of its own.
-// A single tile of queries is taken by both halves of the warps, each with every other block of the keys, as two parts more: a half
+// A single tile of queries of few items is taken by both halves of the warps, each with every other block of the keys, as two parts more: a half
 // alone would wait for its products and they for it.  At most 32 rows are spread over the warps of a tile, as four times the parts:
 // 8 sequences of one query and 8192 keys, 16 heads of 128 that share 4, take 34 us, and 41 where one warp of four has all the rows that count.
 struct Plan {
@@ -621,12 +621,15 @@ Plan plan_of(const surgeon_attention_desc& d) {
   Plan p = {};
   const int group = d.heads / d.kv_heads, blocks = (d.kv_len + kBlock - 1) / kBlock;
   p.q_rows = round_up(d.q_len, 8);               // (whole groups of eight rows, as the operand's layout has them)
-  const long long rows = static_cast<long long>(group) * p.q_rows;
-  p.spread = rows <= 32 && blocks >= 4;
-  p.pack = (group > 1 && rows <= kTile) || p.spread;
   p.tiles = (d.q_len + 2 * kTile - 1) / (2 * kTile);
-  const long long items = static_cast<long long>(p.tiles) * d.batch * (p.pack ? d.kv_heads : d.heads);
-  p.twin = (p.pack || d.q_len <= kTile) && blocks >= 4;
+  const long long rows = static_cast<long long>(group) * d.q_len, padded = static_cast<long long>(group) * p.q_rows;
+  const auto items_of = [&](int pack) { return static_cast<long long>(p.tiles) * d.batch * (pack ? d.kv_heads : d.heads); };
+  // Parts of an item are written and read once more, which counts where there are items for all SMs: 64 x 12 heads of 64 take 44 us for 128 queries
+  // and 512 keys, 106 in two parts; 44 for 32 queries, 62 spread; but 23 spread and 33 not for one query of 16 heads of 128 that share 4.
+  p.spread = padded <= 32 && blocks >= 4 && (items_of(1) <= 148 || 32 * rows <= d.kv_len);
+  p.pack = (group > 1 && padded <= kTile) || p.spread;
+  p.twin = p.spread || ((p.pack || d.q_len <= kTile) && blocks >= 4 && items_of(p.pack) <= 148);
+  const long long items = items_of(p.pack);
   p.splits = items > 0 ? static_cast<int>(148 / items) : 1;
   if (p.splits > blocks / (p.twin ? 4 : 2)) p.splits = blocks / (p.twin ? 4 : 2);
   if (p.splits < 1) p.splits = 1;

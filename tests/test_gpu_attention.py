@@ -139,7 +139,9 @@ def run(q, k, v, causal=False, ql=None, kl=None, scale=None, grad=True, layout_g
 SHAPES = [(1, 1, 1, 1, 1, 64), (2, 1, 77, 3, 3, 64), (1, 5, 3, 2, 1, 8), (2, 63, 64, 2, 2, 64), (1, 64, 65, 1, 1, 16), (2, 127, 129, 2, 1, 128),
           (1, 128, 128, 2, 2, 64), (1, 129, 192, 3, 3, 72), (3, 197, 197, 4, 4, 64), (1, 256, 257, 2, 2, 32), (1, 257, 511, 1, 1, 128), (1, 300, 40, 4, 2, 120),
           (2, 513, 640, 2, 2, 64), (1, 700, 1025, 2, 1, 56), (1, 1, 3000, 8, 2, 128), (2, 7, 1500, 8, 2, 64), (1, 100, 2100, 2, 2, 80), (20, 40, 50, 8, 8, 64),
-          (1, 2000, 1, 2, 2, 64), (1, 1300, 1300, 8, 4, 64)]
+          (1, 2000, 1, 2, 2, 64), (1, 1300, 1300, 8, 4, 64),
+          # few rows: spread over a tile's warps, with items for every SM and without; too many rows for that; heads in one tile, keys not shared out
+          (200, 1, 600, 2, 2, 64), (80, 20, 520, 2, 2, 64), (160, 9, 600, 4, 1, 128), (1, 32, 545, 1, 1, 128), (3, 8, 1025, 4, 1, 40)]
 
 
 @pytest.mark.parametrize("causal", [False, True], ids=["all", "causal"])
@@ -190,6 +192,17 @@ def test_few_queries_of_a_padded_batch(kl):
         v[n, kl[n]:] = float("inf")
     run(q, k, v, False, lengths(2, 1), lengths(*kl))
     run(q[:, :1], k, v, True, None, lengths(*kl))
+
+
+@pytest.mark.parametrize("b,causal", [(7, False), (7, True), (300, False)])
+def test_sequences_of_any_order(b, causal):
+    """The backward pass takes the longest first, as far as a CTA can sort them; ends of blocks, equal lengths and empty ones among them."""
+    n = 150
+    g = torch.Generator().manual_seed(b)
+    ql, kl = (torch.randint(0, n + 1, (b,), generator=g, dtype=torch.int32).cuda() for _ in range(2))
+    ql[:5], kl[:5] = lengths(64, 64, 0, 128, n), lengths(64, 64, n, 1, n)
+    q, k, v, _ = make(b, n, n, 2, 1, 64, seed=b)
+    run(q, k, v, causal, ql, kl)
 
 
 def test_rows_without_a_key():
