@@ -79,9 +79,9 @@ def _bind_calls(l):
     except ImportError:
         return
     module.bind(*(C.cast(f, C.c_void_p).value for f in (l.surgeon_layer_norm, l.surgeon_layer_norm_grad, l.surgeon_linear,
-                                                        l.surgeon_linear_grad, l.surgeon_gradient_norm, l.surgeon_clip_gradients,
-                                                        l.surgeon_attention, l.surgeon_attention_grad, l.surgeon_group_norm,
-                                                        l.surgeon_group_norm_grad, l.surgeon_dropout)))
+                                                        l.surgeon_linear_grad, l.surgeon_gradient_norm, l.surgeon_clip_gradients)))
+    module.bind_more(*(C.cast(f, C.c_void_p).value for f in (l.surgeon_attention, l.surgeon_attention_grad, l.surgeon_group_norm,
+                                                             l.surgeon_group_norm_grad, l.surgeon_dropout)))
     _calls = module
 
 

@@ -176,9 +176,10 @@ struct Place {
 // thread's own, so that nothing but its own copies is waited for, and no register holds what has not arrived.
 template <int DT, int GDT, int E, bool TWO>
 struct Walk {
-  [[maybe_unused]] static constexpr int kX = sizeof(Raw<DT, E>) / 16, kD = TWO ? sizeof(Raw<GDT, E>) / 16 : 0;
-  [[maybe_unused]] static constexpr uint32_t kVector = kMaxThreads * 16, kRow = (kX + kD) * kVector;                // bytes of a CTA's vectors, of its rows
-  [[maybe_unused]] static constexpr size_t kPlaces = E == 1 ? 0 : kAhead * kRow;
+  static constexpr int kX = sizeof(Raw<DT, E>) / 16, kD = TWO ? sizeof(Raw<GDT, E>) / 16 : 0;
+  static constexpr uint32_t kVector = kMaxThreads * 16, kRow = (kX + kD) * kVector;                // bytes of a CTA's vectors, of its rows
+  static constexpr size_t kPlaces = E == 1 ? 0 : kAhead * kRow;
+  static_assert(kGradResident * kPlaces <= 200 * 1024, "the places of the CTAs of an SM");
   const char *x, *dy;
   long long at, step;
   int mine;

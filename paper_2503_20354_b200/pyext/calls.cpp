@@ -409,14 +409,25 @@ bool address(PyObject* o, F* to) {
 
 // The entry points' addresses, in the order of their declarations above.
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 11) {
-    PyErr_SetString(PyExc_TypeError, "bind takes eleven addresses");
+  if (n != 6) {
+    PyErr_SetString(PyExc_TypeError, "bind takes six addresses");
     return nullptr;
   }
   if (!address(a[0], &layer_norm_fn) || !address(a[1], &layer_norm_grad_fn) || !address(a[2], &linear_fn) ||
-      !address(a[3], &linear_grad_fn) || !address(a[4], &gradient_norm_fn) || !address(a[5], &clip_gradients_fn) ||
-      !address(a[6], &attention_fn) || !address(a[7], &attention_grad_fn) || !address(a[8], &group_norm_fn) ||
-      !address(a[9], &group_norm_grad_fn) || !address(a[10], &dropout_fn)) {
+      !address(a[3], &linear_grad_fn) || !address(a[4], &gradient_norm_fn) || !address(a[5], &clip_gradients_fn)) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a null address");
+    return nullptr;
+  }
+  Py_RETURN_NONE;
+}
+// Those of attention and what follows it.
+PyObject* bind_more(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 5) {
+    PyErr_SetString(PyExc_TypeError, "bind_more takes five addresses");
+    return nullptr;
+  }
+  if (!address(a[0], &attention_fn) || !address(a[1], &attention_grad_fn) || !address(a[2], &group_norm_fn) ||
+      !address(a[3], &group_norm_grad_fn) || !address(a[4], &dropout_fn)) {
     if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a null address");
     return nullptr;
   }
@@ -424,7 +435,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 #define SURGEON_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {SURGEON_METHOD(bind),        SURGEON_METHOD(layer_norm), SURGEON_METHOD(layer_norm_grad), SURGEON_METHOD(linear),
+PyMethodDef methods[] = {SURGEON_METHOD(bind),        SURGEON_METHOD(bind_more), SURGEON_METHOD(layer_norm), SURGEON_METHOD(layer_norm_grad), SURGEON_METHOD(linear),
                          SURGEON_METHOD(linear_grad), SURGEON_METHOD(gradients),  SURGEON_METHOD(attention), SURGEON_METHOD(attention_grad),
                          SURGEON_METHOD(group_norm),  SURGEON_METHOD(group_norm_grad), SURGEON_METHOD(dropout), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
